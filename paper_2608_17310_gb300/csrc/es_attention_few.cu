@@ -35,7 +35,7 @@ constexpr int kWarps = kThreads / 32;
 template <bool kFp8>
 struct Shape {
   // 16-key blocks that a warp takes at a time: as many bytes in flight for either type
-  static constexpr int subs = kFp8 ? 2 : 1;
+  static constexpr int subs = 1;
   static constexpr int warp_keys = 16 * subs;
   static constexpr int tile = kWarps * warp_keys;
 };
@@ -85,42 +85,38 @@ struct Block {
   uint4 k[2][kk];
   V v[4][vv];
   float k_scale[2], v_scale[2];
-  bool there;
 
-  __device__ __forceinline__ void load_keys(const CacheView& c, int page, int head, int j, int lane) {
-    there = page >= 0;
+  // From a page that exists; what the page's place in the sequence does not hold is masked
+  // by the caller.
+  __device__ __forceinline__ void load_keys(const CacheView& c, int page, uint32_t row, int lane) {
     const int g = lane / 4, t = lane % 4;
-    const uint64_t row = (static_cast<uint64_t>(head) << c.page_shift) + (j & ((1 << c.page_shift) - 1));
-    const uint64_t at = page * c.page_stride + row * D;
+    const char* from = static_cast<const char*>(c.k) +
+                       (page * c.page_stride + row * D + g * D + t * (kFp8 ? 16 : 8)) * (kFp8 ? 1 : 2);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint64_t key = at + (g + 8 * i) * D;
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int p = 0; p < kk; ++p) {
-        const char* from = static_cast<const char*>(c.k) + (kFp8 ? key + p * 64 + t * 16 : (key + p * 32 + t * 8) * 2);
-        k[i][p] = there ? __ldg(reinterpret_cast<const uint4*>(from)) : make_uint4(0, 0, 0, 0);
-      }
-      if (kFp8) {
-        const uint64_t s = page * c.scale_stride + row + g + 8 * i;
-        k_scale[i] = there ? __ldg(c.k_scale + s) : 0.0f;
-        v_scale[i] = there ? __ldg(c.v_scale + s) : 0.0f;
-      }
+      for (int p = 0; p < kk; ++p)
+        k[i][p] = __ldg(reinterpret_cast<const uint4*>(from + i * 8 * D * (kFp8 ? 1 : 2) + p * 64));
+    if (kFp8) {
+      const uint64_t s = page * c.scale_stride + row + g;
+      k_scale[0] = __ldg(c.k_scale + s);
+      k_scale[1] = __ldg(c.k_scale + s + 8);
     }
   }
 
-  __device__ __forceinline__ void load_values(const CacheView& c, int page, int head, int j, int lane) {
+  __device__ __forceinline__ void load_values(const CacheView& c, int page, uint32_t row, int lane) {
     const int g = lane / 4, t = lane % 4;
-    const uint64_t row = (static_cast<uint64_t>(head) << c.page_shift) + (j & ((1 << c.page_shift) - 1));
-    const uint64_t at = page * c.page_stride + row * D;
+    const char* from = static_cast<const char*>(c.v) +
+                       (page * c.page_stride + row * D + 2 * t * D) * (kFp8 ? 1 : 2) + g * vbytes;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint64_t key = at + (2 * t + (i & 1) + 8 * (i >> 1)) * D;
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int p = 0; p < vv; ++p) {
-        const char* from = static_cast<const char*>(c.v) + (kFp8 ? key + g * vbytes : (key + p * 64 + g * 8) * 2);
-        if (page >= 0) v[i][p] = __ldg(reinterpret_cast<const V*>(from));
-        else v[i][p] = V{};
-      }
+      for (int p = 0; p < vv; ++p)
+        v[i][p] = __ldg(reinterpret_cast<const V*>(from + ((i & 1) + 8 * (i >> 1)) * D * (kFp8 ? 1 : 2) + p * 128));
+    if (kFp8) {  // as the scores lie: keys g and g + 8
+      const uint64_t s = page * c.scale_stride + row + g;
+      v_scale[0] = __ldg(c.v_scale + s);
+      v_scale[1] = __ldg(c.v_scale + s + 8);
     }
   }
 
@@ -183,6 +179,17 @@ struct Block {
     }
   }
 };
+
+// A row's interval, position and slope (as bits). The kernel keeps them in shared memory,
+// since only the blocks at the ends of the intervals and biased scores need them: in
+// registers they would cost the loads in flight.
+__device__ __forceinline__ int4 row_info(const int4* p) {
+  int4 r;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
+               : "r"(shared_address(p)));
+  return r;
+}
 
 // The element of a head that row g of product m of a lane stands for (g + 8: the next one).
 template <int D, bool kFp8>
@@ -259,12 +266,12 @@ struct Part {
   float top[16], sum[16];
 };
 
-constexpr int kMinTiles = 2;  // of a block's range
+constexpr int kMinTiles = 1;  // of a block's range
 constexpr int kMaxParts = 2048;  // two for each block
 constexpr uint64_t kCounterBytes = kMaxParts / 2 * sizeof(uint32_t);
 
 template <int D, bool kFp8, int kBlocks>
-__global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 3 : 2)
+__global__ void __launch_bounds__(kThreads, kBlocks == 1 ? (kFp8 ? 4 : 3) : 2)
 few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArgs a, uint32_t* counters,
                 Part<D>* parts) {
   using S = Shape<kFp8>;
@@ -276,9 +283,11 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
   __shared__ int64_t first_tile;
   __shared__ int first_seq;
   __shared__ bool is_last;
+  __shared__ __align__(16) int4 info[kWarps][kRows];
 
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
 
+  wait_for_previous();
   // This block's range of tiles: every thread counts a run of sequences.
   const int run = (batch.sequences + kThreads - 1) / kThreads;
   const int run0 = threadIdx.x * run, run1 = min(run0 + run, batch.sequences);
@@ -301,7 +310,7 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
   }
   const int64_t per = max((all + gridDim.x - 1) / gridDim.x, static_cast<int64_t>(kMinTiles));
   const int64_t begin = blockIdx.x * per, end = min(begin + per, all);
-  if (begin >= end) return;
+  if (begin >= end) return;  // which lets the next kernel start too
   if (begin >= upto - mine && begin < upto) {
     int64_t at = upto - mine;
     for (int s = run0;; ++s) {
@@ -333,8 +342,6 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
     const int tile1 = static_cast<int>(min(unit1, end) - unit0);
 
     // --- the unit's rows: 8 n + 2 t, + 1 in the products' columns of this lane
-    Row row[kBlocks][2];
-    float slope[kBlocks][2];
     float factor[kBlocks][2];  // of a dot product, for a score in units of log 2 (plain scores)
     uint32_t q[kBlocks][D / 16][2];
     const bool plain = a.softcap <= 0.0f && a.slopes == nullptr;
@@ -386,14 +393,18 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int mine = 8 * n + 2 * t + i;
-        row[n][i] = row_of(batch, a, span.begin, span.count, span.base, span.length, mine);
-        slope[n][i] = a.slopes != nullptr ? a.slopes[head * a.group + mine % a.group] : 0.0f;
         // the unit of row 2 t + i is with the lanes of g = 2 t + i
         factor[n][i] = a.scale * __shfl_sync(0xFFFFFFFFu, q_unit, (2 * t + i) * 4);
         if (plain) factor[n][i] *= kLog2e;
       }
     }
+
+    if (lane < kRows) {
+      const Row r = row_of(batch, a, span.begin, span.count, span.base, span.length, lane);
+      const float slope = a.slopes != nullptr ? a.slopes[head * a.group + lane % a.group] : 0.0f;
+      info[warp][lane] = make_int4(r.lo, r.hi, r.pos, __float_as_int(slope));
+    }
+    __syncwarp();
 
     float o[kBlocks][D / 16][4] = {};
     float top[kBlocks][2], sum[kBlocks][2];
@@ -413,19 +424,21 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
       const int j = key_of(tile, sub);
       return tile < tile1 && j < span.hi ? page_of(cache, batch, seq, j) : -1;
     };
+    auto row_at = [&](int tile, int sub) {  // of the page's rows of all heads
+      return (static_cast<uint32_t>(head) << cache.page_shift) + (key_of(tile, sub) & ((1 << cache.page_shift) - 1));
+    };
     Block<D, kFp8> block[kSubs];
-    int page[kSubs];
+    int page[kSubs], next_page[kSubs];  // -1: no tokens, and what is loaded from page 0 instead is masked
 #pragma unroll
     for (int u = 0; u < kSubs; ++u) {
       page[u] = page_at(tile0, u);
-      block[u].load_keys(cache, page[u], head, key_of(tile0, u), lane);
-      block[u].load_values(cache, page[u], head, key_of(tile0, u), lane);
-      page[u] = page_at(tile0 + 1, u);
+      block[u].load_keys(cache, max(page[u], 0), row_at(tile0, u), lane);
+      block[u].load_values(cache, max(page[u], 0), row_at(tile0, u), lane);
+      next_page[u] = page_at(tile0 + 1, u);
     }
     for (int tile = tile0; tile < tile1; ++tile) {
       float s[kSubs][kBlocks][4];
-      float v_scale[kSubs][2];
-      bool there[kSubs];
+      const bool more = tile + 1 < tile1;
       float best[kBlocks][2], scale_most[kBlocks][2];
 #pragma unroll
       for (int n = 0; n < kBlocks; ++n) {
@@ -444,26 +457,53 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
           for (int n = 0; n < kBlocks; ++n) mma<kFp8>(s[u][n], w, q[n][k][0], q[n][k][1]);
         }
         const int j0 = key_of(tile, u);
-        there[u] = block[u].there;
         const float k_scale[2] = {kFp8 ? block[u].k_scale[0] : 1.0f, kFp8 ? block[u].k_scale[1] : 1.0f};
-        v_scale[u][0] = block[u].v_scale[0];
-        v_scale[u][1] = block[u].v_scale[1];
         // the next tile's keys are on their way while this one's scores are worked on
-        block[u].load_keys(cache, page[u], head, key_of(tile + 1, u), lane);
-        const bool whole = there[u] && j0 >= span.in_lo && j0 + 16 <= span.in_hi;
+        if (more) block[u].load_keys(cache, max(next_page[u], 0), row_at(tile + 1, u), lane);
+        const bool whole = page[u] >= 0 && j0 >= span.in_lo && j0 + 16 <= span.in_hi;
+        if (plain && whole) {
 #pragma unroll
-        for (int n = 0; n < kBlocks; ++n)
+          for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int c = i & 1, h = i >> 1, j = j0 + g + 8 * h;
-            float x = s[u][n][i] * (kFp8 ? factor[n][c] * k_scale[h] : factor[n][c]);
-            if (!plain) x = score_of(a, x, slope[n][c], row[n][c].pos - j);
-            const bool seen = whole || (there[u] && j >= row[n][c].lo && j < row[n][c].hi);
-            if (!seen) x = -INFINITY;
-            if (kFp8 && seen && v_scale[u][h] <= FLT_MAX) scale_most[n][c] = fmaxf(scale_most[n][c], v_scale[u][h]);
-            s[u][n][i] = x;
-            best[n][c] = fmaxf(best[n][c], x);  // a NaN stays with the sum
+            for (int i = 0; i < 4; ++i) {
+              s[u][n][i] *= kFp8 ? factor[n][i & 1] * k_scale[i >> 1] : factor[n][i & 1];
+              best[n][i & 1] = fmaxf(best[n][i & 1], s[u][n][i]);  // a NaN stays with the sum
+            }
+        } else {
+#pragma unroll
+          for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              const int4 r = row_info(&info[warp][8 * n + 2 * t + c]);
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const int j = j0 + g + 8 * h;
+                float x = s[u][n][c + 2 * h] * (kFp8 ? factor[n][c] * k_scale[h] : factor[n][c]);
+                if (!plain) x = score_of(a, x, __int_as_float(r.w), r.z - j);
+                const bool seen = whole || (page[u] >= 0 && j >= r.x && j < r.y);
+                if (!seen) x = -INFINITY;
+                s[u][n][c + 2 * h] = x;
+                best[n][c] = fmaxf(best[n][c], x);
+              }
+            }
+        }
+        if (kFp8) {
+          const float most[2] = {fabsf(block[u].v_scale[0]) <= FLT_MAX ? block[u].v_scale[0] : 0.0f,
+                                 fabsf(block[u].v_scale[1]) <= FLT_MAX ? block[u].v_scale[1] : 0.0f};
+          if (whole) {
+            const float m = fmaxf(most[0], most[1]);
+#pragma unroll
+            for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) scale_most[n][c] = fmaxf(scale_most[n][c], m);
+          } else {
+#pragma unroll
+            for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)  // only of keys that the row sees
+                if (s[u][n][i] != -INFINITY) scale_most[n][i & 1] = fmaxf(scale_most[n][i & 1], most[i >> 1]);
           }
+        }
       }
       // running maxima; FP8: the largest value scale too
       bool grows = false;
@@ -530,25 +570,25 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
         }
         const bool inside = j0 >= span.in_lo && j0 + 16 <= span.in_hi;
         uint32_t bad = 0;  // keys whose values hold an infinity or NaN that some row does not see
-        if (!inside && there[u]) {
+        if (!inside || page[u] < 0) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int key = 2 * t + (i & 1) + 8 * (i >> 1), j = j0 + key;
-            if (j < span.lo || j >= span.hi) block[u].clear_value(i);
+            if (j < span.lo || j >= span.hi || page[u] < 0) block[u].clear_value(i);
             else if (block[u].bad_value(i)) bad |= 1u << key;
           }
           if (kFp8) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const int j = j0 + g + 8 * h;
-              if (j < span.lo || j >= span.hi) v_scale[u][h] = 0.0f;
-              else if (!(fabsf(v_scale[u][h]) <= FLT_MAX)) bad |= 1u << (g + 8 * h);
+              if (j < span.lo || j >= span.hi || page[u] < 0) block[u].v_scale[h] = 0.0f;
+              else if (!(fabsf(block[u].v_scale[h]) <= FLT_MAX)) bad |= 1u << (g + 8 * h);
             }
           }
           bad = __reduce_or_sync(0xFFFFFFFFu, bad);
           if (bad != 0) {
-            const uint64_t at_row = (static_cast<uint64_t>(head) << cache.page_shift) + (j0 & ((1 << cache.page_shift) - 1));
-            const uint64_t pg = static_cast<uint64_t>(page_of(cache, batch, seq, j0));
+            const uint64_t at_row = row_at(tile, u);
+            const uint64_t pg = static_cast<uint64_t>(page[u]);
             for (int key = 0; key < 16; ++key) {
               if (!(bad >> key & 1)) continue;
 #pragma unroll
@@ -561,7 +601,8 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
                 for (int c = 0; c < 2; ++c) {
                   const float x = key < 8 ? s[u][n][c] : s[u][n][c + 2];
                   const float w = __shfl_sync(0xFFFFFFFFu, x, key % 8 * 4 + t) * (kFp8 ? own * v_factor[n][c] : 1.0f);
-                  if (j0 + key < row[n][c].lo || j0 + key >= row[n][c].hi) continue;
+                  const int4 r = row_info(&info[warp][8 * n + 2 * t + c]);
+                  if (j0 + key < r.x || j0 + key >= r.y) continue;
 #pragma unroll
                   for (int m = 0; m < D / 16; ++m)
 #pragma unroll
@@ -577,7 +618,7 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
             if (kFp8) {
 #pragma unroll
               for (int h = 0; h < 2; ++h)
-                if (bad >> (g + 8 * h) & 1) v_scale[u][h] = 0.0f;
+                if (bad >> (g + 8 * h) & 1) block[u].v_scale[h] = 0.0f;
             }
           }
         }
@@ -586,8 +627,8 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (kFp8) {
-              p[n][h] = transpose8x8(pack_f16(s[u][n][2 * h] * (v_scale[u][h] * v_factor[n][0]),
-                                              s[u][n][2 * h + 1] * (v_scale[u][h] * v_factor[n][1])));
+              p[n][h] = transpose8x8(pack_f16(s[u][n][2 * h] * (block[u].v_scale[h] * v_factor[n][0]),
+                                              s[u][n][2 * h + 1] * (block[u].v_scale[h] * v_factor[n][1])));
             } else {
               p[n][h] = transpose8x8(pack_bf16(s[u][n][2 * h], s[u][n][2 * h + 1]));
             }
@@ -599,10 +640,13 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
 #pragma unroll
           for (int n = 0; n < kBlocks; ++n) mma<kFp8>(o[n][m], w, p[n][0], p[n][1]);
         }
-        block[u].load_values(cache, page[u], head, key_of(tile + 1, u), lane);
-        page[u] = page_at(tile + 2, u);
+        if (more) block[u].load_values(cache, max(next_page[u], 0), row_at(tile + 1, u), lane);
+        page[u] = next_page[u];
+        next_page[u] = page_at(tile + 2, u);
       }
     }
+
+    if (unit0 + tile1 >= end) let_next_start();
 
     // --- join the warps
 #pragma unroll
@@ -665,10 +709,10 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
       __syncthreads();
     }
     if (c_first == c_last || is_last) {
-      for (int i = threadIdx.x; i < rows * kCols; i += kThreads) {
-        const int r = i / kCols, col = i % kCols * 4;
-        float most = -INFINITY, l = 0.0f;
-        float4 x = make_float4(0, 0, 0, 0);
+      // a warp for each row, a lane for D / 32 of its elements
+      constexpr int kPer = D / 32;
+      for (int r = warp; r < rows; r += kWarps) {
+        float most = -INFINITY, l = 0.0f, x[kPer] = {};
         if (c_first == c_last) {
 #pragma unroll
           for (int w = 0; w < kWarps; ++w) most = fmaxf(most, top_of[w][r]);
@@ -676,34 +720,55 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
 #pragma unroll
           for (int w = 0; w < kWarps; ++w) {
             const float f = exp2_approx(top_of[w][r] - zero);
-            const float4 y = *reinterpret_cast<const float4*>(&o_of[w][r][col]);
-            x.x += y.x * f;
-            x.y += y.y * f;
-            x.z += y.z * f;
-            x.w += y.w * f;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) x[i] += o_of[w][r][lane * kPer + i] * f;
             l += sum_of[w][r] * f;
           }
         } else {
-          for (int c = c_first; c <= c_last; ++c) most = fmaxf(most, __ldcg(&parts[2 * c + (c == c_first)].top[r]));
+          // the parts' maxima and sums a lane each, their elements eight loads at a time
+          const int n = c_last - c_first + 1;
+          auto part_of = [&](int i) -> const Part<D>& { return parts[2 * (c_first + i) + (i == 0)]; };
+          for (int i = lane; i < n; i += 32) most = fmaxf(most, __ldcg(&part_of(i).top[r]));
+#pragma unroll
+          for (int m = 16; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, m));
           const float zero = most == -INFINITY ? 0.0f : most;
-#pragma unroll 4
-          for (int c = c_first; c <= c_last; ++c) {
-            const Part<D>& part = parts[2 * c + (c == c_first)];
-            const float f = exp2_approx(__ldcg(&part.top[r]) - zero);
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(&part.o[r][col]));
-            x.x += y.x * f;
-            x.y += y.y * f;
-            x.z += y.z * f;
-            x.w += y.w * f;
-            l += __ldcg(&part.sum[r]) * f;
+          for (int i0 = 0; i0 < n; i0 += 32) {
+            const int some = min(n - i0, 32);
+            float f = 0.0f;
+            if (lane < some) {
+              f = exp2_approx(__ldcg(&part_of(i0 + lane).top[r]) - zero);
+              l += __ldcg(&part_of(i0 + lane).sum[r]) * f;
+            }
+#pragma unroll 8
+            for (int i = 0; i < some; ++i) {
+              const float g = __shfl_sync(0xFFFFFFFFu, f, i);
+              const float* from = &part_of(i0 + i).o[r][lane * kPer];
+              if constexpr (kPer == 4) {
+                const float4 y = __ldcg(reinterpret_cast<const float4*>(from));
+                x[0] += y.x * g;
+                x[1] += y.y * g;
+                x[2] += y.z * g;
+                x[3] += y.w * g;
+              } else {
+                const float2 y = __ldcg(reinterpret_cast<const float2*>(from));
+                x[0] += y.x * g;
+                x[1] += y.y * g;
+              }
+            }
           }
+#pragma unroll
+          for (int m = 16; m > 0; m >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, m);
         }
         const int token = span.begin + r / a.group, h = head * a.group + r % a.group;
         const bool some = most > -INFINITY || l != l;
         const float inv = some ? 1.0f / l : 0.0f;
-        *reinterpret_cast<uint2*>(a.out + token * a.out_stride + static_cast<uint64_t>(h) * D + col) =
-            some ? make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv)) : make_uint2(0, 0);
-        if (col == 0 && a.lse != nullptr)
+        uint32_t* to = reinterpret_cast<uint32_t*>(a.out + token * a.out_stride + static_cast<uint64_t>(h) * D + lane * kPer);
+        if constexpr (kPer == 4)
+          *reinterpret_cast<uint2*>(to) = some ? make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv))
+                                               : make_uint2(0, 0);
+        else
+          *to = some ? pack_bf16(x[0] * inv, x[1] * inv) : 0u;
+        if (lane == 0 && a.lse != nullptr)
           a.lse[static_cast<uint64_t>(token) * a.q_heads + h] = some ? most * kLn2 + logf(l) : -INFINITY;
       }
     }
@@ -723,10 +788,9 @@ cudaError_t launch(const CacheView& cache, const BatchView& batch, const Attenti
   const int64_t longest = (static_cast<int64_t>(batch.capacity) + 15 + Shape<kFp8>::tile - 1) / Shape<kFp8>::tile;
   const int64_t tiles = longest * cache.kv_heads * batch.sequences;
   const int64_t blocks = std::min({resident, static_cast<int64_t>(kMaxParts / 2), (tiles + kMinTiles - 1) / kMinTiles});
-  kernel<<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(
-      cache, batch, args, static_cast<uint32_t*>(workspace),
-      reinterpret_cast<Part<D>*>(static_cast<char*>(workspace) + kCounterBytes));
-  return cudaGetLastError();
+  return launch_early(kernel, static_cast<int>(blocks), kThreads, 0, stream, cache, batch, args,
+                      static_cast<uint32_t*>(workspace),
+                      reinterpret_cast<Part<D>*>(static_cast<char*>(workspace) + kCounterBytes));
 }
 
 template <int D, bool kFp8>

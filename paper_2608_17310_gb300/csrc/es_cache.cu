@@ -82,6 +82,7 @@ __device__ __forceinline__ bool locate(const BatchView& b, int t, int& seq, int&
 template <int D, bool kFp8>
 __global__ void __launch_bounds__(kThreads)
 append_kernel(const CacheView cache, const BatchView batch, const AppendArgs a) {
+  wait_for_previous();
   constexpr int kLanes = D / 8;
   const int heads = a.q_heads + 2 * cache.kv_heads;
   const int64_t vectors = static_cast<int64_t>(batch.tokens) * heads;
@@ -199,6 +200,7 @@ template <int D, bool kFp8>
 __global__ void __launch_bounds__(kThreads)
 read_kernel(const CacheView cache, const BatchView batch, uint16_t* __restrict__ k_out,
             uint16_t* __restrict__ v_out) {
+  wait_for_previous();
   constexpr int kLanes = D / 8;
   const int heads = 2 * cache.kv_heads;
   const int64_t id = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / kLanes;
@@ -236,8 +238,7 @@ cudaError_t launch_vectors(K kernel, int64_t vectors, int head_dim, cudaStream_t
   const int64_t per_block = kThreads / (head_dim / 8);
   const int64_t blocks = (vectors + per_block - 1) / per_block;
   if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
-  kernel<<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(args...);
-  return cudaGetLastError();
+  return launch_early(kernel, static_cast<int>(blocks), kThreads, 0, stream, args...);
 }
 
 }  // namespace

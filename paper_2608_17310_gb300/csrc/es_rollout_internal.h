@@ -62,6 +62,30 @@ struct AttentionArgs {
 };
 
 #ifdef __CUDACC__
+// Programmatic dependent launch: a kernel may be resident before the one ahead of it in its
+// stream has ended, and touches no memory until that one has.
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// Launches a kernel that calls wait_for_previous before anything else.
+template <class... P, class... A>
+cudaError_t launch_early(void (*kernel)(P...), int grid, int block, size_t shared, cudaStream_t stream,
+                         const A&... args) {
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t config{};
+  config.gridDim = dim3(static_cast<unsigned>(grid));
+  config.blockDim = dim3(static_cast<unsigned>(block));
+  config.dynamicSmemBytes = shared;
+  config.stream = stream;
+  config.attrs = &attr;
+  config.numAttrs = 1;
+  const cudaError_t err = cudaLaunchKernelEx(&config, kernel, P(args)...);
+  const cudaError_t last = cudaGetLastError();
+  return err != cudaSuccess ? err : last;
+}
+
 __device__ __forceinline__ int sequence_length(const BatchView& b, int s) {
   return min(max(b.seq_len[s], 0), b.capacity);
 }
