@@ -25,7 +25,7 @@ LIB = os.path.join(BUILD, "libesopt.so")
 PROBE_LIB = os.path.join(BUILD, "libesprobe.so")
 
 SOURCES = ["es_host.cu", "es_kernels.cu", "es_noalloc.cu", "es_rollout.cu", "es_cache.cu",
-           "es_attention.cu", "es_attention_few.cu"]
+           "es_attention.cu", "es_attention_few.cu", "es_attention_many.cu"]
 PROBE_SOURCES = ["es_probes.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-std=c++17", "-O3", "-lineinfo", "-Xcompiler", "-fPIC,-O2",

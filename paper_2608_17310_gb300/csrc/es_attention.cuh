@@ -1,6 +1,7 @@
 // Device code that the attention kernels share.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include <cfloat>
@@ -53,18 +54,6 @@ __device__ __forceinline__ uint32_t shared_address(const void* p) {
   return static_cast<uint32_t>(__cvta_generic_to_shared(p));
 }
 
-__device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t address) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(address));
-}
-
-__device__ __forceinline__ void load_matrices_transposed(uint32_t (&r)[4], uint32_t address) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(address));
-}
-
 // Whether a word holds a bf16 infinity or NaN.
 __device__ __forceinline__ bool has_nonfinite(uint32_t w) {
   return (w & 0x7F800000u) == 0x7F800000u || (w & 0x7F80u) == 0x7F80u;
@@ -99,9 +88,18 @@ __device__ __forceinline__ float score_of(const AttentionArgs& a, float x, float
   return (x - slope * static_cast<float>(abs(distance))) * kLog2e;
 }
 
-// es_attention of at most 16 rows per (sequence, key head), and what it needs of the workspace.
+// The workspace of es_attention: counters of the blocks that have finished their part of a
+// unit, zero between calls; a flag that a kernel sets when it gave up a wait; what the
+// kernels keep of a call.
+constexpr int kCounters = 1024;
+constexpr uint64_t kWorkspaceHead = kCounters * sizeof(uint32_t) + 256;
+
+// es_attention of at most 16 rows per (sequence, key head), and of any number.
 cudaError_t launch_few_rows(const CacheView& cache, bool fp8, int head_dim, const BatchView& batch,
-                            const AttentionArgs& args, void* workspace, cudaStream_t stream);
+                            const AttentionArgs& args, char* workspace, uint32_t* counters, cudaStream_t stream);
+cudaError_t launch_many_rows(const CacheView& cache, const CUtensorMap* maps, bool fp8, int head_dim, const BatchView& batch,
+                             const AttentionArgs& args, char* workspace, uint32_t* counters, int* flag, cudaStream_t stream);
 uint64_t few_rows_workspace_bytes(int head_dim);
+uint64_t many_rows_workspace_bytes(int head_dim);
 
 }  // namespace esopt

@@ -267,8 +267,7 @@ struct Part {
 };
 
 constexpr int kMinTiles = 1;  // of a block's range
-constexpr int kMaxParts = 2048;  // two for each block
-constexpr uint64_t kCounterBytes = kMaxParts / 2 * sizeof(uint32_t);
+constexpr int kMaxParts = 2 * kCounters;  // two for each block
 
 template <int D, bool kFp8, int kBlocks>
 __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? (kFp8 ? 4 : 3) : 2)
@@ -779,7 +778,7 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
 
 template <int D, bool kFp8, int kBlocks>
 cudaError_t launch(const CacheView& cache, const BatchView& batch, const AttentionArgs& args,
-                   void* workspace, cudaStream_t stream) {
+                   char* workspace, uint32_t* counters, cudaStream_t stream) {
   auto kernel = few_rows_kernel<D, kFp8, kBlocks>;
   int device = 0;
   cudaGetDevice(&device);
@@ -788,29 +787,28 @@ cudaError_t launch(const CacheView& cache, const BatchView& batch, const Attenti
   const int64_t longest = (static_cast<int64_t>(batch.capacity) + 15 + Shape<kFp8>::tile - 1) / Shape<kFp8>::tile;
   const int64_t tiles = longest * cache.kv_heads * batch.sequences;
   const int64_t blocks = std::min({resident, static_cast<int64_t>(kMaxParts / 2), (tiles + kMinTiles - 1) / kMinTiles});
-  return launch_early(kernel, static_cast<int>(blocks), kThreads, 0, stream, cache, batch, args,
-                      static_cast<uint32_t*>(workspace),
-                      reinterpret_cast<Part<D>*>(static_cast<char*>(workspace) + kCounterBytes));
+  return launch_early(kernel, static_cast<int>(blocks), kThreads, 0, stream, cache, batch, args, counters,
+                      reinterpret_cast<Part<D>*>(workspace));
 }
 
 template <int D, bool kFp8>
 cudaError_t launch_rows(const CacheView& cache, const BatchView& batch, const AttentionArgs& args,
-                        void* workspace, cudaStream_t stream) {
-  return batch.max_new * args.group <= 8 ? launch<D, kFp8, 1>(cache, batch, args, workspace, stream)
-                                         : launch<D, kFp8, 2>(cache, batch, args, workspace, stream);
+                        char* workspace, uint32_t* counters, cudaStream_t stream) {
+  return batch.max_new * args.group <= 8 ? launch<D, kFp8, 1>(cache, batch, args, workspace, counters, stream)
+                                         : launch<D, kFp8, 2>(cache, batch, args, workspace, counters, stream);
 }
 
 }  // namespace
 
 uint64_t few_rows_workspace_bytes(int head_dim) {
-  return kCounterBytes + kMaxParts * (head_dim == 128 ? sizeof(Part<128>) : sizeof(Part<64>));
+  return kMaxParts * (head_dim == 128 ? sizeof(Part<128>) : sizeof(Part<64>));
 }
 
 cudaError_t launch_few_rows(const CacheView& cache, bool fp8, int head_dim, const BatchView& batch,
-                            const AttentionArgs& args, void* workspace, cudaStream_t stream) {
+                            const AttentionArgs& args, char* workspace, uint32_t* counters, cudaStream_t stream) {
   auto f = head_dim == 128 ? (fp8 ? launch_rows<128, true> : launch_rows<128, false>)
                            : (fp8 ? launch_rows<64, true> : launch_rows<64, false>);
-  return f(cache, batch, args, workspace, stream);
+  return f(cache, batch, args, workspace, counters, stream);
 }
 
 }  // namespace esopt

@@ -1,0 +1,996 @@
+// es_attention of more than 16 rows per (sequence, key head): prompts, and turns of some
+// tokens over longer caches.
+//
+// What bounds it is the tensor cores, 4 D operations a row and key, and the exponentials,
+// one a row and key. A block takes 256 rows of a key head as two tiles x = 0, 1 of 128, and
+// walks its keys in tiles of 128:
+//   S_x = Q_x K^T     tcgen05, Q and K in shared memory, S in tensor memory
+//   P_x = 2^(S_x - m) a warpgroup for each x, a thread for each row: S is read from tensor
+//                     memory, P written back over it as bf16
+//   O_x += P_x V      tcgen05, P in tensor memory, V in shared memory, O in tensor memory
+// One thread issues the products in the order P_0 V, Q_0 K', P_1 V, Q_1 K', so that each
+// warpgroup's exponentials run beside the other tile's products. The running maximum m only
+// moves where a tile's maximum is more than 2^8 above it, which keeps P in bf16's range
+// and leaves O in tensor memory alone on almost every tile.
+//
+// bf16 pages reach shared memory by TMA, each page of a tile by its own copy; FP8 pages
+// through four warps that turn codes into bf16, which holds them exactly. The scales go to
+// the scores and to P.
+//
+// The key tiles of all units (sequence, row tile, key head) lie end to end and are cut into
+// one range per block, all of one length, so causal triangles and ragged batches leave no
+// block idle. A unit that several blocks share is joined by the last of them, from the parts
+// in the order of the blocks.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "es_attention.cuh"
+#include "es_internal.h"
+#include "es_rollout_internal.h"
+
+namespace esopt {
+namespace {
+
+constexpr int kKeys = 128;   // of a tile
+constexpr int kRows = 256;   // of a unit
+constexpr int kStages = 2;
+constexpr int kMaxGrid = 192;
+constexpr float kSlack = 8.0f;  // log 2 of how far a score may be above the kept maximum
+
+// Where a block's range begins, from the planning kernel.
+struct Start {
+  int64_t pair_tile;  // first tile of (seq, row_tile) in the space of all
+  int seq, row_tile;
+};
+struct Plan {
+  int64_t all, per;
+  Start start[kMaxGrid];
+};
+
+// What the rows of (sequence, row tile) see: their tokens, and the union and the common part
+// of their intervals of the cache.
+struct Pair {
+  int begin, count, base, length;
+  int rows;
+  int lo, hi;
+  int in_lo, in_hi;
+  int tiles;  // one at least where there are rows, so that rows which see nothing are written too
+};
+
+__device__ __forceinline__ int row_tiles_of(const BatchView& b, const AttentionArgs& a, int seq) {
+  int begin, count, base;
+  new_tokens(b, seq, begin, count, base);
+  return static_cast<int>((static_cast<int64_t>(count) * a.group + kRows - 1) / kRows);
+}
+
+// Called by `lanes` threads that are numbered `lane` and share a warp, or by one thread.
+template <int kLanes>
+__device__ __forceinline__ Pair pair_of(const BatchView& b, const AttentionArgs& a, int seq, int row_tile, int lane) {
+  Pair p;
+  p.length = sequence_length(b, seq);
+  new_tokens(b, seq, p.begin, p.count, p.base);
+  const int64_t row0 = static_cast<int64_t>(row_tile) * kRows;
+  p.rows = static_cast<int>(min(static_cast<int64_t>(p.count) * a.group - row0, static_cast<int64_t>(kRows)));
+  const int i0 = static_cast<int>(row0 / a.group), i1 = static_cast<int>((row0 + p.rows - 1) / a.group);
+  int lo = INT32_MAX, hi = 0, in_lo = 0, in_hi = INT32_MAX;
+  if (a.first == nullptr && a.last == nullptr) {
+    // intervals move with the position
+    const Row r0 = row_of(b, a, p.begin, p.count, p.base, p.length, i0 * a.group);
+    const Row r1 = row_of(b, a, p.begin, p.count, p.base, p.length, i1 * a.group);
+    if (r1.hi > r1.lo) {
+      lo = r0.hi > r0.lo ? r0.lo : 0;
+      hi = r1.hi;
+    }
+    in_lo = r1.lo;
+    in_hi = r0.hi;
+  } else {
+    for (int i = i0 + lane; i <= i1; i += kLanes) {
+      const Row r = row_of(b, a, p.begin, p.count, p.base, p.length, i * a.group);
+      if (r.hi > r.lo) {
+        lo = min(lo, r.lo);
+        hi = max(hi, r.hi);
+      }
+      in_lo = max(in_lo, r.lo);
+      in_hi = min(in_hi, r.hi);
+    }
+    if (kLanes == 32) {
+      lo = __reduce_min_sync(0xFFFFFFFFu, lo);
+      hi = __reduce_max_sync(0xFFFFFFFFu, hi);
+      in_lo = __reduce_max_sync(0xFFFFFFFFu, in_lo);
+      in_hi = __reduce_min_sync(0xFFFFFFFFu, in_hi);
+    }
+  }
+  if (hi <= lo) lo = hi = 0;
+  p.lo = lo;
+  p.hi = hi;
+  p.in_lo = in_lo;
+  p.in_hi = in_hi;
+  p.tiles = max(1, (hi - (lo & ~(kKeys - 1)) + kKeys - 1) / kKeys);
+  return p;
+}
+
+// Counts the tiles of all pairs and finds where each block's range begins. One block: pairs
+// are a few thousand at most, and a pair's tiles cost a thread few operations, or with
+// `first` or `last` its tokens' entries.
+constexpr int kPlanThreads = 1024;
+
+__device__ __forceinline__ int64_t scan_block(int64_t x, int64_t* shared, int64_t& total) {
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  int64_t upto = x;
+#pragma unroll
+  for (int m = 1; m < 32; m <<= 1) {
+    const int64_t y = __shfl_up_sync(0xFFFFFFFFu, upto, m);
+    if (lane >= m) upto += y;
+  }
+  __syncthreads();
+  if (lane == 31) shared[warp] = upto;
+  __syncthreads();
+  if (warp == 0) {
+    int64_t y = shared[lane];
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) {
+      const int64_t z = __shfl_up_sync(0xFFFFFFFFu, y, m);
+      if (lane >= m) y += z;
+    }
+    shared[lane] = y;
+  }
+  __syncthreads();
+  total = shared[31];
+  return upto + (warp > 0 ? shared[warp - 1] : 0) - x;  // of the threads before
+}
+
+__global__ void __launch_bounds__(kPlanThreads)
+plan_kernel(const BatchView batch, const AttentionArgs a, int kv_heads, int grid, Plan* plan) {
+  __shared__ int64_t sums[32];
+  __shared__ int first_pair[ES_MAX_SEQUENCES];  // the pairs of a sequence begin here
+  __shared__ int tiles[kPlanThreads];
+  wait_for_previous();
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  int64_t pairs = 0;
+  for (int s0 = 0; s0 < batch.sequences; s0 += kPlanThreads) {
+    const int s = s0 + threadIdx.x;
+    const int n = s < batch.sequences ? row_tiles_of(batch, a, s) : 0;
+    int64_t more;
+    const int64_t before = scan_block(n, sums, more);
+    if (s < batch.sequences) first_pair[s] = static_cast<int>(pairs + before);
+    pairs += more;
+  }
+  __syncthreads();
+  auto sequence_of = [&](int64_t pair) {  // the last one that begins at or before it
+    int lo = 0, hi = batch.sequences - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (first_pair[mid] <= pair) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+  };
+  int64_t all = 0, per = 1;
+  for (int pass = 0; pass < 2; ++pass) {  // the number of tiles, then the blocks' ranges
+    int64_t done = 0;
+    for (int64_t p0 = 0; p0 < pairs; p0 += kPlanThreads) {
+      const int64_t p = p0 + threadIdx.x;
+      const int seq = p < pairs ? sequence_of(p) : 0;
+      const int row_tile = p < pairs ? static_cast<int>(p - first_pair[seq]) : 0;
+      int n = 0;
+      if (a.first == nullptr && a.last == nullptr) {
+        if (p < pairs) n = pair_of<1>(batch, a, seq, row_tile, 0).tiles;
+      } else {
+        if (pass == 0 || pairs > kPlanThreads) {
+          __syncthreads();
+          // a warp for each pair: its tokens' entries are read side by side
+          for (int i = warp; i < kPlanThreads && p0 + i < pairs; i += kPlanThreads / 32) {
+            const int s = sequence_of(p0 + i);
+            const int of_pair = pair_of<32>(batch, a, s, static_cast<int>(p0 + i - first_pair[s]), lane).tiles;
+            if (lane == 0) tiles[i] = of_pair;
+          }
+          __syncthreads();
+        }
+        if (p < pairs) n = tiles[threadIdx.x];
+      }
+      const int64_t mine = static_cast<int64_t>(n) * kv_heads;
+      int64_t more;
+      const int64_t at = done + scan_block(mine, sums, more);
+      if (pass == 1)
+        for (int64_t c = (at + per - 1) / per; c * per < at + mine; ++c) plan->start[c] = Start{at, seq, row_tile};
+      done += more;
+    }
+    if (pass == 0) {
+      all = done;
+      per = max((all + grid - 1) / grid, static_cast<int64_t>(1));
+      if (threadIdx.x == 0) {
+        plan->all = all;
+        plan->per = per;
+      }
+    }
+  }
+}
+
+// --- barriers, copies and products --------------------------------------------------
+
+// No wait is longer than a few tiles' work; one that outlasts this has met an error of the
+// kernel's own, which ends the launch with its flag set in place of hanging the GPU.
+constexpr int kMostTries = 1 << 20;
+
+__device__ __forceinline__ void barrier_init(uint64_t* b, int count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(shared_address(b)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void barrier_arrive(uint64_t* b) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(shared_address(b)) : "memory");
+}
+__device__ __forceinline__ void barrier_expect(uint64_t* b, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_address(b)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool barrier_try(uint64_t* b, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}"
+               : "=r"(done)
+               : "r"(shared_address(b)), "r"(parity)
+               : "memory");
+  return done != 0;
+}
+// false: the wait was given up, here or by another thread of the block
+__device__ __forceinline__ bool barrier_wait(uint64_t* b, uint32_t parity, volatile int* failed) {
+  for (int i = 0; i < kMostTries; ++i) {
+    if (barrier_try(b, parity)) return true;
+    if (*failed) return false;
+  }
+  *failed = 1;
+  return false;
+}
+
+// The same, whatever has failed before: for what must not outlive the block.
+__device__ __forceinline__ void barrier_settle(uint64_t* b, uint32_t parity) {
+  for (int i = 0; i < kMostTries; ++i)
+    if (barrier_try(b, parity)) return;
+}
+
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+__device__ __forceinline__ void load_box(const CUtensorMap* map, uint32_t to, uint64_t* barrier, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(to),
+               "l"(map), "r"(shared_address(barrier)), "r"(x), "r"(y), "r"(z)
+               : "memory");
+}
+
+// Shared-memory operands in 128-byte rows, swizzled by 128 bytes, 8 rows to 1024 bytes.
+__device__ __forceinline__ uint64_t operand(uint32_t address, uint32_t leading) {
+  return static_cast<uint64_t>((address & 0x3FFFF) >> 4) | static_cast<uint64_t>(leading >> 4) << 16 |
+         static_cast<uint64_t>(1024 >> 4) << 32 | static_cast<uint64_t>(1) << 46 | static_cast<uint64_t>(2) << 61;
+}
+
+// bf16 x bf16 -> fp32, M = 128; `transposed`: the second operand's rows are its K
+__host__ __device__ constexpr uint32_t product_of(int n, bool transposed) {
+  return 1u << 4 | 1u << 7 | 1u << 10 | (transposed ? 1u << 16 : 0u) | static_cast<uint32_t>(n >> 3) << 17 | (128u >> 4) << 24;
+}
+
+__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t kind, bool add) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+               "l"(a), "l"(b), "r"(kind), "r"(static_cast<uint32_t>(add))
+               : "memory");
+}
+__device__ __forceinline__ void multiply_from_tensor(uint32_t d, uint32_t a, uint64_t b, uint32_t kind, bool add) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
+               "r"(a), "l"(b), "r"(kind), "r"(static_cast<uint32_t>(add))
+               : "memory");
+}
+// The barrier completes when the products issued before have.
+__device__ __forceinline__ void commit(uint64_t* b) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_address(b)) : "memory");
+}
+
+__device__ __forceinline__ void tensor_load(uint32_t (&r)[32], uint32_t from) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(from));
+}
+// After this the registers of the loads before are valid.
+__device__ __forceinline__ void tensor_loaded(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
+                 "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
+                 "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tensor_store32(uint32_t to, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(to),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tensor_store16(uint32_t to, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(to),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tensor_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// --- the walk over a block's units -----------------------------------------------------
+
+template <int D>
+struct Shared {
+  uint16_t q[2][128 * D];
+  uint16_t k[kStages][kKeys * D];
+  uint16_t v[kStages][kKeys * D];
+  // Read with the scores, when the tile's keys may have made room for others: a slot is
+  // written again four tiles on, which follows the scores of two tiles on.
+  float k_scale[4][kKeys];
+  uint32_t absent[4];  // 16-key pieces of the tile whose page does not exist
+  float v_scale[kStages][kKeys];
+  uint64_t q_full[2], s_full[2], p_full[2], o_done[2];
+  uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages], v_fixed[kStages];
+  uint64_t group[2], drained;
+  uint32_t tensor;           // address of the tensor memory
+  int failed;
+  int poisoned;              // a value that not every row sees was an infinity or NaN
+  int last[2];
+};
+
+// Parts of units that blocks share, as in the kernel of few rows: block c's first unit, if it
+// began in an earlier block, is part 2c, and its last one, if it began here, part 2c + 1.
+template <int D>
+struct Part {
+  float o[kRows][D];
+  float top[kRows], sum[kRows];
+};
+
+// The 128 threads of a warpgroup; false as barrier_wait.
+template <int D>
+__device__ __forceinline__ bool group_sync(Shared<D>& sh, int x, uint32_t& phase) {
+  barrier_arrive(&sh.group[x]);
+  return __all_sync(0xFFFFFFFFu, barrier_wait(&sh.group[x], phase++ & 1, &sh.failed));
+}
+
+// Every warp of a block walks the same units.
+struct Walk {
+  int64_t at, end, per, pair_tile;
+  int seq, row_tile;
+  Pair pair;
+  // the unit
+  int head, tile0, tile1;
+  int64_t unit0;
+  bool two;  // more than 128 rows
+
+  __device__ __forceinline__ Walk(const BatchView& b, const AttentionArgs& a, const Plan* plan, int lane) {
+    per = plan->per;
+    at = blockIdx.x * per;
+    end = min(at + per, plan->all);
+    if (at < end) {
+      const Start& s = plan->start[blockIdx.x];
+      pair_tile = s.pair_tile;
+      seq = s.seq;
+      row_tile = s.row_tile;
+      pair = pair_of<32>(b, a, seq, row_tile, lane);
+    }
+  }
+  __device__ __forceinline__ bool next(const BatchView& b, const AttentionArgs& a, int kv_heads, int lane) {
+    if (at >= end) return false;
+    while (at >= pair_tile + static_cast<int64_t>(pair.tiles) * kv_heads) {
+      pair_tile += static_cast<int64_t>(pair.tiles) * kv_heads;
+      ++row_tile;
+      while (row_tile >= row_tiles_of(b, a, seq)) {
+        ++seq;
+        row_tile = 0;
+      }
+      pair = pair_of<32>(b, a, seq, row_tile, lane);
+    }
+    head = static_cast<int>((at - pair_tile) / pair.tiles);
+    unit0 = pair_tile + static_cast<int64_t>(head) * pair.tiles;
+    tile0 = static_cast<int>(at - unit0);
+    tile1 = static_cast<int>(min(unit0 + pair.tiles, end) - unit0);
+    at = unit0 + tile1;
+    two = pair.rows > 128;
+    return true;
+  }
+  __device__ __forceinline__ int key_of(int tile) const { return (pair.lo & ~(kKeys - 1)) + tile * kKeys; }
+  // Not every row sees all of the tile.
+  __device__ __forceinline__ bool edge(int tile) const {
+    const int j = key_of(tile);
+    return j < pair.in_lo || j + kKeys > pair.in_hi;
+  }
+};
+
+// Offset in elements of 16-byte piece `piece` of row r, in an operand of 128 rows.
+template <int D>
+__device__ __forceinline__ int place_of(int r, int piece) {
+  return piece / 8 * (128 * 64) + r * 64 + ((piece % 8) ^ (r % 8)) * 8;
+}
+
+// --- roles -----------------------------------------------------------------------------
+
+// bf16 pages to shared memory, a lane for each page of the tile.
+template <int D>
+__device__ void copy_tiles(Shared<D>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
+                           const Plan* plan, const CUtensorMap* k_map, const CUtensorMap* v_map, int lane) {
+  const int page_size = 1 << cache.page_shift, pages = kKeys >> cache.page_shift;
+  uint32_t k_done = 0, v_done = 0;
+  bool fine = true;
+  Walk walk(batch, a, plan, lane);
+  while (fine && walk.next(batch, a, cache.kv_heads, lane)) {
+    for (int tile = walk.tile0; tile < walk.tile1; ++tile) {
+      const int stage = k_done % kStages;
+      const uint32_t parity = k_done / kStages & 1;
+      const int j = walk.key_of(tile) + lane * page_size;
+      int page = -1;
+      if (lane < pages && j < walk.pair.hi) page = page_of(cache, batch, walk.seq, j);
+      const uint32_t missing = __ballot_sync(0xFFFFFFFFu, page < 0);
+      uint32_t absent = 0;  // in pieces of 16 keys
+      for (int i = 0; i < 8; ++i) absent |= (missing >> (i * 16 >> cache.page_shift) & 1) << i;
+      // a page past the last one reads as zeros
+      const int z = page < 0 ? cache.num_pages : page, y = walk.head << cache.page_shift;
+      fine = __all_sync(0xFFFFFFFFu, barrier_wait(&sh.k_empty[stage], parity ^ 1, &sh.failed));
+      if (!fine) break;
+      if (lane == 0) {
+        sh.absent[k_done % 4] = absent;
+        barrier_expect(&sh.k_full[stage], kKeys * D * 2);
+      }
+      __syncwarp();
+      if (lane < pages)
+        for (int h = 0; h < D / 64; ++h)
+          load_box(k_map, shared_address(sh.k[stage] + h * 128 * 64 + lane * page_size * 64), &sh.k_full[stage], h * 64, y, z);
+      ++k_done;
+      fine = __all_sync(0xFFFFFFFFu, barrier_wait(&sh.v_empty[stage], parity ^ 1, &sh.failed));
+      if (!fine) break;
+      if (lane == 0) barrier_expect(&sh.v_full[stage], kKeys * D * 2);
+      __syncwarp();
+      if (lane < pages)
+        for (int h = 0; h < D / 64; ++h)
+          load_box(v_map, shared_address(sh.v[stage] + h * 128 * 64 + lane * page_size * 64), &sh.v_full[stage], h * 64, y, z);
+      ++v_done;
+    }
+  }
+  // no copy outlives the block
+  for (uint32_t i = k_done > kStages ? k_done - kStages : 0; i < k_done; ++i) barrier_settle(&sh.k_full[i % kStages], i / kStages & 1);
+  for (uint32_t i = v_done > kStages ? v_done - kStages : 0; i < v_done; ++i) barrier_settle(&sh.v_full[i % kStages], i / kStages & 1);
+}
+
+// bf16 values of tiles at the ends of intervals: those that no row sees become zeros, and
+// infinities and NaN too (a product with p = 0 would carry them into rows that do not see
+// them); the rows that see them get them when the unit is written.
+template <int D>
+__device__ void fix_tiles(Shared<D>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
+                          const Plan* plan, int thread, int lane) {
+  uint32_t done = 0;
+  Walk walk(batch, a, plan, lane);
+  while (walk.next(batch, a, cache.kv_heads, lane)) {
+    for (int tile = walk.tile0; tile < walk.tile1; ++tile, ++done) {
+      if (!walk.edge(tile)) continue;
+      const int stage = done % kStages, j0 = walk.key_of(tile);
+      if (!barrier_wait(&sh.v_full[stage], done / kStages & 1, &sh.failed)) return;
+      for (int i = thread; i < kKeys * D / 8; i += 64) {
+        const int key = i / (D / 8), j = j0 + key;
+        uint4* at = reinterpret_cast<uint4*>(sh.v[stage] + place_of<D>(key, i % (D / 8)));
+        if (j < walk.pair.lo || j >= walk.pair.hi) {
+          *at = make_uint4(0, 0, 0, 0);
+          continue;
+        }
+        uint4 w = *at;
+        if (has_nonfinite(w.x) || has_nonfinite(w.y) || has_nonfinite(w.z) || has_nonfinite(w.w)) {
+          uint32_t* u = reinterpret_cast<uint32_t*>(&w);
+          for (int e = 0; e < 4; ++e) {
+            if ((u[e] & 0x7F80u) == 0x7F80u) u[e] &= 0xFFFF0000u;
+            if ((u[e] & 0x7F800000u) == 0x7F800000u) u[e] &= 0xFFFFu;
+          }
+          *at = w;
+          *static_cast<volatile int*>(&sh.poisoned) = 1;
+        }
+      }
+      fence_async();
+      barrier_arrive(&sh.v_fixed[stage]);
+    }
+  }
+}
+
+// FP8 pages: a warp loads whole keys' codes, 16 to a lane, and writes them as bf16 in place.
+// The codes of the next tile are on their way while this one waits for its stage.
+template <int D>
+struct Codes {
+  static constexpr int kPer = kKeys * D / 16 / 128;  // 16-byte pieces for each of 128 threads
+  uint4 w[kPer];
+  float scale;
+  bool there[kPer];
+};
+
+template <int D>
+__device__ __forceinline__ void load_codes(Codes<D>& c, const void* store, const float* scales, const CacheView& cache,
+                                           const BatchView& batch, const Walk& walk, int tile, int thread) {
+  const int j0 = walk.key_of(tile), mask = (1 << cache.page_shift) - 1;
+#pragma unroll
+  for (int i = 0; i < Codes<D>::kPer; ++i) {
+    const int piece = i * 128 + thread, key = piece / (D / 16), j = j0 + key;
+    const int page = j >= walk.pair.lo && j < walk.pair.hi ? page_of(cache, batch, walk.seq, j) : -1;
+    c.there[i] = page >= 0;
+    c.w[i] = make_uint4(0, 0, 0, 0);
+    if (page >= 0) {
+      const uint64_t row = (static_cast<uint64_t>(walk.head) << cache.page_shift) + (j & mask);
+      c.w[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(store) + page * cache.page_stride + row * D +
+                                                    piece % (D / 16) * 16));
+    }
+  }
+  const int j = j0 + thread;  // and the scale of one key
+  const int page = j >= walk.pair.lo && j < walk.pair.hi ? page_of(cache, batch, walk.seq, j) : -1;
+  c.scale = 0.0f;
+  if (page >= 0)
+    c.scale = __ldg(scales + page * cache.scale_stride + (static_cast<uint64_t>(walk.head) << cache.page_shift) + (j & mask));
+}
+
+template <int D>
+__device__ __forceinline__ void store_codes(const Codes<D>& c, uint16_t* to, float* scales, int thread, bool clean, int* poisoned) {
+#pragma unroll
+  for (int i = 0; i < Codes<D>::kPer; ++i) {
+    const int piece = i * 128 + thread, key = piece / (D / 16), first = piece % (D / 16) * 2;
+    uint32_t u[4] = {c.w[i].x, c.w[i].y, c.w[i].z, c.w[i].w};
+    if (clean) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t bad = ((u[e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;  // NaN codes
+        if (bad != 0) {
+          u[e] &= ~((bad >> 7) * 0xFFu);
+          *static_cast<volatile int*>(poisoned) = 1;
+        }
+      }
+    }
+    *reinterpret_cast<uint4*>(to + place_of<D>(key, first)) =
+        make_uint4(bf16_of_e4m3(u[0]), bf16_of_e4m3(u[0] >> 16), bf16_of_e4m3(u[1]), bf16_of_e4m3(u[1] >> 16));
+    *reinterpret_cast<uint4*>(to + place_of<D>(key, first + 1)) =
+        make_uint4(bf16_of_e4m3(u[2]), bf16_of_e4m3(u[2] >> 16), bf16_of_e4m3(u[3]), bf16_of_e4m3(u[3] >> 16));
+  }
+  scales[thread] = c.scale;
+}
+
+template <int D>
+__device__ void convert_tiles(Shared<D>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
+                              const Plan* plan, int thread, int lane) {
+  uint32_t done = 0;
+  Walk walk(batch, a, plan, lane);
+  while (walk.next(batch, a, cache.kv_heads, lane)) {
+    for (int tile = walk.tile0; tile < walk.tile1; ++tile, ++done) {
+      const int stage = done % kStages;
+      const uint32_t parity = done / kStages & 1;
+      Codes<D> k, v;
+      load_codes(k, cache.k, cache.k_scale, cache, batch, walk, tile, thread);
+      load_codes(v, cache.v, cache.v_scale, cache, batch, walk, tile, thread);
+      uint32_t absent = 0;
+      for (int i = 0; i < 8; ++i) {
+        const int j = walk.key_of(tile) + i * 16;
+        if (j >= walk.pair.hi || page_of(cache, batch, walk.seq, j) < 0) absent |= 1u << i;
+      }
+      if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.k_empty[stage], parity ^ 1, &sh.failed))) return;
+      if (thread == 0) sh.absent[done % 4] = absent;
+      store_codes(k, sh.k[stage], sh.k_scale[done % 4], thread, false, nullptr);
+      fence_async();
+      barrier_arrive(&sh.k_full[stage]);
+      if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.v_empty[stage], parity ^ 1, &sh.failed))) return;
+      store_codes(v, sh.v[stage], sh.v_scale[stage], thread, walk.edge(tile), &sh.poisoned);
+      fence_async();
+      barrier_arrive(&sh.v_full[stage]);
+    }
+  }
+}
+
+// The thread that issues the products.
+template <int D, bool kFp8>
+__device__ void issue_products(Shared<D>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
+                               const Plan* plan, int lane) {
+  constexpr uint32_t kScores = product_of(kKeys, false), kValues = product_of(D, true);
+  const uint32_t tensor = sh.tensor;
+  uint32_t k_done = 0, v_done = 0, units = 0, two_units = 0;
+  uint32_t p_done[2] = {0, 0}, fixed[kStages] = {};
+  auto scores = [&](int x, int stage) {
+    if (lane == 0) {
+      const uint32_t q = shared_address(sh.q[x]), k = shared_address(sh.k[stage]);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        const uint32_t at = i / 4 * (128 * 128) + i % 4 * 32;
+        multiply(tensor + x * 128, operand(q + at, 16), operand(k + at, 16), kScores, i > 0);
+      }
+      commit(&sh.s_full[x]);
+      barrier_arrive(&sh.s_full[x]);  // with what this thread has seen: the tile's scales, its absent pages
+    }
+    __syncwarp();
+  };
+  Walk walk(batch, a, plan, lane);
+  while (walk.next(batch, a, cache.kv_heads, lane)) {
+    const int tiles = walk.two ? 2 : 1;
+    if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.q_full[0], units & 1, &sh.failed))) return;
+    if (walk.two && !__all_sync(0xFFFFFFFFu, barrier_wait(&sh.q_full[1], two_units & 1, &sh.failed))) return;
+    ++units;
+    two_units += walk.two;
+    fence_after();
+    if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.k_full[k_done % kStages], k_done / kStages & 1, &sh.failed))) return;
+    for (int x = 0; x < tiles; ++x) scores(x, k_done % kStages);
+    if (lane == 0) commit(&sh.k_empty[k_done % kStages]);
+    __syncwarp();
+    ++k_done;
+    for (int tile = walk.tile0; tile < walk.tile1; ++tile, ++v_done) {
+      const int stage = v_done % kStages;
+      const bool more = tile + 1 < walk.tile1;
+      for (int x = 0; x < tiles; ++x) {
+        if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.p_full[x], p_done[x] & 1, &sh.failed))) return;
+        ++p_done[x];
+        if (x == 0) {
+          if (!kFp8 && walk.edge(tile)) {
+            if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.v_fixed[stage], fixed[stage] & 1, &sh.failed))) return;
+            ++fixed[stage];
+          } else if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.v_full[stage], v_done / kStages & 1, &sh.failed))) {
+            return;
+          }
+        }
+        fence_after();
+        if (lane == 0) {
+          const uint32_t v = shared_address(sh.v[stage]);
+#pragma unroll
+          for (int i = 0; i < kKeys / 16; ++i)
+            multiply_from_tensor(tensor + 256 + x * 128, tensor + x * 128 + i * 8, operand(v + i * 16 * 128, 128 * 128),
+                                 kValues, i > 0 || tile > walk.tile0);
+          commit(&sh.o_done[x]);
+        }
+        __syncwarp();
+        if (more) {
+          if (x == 0) {
+            if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.k_full[k_done % kStages], k_done / kStages & 1, &sh.failed))) return;
+            fence_after();
+          }
+          scores(x, k_done % kStages);
+        }
+      }
+      if (lane == 0) {
+        commit(&sh.v_empty[stage]);
+        if (more) commit(&sh.k_empty[k_done % kStages]);
+      }
+      __syncwarp();
+      if (more) ++k_done;
+    }
+  }
+}
+
+// A warpgroup's rows: a thread for each.
+template <int D, bool kFp8>
+__device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
+                       const Plan* plan, uint32_t* counters, Part<D>* parts, int x, int thread, int lane) {
+  const uint32_t lanes = static_cast<uint32_t>(thread / 32 * 32) << 16;
+  const uint32_t s_at = sh.tensor + lanes + x * 128, o_at = sh.tensor + lanes + 256 + x * 128;
+  const bool plain = a.softcap <= 0.0f && a.slopes == nullptr;
+  const float factor = plain ? a.scale * kLog2e : a.scale;
+  uint32_t s_done = 0;      // tiles of this warpgroup so far
+  uint32_t tiles_before = 0;  // of all units
+  uint32_t phase = 0;
+  Walk walk(batch, a, plan, lane);
+  while (walk.next(batch, a, cache.kv_heads, lane)) {
+    if (x == 1 && !walk.two) {
+      tiles_before += walk.tile1 - walk.tile0;
+      continue;
+    }
+    const Pair& pair = walk.pair;
+    const int64_t r64 = static_cast<int64_t>(walk.row_tile) * kRows + x * 128 + thread;
+    const int r = static_cast<int>(min(r64, static_cast<int64_t>(INT32_MAX)));
+    const Row row = row_of(batch, a, pair.begin, pair.count, pair.base, pair.length, r);
+    const int h = walk.head * a.group + r % a.group;
+    const float slope = a.slopes != nullptr ? a.slopes[h] : 0.0f;
+    // queries: the products of the unit before have read theirs (its last s_full)
+    {
+      const uint4* from = reinterpret_cast<const uint4*>(a.q + static_cast<uint64_t>(max(row.token, 0)) * a.q_stride +
+                                                         static_cast<uint64_t>(h) * D);
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i)
+        *reinterpret_cast<uint4*>(sh.q[x] + place_of<D>(thread, i)) = row.token >= 0 ? from[i] : make_uint4(0, 0, 0, 0);
+      fence_async();
+      barrier_arrive(&sh.q_full[x]);
+    }
+    float top = -INFINITY, sum = 0.0f;
+    for (int tile = walk.tile0; tile < walk.tile1; ++tile, ++s_done) {
+      const uint32_t all_done = tiles_before + (tile - walk.tile0);
+      const int stage = all_done % kStages;
+      const int j0 = walk.key_of(tile);
+      if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.s_full[x], s_done & 1, &sh.failed))) return;
+      fence_after();
+      if (kFp8 && !__all_sync(0xFFFFFFFFu, barrier_wait(&sh.v_full[stage], all_done / kStages & 1, &sh.failed))) return;
+      const uint32_t absent = sh.absent[all_done % 4];
+      const float* k_scale = sh.k_scale[all_done % 4];
+      const bool whole = __all_sync(0xFFFFFFFFu, row.token < 0 || (row.lo <= j0 && row.hi >= j0 + kKeys)) && absent == 0;
+      const int c_lo = row.lo - j0, c_hi = row.hi - j0;  // the columns that the row sees
+      auto score_at = [&](uint32_t bits, int c) {
+        float y = __uint_as_float(bits) * (kFp8 ? factor * k_scale[c] : factor);
+        if (!plain) y = score_of(a, y, slope, row.pos - (j0 + c));
+        return y;
+      };
+      auto sees = [&](int c) { return c >= c_lo && c < c_hi && !(absent >> (c / 16) & 1); };
+
+      float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int c = 0; c < kKeys; c += 32) {
+        uint32_t w[32];
+        tensor_load(w, s_at + c);
+        tensor_loaded(w);
+        if (whole) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) tops[i % 4] = fmaxf(tops[i % 4], score_at(w[i], c + i));
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) tops[i % 4] = fmaxf(tops[i % 4], sees(c + i) ? score_at(w[i], c + i) : -INFINITY);
+        }
+      }
+      float best = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+      if (!(best > top + kSlack)) best = top;
+      const bool moves = best > top;
+      if (__any_sync(0xFFFFFFFFu, moves && top > -INFINITY)) {
+        // the product before has to be done with O
+        if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.o_done[x], (s_done - 1) & 1, &sh.failed))) return;
+        fence_after();
+        const float keep = moves ? exp2_approx(top - best) : 1.0f;
+#pragma unroll
+        for (int c = 0; c < D; c += 32) {
+          uint32_t w[32];
+          tensor_load(w, o_at + c);
+          tensor_loaded(w);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) * keep);
+          tensor_store32(o_at + c, w);
+        }
+        sum *= keep;
+      }
+      top = best;
+      const float zero = top == -INFINITY ? 0.0f : top;
+      float sums[4] = {sum, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int c = 0; c < kKeys; c += 32) {
+        uint32_t w[32], p[16];
+        tensor_load(w, s_at + c);
+        tensor_loaded(w);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          float y = score_at(w[i], c + i);
+          if (!whole && !sees(c + i)) y = -INFINITY;
+          y = exp2_approx(y - zero);
+          sums[i % 4] += y;
+          if (kFp8) y = whole || sees(c + i) ? y * sh.v_scale[stage][c + i] : 0.0f;
+          w[i] = __float_as_uint(y);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = pack_bf16(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+        tensor_store16(s_at + c / 2, p);
+      }
+      sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+      tensor_stored();
+      fence_before();
+      barrier_arrive(&sh.p_full[x]);
+    }
+
+    // --- the unit's rows are done, here at least
+    if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.o_done[x], (s_done - 1) & 1, &sh.failed))) return;
+    fence_after();
+    const int c_first = static_cast<int>(walk.unit0 / walk.per), c_last = static_cast<int>((walk.unit0 + pair.tiles - 1) / walk.per);
+    const int self = static_cast<int>(blockIdx.x);
+    const bool shared_unit = c_first != c_last;
+    const bool poisoned = *static_cast<volatile int*>(&sh.poisoned) != 0;
+    const int r_part = x * 128 + thread;
+    Part<D>& part = parts[self == c_first ? 2 * self + 1 : 2 * self];
+    const bool some = top > -INFINITY || sum != sum;
+    const float inv = some ? 1.0f / sum : 0.0f;
+    uint16_t* out = a.out + static_cast<uint64_t>(max(row.token, 0)) * a.out_stride + static_cast<uint64_t>(h) * D;
+#pragma unroll
+    for (int c = 0; c < D; c += 32) {
+      uint32_t w[32];
+      __syncwarp();
+      tensor_load(w, o_at + c);
+      tensor_loaded(w);
+      if (poisoned && row.token >= 0) {
+        for (int tile = walk.tile0; tile < walk.tile1; ++tile) {
+          if (!walk.edge(tile)) continue;
+          const int j0 = walk.key_of(tile);
+          for (int j = max(j0, row.lo); j < min(j0 + kKeys, row.hi); ++j) {
+            const int page = page_of(cache, batch, walk.seq, j);
+            if (page < 0) continue;
+            const uint64_t at = page * cache.page_stride +
+                                ((static_cast<uint64_t>(walk.head) << cache.page_shift) + (j & ((1 << cache.page_shift) - 1))) * D + c;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              float v;
+              if (kFp8) v = __uint_as_float(bf16_of_e4m3(static_cast<const uint8_t*>(cache.v)[at + i]) << 16);
+              else v = __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(cache.v)[at + i]) << 16);
+              if (!(fabsf(v) <= FLT_MAX)) w[i] = __float_as_uint(__uint_as_float(w[i]) + v);
+            }
+          }
+        }
+      }
+      if (row.token < 0) continue;
+      if (shared_unit) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(&part.o[r_part][c + i]) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 32; i += 8) {
+          uint32_t y[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            y[e] = some ? pack_bf16(__uint_as_float(w[i + 2 * e]) * inv, __uint_as_float(w[i + 2 * e + 1]) * inv) : 0u;
+          *reinterpret_cast<uint4*>(out + c + i) = make_uint4(y[0], y[1], y[2], y[3]);
+        }
+      }
+    }
+    if (shared_unit) {
+      if (row.token >= 0) {
+        part.top[r_part] = top;
+        part.sum[r_part] = sum;
+      }
+      __threadfence();
+      if (!group_sync(sh, x, phase)) return;
+      if (thread == 0) {
+        const uint32_t before = atomicAdd(&counters[2 * c_first + x], 1u);
+        sh.last[x] = before == static_cast<uint32_t>(c_last - c_first);
+        if (sh.last[x]) counters[2 * c_first + x] = 0;
+        __threadfence();
+      }
+      if (!group_sync(sh, x, phase)) return;
+      if (sh.last[x]) {
+        // a warp for each row, a lane for D / 32 of its elements
+        constexpr int kPer = D / 32;
+        const int rows = min(128, pair.rows - x * 128);
+        for (int q = thread / 32; q < rows; q += 4) {
+          const int n = c_last - c_first + 1, at = x * 128 + q;
+          auto part_of = [&](int i) -> const Part<D>& { return parts[2 * (c_first + i) + (i == 0)]; };
+          float most = -INFINITY, l = 0.0f, y[kPer] = {};
+          for (int i = lane; i < n; i += 32) most = fmaxf(most, __ldcg(&part_of(i).top[at]));
+#pragma unroll
+          for (int m = 16; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, m));
+          const float z = most == -INFINITY ? 0.0f : most;
+          for (int i0 = 0; i0 < n; i0 += 32) {
+            const int count = min(n - i0, 32);
+            float f = 0.0f;
+            if (lane < count) {
+              f = exp2_approx(__ldcg(&part_of(i0 + lane).top[at]) - z);
+              l += __ldcg(&part_of(i0 + lane).sum[at]) * f;
+            }
+#pragma unroll 4
+            for (int i = 0; i < count; ++i) {
+              const float g = __shfl_sync(0xFFFFFFFFu, f, i);
+              const float* from = &part_of(i0 + i).o[at][lane * kPer];
+#pragma unroll
+              for (int e = 0; e < kPer; ++e) y[e] += __ldcg(from + e) * g;
+            }
+          }
+#pragma unroll
+          for (int m = 16; m > 0; m >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, m);
+          const int64_t rr = static_cast<int64_t>(walk.row_tile) * kRows + at;
+          const int token = pair.begin + static_cast<int>(rr / a.group), hh = walk.head * a.group + static_cast<int>(rr % a.group);
+          const bool any = most > -INFINITY || l != l;
+          const float i1 = any ? 1.0f / l : 0.0f;
+          uint32_t* to = reinterpret_cast<uint32_t*>(a.out + static_cast<uint64_t>(token) * a.out_stride + static_cast<uint64_t>(hh) * D + lane * kPer);
+#pragma unroll
+          for (int e = 0; e < kPer / 2; ++e) to[e] = any ? pack_bf16(y[2 * e] * i1, y[2 * e + 1] * i1) : 0u;
+          if (lane == 0 && a.lse != nullptr)
+            a.lse[static_cast<uint64_t>(token) * a.q_heads + hh] = any ? most * kLn2 + logf(l) : -INFINITY;
+        }
+      }
+      if (!group_sync(sh, x, phase)) return;  // sh.last has been read
+    } else if (row.token >= 0 && a.lse != nullptr) {
+      a.lse[static_cast<uint64_t>(row.token) * a.q_heads + h] = some ? top * kLn2 + logf(sum) : -INFINITY;
+    }
+    __syncwarp();
+    fence_before();  // before the next unit's products write O
+    tiles_before += walk.tile1 - walk.tile0;
+  }
+}
+
+template <bool kFp8>
+constexpr int threads_of() { return kFp8 ? 416 : 384; }
+
+template <int D, bool kFp8>
+__global__ void __launch_bounds__(threads_of<kFp8>(), 1)
+many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArgs a, const Plan* plan, uint32_t* counters,
+                 int* flag, Part<D>* parts, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+  extern __shared__ uint8_t raw[];
+  Shared<D>& sh = *reinterpret_cast<Shared<D>*>(raw + ((1024 - (shared_address(raw) & 1023)) & 1023));
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      barrier_init(&sh.q_full[i], 128);
+      barrier_init(&sh.s_full[i], 2);
+      barrier_init(&sh.p_full[i], 128);
+      barrier_init(&sh.o_done[i], 1);
+      barrier_init(&sh.group[i], 128);
+    }
+    for (int i = 0; i < kStages; ++i) {
+      barrier_init(&sh.k_full[i], kFp8 ? 128 : 1);
+      barrier_init(&sh.k_empty[i], 1);
+      barrier_init(&sh.v_full[i], kFp8 ? 128 : 1);
+      barrier_init(&sh.v_empty[i], 1);
+      barrier_init(&sh.v_fixed[i], 64);
+    }
+    barrier_init(&sh.drained, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    sh.failed = 0;
+    sh.poisoned = 0;
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(shared_address(&sh.tensor)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  wait_for_previous();
+
+  if (warp < 8) {
+    soften<D, kFp8>(sh, cache, batch, a, plan, counters, parts, warp / 4, threadIdx.x % 128, lane);
+  } else if (warp == 8) {
+    issue_products<D, kFp8>(sh, cache, batch, a, plan, lane);
+    if (lane == 0) commit(&sh.drained);  // no product outlives the tensor memory
+    __syncwarp();
+    barrier_settle(&sh.drained, 0);
+  } else if (kFp8) {
+    convert_tiles<D>(sh, cache, batch, a, plan, threadIdx.x - 9 * 32, lane);
+  } else if (warp == 9) {
+    copy_tiles<D>(sh, cache, batch, a, plan, &k_map, &v_map, lane);
+  } else {
+    fix_tiles<D>(sh, cache, batch, a, plan, threadIdx.x - 10 * 32, lane);
+  }
+  __syncwarp();
+  let_next_start();
+  fence_before();
+  __syncthreads();
+  fence_after();
+  if (threadIdx.x == 0 && sh.failed) *flag = 1;
+  if (warp == 8)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tensor) : "memory");
+}
+
+constexpr uint64_t kPlanBytes = (sizeof(Plan) + 255) / 256 * 256;
+
+template <int D, bool kFp8>
+cudaError_t launch(const CacheView& cache, const CUtensorMap* maps, const BatchView& batch, const AttentionArgs& args,
+                   char* workspace, uint32_t* counters, int* flag, cudaStream_t stream) {
+  auto kernel = many_rows_kernel<D, kFp8>;
+  constexpr int kShared = static_cast<int>(sizeof(Shared<D>)) + 1024;
+  int device = 0;
+  cudaGetDevice(&device);
+  // SMs of each device whose kernel has been given its shared memory
+  static std::atomic<int> sms_of[64];
+  int sms = device < 64 ? sms_of[device].load(std::memory_order_relaxed) : 0;
+  if (sms == 0) {
+    cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
+    if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (err != cudaSuccess) {
+      cudaGetLastError();
+      return err;
+    }
+    if (device < 64) sms_of[device].store(sms, std::memory_order_relaxed);
+  }
+  const int grid = std::min(sms, kMaxGrid);
+  Plan* plan = reinterpret_cast<Plan*>(workspace);
+  const cudaError_t err = launch_early(plan_kernel, 1, kPlanThreads, 0, stream, batch, args, cache.kv_heads, grid, plan);
+  if (err != cudaSuccess) return err;
+  return launch_early(kernel, grid, threads_of<kFp8>(), kShared, stream, cache, batch, args, static_cast<const Plan*>(plan), counters,
+                      flag, reinterpret_cast<Part<D>*>(workspace + kPlanBytes), maps[0], maps[1]);
+}
+
+}  // namespace
+
+uint64_t many_rows_workspace_bytes(int head_dim) {
+  return kPlanBytes + 2 * kMaxGrid * (head_dim == 128 ? sizeof(Part<128>) : sizeof(Part<64>));
+}
+
+cudaError_t launch_many_rows(const CacheView& cache, const CUtensorMap* maps, bool fp8, int head_dim, const BatchView& batch,
+                             const AttentionArgs& args, char* workspace, uint32_t* counters, int* flag, cudaStream_t stream) {
+  auto f = head_dim == 128 ? (fp8 ? launch<128, true> : launch<128, false>) : (fp8 ? launch<64, true> : launch<64, false>);
+  return f(cache, maps, batch, args, workspace, counters, flag, stream);
+}
+
+}  // namespace esopt

@@ -17,6 +17,7 @@ struct es_cache {
   int page_size;
   int head_dim;
   esopt::CacheView view;
+  CUtensorMap maps[2];  // of k and v; bf16 only
 };
 
 namespace {
@@ -108,6 +109,26 @@ es_status_t check_stride(uint64_t stride, int heads, int head_dim, const char* c
   return ES_OK;
 }
 
+// Pages as [page][head and slot][element], read in boxes of one page of a head by 64 elements
+// (128 bytes, swizzled); pages past the last one read as zeros.
+es_status_t make_map(CUtensorMap* map, void* base, const es_cache_desc_t& d, const char* call) {
+  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  void* found = nullptr;
+  cudaDriverEntryPointQueryResult result;
+  const cudaError_t err = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &found, 12000, cudaEnableDefault, &result);
+  if (err != cudaSuccess || found == nullptr) return cuda_fail(err != cudaSuccess ? err : cudaErrorNotSupported, "cuTensorMapEncodeTiled");
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d.head_dim), static_cast<cuuint64_t>(d.kv_heads) * d.page_size, d.num_pages};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(d.head_dim) * 2, d.page_stride * 2};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(d.page_size), 1}, steps[3] = {1, 1, 1};
+  const CUresult made = reinterpret_cast<Encode>(found)(
+      map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (made != CUDA_SUCCESS) return fail(ES_ERR_CUDA, "%s: cuTensorMapEncodeTiled returned %d", call, static_cast<int>(made));
+  return ES_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -133,7 +154,7 @@ es_status_t es_cache_create(const es_cache_desc_t* d, es_cache_t* out) {
   if (d->num_pages < 1 || d->num_pages > static_cast<uint64_t>(INT32_MAX))
     return fail(ES_ERR_INVALID_ARG, "%s: num_pages is not within 1 .. 2^31 - 1", call);
   const uint64_t tokens = static_cast<uint64_t>(d->kv_heads) * d->page_size;
-  if (d->page_stride < tokens * d->head_dim || d->page_stride > (uint64_t{1} << 40))
+  if (d->page_stride < tokens * d->head_dim || d->page_stride > (uint64_t{1} << 38))
     return fail(ES_ERR_INVALID_ARG, "%s: page_stride is less than a page or out of range", call);
   if (d->page_stride % (fp8 ? 16 : 8) != 0)
     return fail(ES_ERR_ALIGNMENT, "%s: page_stride is not a multiple of 16 bytes", call);
@@ -163,6 +184,10 @@ es_status_t es_cache_create(const es_cache_desc_t* d, es_cache_t* out) {
   c->head_dim = d->head_dim;
   c->view = esopt::CacheView{d->k, d->v, d->k_scale, d->v_scale, d->page_stride, d->scale_stride,
                              static_cast<int>(d->num_pages), shift, d->kv_heads};
+  if (!fp8 && ((st = make_map(&c->maps[0], d->k, *d, call)) != ES_OK || (st = make_map(&c->maps[1], d->v, *d, call)) != ES_OK)) {
+    delete c;
+    return st;
+  }
   *out = c;
   return ok();
 }
@@ -263,7 +288,7 @@ es_status_t es_attention(es_cache_t cache, const es_batch_t* batch, const es_att
                                   a->lse, a->slopes, a->first, a->last, a->q_stride, a->out_stride,
                                   a->q_heads, a->q_heads / cache->view.kv_heads, a->window,
                                   a->scale, a->softcap};
-  const cudaError_t err = esopt::launch_attention(cache->view, cache->dtype == ES_FP8_E4M3, d, b,
+  const cudaError_t err = esopt::launch_attention(cache->view, cache->maps, cache->dtype == ES_FP8_E4M3, d, b,
                                                   args, workspace, static_cast<cudaStream_t>(stream));
   if (err != cudaSuccess) return cuda_fail(err, call);
   return ok();
@@ -273,7 +298,7 @@ uint64_t es_attention_workspace(es_cache_t cache, int q_heads) {
   if (cache == nullptr || q_heads < 1 || q_heads % cache->view.kv_heads != 0 ||
       q_heads / cache->view.kv_heads > 16)
     return 0;
-  return esopt::attention_workspace_bytes(cache->head_dim, q_heads / cache->view.kv_heads);
+  return esopt::attention_workspace_bytes(cache->head_dim);
 }
 
 }  // extern "C"

@@ -1,6 +1,7 @@
 // Shared by the rollout operators' host layer and kernels.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -117,8 +118,9 @@ cudaError_t launch_append(const CacheView& cache, bool fp8, int head_dim, const 
                           const AppendArgs& args, cudaStream_t stream);
 cudaError_t launch_read(const CacheView& cache, bool fp8, int head_dim, const BatchView& batch,
                         uint16_t* k_out, uint16_t* v_out, cudaStream_t stream);
-cudaError_t launch_attention(const CacheView& cache, bool fp8, int head_dim, const BatchView& batch,
+// maps: of the keys and the values of a bf16 cache, for TMA.
+cudaError_t launch_attention(const CacheView& cache, const CUtensorMap* maps, bool fp8, int head_dim, const BatchView& batch,
                              const AttentionArgs& args, void* workspace, cudaStream_t stream);
-uint64_t attention_workspace_bytes(int head_dim, int group);
+uint64_t attention_workspace_bytes(int head_dim);
 
 }  // namespace esopt
