@@ -463,7 +463,8 @@ __device__ void copy_tiles(Shared<D>& sh, const CacheView& cache, const BatchVie
 
 // bf16 values of tiles at the ends of intervals: those that no row sees become zeros, and
 // infinities and NaN too (a product with p = 0 would carry them into rows that do not see
-// them); the rows that see them get them when the unit is written.
+// them); the rows that see them get them when the unit is written. Every tile passes here,
+// so that the barriers of the stages are never a round ahead.
 template <int D>
 __device__ void fix_tiles(Shared<D>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
                           const Plan* plan, int thread, int lane) {
@@ -471,29 +472,31 @@ __device__ void fix_tiles(Shared<D>& sh, const CacheView& cache, const BatchView
   Walk walk(batch, a, plan, lane);
   while (walk.next(batch, a, cache.kv_heads, lane)) {
     for (int tile = walk.tile0; tile < walk.tile1; ++tile, ++done) {
-      if (!walk.edge(tile)) continue;
       const int stage = done % kStages, j0 = walk.key_of(tile);
-      if (!barrier_wait(&sh.v_full[stage], done / kStages & 1, &sh.failed)) return;
-      for (int i = thread; i < kKeys * D / 8; i += 64) {
-        const int key = i / (D / 8), j = j0 + key;
-        uint4* at = reinterpret_cast<uint4*>(sh.v[stage] + place_of<D>(key, i % (D / 8)));
-        if (j < walk.pair.lo || j >= walk.pair.hi) {
-          *at = make_uint4(0, 0, 0, 0);
-          continue;
-        }
-        uint4 w = *at;
-        if (has_nonfinite(w.x) || has_nonfinite(w.y) || has_nonfinite(w.z) || has_nonfinite(w.w)) {
-          uint32_t* u = reinterpret_cast<uint32_t*>(&w);
-          for (int e = 0; e < 4; ++e) {
-            if ((u[e] & 0x7F80u) == 0x7F80u) u[e] &= 0xFFFF0000u;
-            if ((u[e] & 0x7F800000u) == 0x7F800000u) u[e] &= 0xFFFFu;
+      if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.v_full[stage], done / kStages & 1, &sh.failed))) return;
+      if (walk.edge(tile)) {
+        for (int i = thread; i < kKeys * D / 8; i += 64) {
+          const int key = i / (D / 8), j = j0 + key;
+          uint4* at = reinterpret_cast<uint4*>(sh.v[stage] + place_of<D>(key, i % (D / 8)));
+          if (j < walk.pair.lo || j >= walk.pair.hi) {
+            *at = make_uint4(0, 0, 0, 0);
+            continue;
           }
-          *at = w;
-          *static_cast<volatile int*>(&sh.poisoned) = 1;
+          uint4 w = *at;
+          if (has_nonfinite(w.x) || has_nonfinite(w.y) || has_nonfinite(w.z) || has_nonfinite(w.w)) {
+            uint32_t* u = reinterpret_cast<uint32_t*>(&w);
+            for (int e = 0; e < 4; ++e) {
+              if ((u[e] & 0x7F80u) == 0x7F80u) u[e] &= 0xFFFF0000u;
+              if ((u[e] & 0x7F800000u) == 0x7F800000u) u[e] &= 0xFFFFu;
+            }
+            *at = w;
+            *static_cast<volatile int*>(&sh.poisoned) = 1;
+          }
         }
+        fence_async();
       }
-      fence_async();
-      barrier_arrive(&sh.v_fixed[stage]);
+      __syncwarp();
+      if (lane == 0) barrier_arrive(&sh.v_fixed[stage]);
     }
   }
 }
@@ -592,7 +595,7 @@ __device__ void issue_products(Shared<D>& sh, const CacheView& cache, const Batc
   constexpr uint32_t kScores = product_of(kKeys, false), kValues = product_of(D, true);
   const uint32_t tensor = sh.tensor;
   uint32_t k_done = 0, v_done = 0, units = 0, two_units = 0;
-  uint32_t p_done[2] = {0, 0}, fixed[kStages] = {};
+  uint32_t p_done[2] = {0, 0};
   auto scores = [&](int x, int stage) {
     if (lane == 0) {
       const uint32_t q = shared_address(sh.q[x]), k = shared_address(sh.k[stage]);
@@ -626,12 +629,8 @@ __device__ void issue_products(Shared<D>& sh, const CacheView& cache, const Batc
         if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.p_full[x], p_done[x] & 1, &sh.failed))) return;
         ++p_done[x];
         if (x == 0) {
-          if (!kFp8 && walk.edge(tile)) {
-            if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.v_fixed[stage], fixed[stage] & 1, &sh.failed))) return;
-            ++fixed[stage];
-          } else if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.v_full[stage], v_done / kStages & 1, &sh.failed))) {
-            return;
-          }
+          uint64_t* ready = kFp8 ? &sh.v_full[stage] : &sh.v_fixed[stage];
+          if (!__all_sync(0xFFFFFFFFu, barrier_wait(ready, v_done / kStages & 1, &sh.failed))) return;
         }
         fence_after();
         if (lane == 0) {
@@ -662,13 +661,12 @@ __device__ void issue_products(Shared<D>& sh, const CacheView& cache, const Batc
 }
 
 // A warpgroup's rows: a thread for each.
-template <int D, bool kFp8>
+template <int D, bool kFp8, bool kPlain>
 __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
                        const Plan* plan, uint32_t* counters, Part<D>* parts, int x, int thread, int lane) {
   const uint32_t lanes = static_cast<uint32_t>(thread / 32 * 32) << 16;
   const uint32_t s_at = sh.tensor + lanes + x * 128, o_at = sh.tensor + lanes + 256 + x * 128;
-  const bool plain = a.softcap <= 0.0f && a.slopes == nullptr;
-  const float factor = plain ? a.scale * kLog2e : a.scale;
+  const float factor = kPlain ? a.scale * kLog2e : a.scale;
   uint32_t s_done = 0;      // tiles of this warpgroup so far
   uint32_t tiles_before = 0;  // of all units
   uint32_t phase = 0;
@@ -703,29 +701,57 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
       fence_after();
       if (kFp8 && !__all_sync(0xFFFFFFFFu, barrier_wait(&sh.v_full[stage], all_done / kStages & 1, &sh.failed))) return;
       const uint32_t absent = sh.absent[all_done % 4];
-      const float* k_scale = sh.k_scale[all_done % 4];
       const bool whole = __all_sync(0xFFFFFFFFu, row.token < 0 || (row.lo <= j0 && row.hi >= j0 + kKeys)) && absent == 0;
-      const int c_lo = row.lo - j0, c_hi = row.hi - j0;  // the columns that the row sees
-      auto score_at = [&](uint32_t bits, int c) {
-        float y = __uint_as_float(bits) * (kFp8 ? factor * k_scale[c] : factor);
-        if (!plain) y = score_of(a, y, slope, row.pos - (j0 + c));
-        return y;
-      };
-      auto sees = [&](int c) { return c >= c_lo && c < c_hi && !(absent >> (c / 16) & 1); };
-
       float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      float unit;  // of what S holds, in scores
+      if (!kFp8 && kPlain && whole) {
+        unit = factor;
 #pragma unroll
-      for (int c = 0; c < kKeys; c += 32) {
-        uint32_t w[32];
-        tensor_load(w, s_at + c);
-        tensor_loaded(w);
-        if (whole) {
+        for (int c = 0; c < kKeys; c += 32) {
+          uint32_t w[32];
+          tensor_load(w, s_at + c);
+          tensor_loaded(w);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) tops[i % 4] = fmaxf(tops[i % 4], score_at(w[i], c + i));
-        } else {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) tops[i % 4] = fmaxf(tops[i % 4], sees(c + i) ? score_at(w[i], c + i) : -INFINITY);
+          for (int i = 0; i < 32; ++i) tops[i % 4] = fmaxf(tops[i % 4], __uint_as_float(w[i]));
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tops[i] *= factor;
+      } else {
+        // scores that take more than a factor are made once and put back
+        unit = 1.0f;
+        const int c_lo = row.lo - j0, c_hi = row.hi - j0;  // the columns that the row sees
+#pragma unroll 1
+        for (int c = 0; c < kKeys; c += 32) {
+          uint32_t w[32];
+          tensor_load(w, s_at + c);
+          tensor_loaded(w);
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            float f[4] = {factor, factor, factor, factor};
+            if (kFp8) {
+              const float4 k = *reinterpret_cast<const float4*>(&sh.k_scale[all_done % 4][c + i]);
+              f[0] *= k.x;
+              f[1] *= k.y;
+              f[2] *= k.z;
+              f[3] *= k.w;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float y = __uint_as_float(w[i + e]) * f[e];
+              if (!kPlain) y = score_of(a, y, slope, row.pos - (j0 + c + i + e));
+              w[i + e] = __float_as_uint(y);
+            }
+          }
+          if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (!(c + i >= c_lo && c + i < c_hi) || (absent >> ((c + i) / 16) & 1)) w[i] = __float_as_uint(-INFINITY);
+          }
+#pragma unroll
+          for (int i = 0; i < 32; ++i) tops[i % 4] = fmaxf(tops[i % 4], __uint_as_float(w[i]));
+          tensor_store32(s_at + c, w);
+        }
+        tensor_stored();
       }
       float best = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
       if (!(best > top + kSlack)) best = top;
@@ -756,12 +782,22 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
         tensor_loaded(w);
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-          float y = score_at(w[i], c + i);
-          if (!whole && !sees(c + i)) y = -INFINITY;
-          y = exp2_approx(y - zero);
+          const float y = exp2_approx(fmaf(__uint_as_float(w[i]), unit, -zero));
           sums[i % 4] += y;
-          if (kFp8) y = whole || sees(c + i) ? y * sh.v_scale[stage][c + i] : 0.0f;
           w[i] = __float_as_uint(y);
+        }
+        if (kFp8) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(&sh.v_scale[stage][c + i]);
+            const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float y = __uint_as_float(w[i + e]);
+              // an infinite scale stays with the rows that see its key
+              w[i + e] = __float_as_uint(whole || y > 0.0f ? y * f[e] : 0.0f);
+            }
+          }
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) p[i] = pack_bf16(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
@@ -892,7 +928,8 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
 template <bool kFp8>
 constexpr int threads_of() { return kFp8 ? 416 : 384; }
 
-template <int D, bool kFp8>
+// kPlain: scores are scale q.k, with scale > 0, alone.
+template <int D, bool kFp8, bool kPlain>
 __global__ void __launch_bounds__(threads_of<kFp8>(), 1)
 many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArgs a, const Plan* plan, uint32_t* counters,
                  int* flag, Part<D>* parts, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
@@ -912,7 +949,7 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
       barrier_init(&sh.k_empty[i], 1);
       barrier_init(&sh.v_full[i], kFp8 ? 128 : 1);
       barrier_init(&sh.v_empty[i], 1);
-      barrier_init(&sh.v_fixed[i], 64);
+      barrier_init(&sh.v_fixed[i], 2);
     }
     barrier_init(&sh.drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -929,7 +966,7 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
   wait_for_previous();
 
   if (warp < 8) {
-    soften<D, kFp8>(sh, cache, batch, a, plan, counters, parts, warp / 4, threadIdx.x % 128, lane);
+    soften<D, kFp8, kPlain>(sh, cache, batch, a, plan, counters, parts, warp / 4, threadIdx.x % 128, lane);
   } else if (warp == 8) {
     issue_products<D, kFp8>(sh, cache, batch, a, plan, lane);
     if (lane == 0) commit(&sh.drained);  // no product outlives the tensor memory
@@ -954,10 +991,10 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
 
 constexpr uint64_t kPlanBytes = (sizeof(Plan) + 255) / 256 * 256;
 
-template <int D, bool kFp8>
-cudaError_t launch(const CacheView& cache, const CUtensorMap* maps, const BatchView& batch, const AttentionArgs& args,
+template <int D, bool kFp8, bool kPlain>
+cudaError_t launch_kernel(const CacheView& cache, const CUtensorMap* maps, const BatchView& batch, const AttentionArgs& args,
                    char* workspace, uint32_t* counters, int* flag, cudaStream_t stream) {
-  auto kernel = many_rows_kernel<D, kFp8>;
+  auto kernel = many_rows_kernel<D, kFp8, kPlain>;
   constexpr int kShared = static_cast<int>(sizeof(Shared<D>)) + 1024;
   int device = 0;
   cudaGetDevice(&device);
@@ -979,6 +1016,14 @@ cudaError_t launch(const CacheView& cache, const CUtensorMap* maps, const BatchV
   if (err != cudaSuccess) return err;
   return launch_early(kernel, grid, threads_of<kFp8>(), kShared, stream, cache, batch, args, static_cast<const Plan*>(plan), counters,
                       flag, reinterpret_cast<Part<D>*>(workspace + kPlanBytes), maps[0], maps[1]);
+}
+
+template <int D, bool kFp8>
+cudaError_t launch(const CacheView& cache, const CUtensorMap* maps, const BatchView& batch, const AttentionArgs& args,
+                   char* workspace, uint32_t* counters, int* flag, cudaStream_t stream) {
+  const bool plain = args.softcap <= 0.0f && args.slopes == nullptr && args.scale > 0.0f;
+  return plain ? launch_kernel<D, kFp8, true>(cache, maps, batch, args, workspace, counters, flag, stream)
+               : launch_kernel<D, kFp8, false>(cache, maps, batch, args, workspace, counters, flag, stream);
 }
 
 }  // namespace
