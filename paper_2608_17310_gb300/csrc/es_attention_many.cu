@@ -38,6 +38,9 @@ constexpr int kKeys = 128;   // of a tile
 constexpr int kRows = 256;   // of a unit
 constexpr int kStages = 2;
 constexpr int kMaxGrid = 192;
+// What a unit costs beside its tiles, in tiles: its queries, the first tile's way through the
+// pipeline, its results.
+constexpr int kUnitCost = 2;
 constexpr float kSlack = 8.0f;  // log 2 of how far a score may be above the kept maximum
 
 // Where a block's range begins, from the planning kernel.
@@ -190,7 +193,7 @@ plan_kernel(const BatchView batch, const AttentionArgs a, int kv_heads, int grid
         }
         if (p < pairs) n = tiles[threadIdx.x];
       }
-      const int64_t mine = static_cast<int64_t>(n) * kv_heads;
+      const int64_t mine = p < pairs ? static_cast<int64_t>(n + kUnitCost) * kv_heads : 0;
       int64_t more;
       const int64_t at = done + scan_block(mine, sums, more);
       if (pass == 1)
@@ -365,7 +368,7 @@ struct Walk {
   Pair pair;
   // the unit
   int head, tile0, tile1;
-  int64_t unit0;
+  int64_t unit0;  // of its first tile
   bool two;  // more than 128 rows
 
   __device__ __forceinline__ Walk(const BatchView& b, const AttentionArgs& a, const Plan* plan, int lane) {
@@ -382,8 +385,8 @@ struct Walk {
   }
   __device__ __forceinline__ bool next(const BatchView& b, const AttentionArgs& a, int kv_heads, int lane) {
     if (at >= end) return false;
-    while (at >= pair_tile + static_cast<int64_t>(pair.tiles) * kv_heads) {
-      pair_tile += static_cast<int64_t>(pair.tiles) * kv_heads;
+    while (at >= pair_tile + static_cast<int64_t>(pair.tiles + kUnitCost) * kv_heads) {
+      pair_tile += static_cast<int64_t>(pair.tiles + kUnitCost) * kv_heads;
       ++row_tile;
       while (row_tile >= row_tiles_of(b, a, seq)) {
         ++seq;
@@ -391,13 +394,14 @@ struct Walk {
       }
       pair = pair_of<32>(b, a, seq, row_tile, lane);
     }
-    head = static_cast<int>((at - pair_tile) / pair.tiles);
-    unit0 = pair_tile + static_cast<int64_t>(head) * pair.tiles;
-    tile0 = static_cast<int>(at - unit0);
+    const int length = pair.tiles + kUnitCost;
+    head = static_cast<int>((at - pair_tile) / length);
+    unit0 = pair_tile + static_cast<int64_t>(head) * length + kUnitCost;
+    tile0 = static_cast<int>(max(at - unit0, static_cast<int64_t>(0)));
     tile1 = static_cast<int>(min(unit0 + pair.tiles, end) - unit0);
     at = unit0 + tile1;
     two = pair.rows > 128;
-    return true;
+    return tile1 > tile0;  // else the range ends in what comes before the unit's tiles
   }
   __device__ __forceinline__ int key_of(int tile) const { return (pair.lo & ~(kKeys - 1)) + tile * kKeys; }
   // Not every row sees all of the tile.
@@ -660,6 +664,49 @@ __device__ void issue_products(Shared<D>& sh, const CacheView& cache, const Batc
   }
 }
 
+__device__ __forceinline__ uint64_t pack(float lo, float hi) {
+  uint64_t y;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(lo), "f"(hi));
+  return y;
+}
+__device__ __forceinline__ void unpack(uint64_t x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t y;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
+  return y;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t y;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+  return y;
+}
+
+// 16 bytes to shared memory without a register in between; zeros where `from` is not to be read.
+__device__ __forceinline__ void copy_async(uint32_t to, const void* from, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+
+// This thread's row of the walk's unit, and its query on the way to shared memory.
+template <int D>
+__device__ __forceinline__ Row take_row(Shared<D>& sh, const BatchView& batch, const AttentionArgs& a, const Walk& walk, int x,
+                                        int thread, int& h) {
+  const Pair& pair = walk.pair;
+  const int r = walk.row_tile * kRows + x * 128 + thread;
+  const Row row = row_of(batch, a, pair.begin, pair.count, pair.base, pair.length, r);
+  h = walk.head * a.group + r % a.group;
+  const uint16_t* from = a.q + static_cast<uint64_t>(max(row.token, 0)) * a.q_stride + static_cast<uint64_t>(h) * D;
+#pragma unroll
+  for (int i = 0; i < D / 8; ++i) copy_async(shared_address(sh.q[x] + place_of<D>(thread, i)), from + i * 8, row.token >= 0);
+  asm volatile("cp.async.commit_group;" ::: "memory");
+  return row;
+}
+template <int D>
+__device__ __forceinline__ void hand_over(Shared<D>& sh, int x) {
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  fence_async();
+  barrier_arrive(&sh.q_full[x]);
+}
+
 // A warpgroup's rows: a thread for each.
 template <int D, bool kFp8, bool kPlain>
 __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
@@ -667,31 +714,35 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
   const uint32_t lanes = static_cast<uint32_t>(thread / 32 * 32) << 16;
   const uint32_t s_at = sh.tensor + lanes + x * 128, o_at = sh.tensor + lanes + 256 + x * 128;
   const float factor = kPlain ? a.scale * kLog2e : a.scale;
-  uint32_t s_done = 0;      // tiles of this warpgroup so far
+  uint32_t s_done = 0;        // tiles of this warpgroup so far
   uint32_t tiles_before = 0;  // of all units
   uint32_t phase = 0;
-  Walk walk(batch, a, plan, lane);
-  while (walk.next(batch, a, cache.kv_heads, lane)) {
-    if (x == 1 && !walk.two) {
-      tiles_before += walk.tile1 - walk.tile0;
-      continue;
+  Walk next(batch, a, plan, lane);
+  // The next unit in which this warpgroup has rows. Its queries are fetched while the unit
+  // before is finished.
+  auto find = [&](uint32_t& skipped) {
+    skipped = 0;
+    while (next.next(batch, a, cache.kv_heads, lane)) {
+      if (x == 0 || next.two) return true;
+      skipped += next.tile1 - next.tile0;
     }
+    return false;
+  };
+  uint32_t skipped;
+  bool more = find(skipped);
+  Row row_next{};
+  int h_next = 0;
+  if (more) {
+    row_next = take_row<D>(sh, batch, a, next, x, thread, h_next);
+    hand_over<D>(sh, x);
+  }
+  while (more) {
+    const Walk walk = next;
     const Pair& pair = walk.pair;
-    const int64_t r64 = static_cast<int64_t>(walk.row_tile) * kRows + x * 128 + thread;
-    const int r = static_cast<int>(min(r64, static_cast<int64_t>(INT32_MAX)));
-    const Row row = row_of(batch, a, pair.begin, pair.count, pair.base, pair.length, r);
-    const int h = walk.head * a.group + r % a.group;
-    const float slope = a.slopes != nullptr ? a.slopes[h] : 0.0f;
-    // queries: the products of the unit before have read theirs (its last s_full)
-    {
-      const uint4* from = reinterpret_cast<const uint4*>(a.q + static_cast<uint64_t>(max(row.token, 0)) * a.q_stride +
-                                                         static_cast<uint64_t>(h) * D);
-#pragma unroll
-      for (int i = 0; i < D / 8; ++i)
-        *reinterpret_cast<uint4*>(sh.q[x] + place_of<D>(thread, i)) = row.token >= 0 ? from[i] : make_uint4(0, 0, 0, 0);
-      fence_async();
-      barrier_arrive(&sh.q_full[x]);
-    }
+    const Row row = row_next;
+    const int h = h_next;
+    tiles_before += skipped;
+    const float slope = !kPlain && a.slopes != nullptr ? a.slopes[h] : 0.0f;
     float top = -INFINITY, sum = 0.0f;
     for (int tile = walk.tile0; tile < walk.tile1; ++tile, ++s_done) {
       const uint32_t all_done = tiles_before + (tile - walk.tile0);
@@ -702,23 +753,10 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
       if (kFp8 && !__all_sync(0xFFFFFFFFu, barrier_wait(&sh.v_full[stage], all_done / kStages & 1, &sh.failed))) return;
       const uint32_t absent = sh.absent[all_done % 4];
       const bool whole = __all_sync(0xFFFFFFFFu, row.token < 0 || (row.lo <= j0 && row.hi >= j0 + kKeys)) && absent == 0;
+      const bool direct = !kFp8 && kPlain && whole;
       float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-      float unit;  // of what S holds, in scores
-      if (!kFp8 && kPlain && whole) {
-        unit = factor;
-#pragma unroll
-        for (int c = 0; c < kKeys; c += 32) {
-          uint32_t w[32];
-          tensor_load(w, s_at + c);
-          tensor_loaded(w);
-#pragma unroll
-          for (int i = 0; i < 32; ++i) tops[i % 4] = fmaxf(tops[i % 4], __uint_as_float(w[i]));
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tops[i] *= factor;
-      } else {
-        // scores that take more than a factor are made once and put back
-        unit = 1.0f;
+      if (!direct) {
+        // scores that take more than a factor are made here and put back
         const int c_lo = row.lo - j0, c_hi = row.hi - j0;  // the columns that the row sees
 #pragma unroll 1
         for (int c = 0; c < kKeys; c += 32) {
@@ -753,6 +791,20 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
         }
         tensor_stored();
       }
+      uint32_t w[kKeys / 32][32];
+#pragma unroll
+      for (int c = 0; c < kKeys / 32; ++c) tensor_load(w[c], s_at + c * 32);
+#pragma unroll
+      for (int c = 0; c < kKeys / 32; ++c) tensor_loaded(w[c]);
+      const float unit = direct ? factor : 1.0f;  // of what S holds, in scores
+      if (direct) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 2)
+#pragma unroll
+          for (int c = 0; c < kKeys / 32; ++c) tops[c] = fmaxf(tops[c], fmaxf(__uint_as_float(w[c][i]), __uint_as_float(w[c][i + 1])));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tops[i] *= factor;
+      }
       float best = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
       if (!(best > top + kSlack)) best = top;
       const bool moves = best > top;
@@ -761,53 +813,58 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
         if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.o_done[x], (s_done - 1) & 1, &sh.failed))) return;
         fence_after();
         const float keep = moves ? exp2_approx(top - best) : 1.0f;
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < D; c += 32) {
-          uint32_t w[32];
-          tensor_load(w, o_at + c);
-          tensor_loaded(w);
+          uint32_t o[32];
+          tensor_load(o, o_at + c);
+          tensor_loaded(o);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) * keep);
-          tensor_store32(o_at + c, w);
+          for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * keep);
+          tensor_store32(o_at + c, o);
         }
         sum *= keep;
       }
       top = best;
       const float zero = top == -INFINITY ? 0.0f : top;
-      float sums[4] = {sum, 0.0f, 0.0f, 0.0f};
+      const uint64_t units = pack(unit, unit), zeros = pack(-zero, -zero);
+      uint64_t sums[2] = {pack(sum, 0.0f), pack(0.0f, 0.0f)};
 #pragma unroll
-      for (int c = 0; c < kKeys; c += 32) {
-        uint32_t w[32], p[16];
-        tensor_load(w, s_at + c);
-        tensor_loaded(w);
+      for (int c = 0; c < kKeys / 32; ++c) {
+        uint32_t p[16];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const float y = exp2_approx(fmaf(__uint_as_float(w[i]), unit, -zero));
-          sums[i % 4] += y;
-          w[i] = __float_as_uint(y);
-        }
-        if (kFp8) {
-#pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            const float4 v = *reinterpret_cast<const float4*>(&sh.v_scale[stage][c + i]);
-            const float f[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float y = __uint_as_float(w[i + e]);
-              // an infinite scale stays with the rows that see its key
-              w[i + e] = __float_as_uint(whole || y > 0.0f ? y * f[e] : 0.0f);
-            }
+        for (int i = 0; i < 32; i += 2) {
+          float y, z;
+          unpack(fma2(pack(__uint_as_float(w[c][i]), __uint_as_float(w[c][i + 1])), units, zeros), y, z);
+          y = exp2_approx(y);
+          z = exp2_approx(z);
+          sums[i / 2 % 2] = add2(sums[i / 2 % 2], pack(y, z));
+          if (kFp8) {
+            const float2 v = *reinterpret_cast<const float2*>(&sh.v_scale[stage][c * 32 + i]);
+            // an infinite scale stays with the rows that see its key
+            y = whole || y > 0.0f ? y * v.x : 0.0f;
+            z = whole || z > 0.0f ? z * v.y : 0.0f;
           }
+          p[i / 2] = pack_bf16(y, z);
         }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) p[i] = pack_bf16(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
-        tensor_store16(s_at + c / 2, p);
+        tensor_store16(s_at + c * 16, p);
       }
-      sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+      {
+        float s0, s1, s2, s3;
+        unpack(sums[0], s0, s1);
+        unpack(sums[1], s2, s3);
+        sum = (s0 + s1) + (s2 + s3);
+      }
       tensor_stored();
       fence_before();
       barrier_arrive(&sh.p_full[x]);
+      if (tile + 1 == walk.tile1) {
+        // the products have read the last of this unit's queries
+        more = find(skipped);
+        if (more) row_next = take_row<D>(sh, batch, a, next, x, thread, h_next);
+      }
     }
+    if (more) hand_over<D>(sh, x);
+    tiles_before += walk.tile1 - walk.tile0;
 
     // --- the unit's rows are done, here at least
     if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.o_done[x], (s_done - 1) & 1, &sh.failed))) return;
@@ -921,12 +978,11 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
     }
     __syncwarp();
     fence_before();  // before the next unit's products write O
-    tiles_before += walk.tile1 - walk.tile0;
   }
 }
 
 template <bool kFp8>
-constexpr int threads_of() { return kFp8 ? 416 : 384; }
+constexpr int threads_of() { return kFp8 ? 512 : 384; }
 
 // kPlain: scores are scale q.k, with scale > 0, alone.
 template <int D, bool kFp8, bool kPlain>
@@ -956,7 +1012,8 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
     sh.failed = 0;
     sh.poisoned = 0;
   }
-  if (warp == 8) {
+  constexpr int kIssuer = kFp8 ? 12 : 8;
+  if (warp == kIssuer) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(shared_address(&sh.tensor)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -965,27 +1022,36 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
   fence_after();
   wait_for_previous();
 
+  // the warpgroups of the rows hold a tile's scores in registers
+  if (warp < 8) {
+    if (kFp8) asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+  } else {
+    if (kFp8) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+  }
   if (warp < 8) {
     soften<D, kFp8, kPlain>(sh, cache, batch, a, plan, counters, parts, warp / 4, threadIdx.x % 128, lane);
-  } else if (warp == 8) {
+  } else if (warp == kIssuer) {
     issue_products<D, kFp8>(sh, cache, batch, a, plan, lane);
     if (lane == 0) commit(&sh.drained);  // no product outlives the tensor memory
     __syncwarp();
     barrier_settle(&sh.drained, 0);
   } else if (kFp8) {
-    convert_tiles<D>(sh, cache, batch, a, plan, threadIdx.x - 9 * 32, lane);
+    if (warp < 12) convert_tiles<D>(sh, cache, batch, a, plan, threadIdx.x - 256, lane);
   } else if (warp == 9) {
     copy_tiles<D>(sh, cache, batch, a, plan, &k_map, &v_map, lane);
   } else {
     fix_tiles<D>(sh, cache, batch, a, plan, threadIdx.x - 10 * 32, lane);
   }
   __syncwarp();
+  asm volatile("cp.async.wait_all;" ::: "memory");
   let_next_start();
   fence_before();
   __syncthreads();
   fence_after();
   if (threadIdx.x == 0 && sh.failed) *flag = 1;
-  if (warp == 8)
+  if (warp == kIssuer)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tensor) : "memory");
 }
 

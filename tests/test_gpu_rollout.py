@@ -569,3 +569,26 @@ def test_cache_refusals(es, ro):
         ro.es_cache_create(x.float(), x.float())
     with pytest.raises(ValueError):
         ro.es_cache_create(x.cpu(), x.cpu())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("kw", [{}, {"softcap": 20.0}], ids=["plain", "cap"])
+def test_prompts_of_many_tiles(ro, dtype, kw):
+    # blocks walk many tiles and units, most of them seen whole; units are shared by blocks
+    s = Setup(ro, [3000, 700, 1500], [900, 700, 70], 2, 128, 64, dtype, seed=12)
+    q, out, lse = attend(s, 8, **kw)
+    k, v = s.dense()
+    t = 0
+    for b, n in enumerate(s.new):
+        p = torch.arange(s.seq_len[b] - n, s.seq_len[b])[:, None]
+        hide = torch.arange(s.seq_len[b])[None] > p
+        for h in range(8):
+            x = (q[t:t + n, h].cpu().double() @ k[b][:, h // 4].T) * s.d ** -0.5
+            if "softcap" in kw:
+                x = kw["softcap"] * torch.tanh(x / kw["softcap"])
+            x = x.masked_fill(hide, -math.inf)
+            w = torch.softmax(x, -1)
+            err = (out[t:t + n, h].cpu().double() - w @ v[b][:, h // 4]).abs()
+            assert (err <= (2.0 ** -7 + 2.0 ** -12) * (w @ v[b][:, h // 4].abs())).all()
+            assert ((lse[t:t + n, h].cpu().double() - torch.logsumexp(x, -1)).abs() <= 1e-4).all()
+        t += n
