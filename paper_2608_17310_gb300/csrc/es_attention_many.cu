@@ -505,41 +505,39 @@ __device__ void fix_tiles(Shared<D>& sh, const CacheView& cache, const BatchView
   }
 }
 
-// FP8 pages: a warp loads whole keys' codes, 16 to a lane, and writes them as bf16 in place.
-// The codes of the next tile are on their way while this one waits for its stage.
+// FP8 pages: four warps load codes, 16 to a thread and piece, and write them as bf16. The
+// codes of the next tile are on their way while this one's are written.
 template <int D>
 struct Codes {
-  static constexpr int kPer = kKeys * D / 16 / 128;  // 16-byte pieces for each of 128 threads
+  static constexpr int kPer = kKeys * D / 16 / 128;  // pieces for each of 128 threads
   uint4 w[kPer];
   float scale;
-  bool there[kPer];
 };
 
+// pages: lane i's is the page of the tile's keys 16 i and up, -1 where there is none.
 template <int D>
-__device__ __forceinline__ void load_codes(Codes<D>& c, const void* store, const float* scales, const CacheView& cache,
-                                           const BatchView& batch, const Walk& walk, int tile, int thread) {
-  const int j0 = walk.key_of(tile), mask = (1 << cache.page_shift) - 1;
+__device__ __forceinline__ void load_codes(Codes<D>& c, const void* store, const float* scales, const CacheView& cache, int head,
+                                           int j0, int pages, int thread) {
+  const int mask = (1 << cache.page_shift) - 1;
+  const uint32_t rows = static_cast<uint32_t>(head) << cache.page_shift;
 #pragma unroll
   for (int i = 0; i < Codes<D>::kPer; ++i) {
-    const int piece = i * 128 + thread, key = piece / (D / 16), j = j0 + key;
-    const int page = j >= walk.pair.lo && j < walk.pair.hi ? page_of(cache, batch, walk.seq, j) : -1;
-    c.there[i] = page >= 0;
+    const int piece = i * 128 + thread, key = piece / (D / 16);
+    const int page = __shfl_sync(0xFFFFFFFFu, pages, key / 16);
     c.w[i] = make_uint4(0, 0, 0, 0);
-    if (page >= 0) {
-      const uint64_t row = (static_cast<uint64_t>(walk.head) << cache.page_shift) + (j & mask);
-      c.w[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(store) + page * cache.page_stride + row * D +
-                                                    piece % (D / 16) * 16));
-    }
+    if (page >= 0)
+      c.w[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(store) + page * cache.page_stride +
+                                                    (rows + ((j0 + key) & mask)) * D + piece % (D / 16) * 16));
   }
-  const int j = j0 + thread;  // and the scale of one key
-  const int page = j >= walk.pair.lo && j < walk.pair.hi ? page_of(cache, batch, walk.seq, j) : -1;
+  const int page = __shfl_sync(0xFFFFFFFFu, pages, thread / 16);  // and the scale of one key
   c.scale = 0.0f;
-  if (page >= 0)
-    c.scale = __ldg(scales + page * cache.scale_stride + (static_cast<uint64_t>(walk.head) << cache.page_shift) + (j & mask));
+  if (page >= 0) c.scale = __ldg(scales + page * cache.scale_stride + rows + ((j0 + thread) & mask));
 }
 
+// clean: keys outside [lo, hi) become zeros, and NaN codes too.
 template <int D>
-__device__ __forceinline__ void store_codes(const Codes<D>& c, uint16_t* to, float* scales, int thread, bool clean, int* poisoned) {
+__device__ __forceinline__ void store_codes(const Codes<D>& c, uint16_t* to, float* scales, int thread, bool clean, int lo, int hi,
+                                            int* poisoned) {
 #pragma unroll
   for (int i = 0; i < Codes<D>::kPer; ++i) {
     const int piece = i * 128 + thread, key = piece / (D / 16), first = piece % (D / 16) * 2;
@@ -547,7 +545,8 @@ __device__ __forceinline__ void store_codes(const Codes<D>& c, uint16_t* to, flo
     if (clean) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t bad = ((u[e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;  // NaN codes
+        if (key < lo || key >= hi) u[e] = 0;
+        const uint32_t bad = ((u[e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
         if (bad != 0) {
           u[e] &= ~((bad >> 7) * 0xFFu);
           *static_cast<volatile int*>(poisoned) = 1;
@@ -559,7 +558,7 @@ __device__ __forceinline__ void store_codes(const Codes<D>& c, uint16_t* to, flo
     *reinterpret_cast<uint4*>(to + place_of<D>(key, first + 1)) =
         make_uint4(bf16_of_e4m3(u[2]), bf16_of_e4m3(u[2] >> 16), bf16_of_e4m3(u[3]), bf16_of_e4m3(u[3] >> 16));
   }
-  scales[thread] = c.scale;
+  scales[thread] = clean && (thread < lo || thread >= hi) ? 0.0f : c.scale;
 }
 
 template <int D>
@@ -568,26 +567,32 @@ __device__ void convert_tiles(Shared<D>& sh, const CacheView& cache, const Batch
   uint32_t done = 0;
   Walk walk(batch, a, plan, lane);
   while (walk.next(batch, a, cache.kv_heads, lane)) {
+    auto pages_of = [&](int tile) {
+      const int j = walk.key_of(tile) + lane * 16;
+      return lane < 8 && tile < walk.tile1 && j < walk.pair.hi ? page_of(cache, batch, walk.seq, j) : -1;
+    };
+    int pages = pages_of(walk.tile0), next_pages = pages_of(walk.tile0 + 1);
+    Codes<D> k, v;
+    load_codes(k, cache.k, cache.k_scale, cache, walk.head, walk.key_of(walk.tile0), pages, thread);
+    load_codes(v, cache.v, cache.v_scale, cache, walk.head, walk.key_of(walk.tile0), pages, thread);
     for (int tile = walk.tile0; tile < walk.tile1; ++tile, ++done) {
-      const int stage = done % kStages;
+      const int stage = done % kStages, j0 = walk.key_of(tile);
       const uint32_t parity = done / kStages & 1;
-      Codes<D> k, v;
-      load_codes(k, cache.k, cache.k_scale, cache, batch, walk, tile, thread);
-      load_codes(v, cache.v, cache.v_scale, cache, batch, walk, tile, thread);
-      uint32_t absent = 0;
-      for (int i = 0; i < 8; ++i) {
-        const int j = walk.key_of(tile) + i * 16;
-        if (j >= walk.pair.hi || page_of(cache, batch, walk.seq, j) < 0) absent |= 1u << i;
-      }
+      const uint32_t absent = __ballot_sync(0xFFFFFFFFu, pages < 0) & 0xFFu;
+      const bool more = tile + 1 < walk.tile1;
       if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.k_empty[stage], parity ^ 1, &sh.failed))) return;
       if (thread == 0) sh.absent[done % 4] = absent;
-      store_codes(k, sh.k[stage], sh.k_scale[done % 4], thread, false, nullptr);
+      store_codes(k, sh.k[stage], sh.k_scale[done % 4], thread, false, 0, 0, nullptr);
       fence_async();
       barrier_arrive(&sh.k_full[stage]);
+      if (more) load_codes(k, cache.k, cache.k_scale, cache, walk.head, j0 + kKeys, next_pages, thread);
       if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.v_empty[stage], parity ^ 1, &sh.failed))) return;
-      store_codes(v, sh.v[stage], sh.v_scale[stage], thread, walk.edge(tile), &sh.poisoned);
+      store_codes(v, sh.v[stage], sh.v_scale[stage], thread, walk.edge(tile), walk.pair.lo - j0, walk.pair.hi - j0, &sh.poisoned);
       fence_async();
       barrier_arrive(&sh.v_full[stage]);
+      if (more) load_codes(v, cache.v, cache.v_scale, cache, walk.head, j0 + kKeys, next_pages, thread);
+      pages = next_pages;
+      next_pages = pages_of(tile + 2);
     }
   }
 }
@@ -681,6 +686,14 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   return y;
 }
 
+__device__ __forceinline__ float reciprocal(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Bits n and up of 32; all for n <= 0, none for n >= 32.
+__device__ __forceinline__ uint32_t bits_from(int n) { return n >= 32 ? 0u : 0xFFFFFFFFu << max(n, 0); }
+
 // 16 bytes to shared memory without a register in between; zeros where `from` is not to be read.
 __device__ __forceinline__ void copy_async(uint32_t to, const void* from, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
@@ -713,7 +726,11 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
                        const Plan* plan, uint32_t* counters, Part<D>* parts, int x, int thread, int lane) {
   const uint32_t lanes = static_cast<uint32_t>(thread / 32 * 32) << 16;
   const uint32_t s_at = sh.tensor + lanes + x * 128, o_at = sh.tensor + lanes + 256 + x * 128;
-  const float factor = kPlain ? a.scale * kLog2e : a.scale;
+  // Scores in units of log 2. Capped: cap tanh(x / cap) = cap - 2 cap / (2^(2 x log2(e) / cap) + 1),
+  // off by 1e-7 cap at most.
+  const bool capped = a.softcap > 0.0f;
+  const float cap = a.softcap * kLog2e;
+  const float factor = a.scale * (capped ? 2.0f * kLog2e / a.softcap : kLog2e);
   uint32_t s_done = 0;        // tiles of this warpgroup so far
   uint32_t tiles_before = 0;  // of all units
   uint32_t phase = 0;
@@ -742,7 +759,7 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
     const Row row = row_next;
     const int h = h_next;
     tiles_before += skipped;
-    const float slope = !kPlain && a.slopes != nullptr ? a.slopes[h] : 0.0f;
+    const float slope = !kPlain && a.slopes != nullptr ? a.slopes[h] * kLog2e : 0.0f;
     float top = -INFINITY, sum = 0.0f;
     for (int tile = walk.tile0; tile < walk.tile1; ++tile, ++s_done) {
       const uint32_t all_done = tiles_before + (tile - walk.tile0);
@@ -753,11 +770,12 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
       if (kFp8 && !__all_sync(0xFFFFFFFFu, barrier_wait(&sh.v_full[stage], all_done / kStages & 1, &sh.failed))) return;
       const uint32_t absent = sh.absent[all_done % 4];
       const bool whole = __all_sync(0xFFFFFFFFu, row.token < 0 || (row.lo <= j0 && row.hi >= j0 + kKeys)) && absent == 0;
-      const bool direct = !kFp8 && kPlain && whole;
+      const bool direct = kPlain && whole;
       float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
       if (!direct) {
         // scores that take more than a factor are made here and put back
         const int c_lo = row.lo - j0, c_hi = row.hi - j0;  // the columns that the row sees
+        float away = static_cast<float>(row.pos - j0);
 #pragma unroll 1
         for (int c = 0; c < kKeys; c += 32) {
           uint32_t w[32];
@@ -776,14 +794,20 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               float y = __uint_as_float(w[i + e]) * f[e];
-              if (!kPlain) y = score_of(a, y, slope, row.pos - (j0 + c + i + e));
+              if (!kPlain && capped) y = fmaf(-2.0f * cap, reciprocal(exp2_approx(y) + 1.0f), cap);
+              if (!kPlain) y = fmaf(-slope, fabsf(away - static_cast<float>(i + e)), y);
               w[i + e] = __float_as_uint(y);
             }
           }
+          away -= 32.0f;
           if (!whole) {
+            // columns of this chunk as bits
+            uint32_t seen = bits_from(c_lo - c) & ~bits_from(c_hi - c);
+            if (absent >> (c / 16) & 1) seen &= 0xFFFF0000u;
+            if (absent >> (c / 16 + 1) & 1) seen &= 0xFFFFu;
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (!(c + i >= c_lo && c + i < c_hi) || (absent >> ((c + i) / 16) & 1)) w[i] = __float_as_uint(-INFINITY);
+              if (!(seen >> i & 1)) w[i] = __float_as_uint(-INFINITY);
           }
 #pragma unroll
           for (int i = 0; i < 32; ++i) tops[i % 4] = fmaxf(tops[i % 4], __uint_as_float(w[i]));
@@ -796,8 +820,22 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
       for (int c = 0; c < kKeys / 32; ++c) tensor_load(w[c], s_at + c * 32);
 #pragma unroll
       for (int c = 0; c < kKeys / 32; ++c) tensor_loaded(w[c]);
-      const float unit = direct ? factor : 1.0f;  // of what S holds, in scores
-      if (direct) {
+      const float unit = direct && !kFp8 ? factor : 1.0f;  // of what w holds, in scores
+      if (kFp8 && direct) {
+#pragma unroll
+        for (int c = 0; c < kKeys / 32; ++c)
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const float4 k = *reinterpret_cast<const float4*>(&sh.k_scale[all_done % 4][c * 32 + i]);
+            const float f[4] = {k.x * factor, k.y * factor, k.z * factor, k.w * factor};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float y = __uint_as_float(w[c][i + e]) * f[e];
+              tops[e] = fmaxf(tops[e], y);
+              w[c][i + e] = __float_as_uint(y);
+            }
+          }
+      } else if (direct) {
 #pragma unroll
         for (int i = 0; i < 32; i += 2)
 #pragma unroll
@@ -933,43 +971,66 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
       }
       if (!group_sync(sh, x, phase)) return;
       if (sh.last[x]) {
-        // a warp for each row, a lane for D / 32 of its elements
+        // Each lane weighs the parts of its own row; then the warp goes through its 32 rows,
+        // 16 at a time with all their loads in flight, a lane for D / 32 of a row's elements.
         constexpr int kPer = D / 32;
-        const int rows = min(128, pair.rows - x * 128);
-        for (int q = thread / 32; q < rows; q += 4) {
-          const int n = c_last - c_first + 1, at = x * 128 + q;
-          auto part_of = [&](int i) -> const Part<D>& { return parts[2 * (c_first + i) + (i == 0)]; };
-          float most = -INFINITY, l = 0.0f, y[kPer] = {};
-          for (int i = lane; i < n; i += 32) most = fmaxf(most, __ldcg(&part_of(i).top[at]));
-#pragma unroll
-          for (int m = 16; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, m));
-          const float z = most == -INFINITY ? 0.0f : most;
-          for (int i0 = 0; i0 < n; i0 += 32) {
-            const int count = min(n - i0, 32);
-            float f = 0.0f;
-            if (lane < count) {
-              f = exp2_approx(__ldcg(&part_of(i0 + lane).top[at]) - z);
-              l += __ldcg(&part_of(i0 + lane).sum[at]) * f;
-            }
+        const int n = c_last - c_first + 1;
+        auto part_of = [&](int i) -> const Part<D>& { return parts[2 * (c_first + i) + (i == 0)]; };
+        float most = -INFINITY, l = 0.0f;
+        if (row.token >= 0) {
 #pragma unroll 4
-            for (int i = 0; i < count; ++i) {
-              const float g = __shfl_sync(0xFFFFFFFFu, f, i);
-              const float* from = &part_of(i0 + i).o[at][lane * kPer];
+          for (int i = 0; i < n; ++i) most = fmaxf(most, __ldcg(&part_of(i).top[r_part]));
+#pragma unroll 4
+          for (int i = 0; i < n; ++i)
+            l += __ldcg(&part_of(i).sum[r_part]) * exp2_approx(__ldcg(&part_of(i).top[r_part]) - (most == -INFINITY ? 0.0f : most));
+          if (a.lse != nullptr)
+            a.lse[static_cast<uint64_t>(row.token) * a.q_heads + h] = most > -INFINITY || l != l ? most * kLn2 + logf(l) : -INFINITY;
+        }
+        const float z = most == -INFINITY ? 0.0f : most;
+        const float i1 = most > -INFINITY || l != l ? 1.0f / l : 0.0f;
+        const int rows = min(32, pair.rows - x * 128 - thread / 32 * 32), at = x * 128 + thread / 32 * 32;
+#pragma unroll 1
+        for (int r0 = 0; r0 < rows; r0 += 16) {
+          float y[16][kPer] = {};
+#pragma unroll 1
+          for (int i = 0; i < n; ++i) {
+            const Part<D>& from = part_of(i);
+            const float f = row.token >= 0 ? exp2_approx(__ldcg(&from.top[r_part]) - z) : 0.0f;
+            float v[16][kPer];
 #pragma unroll
-              for (int e = 0; e < kPer; ++e) y[e] += __ldcg(from + e) * g;
+            for (int q = 0; q < 16; ++q) {
+              const float* o = &from.o[at + r0 + q][lane * kPer];
+              if constexpr (kPer == 4) {
+                const float4 w = r0 + q < rows ? __ldcg(reinterpret_cast<const float4*>(o)) : make_float4(0, 0, 0, 0);
+                v[q][0] = w.x;
+                v[q][1] = w.y;
+                v[q][2] = w.z;
+                v[q][3] = w.w;
+              } else {
+                const float2 w = r0 + q < rows ? __ldcg(reinterpret_cast<const float2*>(o)) : make_float2(0, 0);
+                v[q][0] = w.x;
+                v[q][1] = w.y;
+              }
+            }
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+              const float g = __shfl_sync(0xFFFFFFFFu, f, r0 + q);
+#pragma unroll
+              for (int e = 0; e < kPer; ++e) y[q][e] += v[q][e] * g;
             }
           }
 #pragma unroll
-          for (int m = 16; m > 0; m >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, m);
-          const int64_t rr = static_cast<int64_t>(walk.row_tile) * kRows + at;
-          const int token = pair.begin + static_cast<int>(rr / a.group), hh = walk.head * a.group + static_cast<int>(rr % a.group);
-          const bool any = most > -INFINITY || l != l;
-          const float i1 = any ? 1.0f / l : 0.0f;
-          uint32_t* to = reinterpret_cast<uint32_t*>(a.out + static_cast<uint64_t>(token) * a.out_stride + static_cast<uint64_t>(hh) * D + lane * kPer);
-#pragma unroll
-          for (int e = 0; e < kPer / 2; ++e) to[e] = any ? pack_bf16(y[2 * e] * i1, y[2 * e + 1] * i1) : 0u;
-          if (lane == 0 && a.lse != nullptr)
-            a.lse[static_cast<uint64_t>(token) * a.q_heads + hh] = any ? most * kLn2 + logf(l) : -INFINITY;
+          for (int q = 0; q < 16; ++q) {
+            const int token = __shfl_sync(0xFFFFFFFFu, row.token, r0 + q), hh = __shfl_sync(0xFFFFFFFFu, h, r0 + q);
+            const float g = __shfl_sync(0xFFFFFFFFu, i1, r0 + q);
+            const bool any = __shfl_sync(0xFFFFFFFFu, static_cast<int>(i1 != 0.0f), r0 + q) != 0;
+            if (token < 0) continue;
+            uint32_t* to = reinterpret_cast<uint32_t*>(a.out + static_cast<uint64_t>(token) * a.out_stride + static_cast<uint64_t>(hh) * D + lane * kPer);
+            if constexpr (kPer == 4)
+              *reinterpret_cast<uint2*>(to) = any ? make_uint2(pack_bf16(y[q][0] * g, y[q][1] * g), pack_bf16(y[q][2] * g, y[q][3] * g)) : make_uint2(0, 0);
+            else
+              *to = any ? pack_bf16(y[q][0] * g, y[q][1] * g) : 0u;
+          }
         }
       }
       if (!group_sync(sh, x, phase)) return;  // sh.last has been read
@@ -1024,10 +1085,10 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
 
   // the warpgroups of the rows hold a tile's scores in registers
   if (warp < 8) {
-    if (kFp8) asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+    if (kFp8) asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
     else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
   } else {
-    if (kFp8) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (kFp8) asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   }
   if (warp < 8) {
