@@ -13,7 +13,7 @@
 // moves where a tile's maximum is more than 2^8 above it, which keeps P in bf16's range
 // and leaves O in tensor memory alone on almost every tile.
 //
-// bf16 pages reach shared memory by TMA, each page of a tile by its own copy; FP8 pages
+// Pages reach shared memory by TMA, each page of a tile by its own copy; FP8 pages then pass
 // through four warps that turn codes into bf16, which holds them exactly. The scales go to
 // the scores and to P.
 //
@@ -244,6 +244,16 @@ __device__ __forceinline__ bool barrier_wait(uint64_t* b, uint32_t parity, volat
   return false;
 }
 
+// By all lanes: through one of them and a shuffle measured 25 % slower over a whole prompt.
+__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, volatile int* failed) {
+  return __all_sync(0xFFFFFFFFu, barrier_wait(b, parity, failed));
+}
+// One lane arrives, with what all lanes did before.
+__device__ __forceinline__ void warp_arrive(uint64_t* b, int lane) {
+  __syncwarp();
+  if (lane == 0) barrier_arrive(b);
+}
+
 // The same, whatever has failed before: for what must not outlive the block.
 __device__ __forceinline__ void barrier_settle(uint64_t* b, uint32_t parity) {
   for (int i = 0; i < kMostTries; ++i)
@@ -327,11 +337,16 @@ __device__ __forceinline__ void tensor_stored() { asm volatile("tcgen05.wait::st
 
 // --- the walk over a block's units -----------------------------------------------------
 
-template <int D>
+// FP8: half tiles of codes on their way from the pages to the converting warps.
+constexpr int kRaw = 3;
+constexpr int kHalf = 64;  // keys
+
+template <int D, bool kFp8>
 struct Shared {
   uint16_t q[2][128 * D];
   uint16_t k[kStages][kKeys * D];
   uint16_t v[kStages][kKeys * D];
+  uint8_t raw[kFp8 ? kRaw : 1][kFp8 ? kHalf * D : 128];
   // Read with the scores, when the tile's keys may have made room for others: a slot is
   // written again four tiles on, which follows the scores of two tiles on.
   float k_scale[4][kKeys];
@@ -340,6 +355,7 @@ struct Shared {
   uint64_t q_full[2], s_full[2], p_full[2], o_done[2];
   uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages], v_fixed[kStages];
   uint64_t group[2], drained;
+  uint64_t raw_full[kRaw], raw_empty[kRaw];
   uint32_t tensor;           // address of the tensor memory
   int failed;
   int poisoned;              // a value that not every row sees was an infinity or NaN
@@ -354,11 +370,11 @@ struct Part {
   float top[kRows], sum[kRows];
 };
 
-// The 128 threads of a warpgroup; false as barrier_wait.
-template <int D>
-__device__ __forceinline__ bool group_sync(Shared<D>& sh, int x, uint32_t& phase) {
-  barrier_arrive(&sh.group[x]);
-  return __all_sync(0xFFFFFFFFu, barrier_wait(&sh.group[x], phase++ & 1, &sh.failed));
+// The four warps of a warpgroup; false as barrier_wait.
+template <class Sh>
+__device__ __forceinline__ bool group_sync(Sh& sh, int x, uint32_t& phase, int lane) {
+  warp_arrive(&sh.group[x], lane);
+  return warp_wait(&sh.group[x], phase++ & 1, &sh.failed);
 }
 
 // Every warp of a block walks the same units.
@@ -421,7 +437,7 @@ __device__ __forceinline__ int place_of(int r, int piece) {
 
 // bf16 pages to shared memory, a lane for each page of the tile.
 template <int D>
-__device__ void copy_tiles(Shared<D>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
+__device__ void copy_tiles(Shared<D, false>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
                            const Plan* plan, const CUtensorMap* k_map, const CUtensorMap* v_map, int lane) {
   const int page_size = 1 << cache.page_shift, pages = kKeys >> cache.page_shift;
   uint32_t k_done = 0, v_done = 0;
@@ -439,7 +455,7 @@ __device__ void copy_tiles(Shared<D>& sh, const CacheView& cache, const BatchVie
       for (int i = 0; i < 8; ++i) absent |= (missing >> (i * 16 >> cache.page_shift) & 1) << i;
       // a page past the last one reads as zeros
       const int z = page < 0 ? cache.num_pages : page, y = walk.head << cache.page_shift;
-      fine = __all_sync(0xFFFFFFFFu, barrier_wait(&sh.k_empty[stage], parity ^ 1, &sh.failed));
+      fine = warp_wait(&sh.k_empty[stage], parity ^ 1, &sh.failed);
       if (!fine) break;
       if (lane == 0) {
         sh.absent[k_done % 4] = absent;
@@ -450,7 +466,7 @@ __device__ void copy_tiles(Shared<D>& sh, const CacheView& cache, const BatchVie
         for (int h = 0; h < D / 64; ++h)
           load_box(k_map, shared_address(sh.k[stage] + h * 128 * 64 + lane * page_size * 64), &sh.k_full[stage], h * 64, y, z);
       ++k_done;
-      fine = __all_sync(0xFFFFFFFFu, barrier_wait(&sh.v_empty[stage], parity ^ 1, &sh.failed));
+      fine = warp_wait(&sh.v_empty[stage], parity ^ 1, &sh.failed);
       if (!fine) break;
       if (lane == 0) barrier_expect(&sh.v_full[stage], kKeys * D * 2);
       __syncwarp();
@@ -470,14 +486,14 @@ __device__ void copy_tiles(Shared<D>& sh, const CacheView& cache, const BatchVie
 // them); the rows that see them get them when the unit is written. Every tile passes here,
 // so that the barriers of the stages are never a round ahead.
 template <int D>
-__device__ void fix_tiles(Shared<D>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
+__device__ void fix_tiles(Shared<D, false>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
                           const Plan* plan, int thread, int lane) {
   uint32_t done = 0;
   Walk walk(batch, a, plan, lane);
   while (walk.next(batch, a, cache.kv_heads, lane)) {
     for (int tile = walk.tile0; tile < walk.tile1; ++tile, ++done) {
       const int stage = done % kStages, j0 = walk.key_of(tile);
-      if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.v_full[stage], done / kStages & 1, &sh.failed))) return;
+      if (!warp_wait(&sh.v_full[stage], done / kStages & 1, &sh.failed)) return;
       if (walk.edge(tile)) {
         for (int i = thread; i < kKeys * D / 8; i += 64) {
           const int key = i / (D / 8), j = j0 + key;
@@ -499,52 +515,56 @@ __device__ void fix_tiles(Shared<D>& sh, const CacheView& cache, const BatchView
         }
         fence_async();
       }
-      __syncwarp();
-      if (lane == 0) barrier_arrive(&sh.v_fixed[stage]);
+      warp_arrive(&sh.v_fixed[stage], lane);
     }
   }
 }
 
-// FP8 pages: four warps load codes, 16 to a thread and piece, and write them as bf16. The
-// codes of the next tile are on their way while this one's are written.
+// FP8 pages to shared memory as they are, a half tile of keys at a time and of values after it.
 template <int D>
-struct Codes {
-  static constexpr int kPer = kKeys * D / 16 / 128;  // pieces for each of 128 threads
-  uint4 w[kPer];
-  float scale;
-};
-
-// pages: lane i's is the page of the tile's keys 16 i and up, -1 where there is none.
-template <int D>
-__device__ __forceinline__ void load_codes(Codes<D>& c, const void* store, const float* scales, const CacheView& cache, int head,
-                                           int j0, int pages, int thread) {
-  const int mask = (1 << cache.page_shift) - 1;
-  const uint32_t rows = static_cast<uint32_t>(head) << cache.page_shift;
-#pragma unroll
-  for (int i = 0; i < Codes<D>::kPer; ++i) {
-    const int piece = i * 128 + thread, key = piece / (D / 16);
-    const int page = __shfl_sync(0xFFFFFFFFu, pages, key / 16);
-    c.w[i] = make_uint4(0, 0, 0, 0);
-    if (page >= 0)
-      c.w[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(store) + page * cache.page_stride +
-                                                    (rows + ((j0 + key) & mask)) * D + piece % (D / 16) * 16));
+__device__ void copy_codes(Shared<D, true>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
+                           const Plan* plan, const CUtensorMap* k_map, const CUtensorMap* v_map, int lane) {
+  const int box = min(1 << cache.page_shift, kHalf), boxes = kHalf / box;  // keys of a copy, copies of a half
+  uint32_t done = 0;
+  bool fine = true;
+  Walk walk(batch, a, plan, lane);
+  while (fine && walk.next(batch, a, cache.kv_heads, lane)) {
+    for (int tile = walk.tile0; fine && tile < walk.tile1; ++tile) {
+      // the copies of both halves: lane i's keys are 16 i and up
+      const int j = walk.key_of(tile) + lane * 16;
+      const int page = lane < 8 && j < walk.pair.hi ? page_of(cache, batch, walk.seq, j) : -1;
+#pragma unroll 1
+      for (int part = 0; part < 4; ++part, ++done) {
+        const int slot = done % kRaw, j0 = walk.key_of(tile) + (part & 1) * kHalf;
+        const int mine = __shfl_sync(0xFFFFFFFFu, page, (part & 1) * 4 + lane * box / 16);
+        fine = warp_wait(&sh.raw_empty[slot], (done / kRaw & 1) ^ 1, &sh.failed);
+        if (!fine) break;
+        if (lane == 0) barrier_expect(&sh.raw_full[slot], kHalf * D);
+        __syncwarp();
+        if (lane < boxes)
+          load_box(part < 2 ? k_map : v_map, shared_address(sh.raw[slot] + lane * box * D), &sh.raw_full[slot], 0,
+                   (walk.head << cache.page_shift) + ((j0 + lane * box) & ((1 << cache.page_shift) - 1)), mine < 0 ? cache.num_pages : mine);
+      }
+    }
   }
-  const int page = __shfl_sync(0xFFFFFFFFu, pages, thread / 16);  // and the scale of one key
-  c.scale = 0.0f;
-  if (page >= 0) c.scale = __ldg(scales + page * cache.scale_stride + rows + ((j0 + thread) & mask));
+  // no copy outlives the block
+  for (uint32_t i = done > kRaw ? done - kRaw : 0; i < done; ++i) barrier_settle(&sh.raw_full[i % kRaw], i / kRaw & 1);
 }
 
+// A half tile of codes to bf16: 8 codes (16 bytes of bf16) to a thread and step, so that the
+// eight threads that write side by side write all of one 128-byte row.
 // clean: keys outside [lo, hi) become zeros, and NaN codes too.
 template <int D>
-__device__ __forceinline__ void store_codes(const Codes<D>& c, uint16_t* to, float* scales, int thread, bool clean, int lo, int hi,
-                                            int* poisoned) {
+__device__ __forceinline__ void convert_half(const uint8_t* raw, uint16_t* to, int key0, int thread, bool clean, int lo, int hi,
+                                             int* poisoned) {
 #pragma unroll
-  for (int i = 0; i < Codes<D>::kPer; ++i) {
-    const int piece = i * 128 + thread, key = piece / (D / 16), first = piece % (D / 16) * 2;
-    uint32_t u[4] = {c.w[i].x, c.w[i].y, c.w[i].z, c.w[i].w};
+  for (int i = 0; i < kHalf * D / 8 / 128; ++i) {
+    const int piece = i * 128 + thread, key = key0 + piece / (D / 8);
+    const uint2 w = *reinterpret_cast<const uint2*>(raw + piece * 8);
+    uint32_t u[2] = {w.x, w.y};
     if (clean) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
+      for (int e = 0; e < 2; ++e) {
         if (key < lo || key >= hi) u[e] = 0;
         const uint32_t bad = ((u[e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
         if (bad != 0) {
@@ -553,119 +573,143 @@ __device__ __forceinline__ void store_codes(const Codes<D>& c, uint16_t* to, flo
         }
       }
     }
-    *reinterpret_cast<uint4*>(to + place_of<D>(key, first)) =
+    *reinterpret_cast<uint4*>(to + place_of<D>(key, piece % (D / 8))) =
         make_uint4(bf16_of_e4m3(u[0]), bf16_of_e4m3(u[0] >> 16), bf16_of_e4m3(u[1]), bf16_of_e4m3(u[1] >> 16));
-    *reinterpret_cast<uint4*>(to + place_of<D>(key, first + 1)) =
-        make_uint4(bf16_of_e4m3(u[2]), bf16_of_e4m3(u[2] >> 16), bf16_of_e4m3(u[3]), bf16_of_e4m3(u[3] >> 16));
   }
-  scales[thread] = clean && (thread < lo || thread >= hi) ? 0.0f : c.scale;
 }
 
 template <int D>
-__device__ void convert_tiles(Shared<D>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
+__device__ void convert_tiles(Shared<D, true>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
                               const Plan* plan, int thread, int lane) {
-  uint32_t done = 0;
+  uint32_t done = 0, raw_done = 0;
   Walk walk(batch, a, plan, lane);
   while (walk.next(batch, a, cache.kv_heads, lane)) {
-    auto pages_of = [&](int tile) {
+    auto pages_of = [&](int tile) {  // lane i's is the page of the tile's keys 16 i and up
       const int j = walk.key_of(tile) + lane * 16;
       return lane < 8 && tile < walk.tile1 && j < walk.pair.hi ? page_of(cache, batch, walk.seq, j) : -1;
     };
+    auto scale_of = [&](const float* scales, int pages, int tile) {  // of key `thread` of the tile
+      const int page = __shfl_sync(0xFFFFFFFFu, pages, thread / 16);
+      const uint64_t row = (static_cast<uint64_t>(walk.head) << cache.page_shift) + ((walk.key_of(tile) + thread) & ((1 << cache.page_shift) - 1));
+      return page >= 0 ? __ldg(scales + page * cache.scale_stride + row) : 0.0f;
+    };
     int pages = pages_of(walk.tile0), next_pages = pages_of(walk.tile0 + 1);
-    Codes<D> k, v;
-    load_codes(k, cache.k, cache.k_scale, cache, walk.head, walk.key_of(walk.tile0), pages, thread);
-    load_codes(v, cache.v, cache.v_scale, cache, walk.head, walk.key_of(walk.tile0), pages, thread);
+    float k_scale = scale_of(cache.k_scale, pages, walk.tile0), v_scale = scale_of(cache.v_scale, pages, walk.tile0);
     for (int tile = walk.tile0; tile < walk.tile1; ++tile, ++done) {
       const int stage = done % kStages, j0 = walk.key_of(tile);
       const uint32_t parity = done / kStages & 1;
       const uint32_t absent = __ballot_sync(0xFFFFFFFFu, pages < 0) & 0xFFu;
-      const bool more = tile + 1 < walk.tile1;
-      if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.k_empty[stage], parity ^ 1, &sh.failed))) return;
+      const float next_k = scale_of(cache.k_scale, next_pages, tile + 1), next_v = scale_of(cache.v_scale, next_pages, tile + 1);
+      const int lo = walk.pair.lo - j0, hi = walk.pair.hi - j0;
+      const bool clean = walk.edge(tile);
+      if (!warp_wait(&sh.k_empty[stage], parity ^ 1, &sh.failed)) return;
       if (thread == 0) sh.absent[done % 4] = absent;
-      store_codes(k, sh.k[stage], sh.k_scale[done % 4], thread, false, 0, 0, nullptr);
+      sh.k_scale[done % 4][thread] = k_scale;
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half, ++raw_done) {
+        const int slot = raw_done % kRaw;
+        if (!warp_wait(&sh.raw_full[slot], raw_done / kRaw & 1, &sh.failed)) return;
+        convert_half<D>(sh.raw[slot], sh.k[stage], half * kHalf, thread, false, 0, 0, nullptr);
+        warp_arrive(&sh.raw_empty[slot], lane);
+      }
       fence_async();
-      barrier_arrive(&sh.k_full[stage]);
-      if (more) load_codes(k, cache.k, cache.k_scale, cache, walk.head, j0 + kKeys, next_pages, thread);
-      if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.v_empty[stage], parity ^ 1, &sh.failed))) return;
-      store_codes(v, sh.v[stage], sh.v_scale[stage], thread, walk.edge(tile), walk.pair.lo - j0, walk.pair.hi - j0, &sh.poisoned);
+      warp_arrive(&sh.k_full[stage], lane);
+      if (!warp_wait(&sh.v_empty[stage], parity ^ 1, &sh.failed)) return;
+      sh.v_scale[stage][thread] = clean && (thread < lo || thread >= hi) ? 0.0f : v_scale;
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half, ++raw_done) {
+        const int slot = raw_done % kRaw;
+        if (!warp_wait(&sh.raw_full[slot], raw_done / kRaw & 1, &sh.failed)) return;
+        convert_half<D>(sh.raw[slot], sh.v[stage], half * kHalf, thread, clean, lo, hi, &sh.poisoned);
+        warp_arrive(&sh.raw_empty[slot], lane);
+      }
       fence_async();
-      barrier_arrive(&sh.v_full[stage]);
-      if (more) load_codes(v, cache.v, cache.v_scale, cache, walk.head, j0 + kKeys, next_pages, thread);
+      warp_arrive(&sh.v_full[stage], lane);
+      k_scale = next_k;
+      v_scale = next_v;
       pages = next_pages;
       next_pages = pages_of(tile + 2);
     }
   }
 }
 
-// The thread that issues the products.
+// True in one lane of a converged warp. The products' operands have to be the warp's own
+// (uniform registers): under a test of the lane number the compiler cannot know that one
+// thread alone is left, and makes every product a loop over the lanes.
+__device__ __forceinline__ bool elected() {
+  uint32_t yes;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(yes));
+  return yes != 0;
+}
+
+// The warp that issues the products.
 template <int D, bool kFp8>
-__device__ void issue_products(Shared<D>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
+__device__ void issue_products(Shared<D, kFp8>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
                                const Plan* plan, int lane) {
   constexpr uint32_t kScores = product_of(kKeys, false), kValues = product_of(D, true);
   const uint32_t tensor = sh.tensor;
   uint32_t k_done = 0, v_done = 0, units = 0, two_units = 0;
-  uint32_t p_done[2] = {0, 0};
-  auto scores = [&](int x, int stage) {
-    if (lane == 0) {
-      const uint32_t q = shared_address(sh.q[x]), k = shared_address(sh.k[stage]);
+  uint32_t p_done = 0, p_done_two = 0;  // of the first tile of rows, and of the second
+  // The operands' descriptors: only the address in their low word changes.
+  const uint64_t plain_rows = operand(0, 16), value_rows = operand(0, 128 * 128);
+  const uint32_t q_at = shared_address(sh.q[0]) >> 4;
+  const uint32_t k_at = shared_address(sh.k[0]) >> 4, v_at = shared_address(sh.v[0]) >> 4;
+  constexpr uint32_t kOperand = 128 * D * 2 / 16;
+  auto scores = [&](uint32_t x, uint32_t stage) {
+    const uint64_t q = plain_rows + (q_at + x * kOperand), k = plain_rows + (k_at + stage * kOperand);
+    if (elected()) {
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
-        const uint32_t at = i / 4 * (128 * 128) + i % 4 * 32;
-        multiply(tensor + x * 128, operand(q + at, 16), operand(k + at, 16), kScores, i > 0);
+        const uint32_t at = (i / 4 * (128 * 128) + i % 4 * 32) / 16;
+        multiply(tensor + x * 128, q + at, k + at, kScores, i > 0);
       }
       commit(&sh.s_full[x]);
       barrier_arrive(&sh.s_full[x]);  // with what this thread has seen: the tile's scales, its absent pages
     }
     __syncwarp();
   };
+  auto wait = [&](uint64_t* b, uint32_t parity) { return warp_wait(b, parity, &sh.failed); };
   Walk walk(batch, a, plan, lane);
   while (walk.next(batch, a, cache.kv_heads, lane)) {
-    const int tiles = walk.two ? 2 : 1;
-    if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.q_full[0], units & 1, &sh.failed))) return;
-    if (walk.two && !__all_sync(0xFFFFFFFFu, barrier_wait(&sh.q_full[1], two_units & 1, &sh.failed))) return;
-    ++units;
-    two_units += walk.two;
+    const uint32_t count = walk.two ? 2 : 1;
+    const int tiles = walk.tile1 - walk.tile0;
+    if (!wait(&sh.q_full[0], units & 1)) return;
+    if (count == 2 && !wait(&sh.q_full[1], two_units & 1)) return;
+    if (!wait(&sh.k_full[k_done % kStages], k_done / kStages & 1)) return;
     fence_after();
-    if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.k_full[k_done % kStages], k_done / kStages & 1, &sh.failed))) return;
-    for (int x = 0; x < tiles; ++x) scores(x, k_done % kStages);
-    if (lane == 0) commit(&sh.k_empty[k_done % kStages]);
+    for (uint32_t x = 0; x < count; ++x) scores(x, k_done % kStages);
+    if (elected()) commit(&sh.k_empty[k_done % kStages]);
     __syncwarp();
     ++k_done;
-    for (int tile = walk.tile0; tile < walk.tile1; ++tile, ++v_done) {
-      const int stage = v_done % kStages;
-      const bool more = tile + 1 < walk.tile1;
-      for (int x = 0; x < tiles; ++x) {
-        if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.p_full[x], p_done[x] & 1, &sh.failed))) return;
-        ++p_done[x];
-        if (x == 0) {
-          uint64_t* ready = kFp8 ? &sh.v_full[stage] : &sh.v_fixed[stage];
-          if (!__all_sync(0xFFFFFFFFu, barrier_wait(ready, v_done / kStages & 1, &sh.failed))) return;
-        }
+    for (int tile = 0; tile < tiles; ++tile, ++v_done) {
+      const uint32_t stage = v_done % kStages;
+      const bool more = tile + 1 < tiles;
+      if (!wait(kFp8 ? &sh.v_full[stage] : &sh.v_fixed[stage], v_done / kStages & 1)) return;
+      if (more && !wait(&sh.k_full[k_done % kStages], k_done / kStages & 1)) return;
+      for (uint32_t x = 0; x < count; ++x) {
+        if (!wait(&sh.p_full[x], (x == 0 ? p_done : p_done_two) & 1)) return;
         fence_after();
-        if (lane == 0) {
-          const uint32_t v = shared_address(sh.v[stage]);
+        const uint64_t v = value_rows + (v_at + stage * kOperand);
+        if (elected()) {
 #pragma unroll
           for (int i = 0; i < kKeys / 16; ++i)
-            multiply_from_tensor(tensor + 256 + x * 128, tensor + x * 128 + i * 8, operand(v + i * 16 * 128, 128 * 128),
-                                 kValues, i > 0 || tile > walk.tile0);
+            multiply_from_tensor(tensor + 256 + x * 128, tensor + x * 128 + i * 8, v + i * 128, kValues, i > 0 || tile > 0);
           commit(&sh.o_done[x]);
         }
         __syncwarp();
-        if (more) {
-          if (x == 0) {
-            if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.k_full[k_done % kStages], k_done / kStages & 1, &sh.failed))) return;
-            fence_after();
-          }
-          scores(x, k_done % kStages);
-        }
+        if (more) scores(x, k_done % kStages);
       }
-      if (lane == 0) {
+      if (elected()) {
         commit(&sh.v_empty[stage]);
         if (more) commit(&sh.k_empty[k_done % kStages]);
       }
       __syncwarp();
       if (more) ++k_done;
+      ++p_done;
+      p_done_two += count == 2;
     }
+    ++units;
+    two_units += count == 2;
   }
 }
 
@@ -700,8 +744,8 @@ __device__ __forceinline__ void copy_async(uint32_t to, const void* from, bool t
 }
 
 // This thread's row of the walk's unit, and its query on the way to shared memory.
-template <int D>
-__device__ __forceinline__ Row take_row(Shared<D>& sh, const BatchView& batch, const AttentionArgs& a, const Walk& walk, int x,
+template <int D, bool kFp8>
+__device__ __forceinline__ Row take_row(Shared<D, kFp8>& sh, const BatchView& batch, const AttentionArgs& a, const Walk& walk, int x,
                                         int thread, int& h) {
   const Pair& pair = walk.pair;
   const int r = walk.row_tile * kRows + x * 128 + thread;
@@ -713,16 +757,16 @@ __device__ __forceinline__ Row take_row(Shared<D>& sh, const BatchView& batch, c
   asm volatile("cp.async.commit_group;" ::: "memory");
   return row;
 }
-template <int D>
-__device__ __forceinline__ void hand_over(Shared<D>& sh, int x) {
+template <class Sh>
+__device__ __forceinline__ void hand_over(Sh& sh, int x, int lane) {
   asm volatile("cp.async.wait_all;" ::: "memory");
   fence_async();
-  barrier_arrive(&sh.q_full[x]);
+  warp_arrive(&sh.q_full[x], lane);
 }
 
 // A warpgroup's rows: a thread for each.
 template <int D, bool kFp8, bool kPlain>
-__device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
+__device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
                        const Plan* plan, uint32_t* counters, Part<D>* parts, int x, int thread, int lane) {
   const uint32_t lanes = static_cast<uint32_t>(thread / 32 * 32) << 16;
   const uint32_t s_at = sh.tensor + lanes + x * 128, o_at = sh.tensor + lanes + 256 + x * 128;
@@ -750,8 +794,8 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
   Row row_next{};
   int h_next = 0;
   if (more) {
-    row_next = take_row<D>(sh, batch, a, next, x, thread, h_next);
-    hand_over<D>(sh, x);
+    row_next = take_row<D, kFp8>(sh, batch, a, next, x, thread, h_next);
+    hand_over(sh, x, lane);
   }
   while (more) {
     const Walk walk = next;
@@ -765,9 +809,9 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
       const uint32_t all_done = tiles_before + (tile - walk.tile0);
       const int stage = all_done % kStages;
       const int j0 = walk.key_of(tile);
-      if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.s_full[x], s_done & 1, &sh.failed))) return;
+      if (!warp_wait(&sh.s_full[x], s_done & 1, &sh.failed)) return;
       fence_after();
-      if (kFp8 && !__all_sync(0xFFFFFFFFu, barrier_wait(&sh.v_full[stage], all_done / kStages & 1, &sh.failed))) return;
+      if (kFp8 && !warp_wait(&sh.v_full[stage], all_done / kStages & 1, &sh.failed)) return;
       const uint32_t absent = sh.absent[all_done % 4];
       const bool whole = __all_sync(0xFFFFFFFFu, row.token < 0 || (row.lo <= j0 && row.hi >= j0 + kKeys)) && absent == 0;
       const bool direct = kPlain && whole;
@@ -848,7 +892,7 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
       const bool moves = best > top;
       if (__any_sync(0xFFFFFFFFu, moves && top > -INFINITY)) {
         // the product before has to be done with O
-        if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.o_done[x], (s_done - 1) & 1, &sh.failed))) return;
+        if (!warp_wait(&sh.o_done[x], (s_done - 1) & 1, &sh.failed)) return;
         fence_after();
         const float keep = moves ? exp2_approx(top - best) : 1.0f;
 #pragma unroll 1
@@ -894,18 +938,18 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
       }
       tensor_stored();
       fence_before();
-      barrier_arrive(&sh.p_full[x]);
+      warp_arrive(&sh.p_full[x], lane);
       if (tile + 1 == walk.tile1) {
         // the products have read the last of this unit's queries
         more = find(skipped);
-        if (more) row_next = take_row<D>(sh, batch, a, next, x, thread, h_next);
+        if (more) row_next = take_row<D, kFp8>(sh, batch, a, next, x, thread, h_next);
       }
     }
-    if (more) hand_over<D>(sh, x);
+    if (more) hand_over(sh, x, lane);
     tiles_before += walk.tile1 - walk.tile0;
 
     // --- the unit's rows are done, here at least
-    if (!__all_sync(0xFFFFFFFFu, barrier_wait(&sh.o_done[x], (s_done - 1) & 1, &sh.failed))) return;
+    if (!warp_wait(&sh.o_done[x], (s_done - 1) & 1, &sh.failed)) return;
     fence_after();
     const int c_first = static_cast<int>(walk.unit0 / walk.per), c_last = static_cast<int>((walk.unit0 + pair.tiles - 1) / walk.per);
     const int self = static_cast<int>(blockIdx.x);
@@ -962,14 +1006,14 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
         part.sum[r_part] = sum;
       }
       __threadfence();
-      if (!group_sync(sh, x, phase)) return;
+      if (!group_sync(sh, x, phase, lane)) return;
       if (thread == 0) {
         const uint32_t before = atomicAdd(&counters[2 * c_first + x], 1u);
         sh.last[x] = before == static_cast<uint32_t>(c_last - c_first);
         if (sh.last[x]) counters[2 * c_first + x] = 0;
         __threadfence();
       }
-      if (!group_sync(sh, x, phase)) return;
+      if (!group_sync(sh, x, phase, lane)) return;
       if (sh.last[x]) {
         // Each lane weighs the parts of its own row; then the warp goes through its 32 rows,
         // 16 at a time with all their loads in flight, a lane for D / 32 of a row's elements.
@@ -1033,7 +1077,7 @@ __device__ void soften(Shared<D>& sh, const CacheView& cache, const BatchView& b
           }
         }
       }
-      if (!group_sync(sh, x, phase)) return;  // sh.last has been read
+      if (!group_sync(sh, x, phase, lane)) return;  // sh.last has been read
     } else if (row.token >= 0 && a.lse != nullptr) {
       a.lse[static_cast<uint64_t>(row.token) * a.q_heads + h] = some ? top * kLn2 + logf(sum) : -INFINITY;
     }
@@ -1051,22 +1095,26 @@ __global__ void __launch_bounds__(threads_of<kFp8>(), 1)
 many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArgs a, const Plan* plan, uint32_t* counters,
                  int* flag, Part<D>* parts, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   extern __shared__ uint8_t raw[];
-  Shared<D>& sh = *reinterpret_cast<Shared<D>*>(raw + ((1024 - (shared_address(raw) & 1023)) & 1023));
+  Shared<D, kFp8>& sh = *reinterpret_cast<Shared<D, kFp8>*>(raw + ((1024 - (shared_address(raw) & 1023)) & 1023));
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      barrier_init(&sh.q_full[i], 128);
+      barrier_init(&sh.q_full[i], 4);
       barrier_init(&sh.s_full[i], 2);
-      barrier_init(&sh.p_full[i], 128);
+      barrier_init(&sh.p_full[i], 4);
       barrier_init(&sh.o_done[i], 1);
-      barrier_init(&sh.group[i], 128);
+      barrier_init(&sh.group[i], 4);
     }
     for (int i = 0; i < kStages; ++i) {
-      barrier_init(&sh.k_full[i], kFp8 ? 128 : 1);
+      barrier_init(&sh.k_full[i], kFp8 ? 4 : 1);
       barrier_init(&sh.k_empty[i], 1);
-      barrier_init(&sh.v_full[i], kFp8 ? 128 : 1);
+      barrier_init(&sh.v_full[i], kFp8 ? 4 : 1);
       barrier_init(&sh.v_empty[i], 1);
       barrier_init(&sh.v_fixed[i], 2);
+    }
+    for (int i = 0; i < kRaw; ++i) {
+      barrier_init(&sh.raw_full[i], 1);
+      barrier_init(&sh.raw_empty[i], 4);
     }
     barrier_init(&sh.drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -1085,11 +1133,11 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
 
   // the warpgroups of the rows hold a tile's scores in registers
   if (warp < 8) {
-    if (kFp8) asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
-    else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    if (kFp8) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
   } else {
-    if (kFp8) asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
-    else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (kFp8) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
   }
   if (warp < 8) {
     soften<D, kFp8, kPlain>(sh, cache, batch, a, plan, counters, parts, warp / 4, threadIdx.x % 128, lane);
@@ -1098,12 +1146,14 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
     if (lane == 0) commit(&sh.drained);  // no product outlives the tensor memory
     __syncwarp();
     barrier_settle(&sh.drained, 0);
-  } else if (kFp8) {
-    if (warp < 12) convert_tiles<D>(sh, cache, batch, a, plan, threadIdx.x - 256, lane);
-  } else if (warp == 9) {
-    copy_tiles<D>(sh, cache, batch, a, plan, &k_map, &v_map, lane);
   } else {
-    fix_tiles<D>(sh, cache, batch, a, plan, threadIdx.x - 10 * 32, lane);
+    if constexpr (kFp8) {
+      if (warp < 12) convert_tiles<D>(sh, cache, batch, a, plan, threadIdx.x - 256, lane);
+      else if (warp == 13) copy_codes<D>(sh, cache, batch, a, plan, &k_map, &v_map, lane);
+    } else {
+      if (warp == 9) copy_tiles<D>(sh, cache, batch, a, plan, &k_map, &v_map, lane);
+      else fix_tiles<D>(sh, cache, batch, a, plan, threadIdx.x - 10 * 32, lane);
+    }
   }
   __syncwarp();
   asm volatile("cp.async.wait_all;" ::: "memory");
@@ -1122,7 +1172,7 @@ template <int D, bool kFp8, bool kPlain>
 cudaError_t launch_kernel(const CacheView& cache, const CUtensorMap* maps, const BatchView& batch, const AttentionArgs& args,
                    char* workspace, uint32_t* counters, int* flag, cudaStream_t stream) {
   auto kernel = many_rows_kernel<D, kFp8, kPlain>;
-  constexpr int kShared = static_cast<int>(sizeof(Shared<D>)) + 1024;
+  constexpr int kShared = static_cast<int>(sizeof(Shared<D, kFp8>)) + 1024;
   int device = 0;
   cudaGetDevice(&device);
   // SMs of each device whose kernel has been given its shared memory

@@ -17,7 +17,7 @@ struct es_cache {
   int page_size;
   int head_dim;
   esopt::CacheView view;
-  CUtensorMap maps[2];  // of k and v; bf16 only
+  CUtensorMap maps[2];  // of k and v
 };
 
 namespace {
@@ -109,8 +109,9 @@ es_status_t check_stride(uint64_t stride, int heads, int head_dim, const char* c
   return ES_OK;
 }
 
-// Pages as [page][head and slot][element], read in boxes of one page of a head by 64 elements
-// (128 bytes, swizzled); pages past the last one read as zeros.
+// Pages as [page][head and slot][element]; pages past the last one read as zeros. bf16 is read
+// in boxes of one page of a head by 64 elements (128 bytes, swizzled), FP8 in boxes of up to
+// 64 whole codes' vectors as they lie.
 es_status_t make_map(CUtensorMap* map, void* base, const es_cache_desc_t& d, const char* call) {
   using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                               const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -120,11 +121,15 @@ es_status_t make_map(CUtensorMap* map, void* base, const es_cache_desc_t& d, con
   const cudaError_t err = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &found, 12000, cudaEnableDefault, &result);
   if (err != cudaSuccess || found == nullptr) return cuda_fail(err != cudaSuccess ? err : cudaErrorNotSupported, "cuTensorMapEncodeTiled");
   const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d.head_dim), static_cast<cuuint64_t>(d.kv_heads) * d.page_size, d.num_pages};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(d.head_dim) * 2, d.page_stride * 2};
-  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(d.page_size), 1}, steps[3] = {1, 1, 1};
+  const bool fp8 = d.dtype == ES_FP8_E4M3;
+  const cuuint64_t size = fp8 ? 1 : 2;
+  const cuuint64_t strides[2] = {d.head_dim * size, d.page_stride * size};
+  const cuuint32_t box[3] = {fp8 ? static_cast<cuuint32_t>(d.head_dim) : 64u,
+                             static_cast<cuuint32_t>(fp8 && d.page_size > 64 ? 64 : d.page_size), 1};
+  const cuuint32_t steps[3] = {1, 1, 1};
   const CUresult made = reinterpret_cast<Encode>(found)(
-      map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+      map, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+      fp8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (made != CUDA_SUCCESS) return fail(ES_ERR_CUDA, "%s: cuTensorMapEncodeTiled returned %d", call, static_cast<int>(made));
   return ES_OK;
 }
@@ -184,7 +189,7 @@ es_status_t es_cache_create(const es_cache_desc_t* d, es_cache_t* out) {
   c->head_dim = d->head_dim;
   c->view = esopt::CacheView{d->k, d->v, d->k_scale, d->v_scale, d->page_stride, d->scale_stride,
                              static_cast<int>(d->num_pages), shift, d->kv_heads};
-  if (!fp8 && ((st = make_map(&c->maps[0], d->k, *d, call)) != ES_OK || (st = make_map(&c->maps[1], d->v, *d, call)) != ES_OK)) {
+  if ((st = make_map(&c->maps[0], d->k, *d, call)) != ES_OK || (st = make_map(&c->maps[1], d->v, *d, call)) != ES_OK) {
     delete c;
     return st;
   }

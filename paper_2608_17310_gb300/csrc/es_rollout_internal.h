@@ -118,7 +118,7 @@ cudaError_t launch_append(const CacheView& cache, bool fp8, int head_dim, const 
                           const AppendArgs& args, cudaStream_t stream);
 cudaError_t launch_read(const CacheView& cache, bool fp8, int head_dim, const BatchView& batch,
                         uint16_t* k_out, uint16_t* v_out, cudaStream_t stream);
-// maps: of the keys and the values of a bf16 cache, for TMA.
+// maps: of the keys and the values, for TMA.
 cudaError_t launch_attention(const CacheView& cache, const CUtensorMap* maps, bool fp8, int head_dim, const BatchView& batch,
                              const AttentionArgs& args, void* workspace, cudaStream_t stream);
 uint64_t attention_workspace_bytes(int head_dim);
