@@ -40,7 +40,10 @@ constexpr int kStages = 2;
 constexpr int kMaxGrid = 192;
 // What a unit costs beside its tiles, in tiles: its queries, the first tile's way through the
 // pipeline, its results.
-constexpr int kUnitCost = 2;
+constexpr int kUnitCost = 4;
+// No block takes less than this of a unit that others share: a part costs its way through
+// memory, about as much as two tiles.
+constexpr int kLeastShare = 3;
 constexpr float kSlack = 8.0f;  // log 2 of how far a score may be above the kept maximum
 
 // Where a block's range begins, from the planning kernel.
@@ -69,7 +72,8 @@ __device__ __forceinline__ int row_tiles_of(const BatchView& b, const AttentionA
   return static_cast<int>((static_cast<int64_t>(count) * a.group + kRows - 1) / kRows);
 }
 
-// Called by `lanes` threads that are numbered `lane` and share a warp, or by one thread.
+// Called by whole warps, kLanes threads of which (1, 8 or 32) share a pair and are numbered
+// `lane`.
 template <int kLanes>
 __device__ __forceinline__ Pair pair_of(const BatchView& b, const AttentionArgs& a, int seq, int row_tile, int lane) {
   Pair p;
@@ -90,6 +94,7 @@ __device__ __forceinline__ Pair pair_of(const BatchView& b, const AttentionArgs&
     in_lo = r1.lo;
     in_hi = r0.hi;
   } else {
+#pragma unroll 4
     for (int i = i0 + lane; i <= i1; i += kLanes) {
       const Row r = row_of(b, a, p.begin, p.count, p.base, p.length, i * a.group);
       if (r.hi > r.lo) {
@@ -99,11 +104,12 @@ __device__ __forceinline__ Pair pair_of(const BatchView& b, const AttentionArgs&
       in_lo = max(in_lo, r.lo);
       in_hi = min(in_hi, r.hi);
     }
-    if (kLanes == 32) {
-      lo = __reduce_min_sync(0xFFFFFFFFu, lo);
-      hi = __reduce_max_sync(0xFFFFFFFFu, hi);
-      in_lo = __reduce_max_sync(0xFFFFFFFFu, in_lo);
-      in_hi = __reduce_min_sync(0xFFFFFFFFu, in_hi);
+#pragma unroll
+    for (int m = kLanes / 2; m > 0; m >>= 1) {
+      lo = min(lo, __shfl_xor_sync(0xFFFFFFFFu, lo, m));
+      hi = max(hi, __shfl_xor_sync(0xFFFFFFFFu, hi, m));
+      in_lo = max(in_lo, __shfl_xor_sync(0xFFFFFFFFu, in_lo, m));
+      in_hi = min(in_hi, __shfl_xor_sync(0xFFFFFFFFu, in_hi, m));
     }
   }
   if (hi <= lo) lo = hi = 0;
@@ -183,11 +189,13 @@ plan_kernel(const BatchView batch, const AttentionArgs a, int kv_heads, int grid
       } else {
         if (pass == 0 || pairs > kPlanThreads) {
           __syncthreads();
-          // a warp for each pair: its tokens' entries are read side by side
-          for (int i = warp; i < kPlanThreads && p0 + i < pairs; i += kPlanThreads / 32) {
-            const int s = sequence_of(p0 + i);
-            const int of_pair = pair_of<32>(batch, a, s, static_cast<int>(p0 + i - first_pair[s]), lane).tiles;
-            if (lane == 0) tiles[i] = of_pair;
+          // eight threads for each pair: its tokens' entries are read side by side
+          for (int i = warp * 4; i < kPlanThreads && p0 + i < pairs; i += kPlanThreads / 8) {
+            const int mine = i + lane / 8;
+            const int64_t at = min(p0 + mine, pairs - 1);
+            const int s = sequence_of(at);
+            const int of_pair = pair_of<8>(batch, a, s, static_cast<int>(at - first_pair[s]), lane % 8).tiles;
+            if (lane % 8 == 0) tiles[mine] = of_pair;
           }
           __syncthreads();
         }
@@ -364,9 +372,10 @@ struct Shared {
 
 // Parts of units that blocks share, as in the kernel of few rows: block c's first unit, if it
 // began in an earlier block, is part 2c, and its last one, if it began here, part 2c + 1.
+// A row belongs to a thread, so 16 bytes of all rows lie together.
 template <int D>
 struct Part {
-  float o[kRows][D];
+  float4 o[D / 4][kRows];
   float top[kRows], sum[kRows];
 };
 
@@ -399,25 +408,43 @@ struct Walk {
       pair = pair_of<32>(b, a, seq, row_tile, lane);
     }
   }
+  // The tile of the unit at which a block's range that ends at p does: p itself, or the unit's
+  // begin or end where that is near.
+  __device__ __forceinline__ int cut(int64_t p) const {
+    const int n = pair.tiles;
+    const int raw = static_cast<int>(min(max(p - unit0, static_cast<int64_t>(0)), static_cast<int64_t>(n)));
+    if (n < 2 * kLeastShare) return 2 * raw < n ? 0 : n;
+    return raw < kLeastShare ? 0 : n - raw < kLeastShare ? n : raw;
+  }
   __device__ __forceinline__ bool next(const BatchView& b, const AttentionArgs& a, int kv_heads, int lane) {
-    if (at >= end) return false;
-    while (at >= pair_tile + static_cast<int64_t>(pair.tiles + kUnitCost) * kv_heads) {
-      pair_tile += static_cast<int64_t>(pair.tiles + kUnitCost) * kv_heads;
-      ++row_tile;
-      while (row_tile >= row_tiles_of(b, a, seq)) {
-        ++seq;
-        row_tile = 0;
+    while (at < end) {
+      while (at >= pair_tile + static_cast<int64_t>(pair.tiles + kUnitCost) * kv_heads) {
+        pair_tile += static_cast<int64_t>(pair.tiles + kUnitCost) * kv_heads;
+        ++row_tile;
+        while (row_tile >= row_tiles_of(b, a, seq)) {
+          ++seq;
+          row_tile = 0;
+        }
+        pair = pair_of<32>(b, a, seq, row_tile, lane);
       }
-      pair = pair_of<32>(b, a, seq, row_tile, lane);
+      const int length = pair.tiles + kUnitCost;
+      head = static_cast<int>((at - pair_tile) / length);
+      const int64_t begin = pair_tile + static_cast<int64_t>(head) * length;
+      unit0 = begin + kUnitCost;
+      tile0 = at <= begin ? 0 : cut(at);
+      tile1 = end >= begin + length ? pair.tiles : cut(end);
+      at = begin + length;
+      two = pair.rows > 128;
+      if (tile1 > tile0) return true;
     }
-    const int length = pair.tiles + kUnitCost;
-    head = static_cast<int>((at - pair_tile) / length);
-    unit0 = pair_tile + static_cast<int64_t>(head) * length + kUnitCost;
-    tile0 = static_cast<int>(max(at - unit0, static_cast<int64_t>(0)));
-    tile1 = static_cast<int>(min(unit0 + pair.tiles, end) - unit0);
-    at = unit0 + tile1;
-    two = pair.rows > 128;
-    return tile1 > tile0;  // else the range ends in what comes before the unit's tiles
+    return false;
+  }
+  // The blocks that have the unit's first tile and its last.
+  __device__ __forceinline__ void sharers(int& c_first, int& c_last) const {
+    c_first = static_cast<int>((unit0 - kUnitCost) / per);
+    c_last = static_cast<int>((unit0 + pair.tiles - 1) / per);
+    while (c_first < c_last && cut((c_first + 1) * per) == 0) ++c_first;
+    while (c_last > c_first && cut(c_last * per) == pair.tiles) --c_last;
   }
   __device__ __forceinline__ int key_of(int tile) const { return (pair.lo & ~(kKeys - 1)) + tile * kKeys; }
   // Not every row sees all of the tile.
@@ -566,7 +593,7 @@ __device__ __forceinline__ void convert_half(const uint8_t* raw, uint16_t* to, i
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         if (key < lo || key >= hi) u[e] = 0;
-        const uint32_t bad = ((u[e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+        const uint32_t bad = ((u[e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;  // NaN codes
         if (bad != 0) {
           u[e] &= ~((bad >> 7) * 0xFFu);
           *static_cast<volatile int*>(poisoned) = 1;
@@ -799,7 +826,6 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
   }
   while (more) {
     const Walk walk = next;
-    const Pair& pair = walk.pair;
     const Row row = row_next;
     const int h = h_next;
     tiles_before += skipped;
@@ -951,7 +977,8 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
     // --- the unit's rows are done, here at least
     if (!warp_wait(&sh.o_done[x], (s_done - 1) & 1, &sh.failed)) return;
     fence_after();
-    const int c_first = static_cast<int>(walk.unit0 / walk.per), c_last = static_cast<int>((walk.unit0 + pair.tiles - 1) / walk.per);
+    int c_first, c_last;
+    walk.sharers(c_first, c_last);
     const int self = static_cast<int>(blockIdx.x);
     const bool shared_unit = c_first != c_last;
     const bool poisoned = *static_cast<volatile int*>(&sh.poisoned) != 0;
@@ -988,7 +1015,8 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
       if (row.token < 0) continue;
       if (shared_unit) {
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(&part.o[r_part][c + i]) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+        for (int i = 0; i < 32; i += 4)
+          part.o[(c + i) / 4][r_part] = make_float4(__uint_as_float(w[i]), __uint_as_float(w[i + 1]), __uint_as_float(w[i + 2]), __uint_as_float(w[i + 3]));
       } else {
 #pragma unroll
         for (int i = 0; i < 32; i += 8) {
@@ -1015,67 +1043,47 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
       }
       if (!group_sync(sh, x, phase, lane)) return;
       if (sh.last[x]) {
-        // Each lane weighs the parts of its own row; then the warp goes through its 32 rows,
-        // 16 at a time with all their loads in flight, a lane for D / 32 of a row's elements.
-        constexpr int kPer = D / 32;
         const int n = c_last - c_first + 1;
         auto part_of = [&](int i) -> const Part<D>& { return parts[2 * (c_first + i) + (i == 0)]; };
-        float most = -INFINITY, l = 0.0f;
         if (row.token >= 0) {
+          float most = -INFINITY, l = 0.0f;
 #pragma unroll 4
           for (int i = 0; i < n; ++i) most = fmaxf(most, __ldcg(&part_of(i).top[r_part]));
+          const float z = most == -INFINITY ? 0.0f : most;
 #pragma unroll 4
-          for (int i = 0; i < n; ++i)
-            l += __ldcg(&part_of(i).sum[r_part]) * exp2_approx(__ldcg(&part_of(i).top[r_part]) - (most == -INFINITY ? 0.0f : most));
-          if (a.lse != nullptr)
-            a.lse[static_cast<uint64_t>(row.token) * a.q_heads + h] = most > -INFINITY || l != l ? most * kLn2 + logf(l) : -INFINITY;
-        }
-        const float z = most == -INFINITY ? 0.0f : most;
-        const float i1 = most > -INFINITY || l != l ? 1.0f / l : 0.0f;
-        const int rows = min(32, pair.rows - x * 128 - thread / 32 * 32), at = x * 128 + thread / 32 * 32;
+          for (int i = 0; i < n; ++i) l += __ldcg(&part_of(i).sum[r_part]) * exp2_approx(__ldcg(&part_of(i).top[r_part]) - z);
+          const bool any = most > -INFINITY || l != l;
+          const float i1 = any ? 1.0f / l : 0.0f;
+          if (a.lse != nullptr) a.lse[static_cast<uint64_t>(row.token) * a.q_heads + h] = any ? most * kLn2 + logf(l) : -INFINITY;
 #pragma unroll 1
-        for (int r0 = 0; r0 < rows; r0 += 16) {
-          float y[16][kPer] = {};
-#pragma unroll 1
-          for (int i = 0; i < n; ++i) {
-            const Part<D>& from = part_of(i);
-            const float f = row.token >= 0 ? exp2_approx(__ldcg(&from.top[r_part]) - z) : 0.0f;
-            float v[16][kPer];
+          for (int c = 0; c < D / 4; c += 16) {
+            float4 y[16];
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
-              const float* o = &from.o[at + r0 + q][lane * kPer];
-              if constexpr (kPer == 4) {
-                const float4 w = r0 + q < rows ? __ldcg(reinterpret_cast<const float4*>(o)) : make_float4(0, 0, 0, 0);
-                v[q][0] = w.x;
-                v[q][1] = w.y;
-                v[q][2] = w.z;
-                v[q][3] = w.w;
-              } else {
-                const float2 w = r0 + q < rows ? __ldcg(reinterpret_cast<const float2*>(o)) : make_float2(0, 0);
-                v[q][0] = w.x;
-                v[q][1] = w.y;
+            for (int e = 0; e < 16; ++e) y[e] = make_float4(0, 0, 0, 0);
+#pragma unroll 1
+            for (int i = 0; i < n; ++i) {
+              const Part<D>& from = part_of(i);
+              const float f = exp2_approx(__ldcg(&from.top[r_part]) - z);
+              float4 v[16];
+#pragma unroll
+              for (int e = 0; e < 16; ++e) v[e] = __ldcg(&from.o[c + e][r_part]);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                y[e].x += v[e].x * f;
+                y[e].y += v[e].y * f;
+                y[e].z += v[e].z * f;
+                y[e].w += v[e].w * f;
               }
             }
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
-              const float g = __shfl_sync(0xFFFFFFFFu, f, r0 + q);
-#pragma unroll
-              for (int e = 0; e < kPer; ++e) y[q][e] += v[q][e] * g;
-            }
-          }
-#pragma unroll
-          for (int q = 0; q < 16; ++q) {
-            const int token = __shfl_sync(0xFFFFFFFFu, row.token, r0 + q), hh = __shfl_sync(0xFFFFFFFFu, h, r0 + q);
-            const float g = __shfl_sync(0xFFFFFFFFu, i1, r0 + q);
-            const bool any = __shfl_sync(0xFFFFFFFFu, static_cast<int>(i1 != 0.0f), r0 + q) != 0;
-            if (token < 0) continue;
-            uint32_t* to = reinterpret_cast<uint32_t*>(a.out + static_cast<uint64_t>(token) * a.out_stride + static_cast<uint64_t>(hh) * D + lane * kPer);
-            if constexpr (kPer == 4)
-              *reinterpret_cast<uint2*>(to) = any ? make_uint2(pack_bf16(y[q][0] * g, y[q][1] * g), pack_bf16(y[q][2] * g, y[q][3] * g)) : make_uint2(0, 0);
-            else
-              *to = any ? pack_bf16(y[q][0] * g, y[q][1] * g) : 0u;
+            for (int e = 0; e < 16; e += 2)
+              *reinterpret_cast<uint4*>(out + (c + e) * 4) =
+                  any ? make_uint4(pack_bf16(y[e].x * i1, y[e].y * i1), pack_bf16(y[e].z * i1, y[e].w * i1),
+                                   pack_bf16(y[e + 1].x * i1, y[e + 1].y * i1), pack_bf16(y[e + 1].z * i1, y[e + 1].w * i1))
+                      : make_uint4(0, 0, 0, 0);
           }
         }
+        __syncwarp();
       }
       if (!group_sync(sh, x, phase, lane)) return;  // sh.last has been read
     } else if (row.token >= 0 && a.lse != nullptr) {

@@ -592,3 +592,20 @@ def test_prompts_of_many_tiles(ro, dtype, kw):
             assert (err <= (2.0 ** -7 + 2.0 ** -12) * (w @ v[b][:, h // 4].abs())).all()
             assert ((lse[t:t + n, h].cpu().double() - torch.logsumexp(x, -1)).abs() <= 1e-4).all()
         t += n
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_every_e4m3_code_counts_as_its_number(ro, new):
+    # one key holds every code as its value (two heads of 128), and is all that is seen
+    s = Setup(ro, [64], [new], 2, 128, 16, "e4m3")
+    codes = torch.arange(256, dtype=torch.uint8).view(2, 128).cuda()
+    page, slot = s.pages[0][0], 5
+    s.v.view(torch.uint8)[page, :, slot] = codes
+    s.vs[page, :, slot] = torch.tensor([1.0, 0.5], device="cuda")
+    first = torch.full((new,), 5, dtype=torch.int32)
+    q, out, lse = attend(s, 4, first=first, last=first + 1)
+    want = (R.e4m3(codes.cpu()) * torch.tensor([[1.0], [0.5]])).repeat_interleave(2, 0)
+    got = out.cpu().double()
+    assert torch.equal(torch.isnan(got), torch.isnan(want).expand_as(got))
+    keep = ~torch.isnan(want)
+    assert (got[:, keep] == want[keep]).all()
