@@ -579,29 +579,40 @@ __device__ void copy_codes(Shared<D, true>& sh, const CacheView& cache, const Ba
 }
 
 // A half tile of codes to bf16: 8 codes (16 bytes of bf16) to a thread and step, so that the
-// eight threads that write side by side write all of one 128-byte row.
+// eight threads that write side by side write all of one 128-byte row. All steps' codes are
+// read first: step by step a half took four times as long.
 // clean: keys outside [lo, hi) become zeros, and NaN codes too.
 template <int D>
 __device__ __forceinline__ void convert_half(const uint8_t* raw, uint16_t* to, int key0, int thread, bool clean, int lo, int hi,
                                              int* poisoned) {
+  constexpr int kSteps = kHalf * D / 8 / 128;
+  uint32_t u[kSteps][2];
 #pragma unroll
-  for (int i = 0; i < kHalf * D / 8 / 128; ++i) {
-    const int piece = i * 128 + thread, key = key0 + piece / (D / 8);
-    const uint2 w = *reinterpret_cast<const uint2*>(raw + piece * 8);
-    uint32_t u[2] = {w.x, w.y};
-    if (clean) {
+  for (int i = 0; i < kSteps; ++i) {
+    const uint2 w = *reinterpret_cast<const uint2*>(raw + (i * 128 + thread) * 8);
+    u[i][0] = w.x;
+    u[i][1] = w.y;
+  }
+  if (clean) {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const int key = key0 + (i * 128 + thread) / (D / 8);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        if (key < lo || key >= hi) u[e] = 0;
-        const uint32_t bad = ((u[e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;  // NaN codes
+        if (key < lo || key >= hi) u[i][e] = 0;
+        const uint32_t bad = ((u[i][e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;  // NaN codes
         if (bad != 0) {
-          u[e] &= ~((bad >> 7) * 0xFFu);
+          u[i][e] &= ~((bad >> 7) * 0xFFu);
           *static_cast<volatile int*>(poisoned) = 1;
         }
       }
     }
-    *reinterpret_cast<uint4*>(to + place_of<D>(key, piece % (D / 8))) =
-        make_uint4(bf16_of_e4m3(u[0]), bf16_of_e4m3(u[0] >> 16), bf16_of_e4m3(u[1]), bf16_of_e4m3(u[1] >> 16));
+  }
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int piece = i * 128 + thread;
+    *reinterpret_cast<uint4*>(to + place_of<D>(key0 + piece / (D / 8), piece % (D / 8))) =
+        make_uint4(bf16_of_e4m3(u[i][0]), bf16_of_e4m3(u[i][0] >> 16), bf16_of_e4m3(u[i][1]), bf16_of_e4m3(u[i][1] >> 16));
   }
 }
 
@@ -626,7 +637,6 @@ __device__ void convert_tiles(Shared<D, true>& sh, const CacheView& cache, const
       const int stage = done % kStages, j0 = walk.key_of(tile);
       const uint32_t parity = done / kStages & 1;
       const uint32_t absent = __ballot_sync(0xFFFFFFFFu, pages < 0) & 0xFFu;
-      const float next_k = scale_of(cache.k_scale, next_pages, tile + 1), next_v = scale_of(cache.v_scale, next_pages, tile + 1);
       const int lo = walk.pair.lo - j0, hi = walk.pair.hi - j0;
       const bool clean = walk.edge(tile);
       if (!warp_wait(&sh.k_empty[stage], parity ^ 1, &sh.failed)) return;
@@ -641,8 +651,17 @@ __device__ void convert_tiles(Shared<D, true>& sh, const CacheView& cache, const
       }
       fence_async();
       warp_arrive(&sh.k_full[stage], lane);
+      const float next_k = scale_of(cache.k_scale, next_pages, tile + 1), next_v = scale_of(cache.v_scale, next_pages, tile + 1);
       if (!warp_wait(&sh.v_empty[stage], parity ^ 1, &sh.failed)) return;
-      sh.v_scale[stage][thread] = clean && (thread < lo || thread >= hi) ? 0.0f : v_scale;
+      if (clean) {  // as with NaN codes: only rows that see the key get to know its scale
+        if (thread < lo || thread >= hi) {
+          v_scale = 0.0f;
+        } else if (!(fabsf(v_scale) <= FLT_MAX)) {
+          v_scale = 0.0f;
+          *static_cast<volatile int*>(&sh.poisoned) = 1;
+        }
+      }
+      sh.v_scale[stage][thread] = v_scale;
 #pragma unroll 1
       for (int half = 0; half < 2; ++half, ++raw_done) {
         const int slot = raw_done % kRaw;
@@ -948,9 +967,8 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
           sums[i / 2 % 2] = add2(sums[i / 2 % 2], pack(y, z));
           if (kFp8) {
             const float2 v = *reinterpret_cast<const float2*>(&sh.v_scale[stage][c * 32 + i]);
-            // an infinite scale stays with the rows that see its key
-            y = whole || y > 0.0f ? y * v.x : 0.0f;
-            z = whole || z > 0.0f ? z * v.y : 0.0f;
+            y *= v.x;
+            z *= v.y;
           }
           p[i / 2] = pack_bf16(y, z);
         }
@@ -1000,12 +1018,13 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
           for (int j = max(j0, row.lo); j < min(j0 + kKeys, row.hi); ++j) {
             const int page = page_of(cache, batch, walk.seq, j);
             if (page < 0) continue;
-            const uint64_t at = page * cache.page_stride +
-                                ((static_cast<uint64_t>(walk.head) << cache.page_shift) + (j & ((1 << cache.page_shift) - 1))) * D + c;
+            const uint64_t in_page = (static_cast<uint64_t>(walk.head) << cache.page_shift) + (j & ((1 << cache.page_shift) - 1));
+            const uint64_t at = page * cache.page_stride + in_page * D + c;
+            const float scale = kFp8 ? cache.v_scale[page * cache.scale_stride + in_page] : 1.0f;
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
               float v;
-              if (kFp8) v = __uint_as_float(bf16_of_e4m3(static_cast<const uint8_t*>(cache.v)[at + i]) << 16);
+              if (kFp8) v = __uint_as_float(bf16_of_e4m3(static_cast<const uint8_t*>(cache.v)[at + i]) << 16) * scale;
               else v = __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(cache.v)[at + i]) << 16);
               if (!(fabsf(v) <= FLT_MAX)) w[i] = __float_as_uint(__uint_as_float(w[i]) + v);
             }
