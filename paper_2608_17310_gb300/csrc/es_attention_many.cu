@@ -345,6 +345,24 @@ __device__ __forceinline__ void tensor_stored() { asm volatile("tcgen05.wait::st
 
 // --- the walk over a block's units -----------------------------------------------------
 
+// What the warps of a block need of a unit. One warp walks the units and puts them here, a few
+// ahead; kept by every warp for itself they cost registers and a share of each unit's time.
+struct Unit {
+  int valid;
+  int seq, head;
+  int tile0, tile1;  // this block's tiles, of the unit's
+  int key0;          // first key of tile 0
+  int begin, count, base, length;  // of the sequence's new tokens
+  int row0, rows;    // of the unit, among the sequence's
+  int lo, hi, in_lo, in_hi;
+  int c_first, c_last;  // the blocks that share it
+
+  __device__ __forceinline__ int key_of(int tile) const { return key0 + tile * kKeys; }
+  // Not every row sees all of the tile.
+  __device__ __forceinline__ bool edge(int tile) const { return key_of(tile) < in_lo || key_of(tile) + kKeys > in_hi; }
+};
+constexpr int kUnits = 4;
+
 // FP8: half tiles of codes on their way from the pages to the converting warps.
 constexpr int kRaw = 3;
 constexpr int kHalf = 64;  // keys
@@ -357,13 +375,15 @@ struct Shared {
   uint8_t raw[kFp8 ? kRaw : 1][kFp8 ? kHalf * D : 128];
   // Read with the scores, when the tile's keys may have made room for others: a slot is
   // written again four tiles on, which follows the scores of two tiles on.
-  float k_scale[4][kKeys];
+  float k_scale[4][kKeys];  // times the scores' factor
   uint32_t absent[4];  // 16-key pieces of the tile whose page does not exist
   float v_scale[kStages][kKeys];
   uint64_t q_full[2], s_full[2], p_full[2], o_done[2];
   uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages], v_fixed[kStages];
   uint64_t group[2], drained;
   uint64_t raw_full[kRaw], raw_empty[kRaw];
+  uint64_t unit_full[kUnits], unit_empty[kUnits];
+  Unit unit[kUnits];
   uint32_t tensor;           // address of the tensor memory
   int failed;
   int poisoned;              // a value that not every row sees was an infinity or NaN
@@ -386,7 +406,7 @@ __device__ __forceinline__ bool group_sync(Sh& sh, int x, uint32_t& phase, int l
   return warp_wait(&sh.group[x], phase++ & 1, &sh.failed);
 }
 
-// Every warp of a block walks the same units.
+// The units of a block's range, by one warp.
 struct Walk {
   int64_t at, end, per, pair_tile;
   int seq, row_tile;
@@ -394,7 +414,6 @@ struct Walk {
   // the unit
   int head, tile0, tile1;
   int64_t unit0;  // of its first tile
-  bool two;  // more than 128 rows
 
   __device__ __forceinline__ Walk(const BatchView& b, const AttentionArgs& a, const Plan* plan, int lane) {
     per = plan->per;
@@ -434,7 +453,6 @@ struct Walk {
       tile0 = at <= begin ? 0 : cut(at);
       tile1 = end >= begin + length ? pair.tiles : cut(end);
       at = begin + length;
-      two = pair.rows > 128;
       if (tile1 > tile0) return true;
     }
     return false;
@@ -446,13 +464,53 @@ struct Walk {
     while (c_first < c_last && cut((c_first + 1) * per) == 0) ++c_first;
     while (c_last > c_first && cut(c_last * per) == pair.tiles) --c_last;
   }
-  __device__ __forceinline__ int key_of(int tile) const { return (pair.lo & ~(kKeys - 1)) + tile * kKeys; }
-  // Not every row sees all of the tile.
-  __device__ __forceinline__ bool edge(int tile) const {
-    const int j = key_of(tile);
-    return j < pair.in_lo || j + kKeys > pair.in_hi;
-  }
 };
+
+// The walking warp's side: the next unit into its place; false where there is none (which is
+// told as well) or a wait was given up.
+template <class Sh>
+__device__ __forceinline__ bool tell(Sh& sh, Walk& walk, const BatchView& b, const AttentionArgs& a, int kv_heads, uint32_t n, int lane) {
+  const bool more = walk.next(b, a, kv_heads, lane);
+  if (!warp_wait(&sh.unit_empty[n % kUnits], (n / kUnits & 1) ^ 1, &sh.failed)) return false;
+  if (lane == 0) {
+    Unit& u = sh.unit[n % kUnits];
+    u.valid = more;
+    if (more) {
+      const Pair& p = walk.pair;
+      u.seq = walk.seq;
+      u.head = walk.head;
+      u.tile0 = walk.tile0;
+      u.tile1 = walk.tile1;
+      u.key0 = p.lo & ~(kKeys - 1);
+      u.begin = p.begin;
+      u.count = p.count;
+      u.base = p.base;
+      u.length = p.length;
+      u.row0 = walk.row_tile * kRows;
+      u.rows = p.rows;
+      u.lo = p.lo;
+      u.hi = p.hi;
+      u.in_lo = p.in_lo;
+      u.in_hi = p.in_hi;
+      int c_first, c_last;
+      walk.sharers(c_first, c_last);
+      u.c_first = c_first;
+      u.c_last = c_last;
+    }
+  }
+  warp_arrive(&sh.unit_full[n % kUnits], lane);
+  return more;
+}
+// The other warps': waits for unit n; false where there is none.
+template <class Sh>
+__device__ __forceinline__ bool take(Sh& sh, uint32_t n) {
+  return warp_wait(&sh.unit_full[n % kUnits], n / kUnits & 1, &sh.failed) && sh.unit[n % kUnits].valid;
+}
+// This warp is done with it.
+template <class Sh>
+__device__ __forceinline__ void leave(Sh& sh, uint32_t n, int lane) {
+  warp_arrive(&sh.unit_empty[n % kUnits], lane);
+}
 
 // Offset in elements of 16-byte piece `piece` of row r, in an operand of 128 rows.
 template <int D>
@@ -470,11 +528,12 @@ __device__ void copy_tiles(Shared<D, false>& sh, const CacheView& cache, const B
   uint32_t k_done = 0, v_done = 0;
   bool fine = true;
   Walk walk(batch, a, plan, lane);
-  while (fine && walk.next(batch, a, cache.kv_heads, lane)) {
+  for (uint32_t n = 0; fine && tell(sh, walk, batch, a, cache.kv_heads, n, lane); ++n) {
+    const int key0 = walk.pair.lo & ~(kKeys - 1);
     for (int tile = walk.tile0; tile < walk.tile1; ++tile) {
       const int stage = k_done % kStages;
       const uint32_t parity = k_done / kStages & 1;
-      const int j = walk.key_of(tile) + lane * page_size;
+      const int j = key0 + tile * kKeys + lane * page_size;
       int page = -1;
       if (lane < pages && j < walk.pair.hi) page = page_of(cache, batch, walk.seq, j);
       const uint32_t missing = __ballot_sync(0xFFFFFFFFu, page < 0);
@@ -513,19 +572,20 @@ __device__ void copy_tiles(Shared<D, false>& sh, const CacheView& cache, const B
 // them); the rows that see them get them when the unit is written. Every tile passes here,
 // so that the barriers of the stages are never a round ahead.
 template <int D>
-__device__ void fix_tiles(Shared<D, false>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
-                          const Plan* plan, int thread, int lane) {
+__device__ void fix_tiles(Shared<D, false>& sh, int thread, int lane) {
   uint32_t done = 0;
-  Walk walk(batch, a, plan, lane);
-  while (walk.next(batch, a, cache.kv_heads, lane)) {
-    for (int tile = walk.tile0; tile < walk.tile1; ++tile, ++done) {
-      const int stage = done % kStages, j0 = walk.key_of(tile);
+  for (uint32_t n = 0; take(sh, n); ++n) {
+    const Unit& unit = sh.unit[n % kUnits];
+    const int tile1 = unit.tile1;
+    for (int tile = unit.tile0; tile < tile1; ++tile, ++done) {
+      const int stage = done % kStages, j0 = unit.key_of(tile);
       if (!warp_wait(&sh.v_full[stage], done / kStages & 1, &sh.failed)) return;
-      if (walk.edge(tile)) {
+      if (unit.edge(tile)) {
+        const int lo = unit.lo, hi = unit.hi;
         for (int i = thread; i < kKeys * D / 8; i += 64) {
           const int key = i / (D / 8), j = j0 + key;
           uint4* at = reinterpret_cast<uint4*>(sh.v[stage] + place_of<D>(key, i % (D / 8)));
-          if (j < walk.pair.lo || j >= walk.pair.hi) {
+          if (j < lo || j >= hi) {
             *at = make_uint4(0, 0, 0, 0);
             continue;
           }
@@ -544,7 +604,14 @@ __device__ void fix_tiles(Shared<D, false>& sh, const CacheView& cache, const Ba
       }
       warp_arrive(&sh.v_fixed[stage], lane);
     }
+    leave(sh, n, lane);
   }
+}
+
+// What a dot product is multiplied by: to a score in units of log 2, or where scores are capped to
+// the exponent of their cap's 2^x. With FP8 the keys' scales come with it.
+__device__ __forceinline__ float factor_of(const AttentionArgs& a) {
+  return a.scale * (a.softcap > 0.0f ? 2.0f * kLog2e / a.softcap : kLog2e);
 }
 
 // FP8 pages to shared memory as they are, a half tile of keys at a time and of values after it.
@@ -555,14 +622,15 @@ __device__ void copy_codes(Shared<D, true>& sh, const CacheView& cache, const Ba
   uint32_t done = 0;
   bool fine = true;
   Walk walk(batch, a, plan, lane);
-  while (fine && walk.next(batch, a, cache.kv_heads, lane)) {
+  for (uint32_t n = 0; fine && tell(sh, walk, batch, a, cache.kv_heads, n, lane); ++n) {
+    const int key0 = walk.pair.lo & ~(kKeys - 1);
     for (int tile = walk.tile0; fine && tile < walk.tile1; ++tile) {
       // the copies of both halves: lane i's keys are 16 i and up
-      const int j = walk.key_of(tile) + lane * 16;
+      const int j = key0 + tile * kKeys + lane * 16;
       const int page = lane < 8 && j < walk.pair.hi ? page_of(cache, batch, walk.seq, j) : -1;
 #pragma unroll 1
       for (int part = 0; part < 4; ++part, ++done) {
-        const int slot = done % kRaw, j0 = walk.key_of(tile) + (part & 1) * kHalf;
+        const int slot = done % kRaw, j0 = key0 + tile * kKeys + (part & 1) * kHalf;
         const int mine = __shfl_sync(0xFFFFFFFFu, page, (part & 1) * 4 + lane * box / 16);
         fine = warp_wait(&sh.raw_empty[slot], (done / kRaw & 1) ^ 1, &sh.failed);
         if (!fine) break;
@@ -583,8 +651,8 @@ __device__ void copy_codes(Shared<D, true>& sh, const CacheView& cache, const Ba
 // read first: step by step a half took four times as long.
 // clean: keys outside [lo, hi) become zeros, and NaN codes too.
 template <int D>
-__device__ __forceinline__ void convert_half(const uint8_t* raw, uint16_t* to, int key0, int thread, bool clean, int lo, int hi,
-                                             int* poisoned) {
+__device__ __forceinline__ void convert_half(const uint8_t* raw, uint64_t* raw_empty, uint16_t* to, int key0, int thread, int lane,
+                                             bool clean, int lo, int hi, int* poisoned) {
   constexpr int kSteps = kHalf * D / 8 / 128;
   uint32_t u[kSteps][2];
 #pragma unroll
@@ -614,44 +682,49 @@ __device__ __forceinline__ void convert_half(const uint8_t* raw, uint16_t* to, i
     *reinterpret_cast<uint4*>(to + place_of<D>(key0 + piece / (D / 8), piece % (D / 8))) =
         make_uint4(bf16_of_e4m3(u[i][0]), bf16_of_e4m3(u[i][0] >> 16), bf16_of_e4m3(u[i][1]), bf16_of_e4m3(u[i][1] >> 16));
   }
+  // The next codes may come now that these have been used. (After their loads alone have been
+  // issued is too early: a copy of zeros can overtake them.)
+  warp_arrive(raw_empty, lane);
 }
 
 template <int D>
-__device__ void convert_tiles(Shared<D, true>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
-                              const Plan* plan, int thread, int lane) {
+__device__ void convert_tiles(Shared<D, true>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a, int thread,
+                              int lane) {
   uint32_t done = 0, raw_done = 0;
-  Walk walk(batch, a, plan, lane);
-  while (walk.next(batch, a, cache.kv_heads, lane)) {
+  const float factor = factor_of(a);
+  for (uint32_t n = 0; take(sh, n); ++n) {
+    const Unit& unit = sh.unit[n % kUnits];
+    const int tile1 = unit.tile1, seq = unit.seq;
+    const uint32_t rows = static_cast<uint32_t>(unit.head) << cache.page_shift;
     auto pages_of = [&](int tile) {  // lane i's is the page of the tile's keys 16 i and up
-      const int j = walk.key_of(tile) + lane * 16;
-      return lane < 8 && tile < walk.tile1 && j < walk.pair.hi ? page_of(cache, batch, walk.seq, j) : -1;
+      const int j = unit.key_of(tile) + lane * 16;
+      return lane < 8 && tile < tile1 && j < unit.hi ? page_of(cache, batch, seq, j) : -1;
     };
     auto scale_of = [&](const float* scales, int pages, int tile) {  // of key `thread` of the tile
       const int page = __shfl_sync(0xFFFFFFFFu, pages, thread / 16);
-      const uint64_t row = (static_cast<uint64_t>(walk.head) << cache.page_shift) + ((walk.key_of(tile) + thread) & ((1 << cache.page_shift) - 1));
-      return page >= 0 ? __ldg(scales + page * cache.scale_stride + row) : 0.0f;
+      return page >= 0 ? __ldg(scales + page * cache.scale_stride + rows + ((unit.key_of(tile) + thread) & ((1 << cache.page_shift) - 1))) : 0.0f;
     };
-    int pages = pages_of(walk.tile0), next_pages = pages_of(walk.tile0 + 1);
-    float k_scale = scale_of(cache.k_scale, pages, walk.tile0), v_scale = scale_of(cache.v_scale, pages, walk.tile0);
-    for (int tile = walk.tile0; tile < walk.tile1; ++tile, ++done) {
-      const int stage = done % kStages, j0 = walk.key_of(tile);
+    int tile = unit.tile0;
+    int pages = pages_of(tile), next_pages = pages_of(tile + 1);
+    float k_scale = scale_of(cache.k_scale, pages, tile), v_scale = scale_of(cache.v_scale, pages, tile);
+    for (; tile < tile1; ++tile, ++done) {
+      const int stage = done % kStages;
       const uint32_t parity = done / kStages & 1;
       const uint32_t absent = __ballot_sync(0xFFFFFFFFu, pages < 0) & 0xFFu;
-      const int lo = walk.pair.lo - j0, hi = walk.pair.hi - j0;
-      const bool clean = walk.edge(tile);
       if (!warp_wait(&sh.k_empty[stage], parity ^ 1, &sh.failed)) return;
       if (thread == 0) sh.absent[done % 4] = absent;
-      sh.k_scale[done % 4][thread] = k_scale;
+      sh.k_scale[done % 4][thread] = k_scale * factor;
+      k_scale = scale_of(cache.k_scale, next_pages, tile + 1);
 #pragma unroll 1
       for (int half = 0; half < 2; ++half, ++raw_done) {
         const int slot = raw_done % kRaw;
         if (!warp_wait(&sh.raw_full[slot], raw_done / kRaw & 1, &sh.failed)) return;
-        convert_half<D>(sh.raw[slot], sh.k[stage], half * kHalf, thread, false, 0, 0, nullptr);
-        warp_arrive(&sh.raw_empty[slot], lane);
+        convert_half<D>(sh.raw[slot], &sh.raw_empty[slot], sh.k[stage], half * kHalf, thread, lane, false, 0, 0, nullptr);
       }
       fence_async();
       warp_arrive(&sh.k_full[stage], lane);
-      const float next_k = scale_of(cache.k_scale, next_pages, tile + 1), next_v = scale_of(cache.v_scale, next_pages, tile + 1);
+      const bool clean = unit.edge(tile);
+      const int lo = unit.lo - unit.key_of(tile), hi = unit.hi - unit.key_of(tile);
       if (!warp_wait(&sh.v_empty[stage], parity ^ 1, &sh.failed)) return;
       if (clean) {  // as with NaN codes: only rows that see the key get to know its scale
         if (thread < lo || thread >= hi) {
@@ -662,20 +735,19 @@ __device__ void convert_tiles(Shared<D, true>& sh, const CacheView& cache, const
         }
       }
       sh.v_scale[stage][thread] = v_scale;
+      v_scale = scale_of(cache.v_scale, next_pages, tile + 1);
 #pragma unroll 1
       for (int half = 0; half < 2; ++half, ++raw_done) {
         const int slot = raw_done % kRaw;
         if (!warp_wait(&sh.raw_full[slot], raw_done / kRaw & 1, &sh.failed)) return;
-        convert_half<D>(sh.raw[slot], sh.v[stage], half * kHalf, thread, clean, lo, hi, &sh.poisoned);
-        warp_arrive(&sh.raw_empty[slot], lane);
+        convert_half<D>(sh.raw[slot], &sh.raw_empty[slot], sh.v[stage], half * kHalf, thread, lane, clean, lo, hi, &sh.poisoned);
       }
       fence_async();
       warp_arrive(&sh.v_full[stage], lane);
-      k_scale = next_k;
-      v_scale = next_v;
       pages = next_pages;
       next_pages = pages_of(tile + 2);
     }
+    leave(sh, n, lane);
   }
 }
 
@@ -690,8 +762,7 @@ __device__ __forceinline__ bool elected() {
 
 // The warp that issues the products.
 template <int D, bool kFp8>
-__device__ void issue_products(Shared<D, kFp8>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
-                               const Plan* plan, int lane) {
+__device__ void issue_products(Shared<D, kFp8>& sh, int lane) {
   constexpr uint32_t kScores = product_of(kKeys, false), kValues = product_of(D, true);
   const uint32_t tensor = sh.tensor;
   uint32_t k_done = 0, v_done = 0, units = 0, two_units = 0;
@@ -715,10 +786,10 @@ __device__ void issue_products(Shared<D, kFp8>& sh, const CacheView& cache, cons
     __syncwarp();
   };
   auto wait = [&](uint64_t* b, uint32_t parity) { return warp_wait(b, parity, &sh.failed); };
-  Walk walk(batch, a, plan, lane);
-  while (walk.next(batch, a, cache.kv_heads, lane)) {
-    const uint32_t count = walk.two ? 2 : 1;
-    const int tiles = walk.tile1 - walk.tile0;
+  for (uint32_t n = 0; take(sh, n); ++n) {
+    const uint32_t count = sh.unit[n % kUnits].rows > 128 ? 2 : 1;
+    const int tiles = sh.unit[n % kUnits].tile1 - sh.unit[n % kUnits].tile0;
+    leave(sh, n, lane);
     if (!wait(&sh.q_full[0], units & 1)) return;
     if (count == 2 && !wait(&sh.q_full[1], two_units & 1)) return;
     if (!wait(&sh.k_full[k_done % kStages], k_done / kStages & 1)) return;
@@ -770,6 +841,11 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
   return y;
 }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t y;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+  return y;
+}
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t y;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
@@ -789,14 +865,13 @@ __device__ __forceinline__ void copy_async(uint32_t to, const void* from, bool t
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
 }
 
-// This thread's row of the walk's unit, and its query on the way to shared memory.
+// This thread's row of a unit, and its query on the way to shared memory.
 template <int D, bool kFp8>
-__device__ __forceinline__ Row take_row(Shared<D, kFp8>& sh, const BatchView& batch, const AttentionArgs& a, const Walk& walk, int x,
+__device__ __forceinline__ Row take_row(Shared<D, kFp8>& sh, const BatchView& batch, const AttentionArgs& a, const Unit& unit, int x,
                                         int thread, int& h) {
-  const Pair& pair = walk.pair;
-  const int r = walk.row_tile * kRows + x * 128 + thread;
-  const Row row = row_of(batch, a, pair.begin, pair.count, pair.base, pair.length, r);
-  h = walk.head * a.group + r % a.group;
+  const int r = unit.row0 + x * 128 + thread;
+  const Row row = row_of(batch, a, unit.begin, unit.count, unit.base, unit.length, r);
+  h = unit.head * a.group + r % a.group;
   const uint16_t* from = a.q + static_cast<uint64_t>(max(row.token, 0)) * a.q_stride + static_cast<uint64_t>(h) * D;
 #pragma unroll
   for (int i = 0; i < D / 8; ++i) copy_async(shared_address(sh.q[x] + place_of<D>(thread, i)), from + i * 8, row.token >= 0);
@@ -813,47 +888,51 @@ __device__ __forceinline__ void hand_over(Sh& sh, int x, int lane) {
 // A warpgroup's rows: a thread for each.
 template <int D, bool kFp8, bool kPlain>
 __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
-                       const Plan* plan, uint32_t* counters, Part<D>* parts, int x, int thread, int lane) {
+                       uint32_t* counters, Part<D>* parts, int x, int thread, int lane) {
   const uint32_t lanes = static_cast<uint32_t>(thread / 32 * 32) << 16;
   const uint32_t s_at = sh.tensor + lanes + x * 128, o_at = sh.tensor + lanes + 256 + x * 128;
   // Scores in units of log 2. Capped: cap tanh(x / cap) = cap - 2 cap / (2^(2 x log2(e) / cap) + 1),
   // off by 1e-7 cap at most.
   const bool capped = a.softcap > 0.0f;
   const float cap = a.softcap * kLog2e;
-  const float factor = a.scale * (capped ? 2.0f * kLog2e / a.softcap : kLog2e);
+  const float factor = factor_of(a);
   uint32_t s_done = 0;        // tiles of this warpgroup so far
   uint32_t tiles_before = 0;  // of all units
   uint32_t phase = 0;
-  Walk next(batch, a, plan, lane);
-  // The next unit in which this warpgroup has rows. Its queries are fetched while the unit
-  // before is finished.
+  // Unit n is this warpgroup's next one with rows; the tiles of those without are counted.
+  uint32_t n = 0;
   auto find = [&](uint32_t& skipped) {
     skipped = 0;
-    while (next.next(batch, a, cache.kv_heads, lane)) {
-      if (x == 0 || next.two) return true;
-      skipped += next.tile1 - next.tile0;
+    for (;; ++n) {
+      if (!take(sh, n)) return false;
+      const Unit& u = sh.unit[n % kUnits];
+      if (u.rows > x * 128) return true;
+      skipped += u.tile1 - u.tile0;
+      leave(sh, n, lane);
     }
-    return false;
   };
   uint32_t skipped;
   bool more = find(skipped);
   Row row_next{};
   int h_next = 0;
   if (more) {
-    row_next = take_row<D, kFp8>(sh, batch, a, next, x, thread, h_next);
+    row_next = take_row<D, kFp8>(sh, batch, a, sh.unit[n % kUnits], x, thread, h_next);
     hand_over(sh, x, lane);
   }
   while (more) {
-    const Walk walk = next;
+    bool fetched = false, ended = false;
+    const uint32_t mine = n;
+    const Unit& unit = sh.unit[mine % kUnits];
     const Row row = row_next;
     const int h = h_next;
     tiles_before += skipped;
+    const int tile0 = unit.tile0, tile1 = unit.tile1, key0 = unit.key0;
     const float slope = !kPlain && a.slopes != nullptr ? a.slopes[h] * kLog2e : 0.0f;
     float top = -INFINITY, sum = 0.0f;
-    for (int tile = walk.tile0; tile < walk.tile1; ++tile, ++s_done) {
-      const uint32_t all_done = tiles_before + (tile - walk.tile0);
+    for (int tile = tile0; tile < tile1; ++tile, ++s_done) {
+      const uint32_t all_done = tiles_before + (tile - tile0);
       const int stage = all_done % kStages;
-      const int j0 = walk.key_of(tile);
+      const int j0 = key0 + tile * kKeys;
       if (!warp_wait(&sh.s_full[x], s_done & 1, &sh.failed)) return;
       fence_after();
       if (kFp8 && !warp_wait(&sh.v_full[stage], all_done / kStages & 1, &sh.failed)) return;
@@ -875,10 +954,10 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
             float f[4] = {factor, factor, factor, factor};
             if (kFp8) {
               const float4 k = *reinterpret_cast<const float4*>(&sh.k_scale[all_done % 4][c + i]);
-              f[0] *= k.x;
-              f[1] *= k.y;
-              f[2] *= k.z;
-              f[3] *= k.w;
+              f[0] = k.x;
+              f[1] = k.y;
+              f[2] = k.z;
+              f[3] = k.w;
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -915,14 +994,14 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
         for (int c = 0; c < kKeys / 32; ++c)
 #pragma unroll
           for (int i = 0; i < 32; i += 4) {
-            const float4 k = *reinterpret_cast<const float4*>(&sh.k_scale[all_done % 4][c * 32 + i]);
-            const float f[4] = {k.x * factor, k.y * factor, k.z * factor, k.w * factor};
+            const ulonglong2 k = *reinterpret_cast<const ulonglong2*>(&sh.k_scale[all_done % 4][c * 32 + i]);
+            float y[4];
+            unpack(mul2(pack(__uint_as_float(w[c][i]), __uint_as_float(w[c][i + 1])), k.x), y[0], y[1]);
+            unpack(mul2(pack(__uint_as_float(w[c][i + 2]), __uint_as_float(w[c][i + 3])), k.y), y[2], y[3]);
+            tops[i / 4 % 2] = fmaxf(tops[i / 4 % 2], fmaxf(y[0], y[1]));
+            tops[2 + i / 4 % 2] = fmaxf(tops[2 + i / 4 % 2], fmaxf(y[2], y[3]));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float y = __uint_as_float(w[c][i + e]) * f[e];
-              tops[e] = fmaxf(tops[e], y);
-              w[c][i + e] = __float_as_uint(y);
-            }
+            for (int e = 0; e < 4; ++e) w[c][i + e] = __float_as_uint(y[e]);
           }
       } else if (direct) {
 #pragma unroll
@@ -959,18 +1038,25 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
       for (int c = 0; c < kKeys / 32; ++c) {
         uint32_t p[16];
 #pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-          float y, z;
-          unpack(fma2(pack(__uint_as_float(w[c][i]), __uint_as_float(w[c][i + 1])), units, zeros), y, z);
-          y = exp2_approx(y);
-          z = exp2_approx(z);
-          sums[i / 2 % 2] = add2(sums[i / 2 % 2], pack(y, z));
-          if (kFp8) {
-            const float2 v = *reinterpret_cast<const float2*>(&sh.v_scale[stage][c * 32 + i]);
-            y *= v.x;
-            z *= v.y;
+        for (int i = 0; i < 32; i += 4) {
+          float y[4];
+          uint64_t x[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            unpack(fma2(pack(__uint_as_float(w[c][i + 2 * e]), __uint_as_float(w[c][i + 2 * e + 1])), units, zeros), y[2 * e], y[2 * e + 1]);
+            x[e] = pack(exp2_approx(y[2 * e]), exp2_approx(y[2 * e + 1]));
+            sums[e] = add2(sums[e], x[e]);
           }
-          p[i / 2] = pack_bf16(y, z);
+          if (kFp8) {
+            const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(&sh.v_scale[stage][c * 32 + i]);
+            x[0] = mul2(x[0], v.x);
+            x[1] = mul2(x[1], v.y);
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            unpack(x[e], y[2 * e], y[2 * e + 1]);
+            p[i / 2 + e] = pack_bf16(y[2 * e], y[2 * e + 1]);
+          }
         }
         tensor_store16(s_at + c * 16, p);
       }
@@ -983,20 +1069,23 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
       tensor_stored();
       fence_before();
       warp_arrive(&sh.p_full[x], lane);
-      if (tile + 1 == walk.tile1) {
-        // the products have read the last of this unit's queries
-        more = find(skipped);
-        if (more) row_next = take_row<D, kFp8>(sh, batch, a, next, x, thread, h_next);
+      if (tile + 1 == tile1) {
+        // The products have read the last of this unit's queries: those of the next one can
+        // come while this one is finished, if it has rows for this warpgroup. (To look further
+        // with this unit held would stop the walk.)
+        ++n;
+        ended = !take(sh, n);
+        fetched = !ended && sh.unit[n % kUnits].rows > x * 128;
+        if (fetched) row_next = take_row<D, kFp8>(sh, batch, a, sh.unit[n % kUnits], x, thread, h_next);
       }
     }
-    if (more) hand_over(sh, x, lane);
-    tiles_before += walk.tile1 - walk.tile0;
+    if (fetched) hand_over(sh, x, lane);
+    tiles_before += tile1 - tile0;
 
     // --- the unit's rows are done, here at least
     if (!warp_wait(&sh.o_done[x], (s_done - 1) & 1, &sh.failed)) return;
     fence_after();
-    int c_first, c_last;
-    walk.sharers(c_first, c_last);
+    const int c_first = unit.c_first, c_last = unit.c_last;
     const int self = static_cast<int>(blockIdx.x);
     const bool shared_unit = c_first != c_last;
     const bool poisoned = *static_cast<volatile int*>(&sh.poisoned) != 0;
@@ -1012,13 +1101,13 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
       tensor_load(w, o_at + c);
       tensor_loaded(w);
       if (poisoned && row.token >= 0) {
-        for (int tile = walk.tile0; tile < walk.tile1; ++tile) {
-          if (!walk.edge(tile)) continue;
-          const int j0 = walk.key_of(tile);
+        for (int tile = tile0; tile < tile1; ++tile) {
+          if (!unit.edge(tile)) continue;
+          const int j0 = unit.key_of(tile);
           for (int j = max(j0, row.lo); j < min(j0 + kKeys, row.hi); ++j) {
-            const int page = page_of(cache, batch, walk.seq, j);
+            const int page = page_of(cache, batch, unit.seq, j);
             if (page < 0) continue;
-            const uint64_t in_page = (static_cast<uint64_t>(walk.head) << cache.page_shift) + (j & ((1 << cache.page_shift) - 1));
+            const uint64_t in_page = (static_cast<uint64_t>(unit.head) << cache.page_shift) + (j & ((1 << cache.page_shift) - 1));
             const uint64_t at = page * cache.page_stride + in_page * D + c;
             const float scale = kFp8 ? cache.v_scale[page * cache.scale_stride + in_page] : 1.0f;
 #pragma unroll
@@ -1110,6 +1199,16 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
     }
     __syncwarp();
     fence_before();  // before the next unit's products write O
+    leave(sh, mine, lane);
+    more = fetched;
+    skipped = 0;
+    if (!fetched && !ended) {
+      more = find(skipped);
+      if (more) {
+        row_next = take_row<D, kFp8>(sh, batch, a, sh.unit[n % kUnits], x, thread, h_next);
+        hand_over(sh, x, lane);
+      }
+    }
   }
 }
 
@@ -1143,6 +1242,10 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
       barrier_init(&sh.raw_full[i], 1);
       barrier_init(&sh.raw_empty[i], 4);
     }
+    for (int i = 0; i < kUnits; ++i) {
+      barrier_init(&sh.unit_full[i], 1);
+      barrier_init(&sh.unit_empty[i], kFp8 ? 13 : 11);  // the warps that take units
+    }
     barrier_init(&sh.drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sh.failed = 0;
@@ -1167,19 +1270,19 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
   }
   if (warp < 8) {
-    soften<D, kFp8, kPlain>(sh, cache, batch, a, plan, counters, parts, warp / 4, threadIdx.x % 128, lane);
+    soften<D, kFp8, kPlain>(sh, cache, batch, a, counters, parts, warp / 4, threadIdx.x % 128, lane);
   } else if (warp == kIssuer) {
-    issue_products<D, kFp8>(sh, cache, batch, a, plan, lane);
+    issue_products<D, kFp8>(sh, lane);
     if (lane == 0) commit(&sh.drained);  // no product outlives the tensor memory
     __syncwarp();
     barrier_settle(&sh.drained, 0);
   } else {
     if constexpr (kFp8) {
-      if (warp < 12) convert_tiles<D>(sh, cache, batch, a, plan, threadIdx.x - 256, lane);
+      if (warp < 12) convert_tiles<D>(sh, cache, batch, a, threadIdx.x - 256, lane);
       else if (warp == 13) copy_codes<D>(sh, cache, batch, a, plan, &k_map, &v_map, lane);
     } else {
       if (warp == 9) copy_tiles<D>(sh, cache, batch, a, plan, &k_map, &v_map, lane);
-      else fix_tiles<D>(sh, cache, batch, a, plan, threadIdx.x - 10 * 32, lane);
+      else fix_tiles<D>(sh, threadIdx.x - 10 * 32, lane);
     }
   }
   __syncwarp();

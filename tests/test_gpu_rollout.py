@@ -573,16 +573,24 @@ def test_cache_refusals(es, ro):
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("kw", [{}, {"softcap": 20.0}], ids=["plain", "cap"])
-def test_prompts_of_many_tiles(ro, dtype, kw):
-    # blocks walk many tiles and units, most of them seen whole; units are shared by blocks
-    s = Setup(ro, [3000, 700, 1500], [900, 700, 70], 2, 128, 64, dtype, seed=12)
-    q, out, lse = attend(s, 8, **kw)
+@pytest.mark.parametrize("shape", ["tiles", "units"])
+def test_prompts_of_many_tiles(ro, dtype, kw, shape):
+    if shape == "tiles":
+        # blocks walk many tiles and units, most of them seen whole; units are shared by blocks
+        s = Setup(ro, [3000, 700, 1500], [900, 700, 70], 2, 128, 64, dtype, seed=12)
+        heads = 8
+    else:
+        # blocks walk many units, of one and of two tiles of rows in all orders
+        new = [64, 20, 20, 20, 20, 20, 20, 40, 9] * 14
+        s = Setup(ro, [n + 3 * i for i, n in enumerate(new)], new, 8, 64, 32, dtype, seed=12)
+        heads = 32
+    q, out, lse = attend(s, heads, **kw)
     k, v = s.dense()
     t = 0
     for b, n in enumerate(s.new):
         p = torch.arange(s.seq_len[b] - n, s.seq_len[b])[:, None]
         hide = torch.arange(s.seq_len[b])[None] > p
-        for h in range(8):
+        for h in range(heads):
             x = (q[t:t + n, h].cpu().double() @ k[b][:, h // 4].T) * s.d ** -0.5
             if "softcap" in kw:
                 x = kw["softcap"] * torch.tanh(x / kw["softcap"])
