@@ -39,8 +39,11 @@ constexpr int kRows = 256;   // of a unit
 constexpr int kStages = 2;
 constexpr int kMaxGrid = 192;
 // What a unit costs beside its tiles, in tiles: its queries, the first tile's way through the
-// pipeline, its results.
-constexpr int kUnitCost = 4;
+// pipeline, its results. Plain bf16 tiles are the quickest, so more of them fit: a prompt of
+// 8,191 tokens takes 593 us with 2, 499 with 3, 450 with 4, 473 with 6; where tiles take
+// longer 2 is best by 2 to 8 % (FP8, capped or biased scores).
+template <bool kFp8, bool kPlain>
+constexpr int unit_cost() { return kPlain && !kFp8 ? 4 : 2; }
 // No block takes less than this of a unit that others share: a part costs its way through
 // memory, about as much as two tiles.
 constexpr int kLeastShare = 3;
@@ -53,6 +56,7 @@ struct Start {
 };
 struct Plan {
   int64_t all, per;
+  int unit_cost;
   Start start[kMaxGrid];
 };
 
@@ -152,7 +156,7 @@ __device__ __forceinline__ int64_t scan_block(int64_t x, int64_t* shared, int64_
 }
 
 __global__ void __launch_bounds__(kPlanThreads)
-plan_kernel(const BatchView batch, const AttentionArgs a, int kv_heads, int grid, Plan* plan) {
+plan_kernel(const BatchView batch, const AttentionArgs a, int kv_heads, int grid, int unit_cost, Plan* plan) {
   __shared__ int64_t sums[32];
   __shared__ int first_pair[ES_MAX_SEQUENCES];  // the pairs of a sequence begin here
   __shared__ int tiles[kPlanThreads];
@@ -201,7 +205,7 @@ plan_kernel(const BatchView batch, const AttentionArgs a, int kv_heads, int grid
         }
         if (p < pairs) n = tiles[threadIdx.x];
       }
-      const int64_t mine = p < pairs ? static_cast<int64_t>(n + kUnitCost) * kv_heads : 0;
+      const int64_t mine = p < pairs ? static_cast<int64_t>(n + unit_cost) * kv_heads : 0;
       int64_t more;
       const int64_t at = done + scan_block(mine, sums, more);
       if (pass == 1)
@@ -214,6 +218,7 @@ plan_kernel(const BatchView batch, const AttentionArgs a, int kv_heads, int grid
       if (threadIdx.x == 0) {
         plan->all = all;
         plan->per = per;
+        plan->unit_cost = unit_cost;
       }
     }
   }
@@ -410,6 +415,7 @@ __device__ __forceinline__ bool group_sync(Sh& sh, int x, uint32_t& phase, int l
 struct Walk {
   int64_t at, end, per, pair_tile;
   int seq, row_tile;
+  int unit_cost;
   Pair pair;
   // the unit
   int head, tile0, tile1;
@@ -417,6 +423,7 @@ struct Walk {
 
   __device__ __forceinline__ Walk(const BatchView& b, const AttentionArgs& a, const Plan* plan, int lane) {
     per = plan->per;
+    unit_cost = plan->unit_cost;
     at = blockIdx.x * per;
     end = min(at + per, plan->all);
     if (at < end) {
@@ -437,8 +444,8 @@ struct Walk {
   }
   __device__ __forceinline__ bool next(const BatchView& b, const AttentionArgs& a, int kv_heads, int lane) {
     while (at < end) {
-      while (at >= pair_tile + static_cast<int64_t>(pair.tiles + kUnitCost) * kv_heads) {
-        pair_tile += static_cast<int64_t>(pair.tiles + kUnitCost) * kv_heads;
+      while (at >= pair_tile + static_cast<int64_t>(pair.tiles + unit_cost) * kv_heads) {
+        pair_tile += static_cast<int64_t>(pair.tiles + unit_cost) * kv_heads;
         ++row_tile;
         while (row_tile >= row_tiles_of(b, a, seq)) {
           ++seq;
@@ -446,10 +453,10 @@ struct Walk {
         }
         pair = pair_of<32>(b, a, seq, row_tile, lane);
       }
-      const int length = pair.tiles + kUnitCost;
+      const int length = pair.tiles + unit_cost;
       head = static_cast<int>((at - pair_tile) / length);
       const int64_t begin = pair_tile + static_cast<int64_t>(head) * length;
-      unit0 = begin + kUnitCost;
+      unit0 = begin + unit_cost;
       tile0 = at <= begin ? 0 : cut(at);
       tile1 = end >= begin + length ? pair.tiles : cut(end);
       at = begin + length;
@@ -459,7 +466,7 @@ struct Walk {
   }
   // The blocks that have the unit's first tile and its last.
   __device__ __forceinline__ void sharers(int& c_first, int& c_last) const {
-    c_first = static_cast<int>((unit0 - kUnitCost) / per);
+    c_first = static_cast<int>((unit0 - unit_cost) / per);
     c_last = static_cast<int>((unit0 + pair.tiles - 1) / per);
     while (c_first < c_last && cut((c_first + 1) * per) == 0) ++c_first;
     while (c_last > c_first && cut(c_last * per) == pair.tiles) --c_last;
@@ -1319,7 +1326,8 @@ cudaError_t launch_kernel(const CacheView& cache, const CUtensorMap* maps, const
   }
   const int grid = std::min(sms, kMaxGrid);
   Plan* plan = reinterpret_cast<Plan*>(workspace);
-  const cudaError_t err = launch_early(plan_kernel, 1, kPlanThreads, 0, stream, batch, args, cache.kv_heads, grid, plan);
+  const cudaError_t err = launch_early(plan_kernel, 1, kPlanThreads, 0, stream, batch, args, cache.kv_heads, grid,
+                                       unit_cost<kFp8, kPlain>(), plan);
   if (err != cudaSuccess) return err;
   return launch_early(kernel, grid, threads_of<kFp8>(), kShared, stream, cache, batch, args, static_cast<const Plan*>(plan), counters,
                       flag, reinterpret_cast<Part<D>*>(workspace + kPlanBytes), maps[0], maps[1]);
