@@ -210,6 +210,12 @@ __device__ __forceinline__ Span span_of(const BatchView& b, const AttentionArgs&
   Span s;
   s.length = sequence_length(b, seq);
   new_tokens(b, seq, s.begin, s.count, s.base);
+  if (b.max_new == 1) {  // every lane works out the one token: 20 shuffles less before the first load
+    const Row r = row_of(b, a, s.begin, s.count, s.base, s.length, 0);
+    s.lo = s.in_lo = r.lo;
+    s.hi = s.in_hi = r.hi;
+    return s;
+  }
   int lo = INT32_MAX, hi = 0, in_lo = 0, in_hi = INT32_MAX;
   if (lane < s.count) {
     const Row r = row_of(b, a, s.begin, s.count, s.base, s.length, lane * a.group);
@@ -307,7 +313,9 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
     if (w < warp) upto += warp_tiles[w];
     all += warp_tiles[w];
   }
-  const int64_t per = max((all + gridDim.x - 1) / gridDim.x, static_cast<int64_t>(kMinTiles));
+  const int64_t share = all <= UINT32_MAX - gridDim.x ? (static_cast<uint32_t>(all) + gridDim.x - 1) / gridDim.x
+                                                     : (all + gridDim.x - 1) / gridDim.x;
+  const int64_t per = max(share, static_cast<int64_t>(kMinTiles));
   const int64_t begin = blockIdx.x * per, end = min(begin + per, all);
   if (begin >= end) return;  // which lets the next kernel start too
   if (begin >= upto - mine && begin < upto) {
@@ -335,7 +343,9 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
       span = span_of(batch, a, seq, lane);
       tiles = tiles_of(span.count, span.lo, span.hi, S::tile);
     }
-    const int head = static_cast<int>((at - seq_tile) / tiles);
+    const int64_t into = at - seq_tile;
+    const int head = into <= UINT32_MAX ? static_cast<int>(static_cast<uint32_t>(into) / static_cast<uint32_t>(tiles))
+                                        : static_cast<int>(into / tiles);
     const int64_t unit0 = seq_tile + static_cast<int64_t>(head) * tiles, unit1 = unit0 + tiles;
     const int tile0 = static_cast<int>(at - unit0);
     const int tile1 = static_cast<int>(min(unit1, end) - unit0);
@@ -727,7 +737,13 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
           // the parts' maxima and sums a lane each, their elements eight loads at a time
           const int n = c_last - c_first + 1;
           auto part_of = [&](int i) -> const Part<D>& { return parts[2 * (c_first + i) + (i == 0)]; };
-          for (int i = lane; i < n; i += 32) most = fmaxf(most, __ldcg(&part_of(i).top[r]));
+          float first_top = -INFINITY, first_sum = 0.0f;  // of the first 32 parts
+          if (lane < n) {
+            first_top = __ldcg(&part_of(lane).top[r]);
+            first_sum = __ldcg(&part_of(lane).sum[r]);
+          }
+          most = first_top;
+          for (int i = lane + 32; i < n; i += 32) most = fmaxf(most, __ldcg(&part_of(i).top[r]));
 #pragma unroll
           for (int m = 16; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, m));
           const float zero = most == -INFINITY ? 0.0f : most;
@@ -735,8 +751,8 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
             const int some = min(n - i0, 32);
             float f = 0.0f;
             if (lane < some) {
-              f = exp2_approx(__ldcg(&part_of(i0 + lane).top[r]) - zero);
-              l += __ldcg(&part_of(i0 + lane).sum[r]) * f;
+              f = exp2_approx((i0 == 0 ? first_top : __ldcg(&part_of(i0 + lane).top[r])) - zero);
+              l += (i0 == 0 ? first_sum : __ldcg(&part_of(i0 + lane).sum[r])) * f;
             }
 #pragma unroll 8
             for (int i = 0; i < some; ++i) {

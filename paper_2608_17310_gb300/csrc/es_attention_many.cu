@@ -380,7 +380,7 @@ struct Shared {
   uint8_t raw[kFp8 ? kRaw : 1][kFp8 ? kHalf * D : 128];
   // Read with the scores, when the tile's keys may have made room for others: a slot is
   // written again four tiles on, which follows the scores of two tiles on.
-  float k_scale[4][kKeys];  // times the scores' factor
+  float k_scale[4][kKeys];  // times scale log2(e)
   uint32_t absent[4];  // 16-key pieces of the tile whose page does not exist
   float v_scale[kStages][kKeys];
   uint64_t q_full[2], s_full[2], p_full[2], o_done[2];
@@ -615,12 +615,6 @@ __device__ void fix_tiles(Shared<D, false>& sh, int thread, int lane) {
   }
 }
 
-// What a dot product is multiplied by: to a score in units of log 2, or where scores are capped to
-// the exponent of their cap's 2^x. With FP8 the keys' scales come with it.
-__device__ __forceinline__ float factor_of(const AttentionArgs& a) {
-  return a.scale * (a.softcap > 0.0f ? 2.0f * kLog2e / a.softcap : kLog2e);
-}
-
 // FP8 pages to shared memory as they are, a half tile of keys at a time and of values after it.
 template <int D>
 __device__ void copy_codes(Shared<D, true>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
@@ -698,7 +692,7 @@ template <int D>
 __device__ void convert_tiles(Shared<D, true>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a, int thread,
                               int lane) {
   uint32_t done = 0, raw_done = 0;
-  const float factor = factor_of(a);
+  const float factor = a.scale * kLog2e;
   for (uint32_t n = 0; take(sh, n); ++n) {
     const Unit& unit = sh.unit[n % kUnits];
     const int tile1 = unit.tile1, seq = unit.seq;
@@ -898,11 +892,12 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
                        uint32_t* counters, Part<D>* parts, int x, int thread, int lane) {
   const uint32_t lanes = static_cast<uint32_t>(thread / 32 * 32) << 16;
   const uint32_t s_at = sh.tensor + lanes + x * 128, o_at = sh.tensor + lanes + 256 + x * 128;
-  // Scores in units of log 2. Capped: cap tanh(x / cap) = cap - 2 cap / (2^(2 x log2(e) / cap) + 1),
-  // off by 1e-7 cap at most.
-  const bool capped = a.softcap > 0.0f;
+  // Scores in units of log 2. Capped, with c the cap: c tanh(x / c) is x (1 - z / 3 + 2 z^2 / 15 -
+  // 17 z^3 / 315), z = (x / c)^2, off by 1e-7 x at most where all of a chunk have |x| <= c / 4 (the
+  // series' next term is 62 z^4 / 2835), else c - 2 c / (2^(2 x log2(e) / c) + 1), off by 1e-7 c.
+  const bool capped = a.softcap > 0.0f, biased = a.slopes != nullptr;
   const float cap = a.softcap * kLog2e;
-  const float factor = factor_of(a);
+  const float factor = a.scale * kLog2e;
   uint32_t s_done = 0;        // tiles of this warpgroup so far
   uint32_t tiles_before = 0;  // of all units
   uint32_t phase = 0;
@@ -956,23 +951,63 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
           uint32_t w[32];
           tensor_load(w, s_at + c);
           tensor_loaded(w);
+          uint64_t y[16];  // pairs of scores
 #pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            float f[4] = {factor, factor, factor, factor};
-            if (kFp8) {
-              const float4 k = *reinterpret_cast<const float4*>(&sh.k_scale[all_done % 4][c + i]);
-              f[0] = k.x;
-              f[1] = k.y;
-              f[2] = k.z;
-              f[3] = k.w;
-            }
+          for (int i = 0; i < 16; i += 2) {
+            ulonglong2 f = make_ulonglong2(pack(factor, factor), pack(factor, factor));
+            if (kFp8) f = *reinterpret_cast<const ulonglong2*>(&sh.k_scale[all_done % 4][c + 2 * i]);
+            y[i] = mul2(pack(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1])), f.x);
+            y[i + 1] = mul2(pack(__uint_as_float(w[2 * i + 2]), __uint_as_float(w[2 * i + 3])), f.y);
+          }
+          if (!kPlain && capped) {
+            float most = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float y = __uint_as_float(w[i + e]) * f[e];
-              if (!kPlain && capped) y = fmaf(-2.0f * cap, reciprocal(exp2_approx(y) + 1.0f), cap);
-              if (!kPlain) y = fmaf(-slope, fabsf(away - static_cast<float>(i + e)), y);
-              w[i + e] = __float_as_uint(y);
+            for (int i = 0; i < 16; ++i) {
+              float lo, hi;
+              unpack(y[i], lo, hi);
+              most = fmaxf(most, fmaxf(fabsf(lo), fabsf(hi)));
             }
+            if (__all_sync(0xFFFFFFFFu, most <= 0.25f * cap)) {
+              const float inv = 1.0f / (cap * cap);
+              const float c1 = -1.0f / 3.0f * inv, c2 = 2.0f / 15.0f * inv * inv, c3 = -17.0f / 315.0f * inv * inv * inv;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const uint64_t z = mul2(y[i], y[i]);
+                const uint64_t t = fma2(z, fma2(z, fma2(z, pack(c3, c3), pack(c2, c2)), pack(c1, c1)), pack(1.0f, 1.0f));
+                y[i] = mul2(y[i], t);
+              }
+            } else {
+              const float twice = 2.0f * kLog2e / cap;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                float lo, hi;
+                unpack(y[i], lo, hi);
+                y[i] = pack(fmaf(-2.0f * cap, reciprocal(exp2_approx(lo * twice) + 1.0f), cap),
+                            fmaf(-2.0f * cap, reciprocal(exp2_approx(hi * twice) + 1.0f), cap));
+              }
+            }
+          }
+          if (!kPlain && biased) {
+            if (__all_sync(0xFFFFFFFFu, away >= 31.0f)) {  // the chunk is not past the row's position
+              const float base = -slope * away;
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                y[i] = add2(y[i], fma2(pack(slope, slope), pack(2.0f * i, 2.0f * i + 1.0f), pack(base, base)));
+            } else {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                float lo, hi;
+                unpack(y[i], lo, hi);
+                y[i] = pack(fmaf(-slope, fabsf(away - 2.0f * i), lo), fmaf(-slope, fabsf(away - (2.0f * i + 1.0f)), hi));
+              }
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float lo, hi;
+            unpack(y[i], lo, hi);
+            w[2 * i] = __float_as_uint(lo);
+            w[2 * i + 1] = __float_as_uint(hi);
           }
           away -= 32.0f;
           if (!whole) {
@@ -985,7 +1020,8 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
               if (!(seen >> i & 1)) w[i] = __float_as_uint(-INFINITY);
           }
 #pragma unroll
-          for (int i = 0; i < 32; ++i) tops[i % 4] = fmaxf(tops[i % 4], __uint_as_float(w[i]));
+          for (int i = 0; i < 32; i += 2)
+            tops[i / 2 % 4] = fmaxf(tops[i / 2 % 4], fmaxf(__uint_as_float(w[i]), __uint_as_float(w[i + 1])));
           tensor_store32(s_at + c, w);
         }
         tensor_stored();

@@ -21,7 +21,7 @@ from .esopt import ES_BF16, ES_FP8_E4M3, EsError, _check, _stream  # noqa: F401
 
 ES_MAX_SEQUENCES = 4096
 
-_VP, _U64, _INT, _F32 = ctypes.c_void_p, ctypes.c_uint64, ctypes.c_int, ctypes.c_float
+_VP, _U64, _INT, _FLOAT = ctypes.c_void_p, ctypes.c_uint64, ctypes.c_int, ctypes.c_float
 
 
 class es_cache_desc_t(ctypes.Structure):
@@ -39,21 +39,24 @@ class es_append_t(ctypes.Structure):
     _fields_ = [("qkv", _VP), ("q_out", _VP), ("q_weight", _VP), ("k_weight", _VP), ("rope", _VP),
                 ("positions", _VP), ("qkv_stride", _U64), ("q_out_stride", _U64),
                 ("rope_rows", _U64), ("q_heads", _INT), ("rotary_dim", _INT),
-                ("interleaved", _INT), ("eps", _F32)]
+                ("interleaved", _INT), ("eps", _FLOAT)]
 
 
 class es_attention_t(ctypes.Structure):
     _fields_ = [("q", _VP), ("out", _VP), ("lse", _VP), ("slopes", _VP), ("first", _VP),
                 ("last", _VP), ("q_stride", _U64), ("out_stride", _U64), ("q_heads", _INT),
-                ("window", _INT), ("scale", _F32), ("softcap", _F32)]
+                ("window", _INT), ("scale", _FLOAT), ("softcap", _FLOAT)]
 
 
 _calls = None
+_BF16 = _F32 = _I32 = _U8 = None  # torch's, once it is in use
 
 
 def _lib() -> ctypes.CDLL:
-    global _calls
+    global _calls, _BF16, _F32, _I32, _U8
     if _calls is None:
+        import torch
+        _BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
         L = esopt.lib()
         P = ctypes.POINTER
         for name, res, args in (
@@ -69,16 +72,11 @@ def _lib() -> ctypes.CDLL:
     return _calls
 
 
-def _torch():
-    import torch
-    return torch
-
-
 def _tensor(t, dtype, what: str, shape=None) -> int:
     """The address of a contiguous CUDA tensor of this dtype (and shape); None is NULL."""
     if t is None:
         return 0
-    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous CUDA tensor of {dtype}")
     if shape is not None and t.shape != shape:
         raise ValueError(f"{what} has shape {tuple(t.shape)}, not {tuple(shape)}")
@@ -88,19 +86,30 @@ def _tensor(t, dtype, what: str, shape=None) -> int:
 def _rows(t, rows: int, heads: int, head_dim: int, what: str):
     """Address and row stride of bf16 rows [rows, heads, head_dim] or [rows, heads * head_dim]
     whose rows are contiguous."""
-    if not t.is_cuda or t.dtype != _torch().bfloat16:
+    if t.dtype is not _BF16 or not t.is_cuda:
         raise ValueError(f"{what} must be a bfloat16 CUDA tensor")
+    shape = t.shape
+    width = heads * head_dim
+    if (shape == (rows, heads, head_dim) or shape == (rows, width)) and rows:
+        if t.is_contiguous():
+            return t.data_ptr(), width
+        stride = t.stride()
+        if stride[-1] == 1 and (len(shape) == 2 or heads == 1 or stride[1] == head_dim):
+            # torch gives a single row any stride; what it is does not matter then
+            return t.data_ptr(), stride[0] if rows > 1 else width
+    elif rows == 0 and shape[0] == 0:
+        return t.data_ptr(), width
+    raise ValueError(f"{what} must be {rows} contiguous rows of {heads} heads of {head_dim}, got "
+                     f"shape {tuple(shape)} with strides {t.stride()}")
+
+
+def _heads(t, head_dim: int, what: str) -> int:
     n = t.dim()
     if n == 3:
-        fits = t.shape[1] == heads and t.shape[2] == head_dim and t.stride(2) == 1 and \
-            (heads == 1 or t.stride(1) == head_dim)
-    else:
-        fits = n == 2 and t.shape[1] == heads * head_dim and t.stride(1) == 1
-    if not fits or t.shape[0] != rows:
-        raise ValueError(f"{what} must be {rows} contiguous rows of {heads} heads of {head_dim}, got "
-                         f"shape {tuple(t.shape)} with strides {t.stride()}")
-    # torch gives a single row any stride; what it is does not matter then
-    return t.data_ptr(), t.stride(0) if rows > 1 else heads * head_dim
+        return t.shape[1]
+    if n != 2:
+        raise ValueError(f"{what} must be rows of heads")
+    return t.shape[1] // head_dim
 
 
 class Cache:
@@ -134,7 +143,8 @@ def es_cache_create(k, v, k_scale=None, v_scale=None) -> Cache:
     """A cache over page tensors [pages, kv_heads, page_size, head_dim] of bfloat16, or of
     E4M3 codes (float8_e4m3fn or uint8) with float32 scales [pages, kv_heads, page_size].
     Each page is contiguous; pages may lie further apart, alike in k and v."""
-    torch = _torch()
+    import torch
+    _lib()
     if k.dtype == torch.bfloat16:
         dtype = ES_BF16
     elif k.dtype in (torch.float8_e4m3fn, torch.uint8):
@@ -182,7 +192,7 @@ class Batch:
     rewrite between calls. ``tokens`` and ``max_new`` bound what ``start`` may hold then."""
 
     def __init__(self, pages, seq_len, start=None, tokens=None, max_new=None):
-        torch = _torch()
+        _lib()
         if pages.dim() != 2:
             raise ValueError("pages must be [sequences, pages_per_row]")
         n = pages.shape[0]
@@ -192,9 +202,9 @@ class Batch:
             tokens, max_new = n, 1
         self.tokens = int(tokens)
         self._keepalive = (pages, seq_len, start)
-        self.args = es_batch_t(_tensor(pages, torch.int32, "pages"),
-                               _tensor(seq_len, torch.int32, "seq_len", (n,)),
-                               _tensor(start, torch.int32, "start", (n + 1,)),
+        self.args = es_batch_t(_tensor(pages, _I32, "pages"),
+                               _tensor(seq_len, _I32, "seq_len", (n,)),
+                               _tensor(start, _I32, "start", (n + 1,)),
                                pages.shape[1], n, self.tokens, int(max_new))
         self.ref = ctypes.byref(self.args)
 
@@ -204,29 +214,27 @@ def es_cache_append(cache: Cache, batch: Batch, qkv, q_out, q_weight=None, k_wei
                     stream=None) -> None:
     """Head norms, rotation and cache write of the batch's new tokens. ``rope``: float32
     [rows, rotary_dim / 2, 2] of (cos, sin)."""
-    torch = _torch()
     d, n = cache.head_dim, batch.tokens
-    width = q_out.shape[1] * (q_out.shape[2] if q_out.dim() == 3 else 1)
-    q_heads = width // d
+    q_heads = _heads(q_out, d, "q_out")
     q_ptr, q_stride = _rows(q_out, n, q_heads, d, "q_out")
     x_ptr, x_stride = _rows(qkv, n, q_heads + 2 * cache.kv_heads, d, "qkv")
     if rope is not None and (rope.dim() != 3 or rope.shape[2] != 2):
         raise ValueError("rope must be [rows, rotary_dim / 2, 2]")
-    a = es_append_t(x_ptr, q_ptr, _tensor(q_weight, torch.bfloat16, "q_weight", (d,)),
-                    _tensor(k_weight, torch.bfloat16, "k_weight", (d,)),
-                    _tensor(rope, torch.float32, "rope"),
-                    _tensor(positions, torch.int32, "positions", (n,)), x_stride, q_stride,
+    a = es_append_t(x_ptr, q_ptr, _tensor(q_weight, _BF16, "q_weight", (d,)),
+                    _tensor(k_weight, _BF16, "k_weight", (d,)),
+                    _tensor(rope, _F32, "rope"),
+                    _tensor(positions, _I32, "positions", (n,)), x_stride, q_stride,
                     0 if rope is None else rope.shape[0], q_heads,
                     0 if rope is None else 2 * rope.shape[1], int(interleaved), eps)
-    _check(_lib().es_cache_append(cache.handle, batch.ref, ctypes.byref(a), _stream(stream)),
+    _check(_calls.es_cache_append(cache.handle, batch.ref, ctypes.byref(a), _stream(stream)),
            "es_cache_append")
 
 
 def es_cache_read(cache: Cache, batch: Batch, k_out=None, v_out=None, stream=None) -> None:
     """The cached keys and values of the batch's tokens as bfloat16
     [tokens, kv_heads, head_dim]."""
-    shape, bf16 = (batch.tokens, cache.kv_heads, cache.head_dim), _torch().bfloat16
-    _check(_lib().es_cache_read(cache.handle, batch.ref, _tensor(k_out, bf16, "k_out", shape),
+    shape, bf16 = (batch.tokens, cache.kv_heads, cache.head_dim), _BF16
+    _check(_calls.es_cache_read(cache.handle, batch.ref, _tensor(k_out, bf16, "k_out", shape),
                                 _tensor(v_out, bf16, "v_out", shape), _stream(stream)),
            "es_cache_read")
 
@@ -243,17 +251,15 @@ def es_attention(cache: Cache, batch: Batch, q, out, workspace, scale: float, ls
     [tokens, q_heads, head_dim]; ``lse``: float32 [tokens, q_heads]; ``workspace``: a zeroed
     uint8 tensor of es_attention_workspace() bytes, which every call leaves ready for the
     next on its stream."""
-    torch = _torch()
     d, n = cache.head_dim, batch.tokens
-    width = q.shape[1] * (q.shape[2] if q.dim() == 3 else 1)
-    heads = width // d
+    heads = _heads(q, d, "q")
     q_ptr, q_stride = _rows(q, n, heads, d, "q")
     o_ptr, o_stride = _rows(out, n, heads, d, "out")
-    a = es_attention_t(q_ptr, o_ptr, _tensor(lse, torch.float32, "lse", (n, heads)),
-                       _tensor(slopes, torch.float32, "slopes", (heads,)),
-                       _tensor(first, torch.int32, "first", (n,)),
-                       _tensor(last, torch.int32, "last", (n,)), q_stride, o_stride, heads, window,
+    a = es_attention_t(q_ptr, o_ptr, _tensor(lse, _F32, "lse", (n, heads)),
+                       _tensor(slopes, _F32, "slopes", (heads,)),
+                       _tensor(first, _I32, "first", (n,)),
+                       _tensor(last, _I32, "last", (n,)), q_stride, o_stride, heads, window,
                        scale, softcap)
-    _check(_lib().es_attention(cache.handle, batch.ref, ctypes.byref(a),
-                               _tensor(workspace, torch.uint8, "workspace"), workspace.numel(),
+    _check(_calls.es_attention(cache.handle, batch.ref, ctypes.byref(a),
+                               _tensor(workspace, _U8, "workspace"), workspace.numel(),
                                _stream(stream)), "es_attention")
