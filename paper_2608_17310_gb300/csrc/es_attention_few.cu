@@ -707,9 +707,9 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
           part.sum[r] = l;
         }
       }
-      __threadfence();
       __syncthreads();
       if (threadIdx.x == 0) {
+        __threadfence();  // of what the block has written, through the barrier
         const uint32_t before = atomicAdd(&counters[c_first], 1u);
         is_last = before == static_cast<uint32_t>(c_last - c_first);
         if (is_last) counters[c_first] = 0;
@@ -754,20 +754,30 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
               f = exp2_approx((i0 == 0 ? first_top : __ldcg(&part_of(i0 + lane).top[r])) - zero);
               l += (i0 == 0 ? first_sum : __ldcg(&part_of(i0 + lane).sum[r])) * f;
             }
-#pragma unroll 8
-            for (int i = 0; i < some; ++i) {
-              const float g = __shfl_sync(0xFFFFFFFFu, f, i);
-              const float* from = &part_of(i0 + i).o[r][lane * kPer];
-              if constexpr (kPer == 4) {
-                const float4 y = __ldcg(reinterpret_cast<const float4*>(from));
-                x[0] += y.x * g;
-                x[1] += y.y * g;
-                x[2] += y.z * g;
-                x[3] += y.w * g;
-              } else {
-                const float2 y = __ldcg(reinterpret_cast<const float2*>(from));
-                x[0] += y.x * g;
-                x[1] += y.y * g;
+#pragma unroll 1
+            for (int i = 0; i < some; i += 8) {  // eight loads in flight, the last batch's too
+              float y[8][kPer];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const float* from = &part_of(i0 + min(i + e, some - 1)).o[r][lane * kPer];
+                if constexpr (kPer == 4) {
+                  const float4 z = __ldcg(reinterpret_cast<const float4*>(from));
+                  y[e][0] = z.x;
+                  y[e][1] = z.y;
+                  y[e][2] = z.z;
+                  y[e][3] = z.w;
+                } else {
+                  const float2 z = __ldcg(reinterpret_cast<const float2*>(from));
+                  y[e][0] = z.x;
+                  y[e][1] = z.y;
+                }
+              }
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const float g = __shfl_sync(0xFFFFFFFFu, f, min(i + e, 31));
+                if (i + e < some)
+#pragma unroll
+                  for (int j = 0; j < kPer; ++j) x[j] += y[e][j] * g;
               }
             }
           }
