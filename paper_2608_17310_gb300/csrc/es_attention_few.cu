@@ -21,9 +21,9 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "es_attention.cuh"
-#include "es_internal.h"
 #include "es_rollout_internal.h"
 
 namespace esopt {
@@ -808,11 +808,24 @@ cudaError_t launch(const CacheView& cache, const BatchView& batch, const Attenti
   auto kernel = few_rows_kernel<D, kFp8, kBlocks>;
   int device = 0;
   cudaGetDevice(&device);
-  const int64_t resident = resident_ctas(reinterpret_cast<const void*>(kernel), kThreads, device);
+  // resident blocks of this kernel on each device, kept from its first launch there
+  static std::atomic<int> blocks_of[64];
+  int resident = device < 64 ? blocks_of[device].load(std::memory_order_relaxed) : 0;
+  if (resident == 0) {
+    int sms = 0, per_sm = 0;
+    cudaError_t err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (err == cudaSuccess) err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kThreads, 0);
+    if (err != cudaSuccess) {
+      cudaGetLastError();
+      return err;
+    }
+    resident = std::max(sms * per_sm, 1);
+    if (device < 64) blocks_of[device].store(resident, std::memory_order_relaxed);
+  }
   // no more blocks than the longest sequences that the page table allows have work for
   const int64_t longest = (static_cast<int64_t>(batch.capacity) + 15 + Shape<kFp8>::tile - 1) / Shape<kFp8>::tile;
   const int64_t tiles = longest * cache.kv_heads * batch.sequences;
-  const int64_t blocks = std::min({resident, static_cast<int64_t>(kMaxParts / 2), (tiles + kMinTiles - 1) / kMinTiles});
+  const int64_t blocks = std::min({static_cast<int64_t>(resident), static_cast<int64_t>(kMaxParts / 2), (tiles + kMinTiles - 1) / kMinTiles});
   return launch_early(kernel, static_cast<int>(blocks), kThreads, 0, stream, cache, batch, args, counters,
                       reinterpret_cast<Part<D>*>(workspace));
 }

@@ -28,7 +28,6 @@
 #include <atomic>
 
 #include "es_attention.cuh"
-#include "es_internal.h"
 #include "es_rollout_internal.h"
 
 namespace esopt {

@@ -94,8 +94,4 @@ cudaError_t launch_noise_fill(uint64_t seed, uint64_t index_base, uint64_t n,
 // Sets the calling thread's es_last_error() text (es_host.cu).
 es_status_t record_status(es_status_t status, const char* message);
 
-// Resident CTAs of a kernel without dynamic shared memory on one device (SMs x CTAs per SM),
-// kept from the kernel's first launch on it.
-int resident_ctas(const void* kernel, int threads, int dev);
-
 }  // namespace esopt

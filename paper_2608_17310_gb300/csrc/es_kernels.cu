@@ -1303,8 +1303,6 @@ std::mutex g_grid_mutex;
 GridEntry g_grid_cache[kGridCacheSize];
 int g_grid_used = 0;
 
-}  // namespace
-
 int resident_ctas(const void* kernel, int threads, int dev) {
   {
     std::lock_guard<std::mutex> lock(g_grid_mutex);
@@ -1322,8 +1320,6 @@ int resident_ctas(const void* kernel, int threads, int dev) {
   if (g_grid_used < kGridCacheSize) g_grid_cache[g_grid_used++] = GridEntry{kernel, dev, ctas};
   return ctas;
 }
-
-namespace {
 
 // Persistent grid: every SM filled to the kernel's occupancy, never more
 // CTAs than tiles.
