@@ -92,7 +92,8 @@ es_status_t es_cache_destroy(es_cache_t cache);
  *              sequence b is in slot p % page_size of page
  *              pages[b * pages_per_row + p / page_size]
  *   seq_len    [sequences] tokens of each sequence, its new tokens included. A
- *              length above pages_per_row * page_size counts as that.
+ *              length above pages_per_row * page_size (or 2^31 - 1024) counts as
+ *              that, a negative one as 0.
  *   start      [sequences + 1], from 0 and not decreasing: the new tokens of
  *              sequence b are rows start[b] .. start[b + 1] - 1 of the call's
  *              token arrays. They are the sequence's last ones: row start[b] + i
@@ -191,10 +192,13 @@ es_status_t es_cache_read(es_cache_t cache, const es_batch_t* batch, void* k_out
  *   slopes     [q_heads] fp32 (4-byte aligned), or NULL
  *   first,     [tokens] int32 (4-byte aligned), or NULL
  *   last
+ *   softcap    0 for none, or at least 1e-30
  *   workspace  es_attention_workspace() bytes of device memory, zero before its
  *              first use; every call leaves it ready for the next. One workspace
  *              serves calls of any batch one after another, and must not be used
- *              on two streams at once.
+ *              on two streams at once. Its 32-bit word at byte 4096 stays 0: a kernel
+ *              sets it where a wait of its own ran out (an error of the library),
+ *              and that call's outputs are then not to be used.
  * Scores, exponentials and sums are fp32; keys and values enter the products
  * exactly, and exp(x_j) rounded to bf16.
  * Errors: ES_ERR_INVALID_ARG, ES_ERR_ALIGNMENT, ES_ERR_NONFINITE (scale, softcap),

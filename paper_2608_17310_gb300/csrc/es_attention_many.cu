@@ -14,8 +14,8 @@
 // and leaves O in tensor memory alone on almost every tile.
 //
 // Pages reach shared memory by TMA, each page of a tile by its own copy; FP8 pages then pass
-// through four warps that turn codes into bf16, which holds them exactly. The scales go to
-// the scores and to P.
+// through six warps that turn codes into bf16, which holds them exactly. The scales go to the
+// scores and to P.
 //
 // The key tiles of all units (sequence, row tile, key head) lie end to end and are cut into
 // one range per block, all of one length, so causal triangles and ragged batches leave no
@@ -367,16 +367,19 @@ struct Unit {
 };
 constexpr int kUnits = 4;
 
-// FP8: half tiles of codes on their way from the pages to the converting warps.
-constexpr int kRaw = 3;
-constexpr int kHalf = 64;  // keys
+// FP8: codes pass from the pages to the converting warps in pieces of 32 keys or values, four
+// and four to a tile, each warp with a place of its own for them. (Four warps that shared each
+// piece, a half tile, took 6,000 cycles a tile for 3,000 cycles of work.)
+constexpr int kRaw = 6;    // converting warps
+constexpr int kPiece = 32;  // keys
+constexpr int kPieces = 2 * kKeys / kPiece;
 
 template <int D, bool kFp8>
 struct Shared {
   uint16_t q[2][128 * D];
   uint16_t k[kStages][kKeys * D];
   uint16_t v[kStages][kKeys * D];
-  uint8_t raw[kFp8 ? kRaw : 1][kFp8 ? kHalf * D : 128];
+  uint8_t raw[kFp8 ? kRaw : 1][kFp8 ? kPiece * D : 128];
   // Read with the scores, when the tile's keys may have made room for others: a slot is
   // written again four tiles on, which follows the scores of two tiles on.
   float k_scale[4][kKeys];  // times scale log2(e)
@@ -614,31 +617,37 @@ __device__ void fix_tiles(Shared<D, false>& sh, int thread, int lane) {
   }
 }
 
-// FP8 pages to shared memory as they are, a half tile of keys at a time and of values after it.
+// FP8 pages to shared memory as they are: a tile's pieces of keys, then of values, each to the
+// next converting warp.
 template <int D>
 __device__ void copy_codes(Shared<D, true>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
                            const Plan* plan, const CUtensorMap* k_map, const CUtensorMap* v_map, int lane) {
-  const int box = min(1 << cache.page_shift, kHalf), boxes = kHalf / box;  // keys of a copy, copies of a half
-  uint32_t done = 0;
+  const int box = min(1 << cache.page_shift, kPiece), boxes = kPiece / box;  // keys of a copy, copies of a piece
+  uint32_t done = 0, tiles = 0;
   bool fine = true;
   Walk walk(batch, a, plan, lane);
   for (uint32_t n = 0; fine && tell(sh, walk, batch, a, cache.kv_heads, n, lane); ++n) {
     const int key0 = walk.pair.lo & ~(kKeys - 1);
-    for (int tile = walk.tile0; fine && tile < walk.tile1; ++tile) {
-      // the copies of both halves: lane i's keys are 16 i and up
+    for (int tile = walk.tile0; fine && tile < walk.tile1; ++tile, ++tiles) {
+      // lane i's keys are 16 i and up
       const int j = key0 + tile * kKeys + lane * 16;
       const int page = lane < 8 && j < walk.pair.hi ? page_of(cache, batch, walk.seq, j) : -1;
+      const uint32_t absent = __ballot_sync(0xFFFFFFFFu, page < 0) & 0xFFu;
 #pragma unroll 1
-      for (int part = 0; part < 4; ++part, ++done) {
-        const int slot = done % kRaw, j0 = key0 + tile * kKeys + (part & 1) * kHalf;
-        const int mine = __shfl_sync(0xFFFFFFFFu, page, (part & 1) * 4 + lane * box / 16);
+      for (int part = 0; part < kPieces; ++part, ++done) {
+        const int slot = done % kRaw, in_tile = part % (kPieces / 2) * kPiece;
+        const int mine = __shfl_sync(0xFFFFFFFFu, page, (in_tile + lane * box) / 16 % 8);
         fine = warp_wait(&sh.raw_empty[slot], (done / kRaw & 1) ^ 1, &sh.failed);
         if (!fine) break;
-        if (lane == 0) barrier_expect(&sh.raw_full[slot], kHalf * D);
+        if (lane == 0) {
+          if (part == 0) sh.absent[tiles % 4] = absent;
+          barrier_expect(&sh.raw_full[slot], kPiece * D);
+        }
         __syncwarp();
         if (lane < boxes)
-          load_box(part < 2 ? k_map : v_map, shared_address(sh.raw[slot] + lane * box * D), &sh.raw_full[slot], 0,
-                   (walk.head << cache.page_shift) + ((j0 + lane * box) & ((1 << cache.page_shift) - 1)), mine < 0 ? cache.num_pages : mine);
+          load_box(part < kPieces / 2 ? k_map : v_map, shared_address(sh.raw[slot] + lane * box * D), &sh.raw_full[slot], 0,
+                   (walk.head << cache.page_shift) + ((in_tile + lane * box) & ((1 << cache.page_shift) - 1)),
+                   mine < 0 ? cache.num_pages : mine);
       }
     }
   }
@@ -646,106 +655,90 @@ __device__ void copy_codes(Shared<D, true>& sh, const CacheView& cache, const Ba
   for (uint32_t i = done > kRaw ? done - kRaw : 0; i < done; ++i) barrier_settle(&sh.raw_full[i % kRaw], i / kRaw & 1);
 }
 
-// A half tile of codes to bf16: 8 codes (16 bytes of bf16) to a thread and step, so that the
-// eight threads that write side by side write all of one 128-byte row. All steps' codes are
-// read first: step by step a half took four times as long.
+// One warp's piece of codes to bf16, 8 codes (16 bytes of bf16) to a lane and step, so that the
+// eight lanes that write side by side write all of one 128-byte row; eight steps' codes are
+// read before any is converted.
 // clean: keys outside [lo, hi) become zeros, and NaN codes too.
 template <int D>
-__device__ __forceinline__ void convert_half(const uint8_t* raw, uint64_t* raw_empty, uint16_t* to, int key0, int thread, int lane,
-                                             bool clean, int lo, int hi, int* poisoned) {
-  constexpr int kSteps = kHalf * D / 8 / 128;
-  uint32_t u[kSteps][2];
+__device__ __forceinline__ void convert_piece(const uint8_t* raw, uint16_t* to, int key0, int lane, bool clean, int lo, int hi,
+                                              int* poisoned) {
+  constexpr int kSteps = kPiece * D / 8 / 32;
+#pragma unroll 1
+  for (int s0 = 0; s0 < kSteps; s0 += 8) {
+    uint32_t u[8][2];
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const uint2 w = *reinterpret_cast<const uint2*>(raw + (i * 128 + thread) * 8);
-    u[i][0] = w.x;
-    u[i][1] = w.y;
-  }
-  if (clean) {
+    for (int i = 0; i < 8; ++i) {
+      const uint2 w = *reinterpret_cast<const uint2*>(raw + ((s0 + i) * 32 + lane) * 8);
+      u[i][0] = w.x;
+      u[i][1] = w.y;
+    }
+    if (clean) {
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      const int key = key0 + (i * 128 + thread) / (D / 8);
+      for (int i = 0; i < 8; ++i) {
+        const int key = key0 + ((s0 + i) * 32 + lane) / (D / 8);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        if (key < lo || key >= hi) u[i][e] = 0;
-        const uint32_t bad = ((u[i][e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;  // NaN codes
-        if (bad != 0) {
-          u[i][e] &= ~((bad >> 7) * 0xFFu);
-          *static_cast<volatile int*>(poisoned) = 1;
+        for (int e = 0; e < 2; ++e) {
+          if (key < lo || key >= hi) u[i][e] = 0;
+          const uint32_t bad = ((u[i][e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;  // NaN codes
+          if (bad != 0) {
+            u[i][e] &= ~((bad >> 7) * 0xFFu);
+            *static_cast<volatile int*>(poisoned) = 1;
+          }
         }
       }
     }
-  }
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const int piece = i * 128 + thread;
-    *reinterpret_cast<uint4*>(to + place_of<D>(key0 + piece / (D / 8), piece % (D / 8))) =
-        make_uint4(bf16_of_e4m3(u[i][0]), bf16_of_e4m3(u[i][0] >> 16), bf16_of_e4m3(u[i][1]), bf16_of_e4m3(u[i][1] >> 16));
+    for (int i = 0; i < 8; ++i) {
+      const int piece = (s0 + i) * 32 + lane;
+      *reinterpret_cast<uint4*>(to + place_of<D>(key0 + piece / (D / 8), piece % (D / 8))) =
+          make_uint4(bf16_of_e4m3(u[i][0]), bf16_of_e4m3(u[i][0] >> 16), bf16_of_e4m3(u[i][1]), bf16_of_e4m3(u[i][1] >> 16));
+    }
   }
-  // The next codes may come now that these have been used. (After their loads alone have been
-  // issued is too early: a copy of zeros can overtake them.)
-  warp_arrive(raw_empty, lane);
 }
 
 template <int D>
-__device__ void convert_tiles(Shared<D, true>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a, int thread,
+__device__ void convert_tiles(Shared<D, true>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a, int warp,
                               int lane) {
-  uint32_t done = 0, raw_done = 0;
+  uint32_t done = 0;  // tiles
+  uint32_t turns = 0;  // this warp's pieces
   const float factor = a.scale * kLog2e;
   for (uint32_t n = 0; take(sh, n); ++n) {
     const Unit& unit = sh.unit[n % kUnits];
-    const int tile1 = unit.tile1, seq = unit.seq;
-    const uint32_t rows = static_cast<uint32_t>(unit.head) << cache.page_shift;
-    auto pages_of = [&](int tile) {  // lane i's is the page of the tile's keys 16 i and up
-      const int j = unit.key_of(tile) + lane * 16;
-      return lane < 8 && tile < tile1 && j < unit.hi ? page_of(cache, batch, seq, j) : -1;
-    };
-    auto scale_of = [&](const float* scales, int pages, int tile) {  // of key `thread` of the tile
-      const int page = __shfl_sync(0xFFFFFFFFu, pages, thread / 16);
-      return page >= 0 ? __ldg(scales + page * cache.scale_stride + rows + ((unit.key_of(tile) + thread) & ((1 << cache.page_shift) - 1))) : 0.0f;
-    };
-    int tile = unit.tile0;
-    int pages = pages_of(tile), next_pages = pages_of(tile + 1);
-    float k_scale = scale_of(cache.k_scale, pages, tile), v_scale = scale_of(cache.v_scale, pages, tile);
-    for (; tile < tile1; ++tile, ++done) {
-      const int stage = done % kStages;
+    const int tile1 = unit.tile1;
+    for (int tile = unit.tile0; tile < tile1; ++tile, ++done) {
+      const int stage = done % kStages, j0 = unit.key_of(tile);
       const uint32_t parity = done / kStages & 1;
-      const uint32_t absent = __ballot_sync(0xFFFFFFFFu, pages < 0) & 0xFFu;
-      if (!warp_wait(&sh.k_empty[stage], parity ^ 1, &sh.failed)) return;
-      if (thread == 0) sh.absent[done % 4] = absent;
-      sh.k_scale[done % 4][thread] = k_scale * factor;
-      k_scale = scale_of(cache.k_scale, next_pages, tile + 1);
+      // pieces go round: this warp's first one of the tile, and perhaps another
 #pragma unroll 1
-      for (int half = 0; half < 2; ++half, ++raw_done) {
-        const int slot = raw_done % kRaw;
-        if (!warp_wait(&sh.raw_full[slot], raw_done / kRaw & 1, &sh.failed)) return;
-        convert_half<D>(sh.raw[slot], &sh.raw_empty[slot], sh.k[stage], half * kHalf, thread, lane, false, 0, 0, nullptr);
-      }
-      fence_async();
-      warp_arrive(&sh.k_full[stage], lane);
-      const bool clean = unit.edge(tile);
-      const int lo = unit.lo - unit.key_of(tile), hi = unit.hi - unit.key_of(tile);
-      if (!warp_wait(&sh.v_empty[stage], parity ^ 1, &sh.failed)) return;
-      if (clean) {  // as with NaN codes: only rows that see the key get to know its scale
-        if (thread < lo || thread >= hi) {
-          v_scale = 0.0f;
-        } else if (!(fabsf(v_scale) <= FLT_MAX)) {
-          v_scale = 0.0f;
-          *static_cast<volatile int*>(&sh.poisoned) = 1;
+      for (uint32_t part = (warp + kRaw - done * kPieces % kRaw) % kRaw; part < kPieces; part += kRaw, ++turns) {
+        const bool of_keys = part < kPieces / 2;
+        const int key0 = part % (kPieces / 2) * kPiece, j = j0 + key0 + lane;
+        // the scale of this lane's key, while the codes are on their way
+        const int page = j < unit.hi ? page_of(cache, batch, unit.seq, j) : -1;
+        float scale = 0.0f;
+        if (page >= 0)
+          scale = __ldg((of_keys ? cache.k_scale : cache.v_scale) + page * cache.scale_stride +
+                        (static_cast<uint64_t>(unit.head) << cache.page_shift) + (j & ((1 << cache.page_shift) - 1)));
+        const bool clean = !of_keys && unit.edge(tile);
+        if (clean) {  // as with NaN codes: only rows that see the key get to know its scale
+          if (j < unit.lo || j >= unit.hi) {
+            scale = 0.0f;
+          } else if (!(fabsf(scale) <= FLT_MAX)) {
+            scale = 0.0f;
+            *static_cast<volatile int*>(&sh.poisoned) = 1;
+          }
         }
+        if (!warp_wait(of_keys ? &sh.k_empty[stage] : &sh.v_empty[stage], parity ^ 1, &sh.failed)) return;
+        if (of_keys) sh.k_scale[done % 4][key0 + lane] = scale * factor;
+        else sh.v_scale[stage][key0 + lane] = scale;
+        if (!warp_wait(&sh.raw_full[warp], turns & 1, &sh.failed)) return;
+        convert_piece<D>(sh.raw[warp], of_keys ? sh.k[stage] : sh.v[stage], key0, lane, clean, unit.lo - j0, unit.hi - j0, &sh.poisoned);
+        // The next codes may come now that these have been used. (After their loads alone have
+        // been issued is too early: a copy of zeros can overtake them.)
+        warp_arrive(&sh.raw_empty[warp], lane);
+        fence_async();
+        warp_arrive(of_keys ? &sh.k_full[stage] : &sh.v_full[stage], lane);
       }
-      sh.v_scale[stage][thread] = v_scale;
-      v_scale = scale_of(cache.v_scale, next_pages, tile + 1);
-#pragma unroll 1
-      for (int half = 0; half < 2; ++half, ++raw_done) {
-        const int slot = raw_done % kRaw;
-        if (!warp_wait(&sh.raw_full[slot], raw_done / kRaw & 1, &sh.failed)) return;
-        convert_half<D>(sh.raw[slot], &sh.raw_empty[slot], sh.v[stage], half * kHalf, thread, lane, clean, lo, hi, &sh.poisoned);
-      }
-      fence_async();
-      warp_arrive(&sh.v_full[stage], lane);
-      pages = next_pages;
-      next_pages = pages_of(tile + 2);
     }
     leave(sh, n, lane);
   }
@@ -967,11 +960,10 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
               most = fmaxf(most, fmaxf(fabsf(lo), fabsf(hi)));
             }
             if (__all_sync(0xFFFFFFFFu, most <= 0.25f * cap)) {
-              const float inv = 1.0f / (cap * cap);
-              const float c1 = -1.0f / 3.0f * inv, c2 = 2.0f / 15.0f * inv * inv, c3 = -17.0f / 315.0f * inv * inv * inv;
+              const float inv = 1.0f / cap, c1 = -1.0f / 3.0f, c2 = 2.0f / 15.0f, c3 = -17.0f / 315.0f;
 #pragma unroll
               for (int i = 0; i < 16; ++i) {
-                const uint64_t z = mul2(y[i], y[i]);
+                const uint64_t u = mul2(y[i], pack(inv, inv)), z = mul2(u, u);
                 const uint64_t t = fma2(z, fma2(z, fma2(z, pack(c3, c3), pack(c2, c2)), pack(c1, c1)), pack(1.0f, 1.0f));
                 y[i] = mul2(y[i], t);
               }
@@ -1274,26 +1266,26 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
       barrier_init(&sh.group[i], 4);
     }
     for (int i = 0; i < kStages; ++i) {
-      barrier_init(&sh.k_full[i], kFp8 ? 4 : 1);
+      barrier_init(&sh.k_full[i], kFp8 ? kPieces / 2 : 1);
       barrier_init(&sh.k_empty[i], 1);
-      barrier_init(&sh.v_full[i], kFp8 ? 4 : 1);
+      barrier_init(&sh.v_full[i], kFp8 ? kPieces / 2 : 1);
       barrier_init(&sh.v_empty[i], 1);
       barrier_init(&sh.v_fixed[i], 2);
     }
     for (int i = 0; i < kRaw; ++i) {
       barrier_init(&sh.raw_full[i], 1);
-      barrier_init(&sh.raw_empty[i], 4);
+      barrier_init(&sh.raw_empty[i], 1);
     }
     for (int i = 0; i < kUnits; ++i) {
       barrier_init(&sh.unit_full[i], 1);
-      barrier_init(&sh.unit_empty[i], kFp8 ? 13 : 11);  // the warps that take units
+      barrier_init(&sh.unit_empty[i], kFp8 ? 9 + kRaw : 11);  // the warps that take units
     }
     barrier_init(&sh.drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sh.failed = 0;
     sh.poisoned = 0;
   }
-  constexpr int kIssuer = kFp8 ? 12 : 8;
+  constexpr int kIssuer = kFp8 ? 8 + kRaw : 8;
   if (warp == kIssuer) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(shared_address(&sh.tensor)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -1320,8 +1312,8 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
     barrier_settle(&sh.drained, 0);
   } else {
     if constexpr (kFp8) {
-      if (warp < 12) convert_tiles<D>(sh, cache, batch, a, threadIdx.x - 256, lane);
-      else if (warp == 13) copy_codes<D>(sh, cache, batch, a, plan, &k_map, &v_map, lane);
+      if (warp < 8 + kRaw) convert_tiles<D>(sh, cache, batch, a, warp - 8, lane);
+      else copy_codes<D>(sh, cache, batch, a, plan, &k_map, &v_map, lane);
     } else {
       if (warp == 9) copy_tiles<D>(sh, cache, batch, a, plan, &k_map, &v_map, lane);
       else fix_tiles<D>(sh, threadIdx.x - 10 * 32, lane);

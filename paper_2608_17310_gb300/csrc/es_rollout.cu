@@ -1,6 +1,7 @@
 // C-ABI host layer of the rollout operators: cache handles, argument checks, dispatch.
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -36,6 +37,9 @@ es_status_t ok() { return esopt::record_status(ES_OK, ""); }
 es_status_t cuda_fail(cudaError_t err, const char* what) {
   return fail(ES_ERR_CUDA, "%s: %s (%s)", what, cudaGetErrorName(err), cudaGetErrorString(err));
 }
+
+// Positions and the ends of tiles of keys stay within 32 bits.
+constexpr int64_t kLongest = INT32_MAX - 1023;
 
 // A device buffer of the call: present, aligned and device memory.
 es_status_t check_buffer(const void* p, unsigned align, int device, const char* call,
@@ -84,7 +88,7 @@ es_status_t check_batch(es_cache_t cache, const es_batch_t* b, const char* call,
   const int64_t capacity = static_cast<int64_t>(b->pages_per_row) * cache->page_size;
   *view = esopt::BatchView{b->pages, b->seq_len, b->start, b->pages_per_row, b->sequences,
                            b->tokens, b->max_new,
-                           static_cast<int>(capacity < INT32_MAX ? capacity : INT32_MAX)};
+                           static_cast<int>(std::min(capacity, kLongest))};
   return ES_OK;
 }
 
@@ -111,7 +115,7 @@ es_status_t check_stride(uint64_t stride, int heads, int head_dim, const char* c
 
 // Pages as [page][head and slot][element]; pages past the last one read as zeros. bf16 is read
 // in boxes of one page of a head by 64 elements (128 bytes, swizzled), FP8 in boxes of up to
-// 64 whole codes' vectors as they lie.
+// 32 whole codes' vectors as they lie.
 es_status_t make_map(CUtensorMap* map, void* base, const es_cache_desc_t& d, const char* call) {
   using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                               const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -125,7 +129,7 @@ es_status_t make_map(CUtensorMap* map, void* base, const es_cache_desc_t& d, con
   const cuuint64_t size = fp8 ? 1 : 2;
   const cuuint64_t strides[2] = {d.head_dim * size, d.page_stride * size};
   const cuuint32_t box[3] = {fp8 ? static_cast<cuuint32_t>(d.head_dim) : 64u,
-                             static_cast<cuuint32_t>(fp8 && d.page_size > 64 ? 64 : d.page_size), 1};
+                             static_cast<cuuint32_t>(fp8 && d.page_size > 32 ? 32 : d.page_size), 1};
   const cuuint32_t steps[3] = {1, 1, 1};
   const CUresult made = reinterpret_cast<Encode>(found)(
       map, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -270,8 +274,8 @@ es_status_t es_attention(es_cache_t cache, const es_batch_t* batch, const es_att
   if ((st = check_heads(cache, a->q_heads, call)) != ES_OK) return st;
   if (!std::isfinite(a->scale) || !std::isfinite(a->softcap))
     return fail(ES_ERR_NONFINITE, "%s: scale or softcap is not finite", call);
-  if (a->softcap < 0.0f || a->window < 0)
-    return fail(ES_ERR_INVALID_ARG, "%s: softcap or window is negative", call);
+  if (a->softcap < 0.0f || (a->softcap > 0.0f && a->softcap < 1e-30f) || a->window < 0)
+    return fail(ES_ERR_INVALID_ARG, "%s: softcap or window is negative, or softcap below 1e-30", call);
   const int d = cache->head_dim;
   if ((st = check_stride(a->q_stride, a->q_heads, d, call, "q_stride")) != ES_OK) return st;
   if ((st = check_stride(a->out_stride, a->q_heads, d, call, "out_stride")) != ES_OK) return st;

@@ -96,6 +96,7 @@ def attend(s, q_heads, q=None, stream=None, **kw):
         first = out.clone() if _ == 0 else first
     torch.cuda.synchronize()
     assert torch.equal(first.view(torch.int16), out.view(torch.int16)), "two calls differ"
+    assert not ws[:4352].any(), "counters or the flag of a given-up wait are left"
     return q, out, lse
 
 
@@ -512,6 +513,7 @@ def test_refusals(es, ro):
     assert status(es, ro.es_attention, s.cache, s.batch, q, out, ws, scale=1.0, softcap=float("inf")) == es.ES_ERR_NONFINITE
     assert status(es, ro.es_attention, s.cache, s.batch, q, out, ws, scale=1.0, softcap=-1.0) == bad
     assert status(es, ro.es_attention, s.cache, s.batch, q, out, ws, scale=1.0, window=-1) == bad
+    assert status(es, ro.es_attention, s.cache, s.batch, q, out, ws, scale=1.0, softcap=1e-35) == bad
     assert status(es, ro.es_attention, s.cache, s.batch, q, out, ws[:-1], scale=1.0) == bad
     q3 = torch.zeros(5, 3, 128, dtype=torch.bfloat16, device="cuda")  # 3 query heads of 2 key heads
     assert status(es, ro.es_attention, s.cache, s.batch, q3, torch.zeros_like(q3), ws, **good) == bad
