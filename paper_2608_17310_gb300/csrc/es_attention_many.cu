@@ -26,8 +26,8 @@
 // the card's bf16 matrix rate in a burst, the tensor pipe 55 % busy. The chain of a tile of
 // rows (product, scores read, maxima, exponentials, P written, product: 2,000 cycles and its
 // 1,024 of products) is longer than the 2,048 cycles of products of both. Over an FP8 cache
-// 718 us, over capped scores 679 us: more instructions on that chain. Twelve sequences with 9 to
-// 130 tokens over FP8 caches, capped, 255 us; packed documents with a bias 86 us, of which a unit
+// 720 us, over capped scores 653 us: more instructions on that chain. Twelve sequences with 9 to
+// 130 tokens over FP8 caches, capped, 253 us; packed documents with a bias 86 us, of which a unit
 // of four tiles spends two thirds in its tiles.
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -390,7 +390,7 @@ struct Shared {
   uint8_t raw[kFp8 ? kRaw : 1][kFp8 ? kPiece * D : 128];
   // Read with the scores, when the tile's keys may have made room for others: a slot is
   // written again four tiles on, which follows the scores of two tiles on.
-  float k_scale[4][kKeys];  // times scale log2(e)
+  float k_scale[4][kKeys];  // times the scores' factor
   uint32_t absent[4];  // 16-key pieces of the tile whose page does not exist
   float v_scale[kStages][kKeys];
   uint64_t q_full[2], s_full[2], p_full[2], o_done[2];
@@ -709,7 +709,6 @@ __device__ void convert_tiles(Shared<D, true>& sh, const CacheView& cache, const
                               int lane) {
   uint32_t done = 0;  // tiles
   uint32_t turns = 0;  // this warp's pieces
-  const float factor = a.scale * kLog2e;
   for (uint32_t n = 0; take(sh, n); ++n) {
     const Unit& unit = sh.unit[n % kUnits];
     const int tile1 = unit.tile1;
@@ -737,7 +736,7 @@ __device__ void convert_tiles(Shared<D, true>& sh, const CacheView& cache, const
           }
         }
         if (!warp_wait(of_keys ? &sh.k_empty[stage] : &sh.v_empty[stage], parity ^ 1, &sh.failed)) return;
-        if (of_keys) sh.k_scale[done % 4][key0 + lane] = scale * factor;
+        if (of_keys) sh.k_scale[done % 4][key0 + lane] = scale * a.factor;
         else sh.v_scale[stage][key0 + lane] = scale;
         if (!warp_wait(&sh.raw_full[warp], turns & 1, &sh.failed)) return;
         convert_piece<D>(sh.raw[warp], of_keys ? sh.k[stage] : sh.v[stage], key0, lane, clean, unit.lo - j0, unit.hi - j0, &sh.poisoned);
@@ -892,12 +891,11 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
                        uint32_t* counters, Part<D>* parts, int x, int thread, int lane) {
   const uint32_t lanes = static_cast<uint32_t>(thread / 32 * 32) << 16;
   const uint32_t s_at = sh.tensor + lanes + x * 128, o_at = sh.tensor + lanes + 256 + x * 128;
-  // Scores in units of log 2. Capped, with c the cap: c tanh(x / c) is x (1 - z / 3 + 2 z^2 / 15 -
-  // 17 z^3 / 315), z = (x / c)^2, off by 1e-7 x at most where all of a chunk have |x| <= c / 4 (the
-  // series' next term is 62 z^4 / 2835), else c - 2 c / (2^(2 x log2(e) / c) + 1), off by 1e-7 c.
+  // Scores in units of log 2. Capped, with u = x / cap: cap tanh(u) is cap u (1 - z / 3 + 2 z^2 / 15 -
+  // 17 z^3 / 315), z = u^2, off by 1e-7 of it where all of a chunk have |u| <= 1 / 4 (the series' next
+  // term is 62 z^4 / 2835), else cap (1 - 2 / (2^(2 u log2(e)) + 1)), off by 1e-7 cap.
   const bool capped = a.softcap > 0.0f, biased = a.slopes != nullptr;
   const float cap = a.softcap * kLog2e;
-  const float factor = a.scale * kLog2e;
   uint32_t s_done = 0;        // tiles of this warpgroup so far
   uint32_t tiles_before = 0;  // of all units
   uint32_t phase = 0;
@@ -954,7 +952,7 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
           uint64_t y[16];  // pairs of scores
 #pragma unroll
           for (int i = 0; i < 16; i += 2) {
-            ulonglong2 f = make_ulonglong2(pack(factor, factor), pack(factor, factor));
+            ulonglong2 f = make_ulonglong2(pack(a.factor, a.factor), pack(a.factor, a.factor));
             if (kFp8) f = *reinterpret_cast<const ulonglong2*>(&sh.k_scale[all_done % 4][c + 2 * i]);
             y[i] = mul2(pack(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1])), f.x);
             y[i + 1] = mul2(pack(__uint_as_float(w[2 * i + 2]), __uint_as_float(w[2 * i + 3])), f.y);
@@ -967,16 +965,16 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
               unpack(y[i], lo, hi);
               most = fmaxf(most, fmaxf(fabsf(lo), fabsf(hi)));
             }
-            if (__all_sync(0xFFFFFFFFu, most <= 0.25f * cap)) {
-              const float inv = 1.0f / cap, c1 = -1.0f / 3.0f, c2 = 2.0f / 15.0f, c3 = -17.0f / 315.0f;
+            if (__all_sync(0xFFFFFFFFu, most <= 0.25f)) {
+              const float c1 = -1.0f / 3.0f * cap, c2 = 2.0f / 15.0f * cap, c3 = -17.0f / 315.0f * cap;
 #pragma unroll
               for (int i = 0; i < 16; ++i) {
-                const uint64_t u = mul2(y[i], pack(inv, inv)), z = mul2(u, u);
-                const uint64_t t = fma2(z, fma2(z, fma2(z, pack(c3, c3), pack(c2, c2)), pack(c1, c1)), pack(1.0f, 1.0f));
+                const uint64_t z = mul2(y[i], y[i]);
+                const uint64_t t = fma2(z, fma2(z, fma2(z, pack(c3, c3), pack(c2, c2)), pack(c1, c1)), pack(cap, cap));
                 y[i] = mul2(y[i], t);
               }
             } else {
-              const float twice = 2.0f * kLog2e / cap;
+              constexpr float twice = 2.0f * kLog2e;
 #pragma unroll
               for (int i = 0; i < 16; ++i) {
                 float lo, hi;
@@ -1030,7 +1028,7 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
       for (int c = 0; c < kKeys / 32; ++c) tensor_load(w[c], s_at + c * 32);
 #pragma unroll
       for (int c = 0; c < kKeys / 32; ++c) tensor_loaded(w[c]);
-      const float unit = direct && !kFp8 ? factor : 1.0f;  // of what w holds, in scores
+      const float unit = direct && !kFp8 ? a.factor : 1.0f;  // of what w holds, in scores
       if (kFp8 && direct) {
 #pragma unroll
         for (int c = 0; c < kKeys / 32; ++c)
@@ -1051,7 +1049,7 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
 #pragma unroll
           for (int c = 0; c < kKeys / 32; ++c) tops[c] = fmaxf(tops[c], fmaxf(__uint_as_float(w[c][i]), __uint_as_float(w[c][i + 1])));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) tops[i] *= factor;
+        for (int i = 0; i < 4; ++i) tops[i] *= a.factor;
       }
       float best = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
       if (!(best > top + kSlack)) best = top;

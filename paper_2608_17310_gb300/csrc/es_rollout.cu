@@ -274,8 +274,8 @@ es_status_t es_attention(es_cache_t cache, const es_batch_t* batch, const es_att
   if ((st = check_heads(cache, a->q_heads, call)) != ES_OK) return st;
   if (!std::isfinite(a->scale) || !std::isfinite(a->softcap))
     return fail(ES_ERR_NONFINITE, "%s: scale or softcap is not finite", call);
-  if (a->softcap < 0.0f || (a->softcap > 0.0f && a->softcap < 1e-30f) || a->window < 0)
-    return fail(ES_ERR_INVALID_ARG, "%s: softcap or window is negative, or softcap below 1e-30", call);
+  if (a->softcap < 0.0f || (a->softcap > 0.0f && a->softcap < 1e-6f) || a->window < 0)
+    return fail(ES_ERR_INVALID_ARG, "%s: softcap or window is negative, or softcap below 1e-6", call);
   const int d = cache->head_dim;
   if ((st = check_stride(a->q_stride, a->q_heads, d, call, "q_stride")) != ES_OK) return st;
   if ((st = check_stride(a->out_stride, a->q_heads, d, call, "out_stride")) != ES_OK) return st;
@@ -296,7 +296,8 @@ es_status_t es_attention(es_cache_t cache, const es_batch_t* batch, const es_att
   const esopt::AttentionArgs args{static_cast<const uint16_t*>(a->q), static_cast<uint16_t*>(a->out),
                                   a->lse, a->slopes, a->first, a->last, a->q_stride, a->out_stride,
                                   a->q_heads, a->q_heads / cache->view.kv_heads, a->window,
-                                  a->scale, a->softcap};
+                                  a->scale, a->softcap,
+                                  a->softcap > 0.0f ? a->scale / a->softcap : a->scale * 1.4426950408889634f};
   const cudaError_t err = esopt::launch_attention(cache->view, cache->maps, cache->dtype == ES_FP8_E4M3, d, b,
                                                   args, workspace, static_cast<cudaStream_t>(stream));
   if (err != cudaSuccess) return cuda_fail(err, call);

@@ -60,6 +60,7 @@ struct AttentionArgs {
   int q_heads, group;  // group: query heads per key head
   int window;
   float scale, softcap;
+  float factor;  // of a dot product: to a score in units of log 2, or to x / softcap where it is capped
 };
 
 #ifdef __CUDACC__
