@@ -15,9 +15,10 @@ device pointers, where a shape is not needed); errors are ``esopt.EsError``, or
 from __future__ import annotations
 
 import ctypes
+from struct import Struct
 
 from . import esopt
-from .esopt import ES_BF16, ES_FP8_E4M3, EsError, _check, _stream  # noqa: F401
+from .esopt import ES_BF16, ES_FP8_E4M3, EsError, _check  # noqa: F401
 
 ES_MAX_SEQUENCES = 4096
 
@@ -48,23 +49,33 @@ class es_attention_t(ctypes.Structure):
                 ("window", _INT), ("scale", _FLOAT), ("softcap", _FLOAT)]
 
 
+# Small calls are bound by their host time, so the functions pack es_append_t and
+# es_attention_t as bytes (a ctypes structure takes 0.4 us more to make) and ask for the current
+# stream's handle alone.
+_APPEND = Struct("9Q3if")
+_ATTENTION = Struct("8Q2i2f")
+assert _APPEND.size == ctypes.sizeof(es_append_t) and _ATTENTION.size == ctypes.sizeof(es_attention_t)
+
 _calls = None
 _BF16 = _F32 = _I32 = _U8 = None  # torch's, once it is in use
+_raw_stream = _device = None
 
 
 def _lib() -> ctypes.CDLL:
-    global _calls, _BF16, _F32, _I32, _U8
+    global _calls, _BF16, _F32, _I32, _U8, _raw_stream, _device
     if _calls is None:
         import torch
         _BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _device = getattr(torch._C, "_cuda_getDevice", None)
         L = esopt.lib()
         P = ctypes.POINTER
         for name, res, args in (
                 ("es_cache_create", _INT, [P(es_cache_desc_t), P(_VP)]),
                 ("es_cache_destroy", _INT, [_VP]),
-                ("es_cache_append", _INT, [_VP, P(es_batch_t), P(es_append_t), _VP]),
+                ("es_cache_append", _INT, [_VP, P(es_batch_t), _VP, _VP]),
                 ("es_cache_read", _INT, [_VP, P(es_batch_t), _VP, _VP, _VP]),
-                ("es_attention", _INT, [_VP, P(es_batch_t), P(es_attention_t), _VP, _U64, _VP]),
+                ("es_attention", _INT, [_VP, P(es_batch_t), _VP, _VP, _U64, _VP]),
                 ("es_attention_workspace", _U64, [_VP, _INT])):
             fn = getattr(L, name)
             fn.restype, fn.argtypes = res, args
@@ -72,44 +83,48 @@ def _lib() -> ctypes.CDLL:
     return _calls
 
 
-def _tensor(t, dtype, what: str, shape=None) -> int:
-    """The address of a contiguous CUDA tensor of this dtype (and shape); None is NULL."""
+def _stream(stream) -> int:
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(_device())
+    return esopt._stream(stream)
+
+
+def _tensor(t, dtype, what: str, numel=None) -> int:
+    """The address of a contiguous CUDA tensor of this dtype (and number of elements); None is
+    NULL."""
     if t is None:
         return 0
-    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+    if t.dtype is not dtype or not t.is_contiguous() or not t.is_cuda:
         raise ValueError(f"{what} must be a contiguous CUDA tensor of {dtype}")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{what} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if numel is not None and t.numel() != numel:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, not {numel} elements")
     return t.data_ptr()
 
 
-def _rows(t, rows: int, heads: int, head_dim: int, what: str):
-    """Address and row stride of bf16 rows [rows, heads, head_dim] or [rows, heads * head_dim]
-    whose rows are contiguous."""
+def _rows(t, rows: int, heads, head_dim: int, what: str):
+    """Address, row stride and heads of bf16 rows [rows, heads, head_dim] or
+    [rows, heads * head_dim] whose rows are contiguous; heads None: as many as there are."""
     if t.dtype is not _BF16 or not t.is_cuda:
         raise ValueError(f"{what} must be a bfloat16 CUDA tensor")
     shape = t.shape
-    width = heads * head_dim
-    if (shape == (rows, heads, head_dim) or shape == (rows, width)) and rows:
-        if t.is_contiguous():
-            return t.data_ptr(), width
-        stride = t.stride()
-        if stride[-1] == 1 and (len(shape) == 2 or heads == 1 or stride[1] == head_dim):
-            # torch gives a single row any stride; what it is does not matter then
-            return t.data_ptr(), stride[0] if rows > 1 else width
-    elif rows == 0 and shape[0] == 0:
-        return t.data_ptr(), width
-    raise ValueError(f"{what} must be {rows} contiguous rows of {heads} heads of {head_dim}, got "
-                     f"shape {tuple(shape)} with strides {t.stride()}")
-
-
-def _heads(t, head_dim: int, what: str) -> int:
-    n = t.dim()
+    n = len(shape)
     if n == 3:
-        return t.shape[1]
-    if n != 2:
-        raise ValueError(f"{what} must be rows of heads")
-    return t.shape[1] // head_dim
+        have, fits = shape[1], shape[2] == head_dim
+    elif n == 2:
+        have, fits = divmod(shape[1], head_dim)
+        fits = fits == 0
+    else:
+        have, fits = 0, False
+    if fits and shape[0] == rows and (heads is None or heads == have):
+        width = have * head_dim
+        if rows == 0 or t.is_contiguous():
+            return t.data_ptr(), width, have
+        stride = t.stride()
+        if stride[-1] == 1 and (n == 2 or have == 1 or stride[1] == head_dim):
+            # torch gives a single row any stride; what it is does not matter then
+            return t.data_ptr(), stride[0] if rows > 1 else width, have
+    raise ValueError(f"{what} must be {rows} contiguous rows of {heads or 'some'} heads of {head_dim}, got "
+                     f"shape {tuple(shape)} with strides {t.stride()}")
 
 
 class Cache:
@@ -203,8 +218,8 @@ class Batch:
         self.tokens = int(tokens)
         self._keepalive = (pages, seq_len, start)
         self.args = es_batch_t(_tensor(pages, _I32, "pages"),
-                               _tensor(seq_len, _I32, "seq_len", (n,)),
-                               _tensor(start, _I32, "start", (n + 1,)),
+                               _tensor(seq_len, _I32, "seq_len", n),
+                               _tensor(start, _I32, "start", n + 1),
                                pages.shape[1], n, self.tokens, int(max_new))
         self.ref = ctypes.byref(self.args)
 
@@ -215,28 +230,33 @@ def es_cache_append(cache: Cache, batch: Batch, qkv, q_out, q_weight=None, k_wei
     """Head norms, rotation and cache write of the batch's new tokens. ``rope``: float32
     [rows, rotary_dim / 2, 2] of (cos, sin)."""
     d, n = cache.head_dim, batch.tokens
-    q_heads = _heads(q_out, d, "q_out")
-    q_ptr, q_stride = _rows(q_out, n, q_heads, d, "q_out")
-    x_ptr, x_stride = _rows(qkv, n, q_heads + 2 * cache.kv_heads, d, "qkv")
-    if rope is not None and (rope.dim() != 3 or rope.shape[2] != 2):
-        raise ValueError("rope must be [rows, rotary_dim / 2, 2]")
-    a = es_append_t(x_ptr, q_ptr, _tensor(q_weight, _BF16, "q_weight", (d,)),
-                    _tensor(k_weight, _BF16, "k_weight", (d,)),
-                    _tensor(rope, _F32, "rope"),
-                    _tensor(positions, _I32, "positions", (n,)), x_stride, q_stride,
-                    0 if rope is None else rope.shape[0], q_heads,
-                    0 if rope is None else 2 * rope.shape[1], int(interleaved), eps)
-    _check(_calls.es_cache_append(cache.handle, batch.ref, ctypes.byref(a), _stream(stream)),
-           "es_cache_append")
+    q_ptr, q_stride, q_heads = _rows(q_out, n, None, d, "q_out")
+    x_ptr, x_stride, _ = _rows(qkv, n, q_heads + 2 * cache.kv_heads, d, "qkv")
+    rope_ptr = rope_rows = rotary_dim = 0
+    if rope is not None:
+        shape = rope.shape
+        if len(shape) != 3 or shape[2] != 2:
+            raise ValueError("rope must be [rows, rotary_dim / 2, 2]")
+        rope_ptr, rope_rows, rotary_dim = _tensor(rope, _F32, "rope"), shape[0], 2 * shape[1]
+    status = _calls.es_cache_append(cache.handle, batch.ref, _APPEND.pack(
+        x_ptr, q_ptr, _tensor(q_weight, _BF16, "q_weight", d), _tensor(k_weight, _BF16, "k_weight", d),
+        rope_ptr, _tensor(positions, _I32, "positions", n), x_stride, q_stride, rope_rows, q_heads,
+        rotary_dim, interleaved, eps), _stream(stream))
+    if status:
+        _check(status, "es_cache_append")
 
 
 def es_cache_read(cache: Cache, batch: Batch, k_out=None, v_out=None, stream=None) -> None:
     """The cached keys and values of the batch's tokens as bfloat16
     [tokens, kv_heads, head_dim]."""
-    shape, bf16 = (batch.tokens, cache.kv_heads, cache.head_dim), _BF16
-    _check(_calls.es_cache_read(cache.handle, batch.ref, _tensor(k_out, bf16, "k_out", shape),
-                                _tensor(v_out, bf16, "v_out", shape), _stream(stream)),
-           "es_cache_read")
+    shape = (batch.tokens, cache.kv_heads, cache.head_dim)
+    for t, what in ((k_out, "k_out"), (v_out, "v_out")):
+        if t is not None and t.shape != shape:
+            raise ValueError(f"{what} has shape {tuple(t.shape)}, not {shape}")
+    status = _calls.es_cache_read(cache.handle, batch.ref, _tensor(k_out, _BF16, "k_out"),
+                                  _tensor(v_out, _BF16, "v_out"), _stream(stream))
+    if status:
+        _check(status, "es_cache_read")
 
 
 def es_attention_workspace(cache: Cache, q_heads: int) -> int:
@@ -252,14 +272,12 @@ def es_attention(cache: Cache, batch: Batch, q, out, workspace, scale: float, ls
     uint8 tensor of es_attention_workspace() bytes, which every call leaves ready for the
     next on its stream."""
     d, n = cache.head_dim, batch.tokens
-    heads = _heads(q, d, "q")
-    q_ptr, q_stride = _rows(q, n, heads, d, "q")
-    o_ptr, o_stride = _rows(out, n, heads, d, "out")
-    a = es_attention_t(q_ptr, o_ptr, _tensor(lse, _F32, "lse", (n, heads)),
-                       _tensor(slopes, _F32, "slopes", (heads,)),
-                       _tensor(first, _I32, "first", (n,)),
-                       _tensor(last, _I32, "last", (n,)), q_stride, o_stride, heads, window,
-                       scale, softcap)
-    _check(_calls.es_attention(cache.handle, batch.ref, ctypes.byref(a),
-                               _tensor(workspace, _U8, "workspace"), workspace.numel(),
-                               _stream(stream)), "es_attention")
+    q_ptr, q_stride, heads = _rows(q, n, None, d, "q")
+    o_ptr, o_stride, _ = _rows(out, n, heads, d, "out")
+    status = _calls.es_attention(cache.handle, batch.ref, _ATTENTION.pack(
+        q_ptr, o_ptr, _tensor(lse, _F32, "lse", n * heads), _tensor(slopes, _F32, "slopes", heads),
+        _tensor(first, _I32, "first", n), _tensor(last, _I32, "last", n), q_stride, o_stride, heads,
+        window, scale, softcap), _tensor(workspace, _U8, "workspace"), workspace.numel(),
+        _stream(stream))
+    if status:
+        _check(status, "es_attention")
