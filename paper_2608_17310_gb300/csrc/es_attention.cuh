@@ -88,6 +88,14 @@ __device__ __forceinline__ float score_of(const AttentionArgs& a, float x, float
   return (x - slope * static_cast<float>(abs(distance))) * kLog2e;
 }
 
+// Counts one more block as done, after what it wrote (ordered through a barrier of its threads)
+// and before what it reads of the others'.
+__device__ __forceinline__ uint32_t count_done(uint32_t* counter) {
+  uint32_t before;
+  asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
+  return before;
+}
+
 // The workspace of es_attention: counters of the blocks that have finished their part of a
 // unit, zero between calls; a flag that a kernel sets when it gave up a wait; what the
 // kernels keep of a call.

@@ -717,11 +717,8 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
       }
       __syncthreads();
       if (threadIdx.x == 0) {
-        __threadfence();  // of what the block has written, through the barrier
-        const uint32_t before = atomicAdd(&counters[c_first], 1u);
-        is_last = before == static_cast<uint32_t>(c_last - c_first);
+        is_last = count_done(&counters[c_first]) == static_cast<uint32_t>(c_last - c_first);
         if (is_last) counters[c_first] = 0;
-        __threadfence();
       }
       __syncthreads();
     }

@@ -1181,13 +1181,10 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
         part.top[r_part] = top;
         part.sum[r_part] = sum;
       }
-      __threadfence();
       if (!group_sync(sh, x, phase, lane)) return;
       if (thread == 0) {
-        const uint32_t before = atomicAdd(&counters[2 * c_first + x], 1u);
-        sh.last[x] = before == static_cast<uint32_t>(c_last - c_first);
+        sh.last[x] = count_done(&counters[2 * c_first + x]) == static_cast<uint32_t>(c_last - c_first);
         if (sh.last[x]) counters[2 * c_first + x] = 0;
-        __threadfence();
       }
       if (!group_sync(sh, x, phase, lane)) return;
       if (sh.last[x]) {
