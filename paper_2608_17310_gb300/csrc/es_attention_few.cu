@@ -23,7 +23,7 @@
 // 278 us, 6.6 TB/s, 99 % of the card's copy rate; three FP8 caches of 90,000 to 131,071 tokens
 // 129 us, 5.6 TB/s, 84 %, where converting and packing codes keeps the integer pipe 45 % busy and
 // the loads in flight are what registers hold (16 warps of 4 KB an SM); one cache of 777
-// tokens 8.4 us, 16,000 cycles of latency (lengths, pages, keys, a part's way through
+// tokens 8.1 us, 15,500 cycles of latency (lengths, pages, keys, a part's way through
 // memory, the join) in code that each launch reads anew.
 #include <cuda_runtime.h>
 

@@ -26,8 +26,8 @@
 // the card's bf16 matrix rate in a burst, the tensor pipe 55 % busy. The chain of a tile of
 // rows (product, scores read, maxima, exponentials, P written, product: 2,000 cycles and its
 // 1,024 of products) is longer than the 2,048 cycles of products of both. Over an FP8 cache
-// 720 us, over capped scores 653 us: more instructions on that chain. Twelve sequences with 9 to
-// 130 tokens over FP8 caches, capped, 253 us; packed documents with a bias 86 us, of which a unit
+// 706 us, over capped scores 653 us: more instructions on that chain. Twelve sequences with 9 to
+// 130 tokens over FP8 caches, capped, 244 us; packed documents with a bias 86 us, of which a unit
 // of four tiles spends two thirds in its tiles.
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -1298,12 +1298,14 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
   fence_after();
   wait_for_previous();
 
-  // the warpgroups of the rows hold a tile's scores in registers
+  // The warpgroups of the rows hold a tile's scores in registers. The shares add up to what the
+  // block is launched with: 256 x 216 + 128 x 72 = 384 x 168, and 256 x (200 + 56) = 512 x 128
+  // (FP8 prompt of 8,191 tokens: 706 us; 192 + 64 718, 184 + 72 748, 176 + 80 756).
   if (warp < 8) {
-    if (kFp8) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+    if (kFp8) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     else asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
   } else {
-    if (kFp8) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (kFp8) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
   }
   if (warp < 8) {
