@@ -192,7 +192,7 @@ es_status_t es_cache_read(es_cache_t cache, const es_batch_t* batch, void* k_out
  *   slopes     [q_heads] fp32 (4-byte aligned), or NULL
  *   first,     [tokens] int32 (4-byte aligned), or NULL
  *   last
- *   softcap    0 for none, or at least 1e-6
+ *   softcap    0 for none, or at least 1e-6; above 2^100 it counts as 2^100
  *   workspace  es_attention_workspace() bytes of device memory, zero before its
  *              first use; every call leaves it ready for the next. One workspace
  *              serves calls of any batch one after another, and must not be used

@@ -41,6 +41,10 @@ es_status_t cuda_fail(cudaError_t err, const char* what) {
 // Positions and the ends of tiles of keys stay within 32 bits.
 constexpr int64_t kLongest = INT32_MAX - 1023;
 
+// Caps above this one count as it, so that neither cap log2(e) nor scale / cap leaves fp32's normal
+// numbers. Scores beyond a quarter of it are all that could tell.
+constexpr float kLargestCap = 1.2676506002282294e30f;  // 2^100
+
 // A device buffer of the call: present, aligned and device memory.
 es_status_t check_buffer(const void* p, unsigned align, int device, const char* call,
                          const char* name) {
@@ -293,11 +297,12 @@ es_status_t es_attention(es_cache_t cache, const es_batch_t* batch, const es_att
   if ((st = check_optional(a->first, 4, dev, call, "first")) != ES_OK) return st;
   if ((st = check_optional(a->last, 4, dev, call, "last")) != ES_OK) return st;
   if ((st = check_buffer(workspace, 16, dev, call, "workspace")) != ES_OK) return st;
+  const float cap = std::min(a->softcap, kLargestCap);
   const esopt::AttentionArgs args{static_cast<const uint16_t*>(a->q), static_cast<uint16_t*>(a->out),
                                   a->lse, a->slopes, a->first, a->last, a->q_stride, a->out_stride,
                                   a->q_heads, a->q_heads / cache->view.kv_heads, a->window,
-                                  a->scale, a->softcap,
-                                  a->softcap > 0.0f ? a->scale / a->softcap : a->scale * 1.4426950408889634f};
+                                  a->scale, cap,
+                                  cap > 0.0f ? a->scale / cap : a->scale * 1.4426950408889634f};
   const cudaError_t err = esopt::launch_attention(cache->view, cache->maps, cache->dtype == ES_FP8_E4M3, d, b,
                                                   args, workspace, static_cast<cudaStream_t>(stream));
   if (err != cudaSuccess) return cuda_fail(err, call);
