@@ -892,8 +892,9 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
   const uint32_t lanes = static_cast<uint32_t>(thread / 32 * 32) << 16;
   const uint32_t s_at = sh.tensor + lanes + x * 128, o_at = sh.tensor + lanes + 256 + x * 128;
   // Scores in units of log 2. Capped, with u = x / cap: cap tanh(u) is cap u (1 - z / 3 + 2 z^2 / 15 -
-  // 17 z^3 / 315), z = u^2, off by 1e-7 of it where all of a chunk have |u| <= 1 / 4 (the series' next
-  // term is 62 z^4 / 2835), else cap (1 - 2 / (2^(2 u log2(e)) + 1)), off by 1e-7 cap.
+  // 17 z^3 / 315), z = u^2, where |u| <= 1 / 4 (the series' next term is 62 z^4 / 2835: off by 3.4e-7 of it
+  // at most), else cap (1 - 2 / (2^(2 u log2(e)) + 1)), off by 1e-7 cap. By each score's own size,
+  // so that what a row does not see has no part in its last bits.
   const bool capped = a.softcap > 0.0f, biased = a.slopes != nullptr;
   const float cap = a.softcap * kLog2e;
   uint32_t s_done = 0;        // tiles of this warpgroup so far
@@ -965,22 +966,23 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
               unpack(y[i], lo, hi);
               most = fmaxf(most, fmaxf(fabsf(lo), fabsf(hi)));
             }
+            const float c1 = -1.0f / 3.0f * cap, c2 = 2.0f / 15.0f * cap, c3 = -17.0f / 315.0f * cap;
+            auto series = [&](uint64_t u) {
+              const uint64_t z = mul2(u, u);
+              return mul2(u, fma2(z, fma2(z, fma2(z, pack(c3, c3), pack(c2, c2)), pack(c1, c1)), pack(cap, cap)));
+            };
             if (__all_sync(0xFFFFFFFFu, most <= 0.25f)) {
-              const float c1 = -1.0f / 3.0f * cap, c2 = 2.0f / 15.0f * cap, c3 = -17.0f / 315.0f * cap;
 #pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const uint64_t z = mul2(y[i], y[i]);
-                const uint64_t t = fma2(z, fma2(z, fma2(z, pack(c3, c3), pack(c2, c2)), pack(c1, c1)), pack(cap, cap));
-                y[i] = mul2(y[i], t);
-              }
+              for (int i = 0; i < 16; ++i) y[i] = series(y[i]);
             } else {
               constexpr float twice = 2.0f * kLog2e;
 #pragma unroll
               for (int i = 0; i < 16; ++i) {
-                float lo, hi;
+                float lo, hi, lo_small, hi_small;
                 unpack(y[i], lo, hi);
-                y[i] = pack(fmaf(-2.0f * cap, reciprocal(exp2_approx(lo * twice) + 1.0f), cap),
-                            fmaf(-2.0f * cap, reciprocal(exp2_approx(hi * twice) + 1.0f), cap));
+                unpack(series(y[i]), lo_small, hi_small);
+                y[i] = pack(fabsf(lo) <= 0.25f ? lo_small : fmaf(-2.0f * cap, reciprocal(exp2_approx(lo * twice) + 1.0f), cap),
+                            fabsf(hi) <= 0.25f ? hi_small : fmaf(-2.0f * cap, reciprocal(exp2_approx(hi * twice) + 1.0f), cap));
               }
             }
           }

@@ -1,8 +1,9 @@
 """es_attention with capped scores over the whole range of caps: both kernels against the
 definition in 64 bits, with the tolerances of rollout_reference.py (scores within 1e-4)."""
 import pytest
+import torch
 
-from test_gpu_rollout import Setup, check
+from test_gpu_rollout import Setup, attend, check
 
 pytestmark = pytest.mark.gpu
 
@@ -27,3 +28,27 @@ def test_caps_of_every_size(ro, dtype, new, cap):
 @pytest.mark.parametrize("new", [[1, 1], [40, 20]])
 def test_caps_near_the_largest_number(ro, dtype, cap, new):
     check(Setup(ro, [90, 64], new, 2, 64, 16, dtype, seed=22), 8, softcap=cap)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("new", [[1, 1], [70, 33]])
+def test_unseen_keys_leave_capped_scores_as_they_are(ro, dtype, new):
+    # the keys that no row but the last of a sequence sees become 2^6 as large: scores near the cap
+    # beside small ones, and not a bit of the other rows changes
+    s = Setup(ro, [100, 80], new, 2, 128, 32, dtype, seed=23)
+    first = torch.full((s.tokens,), 9, dtype=torch.int32)
+    last = torch.tensor([l - n + i + 1 for l, n in zip(s.seq_len, s.new) for i in range(n)], dtype=torch.int32)
+    if max(new) == 1:
+        last -= 1
+    args = dict(first=first, last=last, softcap=100.0)
+    q, out, lse = attend(s, 8, **args)
+    for b, l in enumerate(s.seq_len):
+        for p in (2, l - 1):
+            page, slot = s.pages[b][p // 32], p % 32
+            if dtype == "bf16":
+                s.k[page, :, slot] *= 64
+            else:
+                s.ks[page, :, slot] *= 64
+    _, out2, lse2 = attend(s, 8, q=q, **args)
+    rows = [t for t in range(s.tokens) if max(new) == 1 or t + 1 not in s.start]
+    assert torch.equal(out[rows].view(torch.int16), out2[rows].view(torch.int16)) and torch.equal(lse[rows], lse2[rows])
