@@ -43,7 +43,7 @@ extern "C" {
  *   k + page * page_stride + (h * page_size + s) * head_dim     (elements),
  * and the same in v; so one head's page is one contiguous block.
  *   dtype        ES_BF16, or ES_FP8_E4M3 with one fp32 scale per vector:
- *                element = scale * code, scale at
+ *                element = scale * code, with scales of either sign, at
  *                k_scale + page * scale_stride + h * page_size + s
  *                (4-byte aligned); NULL for ES_BF16.
  *   num_pages    1 .. 2^31 - 1

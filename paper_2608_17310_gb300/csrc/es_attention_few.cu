@@ -505,8 +505,8 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
             }
         }
         if (kFp8) {
-          const float most[2] = {fabsf(block[u].v_scale[0]) <= FLT_MAX ? block[u].v_scale[0] : 0.0f,
-                                 fabsf(block[u].v_scale[1]) <= FLT_MAX ? block[u].v_scale[1] : 0.0f};
+          const float size[2] = {fabsf(block[u].v_scale[0]), fabsf(block[u].v_scale[1])};
+          const float most[2] = {size[0] <= FLT_MAX ? size[0] : 0.0f, size[1] <= FLT_MAX ? size[1] : 0.0f};
           if (whole) {
             const float m = fmaxf(most[0], most[1]);
 #pragma unroll
