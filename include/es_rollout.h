@@ -200,7 +200,9 @@ es_status_t es_cache_read(es_cache_t cache, const es_batch_t* batch, void* k_out
  *              sets it where a wait of its own ran out (an error of the library),
  *              and that call's outputs are then not to be used.
  * Scores, exponentials and sums are fp32; keys and values enter the products
- * exactly, and exp(x_j) (times an FP8 value's scale) rounded to bf16 or f16.
+ * exactly, and exp(x_j) (times an FP8 value's scale) rounded to bf16, or over FP8
+ * caches with max_new * q_heads / kv_heads up to 16 to f16, where those below 2^-28
+ * of a token's and head's largest are off by up to 2^-37 of it.
  * Errors: ES_ERR_INVALID_ARG, ES_ERR_ALIGNMENT, ES_ERR_NONFINITE (scale, softcap),
  * ES_ERR_WRONG_DEVICE, ES_ERR_CUDA.
  */

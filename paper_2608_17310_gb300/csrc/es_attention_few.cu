@@ -78,6 +78,18 @@ __device__ __forceinline__ float power_of_two(int n) { return __int_as_float((n 
 // The power of two at or below x > 0, as an exponent within [-126, 127].
 __device__ __forceinline__ int exponent_of(float x) { return max((__float_as_int(x) >> 23 & 0xFF) - 127, -126); }
 
+// FP8: exp(x) v_scale becomes f16 in units of 2^(u - 14), where u is this of the row's largest such
+// product (log 2 of a bound within a factor of 2): the largest is at least 2^12 then and below 2^14, so
+// products keep 11 bits down to 2^-28 of it and are off by 2^-37 of it below. Units that go by the scales
+// alone would leave nothing of a key with all of the weight and a scale 2^-40 of another's.
+__device__ __forceinline__ float unit_of(float largest) { return ceilf(fminf(fmaxf(largest, -112.0f), 127.0f)); }
+
+// An exponent e with |scale| < 2^e <= 2 |scale|, for scales that are finite and not tiny.
+__device__ __forceinline__ float size_bound(float scale) {
+  const int e = __float_as_int(scale) >> 23 & 0xFF;
+  return e == 255 ? -INFINITY : static_cast<float>(e - 126);
+}
+
 template <int kBytes> struct Bytes;
 template <> struct Bytes<16> { using type = uint4; };
 template <> struct Bytes<8> { using type = uint2; };
@@ -425,13 +437,13 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
 
     float o[kBlocks][D / 16][4] = {};
     float top[kBlocks][2], sum[kBlocks][2];
-    // FP8: a row's o is in units of 2^(v_unit - 14), in which p v_scale stays below 2^15
-    int v_unit[kBlocks][2];
+    // FP8: log 2 of a bound of the row's largest p |v_scale| so far, with its top, within a factor of 2
+    float largest[kBlocks][2];
 #pragma unroll
     for (int n = 0; n < kBlocks; ++n) {
       top[n][0] = top[n][1] = -INFINITY;
       sum[n][0] = sum[n][1] = 0.0f;
-      v_unit[n][0] = v_unit[n][1] = -112;
+      largest[n][0] = largest[n][1] = -INFINITY;
     }
 
     // --- the keys, a block of 16 per sub and warp, loaded one tile ahead
@@ -456,12 +468,9 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
     for (int tile = tile0; tile < tile1; ++tile) {
       float s[kSubs][kBlocks][4];
       const bool more = tile + 1 < tile1;
-      float best[kBlocks][2], scale_most[kBlocks][2];
+      float best[kBlocks][2];
 #pragma unroll
-      for (int n = 0; n < kBlocks; ++n) {
-        best[n][0] = best[n][1] = -INFINITY;
-        scale_most[n][0] = scale_most[n][1] = 0.0f;
-      }
+      for (int n = 0; n < kBlocks; ++n) best[n][0] = best[n][1] = -INFINITY;
 #pragma unroll
       for (int u = 0; u < kSubs; ++u) {
 #pragma unroll
@@ -504,27 +513,10 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
               }
             }
         }
-        if (kFp8) {
-          const float size[2] = {fabsf(block[u].v_scale[0]), fabsf(block[u].v_scale[1])};
-          const float most[2] = {size[0] <= FLT_MAX ? size[0] : 0.0f, size[1] <= FLT_MAX ? size[1] : 0.0f};
-          if (whole) {
-            const float m = fmaxf(most[0], most[1]);
-#pragma unroll
-            for (int n = 0; n < kBlocks; ++n)
-#pragma unroll
-              for (int c = 0; c < 2; ++c) scale_most[n][c] = fmaxf(scale_most[n][c], m);
-          } else {
-#pragma unroll
-            for (int n = 0; n < kBlocks; ++n)
-#pragma unroll
-              for (int i = 0; i < 4; ++i)  // only of keys that the row sees
-                if (s[u][n][i] != -INFINITY) scale_most[n][i & 1] = fmaxf(scale_most[n][i & 1], most[i >> 1]);
-          }
-        }
       }
-      // running maxima; FP8: the largest value scale too
+      // running maxima
       bool grows = false;
-      float keep[kBlocks][2];
+      float keep[kBlocks][2], rise[kBlocks][2];
 #pragma unroll
       for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
@@ -533,44 +525,54 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
           for (int m = 4; m < 32; m <<= 1) best[n][c] = fmaxf(best[n][c], __shfl_xor_sync(0xFFFFFFFFu, best[n][c], m));
           const float next = fmaxf(top[n][c], best[n][c]);
           grows = grows || next > top[n][c];
-          keep[n][c] = next == -INFINITY ? 1.0f : exp2_approx(top[n][c] - next);
+          rise[n][c] = next > top[n][c] ? next - top[n][c] : 0.0f;
+          keep[n][c] = exp2_approx(-rise[n][c]);
           top[n][c] = next;
         }
-      float v_factor[kBlocks][2];
       if (kFp8) {
-        float f[kBlocks][2];
+        // this tile's products, of this lane's keys; they may need a larger unit
 #pragma unroll
         for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
+            const float zero = top[n][c] == -INFINITY ? 0.0f : top[n][c];
+            best[n][c] = -INFINITY;
 #pragma unroll
-            for (int m = 4; m < 32; m <<= 1)
-              scale_most[n][c] = fmaxf(scale_most[n][c], __shfl_xor_sync(0xFFFFFFFFu, scale_most[n][c], m));
-            const int unit = max(v_unit[n][c], min(exponent_of(scale_most[n][c]) + 1, 127));
-            grows = grows || unit > v_unit[n][c];
-            f[n][c] = power_of_two(max(v_unit[n][c] - unit, -126));
-            v_unit[n][c] = unit;
-            v_factor[n][c] = power_of_two(14 - unit);
+            for (int u = 0; u < kSubs; ++u)
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+                best[n][c] = fmaxf(best[n][c], s[u][n][c + 2 * h] - zero + size_bound(block[u].v_scale[h]));
+            grows = grows || best[n][c] > unit_of(largest[n][c]);
           }
-        if (__any_sync(0xFFFFFFFFu, grows)) {
-#pragma unroll
-          for (int n = 0; n < kBlocks; ++n)
-#pragma unroll
-            for (int m = 0; m < D / 16; ++m)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) o[n][m][i] *= f[n][i & 1];
-        }
       }
       if (__any_sync(0xFFFFFFFFu, grows)) {
 #pragma unroll
         for (int n = 0; n < kBlocks; ++n) {
 #pragma unroll
-          for (int c = 0; c < 2; ++c) sum[n][c] *= keep[n][c];
+          for (int c = 0; c < 2; ++c) {
+            sum[n][c] *= keep[n][c];
+            if (kFp8) {
+#pragma unroll
+              for (int m = 4; m < 32; m <<= 1) best[n][c] = fmaxf(best[n][c], __shfl_xor_sync(0xFFFFFFFFu, best[n][c], m));
+              // by what this row has seen alone, whatever row made the warp come here
+              const float unit = unit_of(largest[n][c]);
+              if (rise[n][c] > 0.0f || best[n][c] > unit) largest[n][c] = fmaxf(largest[n][c] - rise[n][c], best[n][c]);
+              const float step = fminf(fmaxf(unit - unit_of(largest[n][c]), -126.0f), 127.0f);
+              keep[n][c] *= power_of_two(static_cast<int>(step));
+            }
+          }
 #pragma unroll
           for (int m = 0; m < D / 16; ++m)
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[n][m][i] *= keep[n][i & 1];
         }
+      }
+      float v_factor[kBlocks][2];
+      if (kFp8) {
+#pragma unroll
+        for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) v_factor[n][c] = power_of_two(14 - static_cast<int>(unit_of(largest[n][c])));
       }
 #pragma unroll
       for (int u = 0; u < kSubs; ++u) {
@@ -617,7 +619,7 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                   const float x = key < 8 ? s[u][n][c] : s[u][n][c + 2];
-                  const float w = __shfl_sync(0xFFFFFFFFu, x, key % 8 * 4 + t) * (kFp8 ? own * v_factor[n][c] : 1.0f);
+                  const float w = __shfl_sync(0xFFFFFFFFu, x, key % 8 * 4 + t) * own * (kFp8 ? v_factor[n][c] : 1.0f);
                   const int4 r = row_info(&info[warp][8 * n + 2 * t + c]);
                   if (j0 + key < r.x || j0 + key >= r.y) continue;
 #pragma unroll
@@ -644,8 +646,8 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (kFp8) {
-              p[n][h] = transpose8x8(pack_f16(s[u][n][2 * h] * (block[u].v_scale[h] * v_factor[n][0]),
-                                              s[u][n][2 * h + 1] * (block[u].v_scale[h] * v_factor[n][1])));
+              p[n][h] = transpose8x8(pack_f16(s[u][n][2 * h] * block[u].v_scale[h] * v_factor[n][0],
+                                              s[u][n][2 * h + 1] * block[u].v_scale[h] * v_factor[n][1]));
             } else {
               p[n][h] = transpose8x8(pack_bf16(s[u][n][2 * h], s[u][n][2 * h + 1]));
             }
@@ -673,7 +675,7 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
 #pragma unroll
         for (int m = 4; m < 32; m <<= 1) sum[n][c] += __shfl_xor_sync(0xFFFFFFFFu, sum[n][c], m);
         const int r = 8 * n + 2 * t + c;
-        const float o_unit = kFp8 ? power_of_two(v_unit[n][c] - 14) : 1.0f;
+        const float o_unit = kFp8 ? power_of_two(static_cast<int>(unit_of(largest[n][c])) - 14) : 1.0f;
         if (g == 0) {
           top_of[warp][r] = top[n][c];
           sum_of[warp][r] = sum[n][c];
