@@ -202,7 +202,8 @@ es_status_t es_cache_read(es_cache_t cache, const es_batch_t* batch, void* k_out
  * Scores, exponentials and sums are fp32; keys and values enter the products
  * exactly, and exp(x_j) (times an FP8 value's scale) rounded to bf16, or over FP8
  * caches with max_new * q_heads / kv_heads up to 16 to f16, where those below 2^-28
- * of a token's and head's largest are off by up to 2^-37 of it.
+ * of a token's and head's largest are off by up to 2^-37 of it. (There the elements of
+ * q too are f16 times a power of two: exact down to 2^-31 of the head's largest.)
  * Errors: ES_ERR_INVALID_ARG, ES_ERR_ALIGNMENT, ES_ERR_NONFINITE (scale, softcap),
  * ES_ERR_WRONG_DEVICE, ES_ERR_CUDA.
  */

@@ -399,8 +399,9 @@ few_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArg
           }
         most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
         most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-        // q / 2^e is below 2, and a dot with codes below 2 D 448: f16 and fp32 hold both
-        const int e = min(exponent_of(most), 126);
+        // q / 2^e is below 2^15, and a dot with codes below 2^15 D 448: f16 and fp32 hold both. Elements
+        // stay exact down to 2^-31 of the row's largest, where f16 numbers are 2^-24 apart.
+        const int e = max(min(exponent_of(most), 127) - 14, -126);
         q_unit = power_of_two(e);
         const float inv = power_of_two(-e);
 #pragma unroll

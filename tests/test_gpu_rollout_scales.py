@@ -1,5 +1,5 @@
-"""es_attention over FP8 caches whose scales differ in sign and in size: both kernels against the
-definition in 64 bits.
+"""es_attention over FP8 caches whose scales differ in sign and in size, and with queries whose
+elements do: both kernels against the definition in 64 bits.
 
 Tolerances: those of rollout_reference.py (A = sum p |v|), and where scales differ in size what the
 f16 numbers of the few-rows kernel leave out: exp(x) times a value's scale is held there in units in
@@ -9,7 +9,7 @@ import pytest
 import torch
 
 import rollout_reference as R
-from test_gpu_rollout import Setup, attend, check
+from test_gpu_rollout import Setup, assert_attention, attend, check
 
 pytestmark = pytest.mark.gpu
 
@@ -86,3 +86,15 @@ def test_the_weight_on_a_key_whose_value_scale_differs(ro, new, at, weight, powe
     q = (weight * k[0][at].repeat_interleave(2, 0)).bfloat16().expand(s.tokens, 4, 128).contiguous().cuda()
     q, out, lse = attend(s, 4, q=q)
     assert_spread(s, q, out, lse)
+
+
+@pytest.mark.parametrize("new", NEW)
+@pytest.mark.parametrize("d", [64, 128])
+def test_queries_with_one_large_element(ro, new, d):
+    # an element 2^22 times the others, at which every key is 0: the others decide
+    s = Setup(ro, [150, 75], new, 2, d, 32, "e4m3", seed=36)
+    s.k.view(torch.uint8)[..., 5] = 0
+    q = 1.5 * torch.randn(s.tokens, 4, d, generator=s.g)
+    q[..., 5] = 2.0 ** 22
+    q, out, lse = attend(s, 4, q=q.bfloat16().cuda())
+    assert_attention(s, q, out, lse)
