@@ -123,7 +123,10 @@ typedef struct {
  * Queries go to q_out as bf16, keys and values to the token's place in the cache.
  * Arithmetic is fp32, rounded once (to nearest even). In an FP8 cache a vector's
  * scale is max(max|x| / 448, 2^-126) over its finite elements, and its codes are
- * the nearest E4M3 numbers of x / scale, saturating at +-448 (NaN stays NaN).
+ * the E4M3 numbers nearest to x * (1 / scale) in fp32, ties to even, saturating at
+ * +-448 (NaN stays NaN). The two fp32 roundings are within 2^-22 of x / scale, so
+ * a code is not the nearest to x / scale only where that is as close as this to
+ * midway between two codes.
  *   qkv         [tokens] rows of q_heads + 2 * kv_heads heads (queries, keys,
  *               values) of head_dim bf16, qkv_stride elements apart
  *   q_out       [tokens] rows of q_heads heads, q_out_stride elements apart; may
