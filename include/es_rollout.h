@@ -134,8 +134,8 @@ typedef struct {
  *   q_weight,   [head_dim] bf16; NULL: these heads are not normalised
  *   k_weight
  *   rope        [rope_rows][rotary_dim / 2] fp32 pairs (cos, sin), or NULL with
- *               rotary_dim 0. A token whose position has no row gets NaN queries
- *               and keys.
+ *               rotary_dim 0. A token whose position has no row gets NaN in the
+ *               first rotary_dim elements of its queries and keys.
  *   positions   [tokens] (4-byte aligned), or NULL: the position in the sequence.
  *               Only the rotation goes by it.
  *   rotary_dim  a multiple of 16 up to head_dim

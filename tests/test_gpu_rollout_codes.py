@@ -1,4 +1,5 @@
-"""The numbers that an FP8 append writes, to the spacing of the codes.
+"""The numbers that an FP8 append writes, to the spacing of the codes, and what a rotation without its row
+leaves.
 
 Tolerances of the codes, from the roundings made: a value's y = x / scale passes three fp32 roundings
 (the scale, its reciprocal, the product), 2^-22 of it at most; a key's also those of its norm and
@@ -7,7 +8,7 @@ import pytest
 import torch
 
 import rollout_reference as R
-from test_gpu_rollout import append_case
+from test_gpu_rollout import DTYPES, append_case
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +64,22 @@ def test_codes_of_a_scale_of_one(ro, n):
     pg, sl = (torch.tensor(v) for v in zip(*[(sp[2], sp[3]) for sp in spots]))
     assert (s.vs.cpu()[pg, :, sl] == 1).all()
     assert torch.equal(R.e4m3(s.v.view(torch.uint8).cpu())[pg, :, sl], want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_a_rotation_without_its_row_leaves_the_other_elements(ro, dtype, interleaved):
+    # 32 of 128 elements turn: NaN without a row, the norm's result in the rest
+    positions = [0, 49, 50, -1, 2 ** 31 - 1] * 5
+    s, q, (wq, wk, _), spots, _ = append_case(ro, dtype, 128, 32, interleaved, positions=positions)
+    for t, p in enumerate(positions):
+        missing = not 0 <= p < 50
+        got = q[t].cpu().double()
+        assert torch.isnan(got[:, :32]).all() == missing and not torch.isnan(got[:, 32:]).any()
+        if spots[t] is not None:
+            key = s.k.view(torch.uint8) if dtype == "e4m3" else s.k
+            key = key[spots[t][2], :, spots[t][3]].cpu()
+            key = R.e4m3(key) if dtype == "e4m3" else key.double()
+            assert torch.isnan(key[:, :32]).all() == missing and not torch.isnan(key[:, 32:]).any()
+    s0, q0, (w0, _, _), _, _ = append_case(ro, dtype, 128, 32, interleaved, positions=[0] * 25)
+    assert torch.equal(q[:, :, 32:], q0[:, :, 32:])  # the same seed: the same inputs, turned elsewhere
