@@ -168,7 +168,7 @@ es_status_t es_cache_append(es_cache_t cache, const es_batch_t* batch, const es_
 /*
  * The cached keys and values of the batch's tokens (with start = the running sum of
  * seq_len: whole sequences) as [tokens][kv_heads][head_dim] bf16 rows, contiguous;
- * scale * code rounded once. A token whose place does not exist reads as 0. Either
+ * scale * code in fp32, rounded to bf16. A token whose place does not exist reads as 0. Either
  * output may be NULL.
  * Errors: ES_ERR_INVALID_ARG, ES_ERR_ALIGNMENT, ES_ERR_WRONG_DEVICE, ES_ERR_CUDA.
  */
