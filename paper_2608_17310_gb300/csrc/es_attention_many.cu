@@ -1314,7 +1314,8 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
     soften<D, kFp8, kPlain>(sh, cache, batch, a, counters, parts, warp / 4, threadIdx.x % 128, lane);
   } else if (warp == kIssuer) {
     issue_products<D, kFp8>(sh, lane);
-    if (lane == 0) commit(&sh.drained);  // no product outlives the tensor memory
+    __syncwarp();
+    if (elected()) commit(&sh.drained);  // by the lane that issued the products: none outlives the tensor memory
     __syncwarp();
     barrier_settle(&sh.drained, 0);
   } else {
