@@ -375,6 +375,15 @@ struct Unit {
 };
 constexpr int kUnits = 4;
 
+// 32 keys of a unit (bits of `keys`, from position key0) whose values hold an infinity or NaN that
+// not every row sees. A unit's first kBad such pieces are listed; where it has more, all its tiles
+// at the ends of intervals are looked through again.
+struct Bad {
+  int key0;
+  uint32_t keys;
+};
+constexpr uint32_t kBad = 32;
+
 // FP8: codes pass from the pages to the converting warps in pieces of 32 keys or values, four
 // and four to a tile, each warp with a place of its own for them. (Four warps that shared each
 // piece, a half tile, took 6,000 cycles a tile for 3,000 cycles of work.)
@@ -401,7 +410,10 @@ struct Shared {
   Unit unit[kUnits];
   uint32_t tensor;           // address of the tensor memory
   int failed;
-  int poisoned;              // a value that not every row sees was an infinity or NaN
+  CacheView cache;  // for add_bad
+  BatchView batch;
+  uint32_t bad_count[kUnits];  // of each unit here
+  Bad bad[kUnits][kBad];
   int last[2];
 };
 
@@ -492,6 +504,7 @@ __device__ __forceinline__ bool tell(Sh& sh, Walk& walk, const BatchView& b, con
   if (lane == 0) {
     Unit& u = sh.unit[n % kUnits];
     u.valid = more;
+    sh.bad_count[n % kUnits] = 0;
     if (more) {
       const Pair& p = walk.pair;
       u.seq = walk.seq;
@@ -527,6 +540,16 @@ __device__ __forceinline__ bool take(Sh& sh, uint32_t n) {
 template <class Sh>
 __device__ __forceinline__ void leave(Sh& sh, uint32_t n, int lane) {
   warp_arrive(&sh.unit_empty[n % kUnits], lane);
+}
+
+// By a whole warp: unit n's keys key0 + the bits of its lanes are noted.
+template <class Sh>
+__device__ __forceinline__ void note_bad(Sh& sh, uint32_t n, int key0, uint32_t bits, int lane) {
+  const uint32_t keys = __reduce_or_sync(0xFFFFFFFFu, bits);
+  if (keys != 0 && lane == 0) {
+    const uint32_t at = atomicAdd(&sh.bad_count[n % kUnits], 1u);
+    if (at < kBad) sh.bad[n % kUnits][at] = Bad{key0, keys};
+  }
 }
 
 // Offset in elements of 16-byte piece `piece` of row r, in an operand of 128 rows.
@@ -585,8 +608,8 @@ __device__ void copy_tiles(Shared<D, false>& sh, const CacheView& cache, const B
 }
 
 // bf16 values of tiles at the ends of intervals: those that no row sees become zeros, and
-// infinities and NaN too (a product with p = 0 would carry them into rows that do not see
-// them); the rows that see them get them when the unit is written. Every tile passes here,
+// infinities and NaN too (a product with p = 0 would carry them into rows that do not see them), and
+// their keys are noted: the rows that see them get them when the unit is written. Every tile passes here,
 // so that the barriers of the stages are never a round ahead.
 template <int D>
 __device__ void fix_tiles(Shared<D, false>& sh, int thread, int lane) {
@@ -599,23 +622,38 @@ __device__ void fix_tiles(Shared<D, false>& sh, int thread, int lane) {
       if (!warp_wait(&sh.v_full[stage], done / kStages & 1, &sh.failed)) return;
       if (unit.edge(tile)) {
         const int lo = unit.lo, hi = unit.hi;
-        for (int i = thread; i < kKeys * D / 8; i += 64) {
-          const int key = i / (D / 8), j = j0 + key;
-          uint4* at = reinterpret_cast<uint4*>(sh.v[stage] + place_of<D>(key, i % (D / 8)));
-          if (j < lo || j >= hi) {
-            *at = make_uint4(0, 0, 0, 0);
-            continue;
+#pragma unroll 1
+        for (int key0 = 0; key0 < kKeys; key0 += 32) {
+          constexpr int kSteps = D / 16;  // of 64 pieces, to 32 keys
+          auto key_at = [&](int step) { return key0 + (step * 64 + thread) / (D / 8); };
+          auto piece_at = [&](int step) { return reinterpret_cast<uint4*>(sh.v[stage] + place_of<D>(key_at(step), thread % (D / 8))); };
+          uint4 w[kSteps];
+#pragma unroll
+          for (int i = 0; i < kSteps; ++i) w[i] = *piece_at(i);
+          bool spoiled = false;
+#pragma unroll
+          for (int i = 0; i < kSteps; ++i) {
+            const int j = j0 + key_at(i);
+            if (j < lo || j >= hi) *piece_at(i) = make_uint4(0, 0, 0, 0);
+            else spoiled = spoiled || has_nonfinite(w[i].x) || has_nonfinite(w[i].y) || has_nonfinite(w[i].z) || has_nonfinite(w[i].w);
           }
-          uint4 w = *at;
-          if (has_nonfinite(w.x) || has_nonfinite(w.y) || has_nonfinite(w.z) || has_nonfinite(w.w)) {
-            uint32_t* u = reinterpret_cast<uint32_t*>(&w);
+          if (!__any_sync(0xFFFFFFFFu, spoiled)) continue;
+          uint32_t bad = 0;
+#pragma unroll 1
+          for (int i = 0; i < kSteps; ++i) {
+            uint32_t* u = reinterpret_cast<uint32_t*>(piece_at(i));  // zeros outside [lo, hi) by now
+#pragma unroll 1
             for (int e = 0; e < 4; ++e) {
-              if ((u[e] & 0x7F80u) == 0x7F80u) u[e] &= 0xFFFF0000u;
-              if ((u[e] & 0x7F800000u) == 0x7F800000u) u[e] &= 0xFFFFu;
+              uint32_t x = u[e];
+              if (!has_nonfinite(x)) continue;
+              if ((x & 0x7F80u) == 0x7F80u) x &= 0xFFFF0000u;
+              if ((x & 0x7F800000u) == 0x7F800000u) x &= 0xFFFFu;
+              u[e] = x;
+              bad |= 1u << (key_at(i) % 32);
             }
-            *at = w;
-            *static_cast<volatile int*>(&sh.poisoned) = 1;
           }
+          __syncwarp();
+          note_bad(sh, n, j0 + key0, bad, lane);
         }
         fence_async();
       }
@@ -666,11 +704,12 @@ __device__ void copy_codes(Shared<D, true>& sh, const CacheView& cache, const Ba
 // One warp's piece of codes to bf16, 8 codes (16 bytes of bf16) to a lane and step, so that the
 // eight lanes that write side by side write all of one 128-byte row; eight steps' codes are
 // read before any is converted.
-// clean: keys outside [lo, hi) become zeros, and NaN codes too.
+// clean: keys outside [lo, hi) become zeros, and NaN codes too; returns the piece's keys of this
+// lane that had any.
 template <int D>
-__device__ __forceinline__ void convert_piece(const uint8_t* raw, uint16_t* to, int key0, int lane, bool clean, int lo, int hi,
-                                              int* poisoned) {
+__device__ __forceinline__ uint32_t convert_piece(const uint8_t* raw, uint16_t* to, int key0, int lane, bool clean, int lo, int hi) {
   constexpr int kSteps = kPiece * D / 8 / 32;
+  uint32_t bad_keys = 0;
 #pragma unroll 1
   for (int s0 = 0; s0 < kSteps; s0 += 8) {
     uint32_t u[8][2];
@@ -690,7 +729,7 @@ __device__ __forceinline__ void convert_piece(const uint8_t* raw, uint16_t* to, 
           const uint32_t bad = ((u[i][e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;  // NaN codes
           if (bad != 0) {
             u[i][e] &= ~((bad >> 7) * 0xFFu);
-            *static_cast<volatile int*>(poisoned) = 1;
+            bad_keys |= 1u << (key - key0);
           }
         }
       }
@@ -702,6 +741,7 @@ __device__ __forceinline__ void convert_piece(const uint8_t* raw, uint16_t* to, 
           make_uint4(bf16_of_e4m3(u[i][0]), bf16_of_e4m3(u[i][0] >> 16), bf16_of_e4m3(u[i][1]), bf16_of_e4m3(u[i][1] >> 16));
     }
   }
+  return bad_keys;
 }
 
 template <int D>
@@ -727,19 +767,21 @@ __device__ void convert_tiles(Shared<D, true>& sh, const CacheView& cache, const
           scale = __ldg((of_keys ? cache.k_scale : cache.v_scale) + page * cache.scale_stride +
                         (static_cast<uint64_t>(unit.head) << cache.page_shift) + (j & ((1 << cache.page_shift) - 1)));
         const bool clean = !of_keys && unit.edge(tile);
+        uint32_t bad = 0;
         if (clean) {  // as with NaN codes: only rows that see the key get to know its scale
           if (j < unit.lo || j >= unit.hi) {
             scale = 0.0f;
           } else if (!(fabsf(scale) <= FLT_MAX)) {
             scale = 0.0f;
-            *static_cast<volatile int*>(&sh.poisoned) = 1;
+            bad = 1u << lane;
           }
         }
         if (!warp_wait(of_keys ? &sh.k_empty[stage] : &sh.v_empty[stage], parity ^ 1, &sh.failed)) return;
         if (of_keys) sh.k_scale[done % 4][key0 + lane] = scale * a.factor;
         else sh.v_scale[stage][key0 + lane] = scale;
         if (!warp_wait(&sh.raw_full[warp], turns & 1, &sh.failed)) return;
-        convert_piece<D>(sh.raw[warp], of_keys ? sh.k[stage] : sh.v[stage], key0, lane, clean, unit.lo - j0, unit.hi - j0, &sh.poisoned);
+        bad |= convert_piece<D>(sh.raw[warp], of_keys ? sh.k[stage] : sh.v[stage], key0, lane, clean, unit.lo - j0, unit.hi - j0);
+        if (clean) note_bad(sh, n, j0 + key0, bad, lane);
         // The next codes may come now that these have been used. (After their loads alone have
         // been issued is too early: a copy of zeros can overtake them.)
         warp_arrive(&sh.raw_empty[warp], lane);
@@ -883,6 +925,57 @@ __device__ __forceinline__ void hand_over(Sh& sh, int x, int lane) {
   asm volatile("cp.async.wait_all;" ::: "memory");
   fence_async();
   warp_arrive(&sh.q_full[x], lane);
+}
+
+// Adds the infinities and NaN that unit n's noted keys hold in their values to a row that sees
+// [lo, hi): to its results in bf16, or where `part` is given to its part of a shared unit (16 bytes of all
+// rows together). Out of line, and with all it needs in shared memory: in line it costs FP8 tiles 3 to 6 %.
+template <int D, bool kFp8>
+__device__ __noinline__ void add_bad(const Shared<D, kFp8>& sh, uint32_t n, int lo, int hi, uint16_t* out, float* part) {
+  const CacheView& cache = sh.cache;
+  const Unit& unit = sh.unit[n % kUnits];
+  const uint32_t bad = sh.bad_count[n % kUnits];
+  const bool listed = bad <= kBad;
+  const int pieces = listed ? static_cast<int>(bad) : (unit.tile1 - unit.tile0) * (kKeys / 32);
+  auto add = [&](int e, float v) {
+    if (fabsf(v) <= FLT_MAX) return;
+    if (part != nullptr) part[e / 4 * (4 * kRows) + e % 4] += v;
+    else out[e] = static_cast<uint16_t>(pack_bf16(__uint_as_float(static_cast<uint32_t>(out[e]) << 16) + v, 0.0f));
+  };
+#pragma unroll 1
+  for (int i = 0; i < pieces; ++i) {
+    Bad piece;
+    if (listed) {
+      piece = sh.bad[n % kUnits][i];
+    } else {
+      const int tile = unit.tile0 + i / (kKeys / 32);
+      if (!unit.edge(tile)) continue;
+      piece = Bad{unit.key_of(tile) + i % (kKeys / 32) * 32, 0xFFFFFFFFu};
+    }
+    uint32_t keys = piece.keys & bits_from(lo - piece.key0) & ~bits_from(hi - piece.key0);
+#pragma unroll 1
+    for (; keys != 0; keys &= keys - 1) {
+      const int j = piece.key0 + __ffs(static_cast<int>(keys)) - 1;
+      const int page = page_of(cache, sh.batch, unit.seq, j);
+      if (page < 0) continue;
+      const uint64_t in_page = (static_cast<uint64_t>(unit.head) << cache.page_shift) + (j & ((1 << cache.page_shift) - 1));
+      const uint64_t at = page * cache.page_stride + in_page * D;
+      const float scale = kFp8 ? cache.v_scale[page * cache.scale_stride + in_page] : 1.0f;
+      const bool all = !(fabsf(scale) <= FLT_MAX);  // of the vector, whatever its codes
+#pragma unroll 4
+      for (int e = 0; e < D; e += kFp8 ? 4 : 2) {
+        const uint32_t x = *reinterpret_cast<const uint32_t*>(static_cast<const char*>(cache.v) + (at + e) * (kFp8 ? 1 : 2));
+        if (kFp8) {
+          if (!all && (((x & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) == 0) continue;
+#pragma unroll 1
+          for (int b = 0; b < 4; ++b) add(e + b, __uint_as_float(bf16_of_e4m3(x >> (8 * b) & 0xFFu) << 16) * scale);
+        } else if (has_nonfinite(x)) {
+          add(e, __uint_as_float(x << 16));
+          add(e + 1, __uint_as_float(x & 0xFFFF0000u));
+        }
+      }
+    }
+  }
 }
 
 // A warpgroup's rows: a thread for each.
@@ -1130,7 +1223,6 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
     const int c_first = unit.c_first, c_last = unit.c_last;
     const int self = static_cast<int>(blockIdx.x);
     const bool shared_unit = c_first != c_last;
-    const bool poisoned = *static_cast<volatile int*>(&sh.poisoned) != 0;
     const int r_part = x * 128 + thread;
     Part<D>& part = parts[self == c_first ? 2 * self + 1 : 2 * self];
     const bool some = top > -INFINITY || sum != sum;
@@ -1142,26 +1234,6 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
       __syncwarp();
       tensor_load(w, o_at + c);
       tensor_loaded(w);
-      if (poisoned && row.token >= 0) {
-        for (int tile = tile0; tile < tile1; ++tile) {
-          if (!unit.edge(tile)) continue;
-          const int j0 = unit.key_of(tile);
-          for (int j = max(j0, row.lo); j < min(j0 + kKeys, row.hi); ++j) {
-            const int page = page_of(cache, batch, unit.seq, j);
-            if (page < 0) continue;
-            const uint64_t in_page = (static_cast<uint64_t>(unit.head) << cache.page_shift) + (j & ((1 << cache.page_shift) - 1));
-            const uint64_t at = page * cache.page_stride + in_page * D + c;
-            const float scale = kFp8 ? cache.v_scale[page * cache.scale_stride + in_page] : 1.0f;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              float v;
-              if (kFp8) v = __uint_as_float(bf16_of_e4m3(static_cast<const uint8_t*>(cache.v)[at + i]) << 16) * scale;
-              else v = __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(cache.v)[at + i]) << 16);
-              if (!(fabsf(v) <= FLT_MAX)) w[i] = __float_as_uint(__uint_as_float(w[i]) + v);
-            }
-          }
-        }
-      }
       if (row.token < 0) continue;
       if (shared_unit) {
 #pragma unroll
@@ -1178,6 +1250,8 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
         }
       }
     }
+    if (sh.bad_count[mine % kUnits] != 0 && row.token >= 0 && some)
+      add_bad<D, kFp8>(sh, mine, row.lo, row.hi, out, shared_unit ? reinterpret_cast<float*>(&part.o[0][r_part]) : nullptr);
     if (shared_unit) {
       if (row.token >= 0) {
         part.top[r_part] = top;
@@ -1288,7 +1362,8 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
     barrier_init(&sh.drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sh.failed = 0;
-    sh.poisoned = 0;
+    sh.cache = cache;
+    sh.batch = batch;
   }
   constexpr int kIssuer = kFp8 ? 8 + kRaw : 8;
   if (warp == kIssuer) {
