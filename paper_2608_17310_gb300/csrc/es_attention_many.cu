@@ -68,7 +68,8 @@ struct Plan {
 };
 
 // What the rows of (sequence, row tile) see: their tokens, and the union and the common part
-// of their intervals of the cache.
+// of their intervals of the cache. Rows that see nothing have no part in either: whatever a
+// product leaves in them, they are written as zeros.
 struct Pair {
   int begin, count, base, length;
   int rows;
@@ -111,9 +112,9 @@ __device__ __forceinline__ Pair pair_of(const BatchView& b, const AttentionArgs&
       if (r.hi > r.lo) {
         lo = min(lo, r.lo);
         hi = max(hi, r.hi);
+        in_lo = max(in_lo, r.lo);
+        in_hi = min(in_hi, r.hi);
       }
-      in_lo = max(in_lo, r.lo);
-      in_hi = min(in_hi, r.hi);
     }
 #pragma unroll
     for (int m = kLanes / 2; m > 0; m >>= 1) {
@@ -370,7 +371,7 @@ struct Unit {
   int c_first, c_last;  // the blocks that share it
 
   __device__ __forceinline__ int key_of(int tile) const { return key0 + tile * kKeys; }
-  // Not every row sees all of the tile.
+  // Not every row that sees anything sees all of the tile.
   __device__ __forceinline__ bool edge(int tile) const { return key_of(tile) < in_lo || key_of(tile) + kKeys > in_hi; }
 };
 constexpr int kUnits = 4;

@@ -100,3 +100,36 @@ def test_one_such_value_costs_little(ro, dtype):
     other[20:40, :, 9] = 0
     assert torch.isfinite(other).all()
     assert spoiled <= 3 * clean + 1.0, f"{spoiled:.2f} ms in place of {clean:.2f}"
+
+
+def test_an_empty_row_costs_little(ro):
+    # a row that sees nothing makes no tile one whose values have to be looked through
+    sequences, new, length = 24, 60, 8192
+    pages = sequences * length // 64
+    k, v = (torch.randn(pages, 8, 64, 128, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    cache = ro.es_cache_create(k, v)
+    table = torch.arange(pages, device="cuda", dtype=torch.int32).view(sequences, -1)
+    start = torch.arange(0, sequences * new + 1, new, device="cuda", dtype=torch.int32)
+    batch = ro.Batch(table, torch.full((sequences,), length, dtype=torch.int32, device="cuda"), start, sequences * new, new)
+    q = torch.randn(sequences * new, 32, 128, device="cuda").bfloat16()
+    out, ws = torch.empty_like(q), torch.zeros(ro.es_attention_workspace(cache, 32), dtype=torch.uint8, device="cuda")
+    first = torch.zeros(sequences * new, dtype=torch.int32, device="cuda")
+
+    def us():
+        times = []
+        for _ in range(9):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            for _ in range(10):
+                ro.es_attention(cache, batch, q, out, ws, scale=128 ** -0.5, first=first)
+            b.record()
+            torch.cuda.synchronize()
+            times.append(a.elapsed_time(b) * 100)
+        return sorted(times)[4]
+
+    us()
+    without = us()
+    first[3::new] = 10 ** 6
+    with_one = us()
+    assert (out[3::new] == 0).all()
+    assert with_one <= 1.4 * without, f"{with_one:.0f} us in place of {without:.0f}"
