@@ -930,7 +930,8 @@ __device__ __forceinline__ void hand_over(Sh& sh, int x, int lane) {
 
 // Adds the infinities and NaN that unit n's noted keys hold in their values to a row that sees
 // [lo, hi): to its results in bf16, or where `part` is given to its part of a shared unit (16 bytes of all
-// rows together). Out of line, and with all it needs in shared memory: in line it costs FP8 tiles 3 to 6 %.
+// rows together). 32 elements at a time over all keys, until they are all NaN. Out of line, and with all it
+// needs in shared memory: in line it costs FP8 tiles 3 to 6 %.
 template <int D, bool kFp8>
 __device__ __noinline__ void add_bad(const Shared<D, kFp8>& sh, uint32_t n, int lo, int hi, uint16_t* out, float* part) {
   const CacheView& cache = sh.cache;
@@ -938,43 +939,56 @@ __device__ __noinline__ void add_bad(const Shared<D, kFp8>& sh, uint32_t n, int 
   const uint32_t bad = sh.bad_count[n % kUnits];
   const bool listed = bad <= kBad;
   const int pieces = listed ? static_cast<int>(bad) : (unit.tile1 - unit.tile0) * (kKeys / 32);
-  auto add = [&](int e, float v) {
-    if (fabsf(v) <= FLT_MAX) return;
-    if (part != nullptr) part[e / 4 * (4 * kRows) + e % 4] += v;
-    else out[e] = static_cast<uint16_t>(pack_bf16(__uint_as_float(static_cast<uint32_t>(out[e]) << 16) + v, 0.0f));
-  };
 #pragma unroll 1
-  for (int i = 0; i < pieces; ++i) {
-    Bad piece;
-    if (listed) {
-      piece = sh.bad[n % kUnits][i];
-    } else {
-      const int tile = unit.tile0 + i / (kKeys / 32);
-      if (!unit.edge(tile)) continue;
-      piece = Bad{unit.key_of(tile) + i % (kKeys / 32) * 32, 0xFFFFFFFFu};
-    }
-    uint32_t keys = piece.keys & bits_from(lo - piece.key0) & ~bits_from(hi - piece.key0);
+  for (int c = 0; c < D; c += 32) {
+    float sum[32];
+#pragma unroll
+    for (int e = 0; e < 32; ++e) sum[e] = 0.0f;
+    bool more = true;
 #pragma unroll 1
-    for (; keys != 0; keys &= keys - 1) {
-      const int j = piece.key0 + __ffs(static_cast<int>(keys)) - 1;
-      const int page = page_of(cache, sh.batch, unit.seq, j);
-      if (page < 0) continue;
-      const uint64_t in_page = (static_cast<uint64_t>(unit.head) << cache.page_shift) + (j & ((1 << cache.page_shift) - 1));
-      const uint64_t at = page * cache.page_stride + in_page * D;
-      const float scale = kFp8 ? cache.v_scale[page * cache.scale_stride + in_page] : 1.0f;
-      const bool all = !(fabsf(scale) <= FLT_MAX);  // of the vector, whatever its codes
-#pragma unroll 4
-      for (int e = 0; e < D; e += kFp8 ? 4 : 2) {
-        const uint32_t x = *reinterpret_cast<const uint32_t*>(static_cast<const char*>(cache.v) + (at + e) * (kFp8 ? 1 : 2));
-        if (kFp8) {
-          if (!all && (((x & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) == 0) continue;
+    for (int i = 0; more && i < pieces; ++i) {
+      Bad piece;
+      if (listed) {
+        piece = sh.bad[n % kUnits][i];
+      } else {
+        const int tile = unit.tile0 + i / (kKeys / 32);
+        if (!unit.edge(tile)) continue;
+        piece = Bad{unit.key_of(tile) + i % (kKeys / 32) * 32, 0xFFFFFFFFu};
+      }
+      uint32_t keys = piece.keys & bits_from(lo - piece.key0) & ~bits_from(hi - piece.key0);
 #pragma unroll 1
-          for (int b = 0; b < 4; ++b) add(e + b, __uint_as_float(bf16_of_e4m3(x >> (8 * b) & 0xFFu) << 16) * scale);
-        } else if (has_nonfinite(x)) {
-          add(e, __uint_as_float(x << 16));
-          add(e + 1, __uint_as_float(x & 0xFFFF0000u));
+      for (; more && keys != 0; keys &= keys - 1) {
+        const int j = piece.key0 + __ffs(static_cast<int>(keys)) - 1;
+        const int page = page_of(cache, sh.batch, unit.seq, j);
+        if (page < 0) continue;
+        const uint64_t in_page = (static_cast<uint64_t>(unit.head) << cache.page_shift) + (j & ((1 << cache.page_shift) - 1));
+        const uint64_t at = page * cache.page_stride + in_page * D + c;
+        const float scale = kFp8 ? cache.v_scale[page * cache.scale_stride + in_page] : 1.0f;
+        constexpr int kLoads = kFp8 ? 2 : 4;  // of 16 bytes
+        uint4 raw[kLoads];
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l)
+          raw[l] = reinterpret_cast<const uint4*>(static_cast<const char*>(cache.v) + at * (kFp8 ? 1 : 2))[l];
+        more = false;
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+          const uint4& x = raw[e / (32 / kLoads)];
+          const int word = e % (32 / kLoads) / (kFp8 ? 4 : 2);
+          uint32_t y = word == 0 ? x.x : word == 1 ? x.y : word == 2 ? x.z : x.w;
+          if (kFp8) y = bf16_of_e4m3(e % 4 == 0 ? y : y >> 16);
+          const float v0 = __uint_as_float(y << 16) * scale, v1 = __uint_as_float(y & 0xFFFF0000u) * scale;
+          if (!(fabsf(v0) <= FLT_MAX)) sum[e] += v0;
+          if (!(fabsf(v1) <= FLT_MAX)) sum[e + 1] += v1;
+          more = more || sum[e] == sum[e] || sum[e + 1] == sum[e + 1];
         }
       }
+    }
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+      if (fabsf(sum[e]) <= FLT_MAX) continue;
+      const int at = c + e;
+      if (part != nullptr) part[at / 4 * (4 * kRows) + at % 4] += sum[e];
+      else out[at] = static_cast<uint16_t>(pack_bf16(__uint_as_float(static_cast<uint32_t>(out[at]) << 16) + sum[e], 0.0f));
     }
   }
 }

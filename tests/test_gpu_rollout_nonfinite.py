@@ -133,3 +133,33 @@ def test_an_empty_row_costs_little(ro):
     with_one = us()
     assert (out[3::new] == 0).all()
     assert with_one <= 1.4 * without, f"{with_one:.0f} us in place of {without:.0f}"
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_cache_of_nan_costs_little(ro, dtype):
+    # as a member whose parameters went wrong leaves it: every value of every token is NaN
+    n = 3001
+    s = Setup(ro, [n], [n], 2, 128, 64, dtype, seed=55)
+    q = torch.randn(n, 8, 128, generator=s.g).bfloat16().cuda()
+    out, ws = torch.empty_like(q), torch.zeros(ro.es_attention_workspace(s.cache, 8), dtype=torch.uint8, device="cuda")
+
+    def ms():
+        times = []
+        for _ in range(4):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            ro.es_attention(s.cache, s.batch, q, out, ws, scale=s.d ** -0.5)
+            b.record()
+            torch.cuda.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+
+    clean = ms()
+    assert torch.isfinite(out.float()).all()
+    if dtype == "bf16":
+        s.v.fill_(math.nan)
+    else:
+        s.v.view(torch.uint8).fill_(0x7F)
+    spoiled = ms()
+    assert torch.isnan(out.float()).all()
+    assert spoiled <= 3 * clean + 1.0, f"{spoiled:.2f} ms in place of {clean:.2f}"
