@@ -993,6 +993,31 @@ __device__ __noinline__ void add_bad(const Shared<D, kFp8>& sh, uint32_t n, int 
   }
 }
 
+// 32 columns of scores in tensor memory, capped, each by its own size. By whole warps, where a chunk
+// has a score beyond a quarter of the cap; out of line, since in line it costs the others their place in
+// the instruction cache.
+template <bool kFp8>
+__device__ __noinline__ void cap_chunk(uint32_t at, float cap, float factor, const float* k_scale) {
+  const float c1 = -1.0f / 3.0f * cap, c2 = 2.0f / 15.0f * cap, c3 = -17.0f / 315.0f * cap;
+  uint32_t w[32];
+  tensor_load(w, at);
+  tensor_loaded(w);
+#pragma unroll
+  for (int i = 0; i < 32; i += 2) {
+    const uint64_t u = mul2(pack(__uint_as_float(w[i]), __uint_as_float(w[i + 1])),
+                            kFp8 ? *reinterpret_cast<const uint64_t*>(k_scale + i) : pack(factor, factor));
+    const uint64_t z = mul2(u, u);
+    float lo, hi, lo_small, hi_small;
+    unpack(u, lo, hi);
+    unpack(mul2(u, fma2(z, fma2(z, fma2(z, pack(c3, c3), pack(c2, c2)), pack(c1, c1)), pack(cap, cap))), lo_small, hi_small);
+    constexpr float twice = 2.0f * kLog2e;
+    w[i] = __float_as_uint(fabsf(lo) <= 0.25f ? lo_small : fmaf(-2.0f * cap, reciprocal(exp2_approx(lo * twice) + 1.0f), cap));
+    w[i + 1] = __float_as_uint(fabsf(hi) <= 0.25f ? hi_small : fmaf(-2.0f * cap, reciprocal(exp2_approx(hi * twice) + 1.0f), cap));
+  }
+  tensor_store32(at, w);
+  tensor_stored();
+}
+
 // A warpgroup's rows: a thread for each.
 template <int D, bool kFp8, bool kPlain>
 __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
@@ -1074,24 +1099,20 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
               unpack(y[i], lo, hi);
               most = fmaxf(most, fmaxf(fabsf(lo), fabsf(hi)));
             }
-            const float c1 = -1.0f / 3.0f * cap, c2 = 2.0f / 15.0f * cap, c3 = -17.0f / 315.0f * cap;
-            auto series = [&](uint64_t u) {
-              const uint64_t z = mul2(u, u);
-              return mul2(u, fma2(z, fma2(z, fma2(z, pack(c3, c3), pack(c2, c2)), pack(c1, c1)), pack(cap, cap)));
-            };
             if (__all_sync(0xFFFFFFFFu, most <= 0.25f)) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) y[i] = series(y[i]);
-            } else {
-              constexpr float twice = 2.0f * kLog2e;
+              const float c1 = -1.0f / 3.0f * cap, c2 = 2.0f / 15.0f * cap, c3 = -17.0f / 315.0f * cap;
 #pragma unroll
               for (int i = 0; i < 16; ++i) {
-                float lo, hi, lo_small, hi_small;
-                unpack(y[i], lo, hi);
-                unpack(series(y[i]), lo_small, hi_small);
-                y[i] = pack(fabsf(lo) <= 0.25f ? lo_small : fmaf(-2.0f * cap, reciprocal(exp2_approx(lo * twice) + 1.0f), cap),
-                            fabsf(hi) <= 0.25f ? hi_small : fmaf(-2.0f * cap, reciprocal(exp2_approx(hi * twice) + 1.0f), cap));
+                const uint64_t z = mul2(y[i], y[i]);
+                const uint64_t t = fma2(z, fma2(z, fma2(z, pack(c3, c3), pack(c2, c2)), pack(c1, c1)), pack(cap, cap));
+                y[i] = mul2(y[i], t);
               }
+            } else {
+              cap_chunk<kFp8>(s_at + c, cap, a.factor, &sh.k_scale[all_done % 4][c]);
+              tensor_load(w, s_at + c);
+              tensor_loaded(w);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) y[i] = pack(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
             }
           }
           if (!kPlain && biased) {
