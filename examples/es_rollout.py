@@ -133,6 +133,8 @@ def generations(count=3, members=24, sequences=32, prompt=24, new_tokens=12, sig
             written = roll.run(params, prompts, new_tokens)
             rewards.append((written % 2 == 0).float().mean().item())
             es.es_restore(plan, s, sigma)
+        if ro.es_attention_gave_up(roll.workspace):
+            raise RuntimeError("es_attention gave up a wait: this generation's rewards are not to be used")
         rhat = es.es_normalize_rewards(rewards)
         es.es_update(plan, seeds, es.es_update_coeffs(rhat, alpha, sigma))
         history.append(sum(rewards) / members)

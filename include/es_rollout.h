@@ -199,9 +199,11 @@ es_status_t es_cache_read(es_cache_t cache, const es_batch_t* batch, void* k_out
  *   workspace  es_attention_workspace() bytes of device memory, zero before its
  *              first use; every call leaves it ready for the next. One workspace
  *              serves calls of any batch one after another, and must not be used
- *              on two streams at once. Its 32-bit word at byte 4096 stays 0: a kernel
- *              sets it where a wait of its own ran out (an error of the library),
- *              and that call's outputs are then not to be used.
+ *              on two streams at once. Its 32-bit word at byte
+ *              ES_ATTENTION_GAVE_UP stays 0: a kernel sets it where a wait of
+ *              its own ran out (an error of the library). The outputs of
+ *              that call, and of later ones with the workspace, are not to
+ *              be used then until it has been zeroed again.
  * Scores, exponentials and sums are fp32; keys and values enter the products
  * exactly, and exp(x_j) (times an FP8 value's scale) rounded to bf16, or over FP8
  * caches with max_new * q_heads / kv_heads up to 16 to f16, where those below 2^-28
@@ -224,6 +226,8 @@ typedef struct {
   float scale;
   float softcap;
 } es_attention_t;
+
+#define ES_ATTENTION_GAVE_UP 4096
 
 es_status_t es_attention(es_cache_t cache, const es_batch_t* batch, const es_attention_t* args,
                          void* workspace, uint64_t workspace_bytes, void* stream);

@@ -107,6 +107,7 @@ __device__ __forceinline__ uint32_t count_done(uint32_t* counter) {
 // kernels keep of a call.
 constexpr int kCounters = 1024;
 constexpr uint64_t kWorkspaceHead = kCounters * sizeof(uint32_t) + 256;
+static_assert(kCounters * sizeof(uint32_t) == ES_ATTENTION_GAVE_UP, "the flag is behind the counters");
 
 // es_attention of at most 16 rows per (sequence, key head), and of any number.
 cudaError_t launch_few_rows(const CacheView& cache, bool fp8, int head_dim, const BatchView& batch,

@@ -234,9 +234,17 @@ plan_kernel(const BatchView batch, const AttentionArgs a, int kv_heads, int grid
 
 // --- barriers, copies and products --------------------------------------------------
 
-// No wait is longer than a few tiles' work; one that outlasts this has met an error of the
-// kernel's own, which ends the launch with its flag set in place of hanging the GPU.
-constexpr int kMostTries = 1 << 20;
+// A wait that outlasts this many tries (1.48 us each where nothing comes, 6 s) has met an error of the
+// kernel's own, which ends the launch with its flag set in place of hanging the GPU. Waits are a tile's
+// work mostly, but a warpgroup without rows in a unit waits through all its tiles, and the others wait where
+// rows look through a unit's values for infinities and NaN (0.3 s for 131,072 keys that are all to be looked at).
+constexpr int kMostTries = 1 << 22;
+
+// What a wait looks at besides its barrier.
+struct Watch {
+  volatile int* failed;  // a wait of the block was given up
+  int tries;
+};
 
 __device__ __forceinline__ void barrier_init(uint64_t* b, int count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(shared_address(b)), "r"(count) : "memory");
@@ -256,18 +264,18 @@ __device__ __forceinline__ bool barrier_try(uint64_t* b, uint32_t parity) {
   return done != 0;
 }
 // false: the wait was given up, here or by another thread of the block
-__device__ __forceinline__ bool barrier_wait(uint64_t* b, uint32_t parity, volatile int* failed) {
-  for (int i = 0; i < kMostTries; ++i) {
+__device__ __forceinline__ bool barrier_wait(uint64_t* b, uint32_t parity, const Watch& watch) {
+  for (int i = 0; i < watch.tries; ++i) {
     if (barrier_try(b, parity)) return true;
-    if (*failed) return false;
+    if (*watch.failed) return false;
   }
-  *failed = 1;
+  *watch.failed = 1;
   return false;
 }
 
 // By all lanes: through one of them and a shuffle measured 25 % slower over a whole prompt.
-__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, volatile int* failed) {
-  return __all_sync(0xFFFFFFFFu, barrier_wait(b, parity, failed));
+__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, const Watch& watch) {
+  return __all_sync(0xFFFFFFFFu, barrier_wait(b, parity, watch));
 }
 // One lane arrives, with what all lanes did before.
 __device__ __forceinline__ void warp_arrive(uint64_t* b, int lane) {
@@ -429,9 +437,9 @@ struct Part {
 
 // The four warps of a warpgroup; false as barrier_wait.
 template <class Sh>
-__device__ __forceinline__ bool group_sync(Sh& sh, int x, uint32_t& phase, int lane) {
+__device__ __forceinline__ bool group_sync(Sh& sh, const Watch& watch, int x, uint32_t& phase, int lane) {
   warp_arrive(&sh.group[x], lane);
-  return warp_wait(&sh.group[x], phase++ & 1, &sh.failed);
+  return warp_wait(&sh.group[x], phase++ & 1, watch);
 }
 
 // The units of a block's range, by one warp.
@@ -499,9 +507,9 @@ struct Walk {
 // The walking warp's side: the next unit into its place; false where there is none (which is
 // told as well) or a wait was given up.
 template <class Sh>
-__device__ __forceinline__ bool tell(Sh& sh, Walk& walk, const BatchView& b, const AttentionArgs& a, int kv_heads, uint32_t n, int lane) {
+__device__ __forceinline__ bool tell(Sh& sh, const Watch& watch, Walk& walk, const BatchView& b, const AttentionArgs& a, int kv_heads, uint32_t n, int lane) {
   const bool more = walk.next(b, a, kv_heads, lane);
-  if (!warp_wait(&sh.unit_empty[n % kUnits], (n / kUnits & 1) ^ 1, &sh.failed)) return false;
+  if (!warp_wait(&sh.unit_empty[n % kUnits], (n / kUnits & 1) ^ 1, watch)) return false;
   if (lane == 0) {
     Unit& u = sh.unit[n % kUnits];
     u.valid = more;
@@ -534,8 +542,8 @@ __device__ __forceinline__ bool tell(Sh& sh, Walk& walk, const BatchView& b, con
 }
 // The other warps': waits for unit n; false where there is none.
 template <class Sh>
-__device__ __forceinline__ bool take(Sh& sh, uint32_t n) {
-  return warp_wait(&sh.unit_full[n % kUnits], n / kUnits & 1, &sh.failed) && sh.unit[n % kUnits].valid;
+__device__ __forceinline__ bool take(Sh& sh, const Watch& watch, uint32_t n) {
+  return warp_wait(&sh.unit_full[n % kUnits], n / kUnits & 1, watch) && sh.unit[n % kUnits].valid;
 }
 // This warp is done with it.
 template <class Sh>
@@ -563,13 +571,13 @@ __device__ __forceinline__ int place_of(int r, int piece) {
 
 // bf16 pages to shared memory, a lane for each page of the tile.
 template <int D>
-__device__ void copy_tiles(Shared<D, false>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
+__device__ void copy_tiles(Shared<D, false>& sh, const Watch& watch, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
                            const Plan* plan, const CUtensorMap* k_map, const CUtensorMap* v_map, int lane) {
   const int page_size = 1 << cache.page_shift, pages = kKeys >> cache.page_shift;
   uint32_t k_done = 0, v_done = 0;
   bool fine = true;
   Walk walk(batch, a, plan, lane);
-  for (uint32_t n = 0; fine && tell(sh, walk, batch, a, cache.kv_heads, n, lane); ++n) {
+  for (uint32_t n = 0; fine && tell(sh, watch, walk, batch, a, cache.kv_heads, n, lane); ++n) {
     const int key0 = walk.pair.lo & ~(kKeys - 1);
     for (int tile = walk.tile0; tile < walk.tile1; ++tile) {
       const int stage = k_done % kStages;
@@ -582,7 +590,7 @@ __device__ void copy_tiles(Shared<D, false>& sh, const CacheView& cache, const B
       for (int i = 0; i < 8; ++i) absent |= (missing >> (i * 16 >> cache.page_shift) & 1) << i;
       // a page past the last one reads as zeros
       const int z = page < 0 ? cache.num_pages : page, y = walk.head << cache.page_shift;
-      fine = warp_wait(&sh.k_empty[stage], parity ^ 1, &sh.failed);
+      fine = warp_wait(&sh.k_empty[stage], parity ^ 1, watch);
       if (!fine) break;
       if (lane == 0) {
         sh.absent[k_done % 4] = absent;
@@ -593,7 +601,7 @@ __device__ void copy_tiles(Shared<D, false>& sh, const CacheView& cache, const B
         for (int h = 0; h < D / 64; ++h)
           load_box(k_map, shared_address(sh.k[stage] + h * 128 * 64 + lane * page_size * 64), &sh.k_full[stage], h * 64, y, z);
       ++k_done;
-      fine = warp_wait(&sh.v_empty[stage], parity ^ 1, &sh.failed);
+      fine = warp_wait(&sh.v_empty[stage], parity ^ 1, watch);
       if (!fine) break;
       if (lane == 0) barrier_expect(&sh.v_full[stage], kKeys * D * 2);
       __syncwarp();
@@ -613,14 +621,14 @@ __device__ void copy_tiles(Shared<D, false>& sh, const CacheView& cache, const B
 // their keys are noted: the rows that see them get them when the unit is written. Every tile passes here,
 // so that the barriers of the stages are never a round ahead.
 template <int D>
-__device__ void fix_tiles(Shared<D, false>& sh, int thread, int lane) {
+__device__ void fix_tiles(Shared<D, false>& sh, const Watch& watch, int thread, int lane) {
   uint32_t done = 0;
-  for (uint32_t n = 0; take(sh, n); ++n) {
+  for (uint32_t n = 0; take(sh, watch, n); ++n) {
     const Unit& unit = sh.unit[n % kUnits];
     const int tile1 = unit.tile1;
     for (int tile = unit.tile0; tile < tile1; ++tile, ++done) {
       const int stage = done % kStages, j0 = unit.key_of(tile);
-      if (!warp_wait(&sh.v_full[stage], done / kStages & 1, &sh.failed)) return;
+      if (!warp_wait(&sh.v_full[stage], done / kStages & 1, watch)) return;
       if (unit.edge(tile)) {
         const int lo = unit.lo, hi = unit.hi;
 #pragma unroll 1
@@ -667,13 +675,13 @@ __device__ void fix_tiles(Shared<D, false>& sh, int thread, int lane) {
 // FP8 pages to shared memory as they are: a tile's pieces of keys, then of values, each to the
 // next converting warp.
 template <int D>
-__device__ void copy_codes(Shared<D, true>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
+__device__ void copy_codes(Shared<D, true>& sh, const Watch& watch, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
                            const Plan* plan, const CUtensorMap* k_map, const CUtensorMap* v_map, int lane) {
   const int box = min(1 << cache.page_shift, kPiece), boxes = kPiece / box;  // keys of a copy, copies of a piece
   uint32_t done = 0, tiles = 0;
   bool fine = true;
   Walk walk(batch, a, plan, lane);
-  for (uint32_t n = 0; fine && tell(sh, walk, batch, a, cache.kv_heads, n, lane); ++n) {
+  for (uint32_t n = 0; fine && tell(sh, watch, walk, batch, a, cache.kv_heads, n, lane); ++n) {
     const int key0 = walk.pair.lo & ~(kKeys - 1);
     for (int tile = walk.tile0; fine && tile < walk.tile1; ++tile, ++tiles) {
       // lane i's keys are 16 i and up
@@ -684,7 +692,7 @@ __device__ void copy_codes(Shared<D, true>& sh, const CacheView& cache, const Ba
       for (int part = 0; part < kPieces; ++part, ++done) {
         const int slot = done % kRaw, in_tile = part % (kPieces / 2) * kPiece;
         const int mine = __shfl_sync(0xFFFFFFFFu, page, (in_tile + lane * box) / 16 % 8);
-        fine = warp_wait(&sh.raw_empty[slot], (done / kRaw & 1) ^ 1, &sh.failed);
+        fine = warp_wait(&sh.raw_empty[slot], (done / kRaw & 1) ^ 1, watch);
         if (!fine) break;
         if (lane == 0) {
           if (part == 0) sh.absent[tiles % 4] = absent;
@@ -746,11 +754,11 @@ __device__ __forceinline__ uint32_t convert_piece(const uint8_t* raw, uint16_t* 
 }
 
 template <int D>
-__device__ void convert_tiles(Shared<D, true>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a, int warp,
+__device__ void convert_tiles(Shared<D, true>& sh, const Watch& watch, const CacheView& cache, const BatchView& batch, const AttentionArgs& a, int warp,
                               int lane) {
   uint32_t done = 0;  // tiles
   uint32_t turns = 0;  // this warp's pieces
-  for (uint32_t n = 0; take(sh, n); ++n) {
+  for (uint32_t n = 0; take(sh, watch, n); ++n) {
     const Unit& unit = sh.unit[n % kUnits];
     const int tile1 = unit.tile1;
     for (int tile = unit.tile0; tile < tile1; ++tile, ++done) {
@@ -777,10 +785,10 @@ __device__ void convert_tiles(Shared<D, true>& sh, const CacheView& cache, const
             bad = 1u << lane;
           }
         }
-        if (!warp_wait(of_keys ? &sh.k_empty[stage] : &sh.v_empty[stage], parity ^ 1, &sh.failed)) return;
+        if (!warp_wait(of_keys ? &sh.k_empty[stage] : &sh.v_empty[stage], parity ^ 1, watch)) return;
         if (of_keys) sh.k_scale[done % 4][key0 + lane] = scale * a.factor;
         else sh.v_scale[stage][key0 + lane] = scale;
-        if (!warp_wait(&sh.raw_full[warp], turns & 1, &sh.failed)) return;
+        if (!warp_wait(&sh.raw_full[warp], turns & 1, watch)) return;
         bad |= convert_piece<D>(sh.raw[warp], of_keys ? sh.k[stage] : sh.v[stage], key0, lane, clean, unit.lo - j0, unit.hi - j0);
         if (clean) note_bad(sh, n, j0 + key0, bad, lane);
         // The next codes may come now that these have been used. (After their loads alone have
@@ -805,7 +813,7 @@ __device__ __forceinline__ bool elected() {
 
 // The warp that issues the products.
 template <int D, bool kFp8>
-__device__ void issue_products(Shared<D, kFp8>& sh, int lane) {
+__device__ void issue_products(Shared<D, kFp8>& sh, const Watch& watch, int lane) {
   constexpr uint32_t kScores = product_of(kKeys, false), kValues = product_of(D, true);
   const uint32_t tensor = sh.tensor;
   uint32_t k_done = 0, v_done = 0, units = 0, two_units = 0;
@@ -828,8 +836,8 @@ __device__ void issue_products(Shared<D, kFp8>& sh, int lane) {
     }
     __syncwarp();
   };
-  auto wait = [&](uint64_t* b, uint32_t parity) { return warp_wait(b, parity, &sh.failed); };
-  for (uint32_t n = 0; take(sh, n); ++n) {
+  auto wait = [&](uint64_t* b, uint32_t parity) { return warp_wait(b, parity, watch); };
+  for (uint32_t n = 0; take(sh, watch, n); ++n) {
     const uint32_t count = sh.unit[n % kUnits].rows > 128 ? 2 : 1;
     const int tiles = sh.unit[n % kUnits].tile1 - sh.unit[n % kUnits].tile0;
     leave(sh, n, lane);
@@ -1020,7 +1028,7 @@ __device__ __noinline__ void cap_chunk(uint32_t at, float cap, float factor, con
 
 // A warpgroup's rows: a thread for each.
 template <int D, bool kFp8, bool kPlain>
-__device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
+__device__ void soften(Shared<D, kFp8>& sh, const Watch& watch, const CacheView& cache, const BatchView& batch, const AttentionArgs& a,
                        uint32_t* counters, Part<D>* parts, int x, int thread, int lane) {
   const uint32_t lanes = static_cast<uint32_t>(thread / 32 * 32) << 16;
   const uint32_t s_at = sh.tensor + lanes + x * 128, o_at = sh.tensor + lanes + 256 + x * 128;
@@ -1038,7 +1046,7 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
   auto find = [&](uint32_t& skipped) {
     skipped = 0;
     for (;; ++n) {
-      if (!take(sh, n)) return false;
+      if (!take(sh, watch, n)) return false;
       const Unit& u = sh.unit[n % kUnits];
       if (u.rows > x * 128) return true;
       skipped += u.tile1 - u.tile0;
@@ -1067,9 +1075,9 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
       const uint32_t all_done = tiles_before + (tile - tile0);
       const int stage = all_done % kStages;
       const int j0 = key0 + tile * kKeys;
-      if (!warp_wait(&sh.s_full[x], s_done & 1, &sh.failed)) return;
+      if (!warp_wait(&sh.s_full[x], s_done & 1, watch)) return;
       fence_after();
-      if (kFp8 && !warp_wait(&sh.v_full[stage], all_done / kStages & 1, &sh.failed)) return;
+      if (kFp8 && !warp_wait(&sh.v_full[stage], all_done / kStages & 1, watch)) return;
       const uint32_t absent = sh.absent[all_done % 4];
       const bool whole = __all_sync(0xFFFFFFFFu, row.token < 0 || (row.lo <= j0 && row.hi >= j0 + kKeys)) && absent == 0;
       const bool direct = kPlain && whole;
@@ -1187,7 +1195,7 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
       const bool moves = best > top;
       if (__any_sync(0xFFFFFFFFu, moves && top > -INFINITY)) {
         // the product before has to be done with O
-        if (!warp_wait(&sh.o_done[x], (s_done - 1) & 1, &sh.failed)) return;
+        if (!warp_wait(&sh.o_done[x], (s_done - 1) & 1, watch)) return;
         fence_after();
         const float keep = moves ? exp2_approx(top - best) : 1.0f;
 #pragma unroll 1
@@ -1245,7 +1253,7 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
         // come while this one is finished, if it has rows for this warpgroup. (To look further
         // with this unit held would stop the walk.)
         ++n;
-        ended = !take(sh, n);
+        ended = !take(sh, watch, n);
         fetched = !ended && sh.unit[n % kUnits].rows > x * 128;
         if (fetched) row_next = take_row<D, kFp8>(sh, batch, a, sh.unit[n % kUnits], x, thread, h_next);
       }
@@ -1254,7 +1262,7 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
     tiles_before += tile1 - tile0;
 
     // --- the unit's rows are done, here at least
-    if (!warp_wait(&sh.o_done[x], (s_done - 1) & 1, &sh.failed)) return;
+    if (!warp_wait(&sh.o_done[x], (s_done - 1) & 1, watch)) return;
     fence_after();
     const int c_first = unit.c_first, c_last = unit.c_last;
     const int self = static_cast<int>(blockIdx.x);
@@ -1293,12 +1301,12 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
         part.top[r_part] = top;
         part.sum[r_part] = sum;
       }
-      if (!group_sync(sh, x, phase, lane)) return;
+      if (!group_sync(sh, watch, x, phase, lane)) return;
       if (thread == 0) {
         sh.last[x] = count_done(&counters[2 * c_first + x]) == static_cast<uint32_t>(c_last - c_first);
         if (sh.last[x]) counters[2 * c_first + x] = 0;
       }
-      if (!group_sync(sh, x, phase, lane)) return;
+      if (!group_sync(sh, watch, x, phase, lane)) return;
       if (sh.last[x]) {
         const int n = c_last - c_first + 1;
         auto part_of = [&](int i) -> const Part<D>& { return parts[2 * (c_first + i) + (i == 0)]; };
@@ -1342,7 +1350,7 @@ __device__ void soften(Shared<D, kFp8>& sh, const CacheView& cache, const BatchV
         }
         __syncwarp();
       }
-      if (!group_sync(sh, x, phase, lane)) return;  // sh.last has been read
+      if (!group_sync(sh, watch, x, phase, lane)) return;  // sh.last has been read
     } else if (row.token >= 0 && a.lse != nullptr) {
       a.lse[static_cast<uint64_t>(row.token) * a.q_heads + h] = some ? top * kLn2 + logf(sum) : -INFINITY;
     }
@@ -1368,9 +1376,10 @@ constexpr int threads_of() { return kFp8 ? 512 : 384; }
 template <int D, bool kFp8, bool kPlain>
 __global__ void __launch_bounds__(threads_of<kFp8>(), 1)
 many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionArgs a, const Plan* plan, uint32_t* counters,
-                 int* flag, Part<D>* parts, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+                 int* flag, Part<D>* parts, int tries, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   extern __shared__ uint8_t raw[];
   Shared<D, kFp8>& sh = *reinterpret_cast<Shared<D, kFp8>*>(raw + ((1024 - (shared_address(raw) & 1023)) & 1023));
+  const Watch watch{&sh.failed, tries};
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
@@ -1422,20 +1431,20 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
   }
   if (warp < 8) {
-    soften<D, kFp8, kPlain>(sh, cache, batch, a, counters, parts, warp / 4, threadIdx.x % 128, lane);
+    soften<D, kFp8, kPlain>(sh, watch, cache, batch, a, counters, parts, warp / 4, threadIdx.x % 128, lane);
   } else if (warp == kIssuer) {
-    issue_products<D, kFp8>(sh, lane);
+    issue_products<D, kFp8>(sh, watch, lane);
     __syncwarp();
     if (elected()) commit(&sh.drained);  // by the lane that issued the products: none outlives the tensor memory
     __syncwarp();
     barrier_settle(&sh.drained, 0);
   } else {
     if constexpr (kFp8) {
-      if (warp < 8 + kRaw) convert_tiles<D>(sh, cache, batch, a, warp - 8, lane);
-      else copy_codes<D>(sh, cache, batch, a, plan, &k_map, &v_map, lane);
+      if (warp < 8 + kRaw) convert_tiles<D>(sh, watch, cache, batch, a, warp - 8, lane);
+      else copy_codes<D>(sh, watch, cache, batch, a, plan, &k_map, &v_map, lane);
     } else {
-      if (warp == 9) copy_tiles<D>(sh, cache, batch, a, plan, &k_map, &v_map, lane);
-      else fix_tiles<D>(sh, threadIdx.x - 10 * 32, lane);
+      if (warp == 9) copy_tiles<D>(sh, watch, cache, batch, a, plan, &k_map, &v_map, lane);
+      else fix_tiles<D>(sh, watch, threadIdx.x - 10 * 32, lane);
     }
   }
   __syncwarp();
@@ -1448,6 +1457,8 @@ many_rows_kernel(const CacheView cache, const BatchView batch, const AttentionAr
   if (warp == kIssuer)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tensor) : "memory");
 }
+
+std::atomic<int> tries_of_a_wait{kMostTries};
 
 constexpr uint64_t kPlanBytes = (sizeof(Plan) + 255) / 256 * 256;
 
@@ -1476,7 +1487,7 @@ cudaError_t launch_kernel(const CacheView& cache, const CUtensorMap* maps, const
                                        unit_cost<kFp8, kPlain>(), plan);
   if (err != cudaSuccess) return err;
   return launch_early(kernel, grid, threads_of<kFp8>(), kShared, stream, cache, batch, args, static_cast<const Plan*>(plan), counters,
-                      flag, reinterpret_cast<Part<D>*>(workspace + kPlanBytes), maps[0], maps[1]);
+                      flag, reinterpret_cast<Part<D>*>(workspace + kPlanBytes), tries_of_a_wait.load(std::memory_order_relaxed), maps[0], maps[1]);
 }
 
 template <int D, bool kFp8>
@@ -1488,6 +1499,8 @@ cudaError_t launch(const CacheView& cache, const CUtensorMap* maps, const BatchV
 }
 
 }  // namespace
+
+void set_wait_tries(int tries) { tries_of_a_wait.store(tries < 0 ? kMostTries : tries, std::memory_order_relaxed); }
 
 uint64_t many_rows_workspace_bytes(int head_dim) {
   return kPlanBytes + 2 * kMaxGrid * (head_dim == 128 ? sizeof(Part<128>) : sizeof(Part<64>));

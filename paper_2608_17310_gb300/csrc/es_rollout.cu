@@ -316,4 +316,7 @@ uint64_t es_attention_workspace(es_cache_t cache, int q_heads) {
   return esopt::attention_workspace_bytes(cache->head_dim);
 }
 
+// Not in the header: for tests of given-up waits.
+void es_attention_wait_tries(int tries) { esopt::set_wait_tries(tries); }
+
 }  // extern "C"

@@ -123,5 +123,8 @@ cudaError_t launch_read(const CacheView& cache, bool fp8, int head_dim, const Ba
 cudaError_t launch_attention(const CacheView& cache, const CUtensorMap* maps, bool fp8, int head_dim, const BatchView& batch,
                              const AttentionArgs& args, void* workspace, cudaStream_t stream);
 uint64_t attention_workspace_bytes(int head_dim);
+// For tests: tries after which the waits of the kernel of many rows are given up in calls from now on
+// (0: at once; negative: as it was).
+void set_wait_tries(int tries);
 
 }  // namespace esopt

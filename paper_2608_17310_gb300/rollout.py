@@ -21,6 +21,7 @@ from . import esopt
 from .esopt import ES_BF16, ES_FP8_E4M3, EsError, _check  # noqa: F401
 
 ES_MAX_SEQUENCES = 4096
+ES_ATTENTION_GAVE_UP = 4096
 
 _VP, _U64, _INT, _FLOAT = ctypes.c_void_p, ctypes.c_uint64, ctypes.c_int, ctypes.c_float
 
@@ -262,6 +263,13 @@ def es_cache_read(cache: Cache, batch: Batch, k_out=None, v_out=None, stream=Non
 def es_attention_workspace(cache: Cache, q_heads: int) -> int:
     """Bytes of (zeroed) workspace for es_attention with this cache, whatever the batch."""
     return int(_lib().es_attention_workspace(cache.handle, q_heads))
+
+
+def es_attention_gave_up(workspace) -> bool:
+    """Whether a kernel that used this workspace gave up a wait (an error of the library): its
+    outputs since are not to be used, nor the workspace before it has been zeroed. Waits for the
+    current stream; a program asks where it reads results anyway."""
+    return bool(workspace[ES_ATTENTION_GAVE_UP:ES_ATTENTION_GAVE_UP + 4].any())
 
 
 def es_attention(cache: Cache, batch: Batch, q, out, workspace, scale: float, lse=None,
