@@ -5,7 +5,8 @@ key/value cache that is appended to, read back and attended over, between
 Argument marshalling only, as in ``esopt``: every function forwards to the function
 of the same name in ``libesopt.so``. Arguments are torch CUDA tensors (or their
 device pointers, where a shape is not needed); errors are ``esopt.EsError``, or
-``ValueError`` for tensors of the wrong type, shape or layout.
+``ValueError`` for tensors of the wrong type, shape or layout and numbers that C's types do
+not hold.
 
     cache = ro.es_cache_create(k_pages, v_pages)            # [pages, kv_heads, page_size, head_dim]
     batch = ro.Batch(page_table, seq_len, start, tokens, max_new)
@@ -15,7 +16,7 @@ device pointers, where a shape is not needed); errors are ``esopt.EsError``, or
 from __future__ import annotations
 
 import ctypes
-from struct import Struct
+from struct import Struct, error as _StructError
 
 from . import esopt
 from .esopt import ES_BF16, ES_FP8_E4M3, EsError, _check  # noqa: F401
@@ -216,12 +217,14 @@ class Batch:
             if start is not None:
                 raise ValueError("tokens and max_new go with start")
             tokens, max_new = n, 1
-        self.tokens = int(tokens)
+        self.tokens, max_new = int(tokens), int(max_new)
+        if not (-2 ** 31 <= self.tokens < 2 ** 31 and -2 ** 31 <= max_new < 2 ** 31):  # ctypes would cut them
+            raise ValueError(f"tokens {self.tokens} and max_new {max_new} must be 32-bit numbers")
         self._keepalive = (pages, seq_len, start)
         self.args = es_batch_t(_tensor(pages, _I32, "pages"),
                                _tensor(seq_len, _I32, "seq_len", n),
                                _tensor(start, _I32, "start", n + 1),
-                               pages.shape[1], n, self.tokens, int(max_new))
+                               pages.shape[1], n, self.tokens, max_new)
         self.ref = ctypes.byref(self.args)
 
 
@@ -239,10 +242,14 @@ def es_cache_append(cache: Cache, batch: Batch, qkv, q_out, q_weight=None, k_wei
         if len(shape) != 3 or shape[2] != 2:
             raise ValueError("rope must be [rows, rotary_dim / 2, 2]")
         rope_ptr, rope_rows, rotary_dim = _tensor(rope, _F32, "rope"), shape[0], 2 * shape[1]
-    status = _calls.es_cache_append(cache.handle, batch.ref, _APPEND.pack(
-        x_ptr, q_ptr, _tensor(q_weight, _BF16, "q_weight", d), _tensor(k_weight, _BF16, "k_weight", d),
-        rope_ptr, _tensor(positions, _I32, "positions", n), x_stride, q_stride, rope_rows, q_heads,
-        rotary_dim, interleaved, eps), _stream(stream))
+    try:
+        args = _APPEND.pack(
+            x_ptr, q_ptr, _tensor(q_weight, _BF16, "q_weight", d), _tensor(k_weight, _BF16, "k_weight", d),
+            rope_ptr, _tensor(positions, _I32, "positions", n), x_stride, q_stride, rope_rows, q_heads,
+            rotary_dim, interleaved, eps)
+    except (_StructError, OverflowError) as e:
+        raise ValueError(f"es_cache_append: {e}") from None
+    status = _calls.es_cache_append(cache.handle, batch.ref, args, _stream(stream))
     if status:
         _check(status, "es_cache_append")
 
@@ -282,10 +289,14 @@ def es_attention(cache: Cache, batch: Batch, q, out, workspace, scale: float, ls
     d, n = cache.head_dim, batch.tokens
     q_ptr, q_stride, heads = _rows(q, n, None, d, "q")
     o_ptr, o_stride, _ = _rows(out, n, heads, d, "out")
-    status = _calls.es_attention(cache.handle, batch.ref, _ATTENTION.pack(
-        q_ptr, o_ptr, _tensor(lse, _F32, "lse", n * heads), _tensor(slopes, _F32, "slopes", heads),
-        _tensor(first, _I32, "first", n), _tensor(last, _I32, "last", n), q_stride, o_stride, heads,
-        window, scale, softcap), _tensor(workspace, _U8, "workspace"), workspace.numel(),
-        _stream(stream))
+    try:
+        args = _ATTENTION.pack(
+            q_ptr, o_ptr, _tensor(lse, _F32, "lse", n * heads), _tensor(slopes, _F32, "slopes", heads),
+            _tensor(first, _I32, "first", n), _tensor(last, _I32, "last", n), q_stride, o_stride, heads,
+            window, scale, softcap)
+    except (_StructError, OverflowError) as e:
+        raise ValueError(f"es_attention: {e}") from None
+    status = _calls.es_attention(cache.handle, batch.ref, args, _tensor(workspace, _U8, "workspace"),
+                                 workspace.numel(), _stream(stream))
     if status:
         _check(status, "es_attention")
