@@ -11,8 +11,8 @@
 //                 too, so a lane loads 16 bytes of four keys and packs pairs of keys
 //                 with byte permutes.
 // P^T comes out of S^T by transposing 8 x 8 blocks within the warp. FP8 codes become f16,
-// which holds them exactly, and the products run in f16 with q and p scaled by powers of
-// two into its range.
+// which holds them exactly, and the products run in f16 with q and p v_scale scaled by powers of
+// two into its range: q by its row's largest element, p v_scale by the row's largest so far.
 //
 // The tiles of all (sequence, key head) units lie end to end and are cut into one range per
 // block, all of one length, whatever the sequences' lengths. A unit that several blocks
@@ -20,8 +20,8 @@
 // so results do not depend on who is last.
 //
 // Measured (GB300; 4 or 5 rows of 8 key heads of 128): 96 bf16 caches of 200 to 9,000 tokens
-// 278 us, 6.6 TB/s, 99 % of the card's copy rate; three FP8 caches of 90,000 to 131,071 tokens
-// 129 us, 5.6 TB/s, 84 %, where converting and packing codes keeps the integer pipe 45 % busy and
+// 280 us, 6.6 TB/s, 98 % of the card's copy rate; three FP8 caches of 90,000 to 131,071 tokens
+// 127 us, 5.7 TB/s, 85 %, where converting and packing codes keeps the integer pipe 47 % busy and
 // the loads in flight are what registers hold (16 warps of 4 KB an SM); one cache of 777
 // tokens 8.1 us, 15,500 cycles of latency (lengths, pages, keys, a part's way through
 // memory, the join) in code that each launch reads anew.

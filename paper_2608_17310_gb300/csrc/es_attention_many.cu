@@ -22,13 +22,14 @@
 // block idle. A unit that several blocks share is joined by the last of them, from the parts
 // in the order of the blocks.
 //
-// Measured (GB300): a prompt of 8,191 tokens, 32 heads of 128 on 8, 447 us: 1,230 TFLOP/s, 63 % of
-// the card's bf16 matrix rate in a burst, the tensor pipe 55 % busy. The chain of a tile of
+// Measured (GB300): a prompt of 8,191 tokens, 32 heads of 128 on 8, 431 us: 1,275 TFLOP/s, 66 % of
+// the card's bf16 matrix rate in a burst, the tensor pipe 57 % busy. The chain of a tile of
 // rows (product, scores read, maxima, exponentials, P written, product: 2,000 cycles and its
-// 1,024 of products) is longer than the 2,048 cycles of products of both. Over an FP8 cache
-// 706 us, over capped scores 653 us: more instructions on that chain. Twelve sequences with 9 to
-// 130 tokens over FP8 caches, capped, 244 us; packed documents with a bias 86 us, of which a unit
-// of four tiles spends two thirds in its tiles.
+// 1,024 of products) is longer than the 2,048 cycles of products of both. The same inputs pass after pass
+// take 414, over an FP8 cache 671, with capped scores 638: more instructions on that chain. Twelve sequences
+// with 9 to 130 tokens over FP8 caches, capped, 233 us; packed documents with a bias 81 us, of which a unit
+// of four tiles spends two thirds in its tiles. Registers that ptxas spills (up to 80 bytes a thread) are
+// touched outside the tiles' loops: 0.05 % of the prompt's instructions, 0.02 % of the turn's.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -47,12 +48,14 @@ constexpr int kStages = 2;
 constexpr int kMaxGrid = 192;
 // What a unit costs beside its tiles, in tiles: its queries, the first tile's way through the
 // pipeline, its results. Plain bf16 tiles are the quickest, so more of them fit: a prompt of
-// 8,191 tokens takes 593 us with 2, 499 with 3, 450 with 4, 473 with 6; where tiles take
-// longer 2 is best by 2 to 8 % (FP8, capped or biased scores).
+// 8,191 tokens takes 505 us with 2, 430 with 3, 414 with 4, 424 with 6. Where tiles take longer it
+// is 2: over an FP8 cache 772 us with 1, 673 with 2, 680 with 3; with capped scores 745, 638, 643.
 template <bool kFp8, bool kPlain>
 constexpr int unit_cost() { return kPlain && !kFp8 ? 4 : 2; }
 // No block takes less than this of a unit that others share: a part costs its way through
-// memory, about as much as two tiles.
+// memory, about as much as two tiles. So a unit of fewer than six tiles stays whole, and where most are, blocks
+// differ by a unit. With 1, 2, 3, 4: twelve turns over FP8 caches 190, 190, 193, 195 us, packed
+// documents 79, 77, 79, 80, long prompts alike.
 constexpr int kLeastShare = 3;
 constexpr float kSlack = 8.0f;  // log 2 of how far a score may be above the kept maximum
 
