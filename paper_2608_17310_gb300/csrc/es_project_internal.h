@@ -1,0 +1,67 @@
+// Shared by the host layer and the kernels of the products whose rows choose their weights.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "../../include/es_project.h"
+
+namespace esopt {
+
+// The matrices of a product: `groups` of them, element (o, i) of matrix g at
+// data + g * group_stride + o * row_stride + i.
+struct MatrixView {
+  const void* data;
+  const float* scale;  // of each matrix's codes; NULL for bf16
+  uint64_t group_stride, row_stride;
+  int groups, out, in;
+};
+
+struct AdapterView {
+  const uint16_t* a;
+  const uint16_t* b;
+  const float* scale;
+  uint64_t a_stride, b_stride;
+  int count, rank;
+};
+
+// The rows of a product, in segments that go through one matrix each. start comes from device
+// memory and is taken through segment_of, which bounds it.
+struct RowView {
+  const uint16_t* x;
+  uint16_t* y;
+  const int32_t* start;  // NULL: one row a segment
+  const int32_t* group;  // matrix of each segment; NULL: its number
+  const int32_t* index;  // row of x of each row; NULL: its number
+  uint64_t x_stride, y_stride;
+  int segments, rows, x_rows;
+  bool joined;  // all segments are one, through matrix 0
+};
+
+#ifdef __CUDACC__
+// Rows [begin, end) of segment s and its matrix (outside [0, groups): none).
+__device__ __forceinline__ void segment_of(const RowView& r, int s, int& begin, int& end, int& group) {
+  if (r.joined) {
+    begin = group = 0;
+    end = r.start != nullptr ? min(max(r.start[r.segments], 0), r.rows) : r.rows;
+    return;
+  }
+  begin = r.start != nullptr ? min(max(r.start[s], 0), r.rows) : min(s, r.rows);
+  end = r.start != nullptr ? min(max(r.start[s + 1], 0), r.rows) : min(s + 1, r.rows);
+  end = max(begin, end);
+  group = r.group != nullptr ? r.group[s] : s;
+}
+#endif
+
+cudaError_t launch_project(const MatrixView& w, bool fp8, const AdapterView* adapters, const int32_t* adapter, const RowView& rows,
+                           void* workspace, cudaStream_t stream);
+cudaError_t launch_experts(const MatrixView& w, bool fp8, bool gated, const RowView& rows, void* workspace, cudaStream_t stream);
+uint64_t project_workspace_bytes(int rank, int rows);  // rank 0: no adapters
+
+cudaError_t launch_route(const es_route_t& args, void* workspace, cudaStream_t stream);
+uint64_t route_workspace_bytes(int tokens, int experts, int top);
+cudaError_t launch_combine(const es_combine_t& args, cudaStream_t stream);
+
+}  // namespace esopt

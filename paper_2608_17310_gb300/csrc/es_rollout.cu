@@ -3,13 +3,10 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <new>
 
 #include "../../include/es_rollout.h"
-#include "es_internal.h"
-#include "es_memcheck.h"
+#include "es_checks.h"
 #include "es_rollout_internal.h"
 
 struct es_cache {
@@ -23,20 +20,12 @@ struct es_cache {
 
 namespace {
 
-es_status_t fail(es_status_t st, const char* fmt, ...) {
-  char text[400];
-  va_list ap;
-  va_start(ap, fmt);
-  std::vsnprintf(text, sizeof text, fmt, ap);
-  va_end(ap);
-  return esopt::record_status(st, text);
-}
-
-es_status_t ok() { return esopt::record_status(ES_OK, ""); }
-
-es_status_t cuda_fail(cudaError_t err, const char* what) {
-  return fail(ES_ERR_CUDA, "%s: %s (%s)", what, cudaGetErrorName(err), cudaGetErrorString(err));
-}
+using esopt::check_buffer;
+using esopt::check_optional;
+using esopt::check_stride;
+using esopt::cuda_fail;
+using esopt::fail;
+using esopt::ok;
 
 // Positions and the ends of tiles of keys stay within 32 bits.
 constexpr int64_t kLongest = INT32_MAX - 1023;
@@ -44,23 +33,6 @@ constexpr int64_t kLongest = INT32_MAX - 1023;
 // Caps above this one count as it, so that neither cap log2(e) nor scale / cap leaves fp32's normal
 // numbers. Scores beyond a quarter of it are all that could tell.
 constexpr float kLargestCap = 1.2676506002282294e30f;  // 2^100
-
-// A device buffer of the call: present, aligned and device memory.
-es_status_t check_buffer(const void* p, unsigned align, int device, const char* call,
-                         const char* name) {
-  if (p == nullptr) return fail(ES_ERR_INVALID_ARG, "%s: %s is NULL", call, name);
-  if (reinterpret_cast<uintptr_t>(p) % align != 0)
-    return fail(ES_ERR_ALIGNMENT, "%s: %s is not %u-byte aligned", call, name, align);
-  if (!esopt::is_device_memory(p, device))
-    return fail(ES_ERR_INVALID_ARG, "%s: %s is not device memory of the current device %d", call,
-                name, device);
-  return ES_OK;
-}
-
-es_status_t check_optional(const void* p, unsigned align, int device, const char* call,
-                           const char* name) {
-  return p == nullptr ? ES_OK : check_buffer(p, align, device, call, name);
-}
 
 // The checks that every operator makes of its cache and batch; ES_OK fills `view`.
 es_status_t check_batch(es_cache_t cache, const es_batch_t* b, const char* call,
@@ -105,29 +77,13 @@ es_status_t check_heads(es_cache_t cache, int q_heads, const char* call) {
   return ES_OK;
 }
 
-// A row of `heads` heads per token, `stride` elements apart.
-es_status_t check_stride(uint64_t stride, int heads, int head_dim, const char* call,
-                         const char* name) {
-  if (stride < static_cast<uint64_t>(heads) * head_dim || stride > (uint64_t{1} << 40))
-    return fail(ES_ERR_INVALID_ARG, "%s: %s %llu is less than a row or out of range", call, name,
-                static_cast<unsigned long long>(stride));
-  if (stride % 8 != 0)
-    return fail(ES_ERR_ALIGNMENT, "%s: %s %llu is not a multiple of 8", call, name,
-                static_cast<unsigned long long>(stride));
-  return ES_OK;
-}
-
 // Pages as [page][head and slot][element]; pages past the last one read as zeros. bf16 is read
 // in boxes of one page of a head by 64 elements (128 bytes, swizzled), FP8 in boxes of up to
 // 32 whole codes' vectors as they lie.
 es_status_t make_map(CUtensorMap* map, void* base, const es_cache_desc_t& d, const char* call) {
-  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-  void* found = nullptr;
-  cudaDriverEntryPointQueryResult result;
-  const cudaError_t err = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &found, 12000, cudaEnableDefault, &result);
-  if (err != cudaSuccess || found == nullptr) return cuda_fail(err != cudaSuccess ? err : cudaErrorNotSupported, "cuTensorMapEncodeTiled");
+  esopt::EncodeTiled encode = nullptr;
+  const es_status_t st = esopt::encode_tiled(&encode);
+  if (st != ES_OK) return st;
   const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d.head_dim), static_cast<cuuint64_t>(d.kv_heads) * d.page_size, d.num_pages};
   const bool fp8 = d.dtype == ES_FP8_E4M3;
   const cuuint64_t size = fp8 ? 1 : 2;
@@ -135,7 +91,7 @@ es_status_t make_map(CUtensorMap* map, void* base, const es_cache_desc_t& d, con
   const cuuint32_t box[3] = {fp8 ? static_cast<cuuint32_t>(d.head_dim) : 64u,
                              static_cast<cuuint32_t>(fp8 && d.page_size > 32 ? 32 : d.page_size), 1};
   const cuuint32_t steps[3] = {1, 1, 1};
-  const CUresult made = reinterpret_cast<Encode>(found)(
+  const CUresult made = encode(
       map, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
       fp8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (made != CUDA_SUCCESS) return fail(ES_ERR_CUDA, "%s: cuTensorMapEncodeTiled returned %d", call, static_cast<int>(made));
@@ -228,10 +184,9 @@ es_status_t es_cache_append(es_cache_t cache, const es_batch_t* batch, const es_
     return fail(ES_ERR_INVALID_ARG, "%s: rope and rotary_dim go together", call);
   if (a->interleaved != 0 && a->interleaved != 1)
     return fail(ES_ERR_INVALID_ARG, "%s: interleaved is %d", call, a->interleaved);
-  if ((st = check_stride(a->qkv_stride, a->q_heads + 2 * cache->view.kv_heads, d, call,
-                         "qkv_stride")) != ES_OK)
+  if ((st = check_stride(a->qkv_stride, int64_t{d} * (a->q_heads + 2 * cache->view.kv_heads), call, "qkv_stride")) != ES_OK)
     return st;
-  if ((st = check_stride(a->q_out_stride, a->q_heads, d, call, "q_out_stride")) != ES_OK) return st;
+  if ((st = check_stride(a->q_out_stride, int64_t{d} * a->q_heads, call, "q_out_stride")) != ES_OK) return st;
   if (b.tokens == 0) return ok();
   const int dev = cache->device;
   if ((st = check_buffer(a->qkv, 16, dev, call, "qkv")) != ES_OK) return st;
@@ -281,8 +236,8 @@ es_status_t es_attention(es_cache_t cache, const es_batch_t* batch, const es_att
   if (a->softcap < 0.0f || (a->softcap > 0.0f && a->softcap < 1e-6f) || a->window < 0)
     return fail(ES_ERR_INVALID_ARG, "%s: softcap or window is negative, or softcap below 1e-6", call);
   const int d = cache->head_dim;
-  if ((st = check_stride(a->q_stride, a->q_heads, d, call, "q_stride")) != ES_OK) return st;
-  if ((st = check_stride(a->out_stride, a->q_heads, d, call, "out_stride")) != ES_OK) return st;
+  if ((st = check_stride(a->q_stride, int64_t{d} * a->q_heads, call, "q_stride")) != ES_OK) return st;
+  if ((st = check_stride(a->out_stride, int64_t{d} * a->q_heads, call, "out_stride")) != ES_OK) return st;
   const uint64_t need = es_attention_workspace(cache, a->q_heads);
   if (workspace_bytes < need)
     return fail(ES_ERR_INVALID_ARG, "%s: the workspace has %llu bytes and needs %llu", call,

@@ -1,0 +1,339 @@
+// es_route and es_combine: tokens to experts and back.
+#include <cfloat>
+
+#include "es_attention.cuh"
+#include "es_project_internal.h"
+
+namespace esopt {
+namespace {
+
+constexpr int kRouteThreads = 512;
+constexpr int kRouteWarps = kRouteThreads / 32;
+constexpr int kRouteGrid = 152;
+
+struct RouteArgs {
+  const void* scores;
+  int32_t* chosen;
+  float* weights;
+  int32_t* start;
+  int32_t* rows;
+  int32_t* places;
+  uint64_t stride;
+  int tokens, experts, top, normalise;
+  int share;  // tokens of a warp
+};
+
+// Order-preserving code of a score; 0 for one that is never chosen.
+__device__ __forceinline__ uint32_t code_of(float x) {
+  if (!(x > -INFINITY)) return 0;
+  const uint32_t w = __float_as_uint(fminf(x, FLT_MAX));
+  return w & 0x80000000u ? ~w : w | 0x80000000u;
+}
+__device__ __forceinline__ float score_of_code(uint32_t c) {
+  return __uint_as_float(c & 0x80000000u ? c & 0x7FFFFFFFu : ~c);
+}
+
+// One token by one warp: lane j gets the j-th choice (its expert or -1, its weight).
+template <int kPerLane, bool kBf16>
+__device__ __forceinline__ void choose(const RouteArgs& a, int token, int lane, int& expert, float& weight) {
+  uint32_t code[kPerLane];
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {
+    const int e = i * 32 + lane;
+    code[i] = 0;
+    if (e < a.experts) {
+      const uint64_t at = token * a.stride + e;
+      code[i] = code_of(kBf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(a.scores)[at]) << 16)
+                              : static_cast<const float*>(a.scores)[at]);
+    }
+  }
+  uint32_t best = 0;
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) best = max(best, code[i]);
+  const uint32_t first = __reduce_max_sync(0xFFFFFFFFu, best);
+  const float top = first != 0 ? score_of_code(first) : 0.0f;
+  float all = 0.0f;
+  if (!a.normalise) {
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i)
+      if (code[i] != 0) all += expf(score_of_code(code[i]) - top);
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, m);
+  }
+  expert = -1;
+  uint32_t mine = 0;
+  for (int j = 0; j < a.top; ++j) {
+    const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, best);
+    if (most == 0) break;
+    uint32_t at = 0xFFFFFFFFu;
+#pragma unroll
+    for (int i = kPerLane - 1; i >= 0; --i)
+      if (code[i] == most) at = i * 32 + lane;
+    at = __reduce_min_sync(0xFFFFFFFFu, at);
+    best = 0;
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) {
+      if (i * 32 + lane == static_cast<int>(at)) code[i] = 0;
+      best = max(best, code[i]);
+    }
+    if (lane == j) {
+      expert = static_cast<int>(at);
+      mine = most;
+    }
+  }
+  weight = expert >= 0 ? expf(score_of_code(mine) - top) : 0.0f;
+  if (a.normalise) {
+    all = weight;
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, m);
+  }
+  if (expert >= 0) weight = weight / all;
+}
+
+// Walks the pairs [begin, end) of one warp in order: next[e] is the place of the next pair of
+// expert e. kPlace: writes places and rows; else it only counts.
+template <bool kPlace>
+__device__ __forceinline__ void walk(const RouteArgs& a, int begin, int end, int32_t* next, int lane) {
+  for (int p0 = begin; p0 < end; p0 += 32) {
+    const int p = p0 + lane;
+    const int e = p < end ? a.chosen[p] : -1;
+    const uint32_t same = __match_any_sync(0xFFFFFFFFu, e);
+    const int before = __popc(same & ((1u << lane) - 1));
+    const int base = e >= 0 ? next[e] : 0;
+    __syncwarp();
+    if (e >= 0 && before == 0) next[e] = base + __popc(same);
+    __syncwarp();
+    if (kPlace && p < end) {
+      a.places[p] = e >= 0 ? base + before : -1;
+      if (e >= 0) a.rows[base + before] = p / a.top;
+    }
+  }
+}
+
+// Sum over the block's threads before this one; total: over all.
+__device__ __forceinline__ int scan_before(int x, int* shared, int& total) {
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  int sum = x;
+#pragma unroll
+  for (int m = 1; m < 32; m <<= 1) {
+    const int y = __shfl_up_sync(0xFFFFFFFFu, sum, m);
+    if (lane >= m) sum += y;
+  }
+  if (lane == 31) shared[warp] = sum;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+  for (int w = 0; w < kRouteWarps; ++w) {
+    if (w < warp) before += shared[w];
+    total += shared[w];
+  }
+  __syncthreads();
+  return before + sum - x;
+}
+
+// Chooses the experts of the block's tokens and counts them: counts[block][expert]. With one
+// block (kAll) it goes on to the places itself.
+//
+// A warp has a token's scores in registers, as order-preserving codes, and takes the largest
+// `top` times (one reduction for the value, one for the lowest index). Pairs are then placed
+// by a counting sort: a warp's pairs are a range of their own, so a pair's place is its
+// expert's start, the pairs of earlier blocks and warps, and those before it in the warp
+// (__match_any_sync), whatever the timing.
+template <int kPerLane, bool kBf16, bool kAll>
+__global__ void __launch_bounds__(kRouteThreads)
+choose_kernel(const RouteArgs a, int32_t* counts) {
+  extern __shared__ int32_t next[];  // [warp][expert]
+  __shared__ int sums[kRouteWarps];
+  wait_for_previous();
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int64_t t0 = min((static_cast<int64_t>(blockIdx.x) * kRouteWarps + warp) * a.share, static_cast<int64_t>(a.tokens));
+  const int64_t t1 = min(t0 + a.share, static_cast<int64_t>(a.tokens));
+  int32_t* mine = next + warp * a.experts;
+  for (int e = lane; e < a.experts; e += 32) mine[e] = 0;
+  __syncwarp();
+  for (int64_t t = t0; t < t1; ++t) {
+    int expert;
+    float weight;
+    choose<kPerLane, kBf16>(a, static_cast<int>(t), lane, expert, weight);
+    if (lane < a.top) {
+      a.chosen[t * a.top + lane] = expert;
+      a.weights[t * a.top + lane] = weight;
+      if (expert >= 0) ++mine[expert];  // a token's experts differ
+    }
+    __syncwarp();
+  }
+  __syncthreads();
+  if (!kAll) {
+    for (int e = threadIdx.x; e < a.experts; e += kRouteThreads) {
+      int sum = 0;
+      for (int w = 0; w < kRouteWarps; ++w) sum += next[w * a.experts + e];
+      counts[static_cast<int64_t>(blockIdx.x) * a.experts + e] = sum;
+    }
+    return;
+  }
+  int base = 0;
+  for (int e0 = 0; e0 < a.experts; e0 += kRouteThreads) {
+    const int e = e0 + threadIdx.x;
+    int sum = 0;
+    if (e < a.experts)
+      for (int w = 0; w < kRouteWarps; ++w) sum += next[w * a.experts + e];
+    int total;
+    int at = base + scan_before(sum, sums, total);
+    if (e < a.experts) {
+      a.start[e] = at;
+      for (int w = 0; w < kRouteWarps; ++w) {
+        const int n = next[w * a.experts + e];
+        next[w * a.experts + e] = at;
+        at += n;
+      }
+    }
+    base += total;
+  }
+  if (threadIdx.x == 0) a.start[a.experts] = base;
+  __syncthreads();
+  walk<true>(a, static_cast<int>(t0) * a.top, static_cast<int>(t1) * a.top, mine, lane);
+}
+
+// Places the pairs of the block's tokens, with the counts of all blocks.
+__global__ void __launch_bounds__(kRouteThreads)
+place_kernel(const RouteArgs a, const int32_t* counts) {
+  extern __shared__ int32_t next[];
+  __shared__ int sums[kRouteWarps];
+  wait_for_previous();
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int64_t t0 = min((static_cast<int64_t>(blockIdx.x) * kRouteWarps + warp) * a.share, static_cast<int64_t>(a.tokens));
+  const int64_t t1 = min(t0 + a.share, static_cast<int64_t>(a.tokens));
+  int32_t* mine = next + warp * a.experts;
+  for (int e = lane; e < a.experts; e += 32) mine[e] = 0;
+  __syncwarp();
+  walk<false>(a, static_cast<int>(t0) * a.top, static_cast<int>(t1) * a.top, mine, lane);
+  __syncthreads();
+  int base = 0;
+  for (int e0 = 0; e0 < a.experts; e0 += kRouteThreads) {
+    const int e = e0 + threadIdx.x;
+    int sum = 0, before = 0;
+    if (e < a.experts)
+      for (int b = 0; b < static_cast<int>(gridDim.x); ++b) {
+        const int n = counts[static_cast<int64_t>(b) * a.experts + e];
+        if (b < static_cast<int>(blockIdx.x)) before += n;
+        sum += n;
+      }
+    int total;
+    int at = base + scan_before(sum, sums, total);
+    if (e < a.experts) {
+      if (blockIdx.x == 0) a.start[e] = at;
+      at += before;
+      for (int w = 0; w < kRouteWarps; ++w) {
+        const int n = next[w * a.experts + e];
+        next[w * a.experts + e] = at;
+        at += n;
+      }
+    }
+    base += total;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.start[a.experts] = base;
+  __syncthreads();
+  walk<true>(a, static_cast<int>(t0) * a.top, static_cast<int>(t1) * a.top, mine, lane);
+}
+
+template <int kPerLane, bool kBf16>
+cudaError_t route(RouteArgs a, int32_t* counts, cudaStream_t stream) {
+  const size_t shared = sizeof(int32_t) * kRouteWarps * a.experts;
+  auto one = choose_kernel<kPerLane, kBf16, true>;
+  auto many = choose_kernel<kPerLane, kBf16, false>;
+  if (shared > 48 * 1024) {
+    cudaError_t err = cudaFuncSetAttribute(one, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
+    if (err == cudaSuccess) err = cudaFuncSetAttribute(many, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
+    if (err == cudaSuccess) err = cudaFuncSetAttribute(place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
+    if (err != cudaSuccess) {
+      cudaGetLastError();
+      return err;
+    }
+  }
+  if (a.tokens <= 16 * kRouteWarps) {
+    a.share = (a.tokens + kRouteWarps - 1) / kRouteWarps;
+    return launch_early(one, 1, kRouteThreads, shared, stream, a, counts);
+  }
+  a.share = (a.tokens + kRouteWarps * kRouteGrid - 1) / (kRouteWarps * kRouteGrid);
+  const int grid = (a.tokens + kRouteWarps * a.share - 1) / (kRouteWarps * a.share);
+  const cudaError_t err = launch_early(many, grid, kRouteThreads, shared, stream, a, counts);
+  if (err != cudaSuccess) return err;
+  return launch_early(place_kernel, grid, kRouteThreads, shared, stream, a, static_cast<const int32_t*>(counts));
+}
+
+struct CombineArgs {
+  const uint16_t* y;
+  const int32_t* places;
+  const float* weights;
+  const uint16_t* add;
+  uint16_t* out;
+  uint64_t y_stride, add_stride, out_stride;
+  int slots, tokens, top, features;
+};
+
+__device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// A thread has eight features of a token. Bound by memory.
+__global__ void __launch_bounds__(256)
+combine_kernel(const CombineArgs a) {
+  wait_for_previous();
+  const int width = a.features / 8;
+  const int64_t all = static_cast<int64_t>(a.tokens) * width;
+  for (int64_t n = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; n < all;
+       n += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+    const int64_t t = n / width;
+    const int f = static_cast<int>(n - t * width) * 8;
+    float sum[8] = {};
+#pragma unroll 4
+    for (int j = 0; j < a.top; ++j) {
+      const int place = a.places[t * a.top + j];
+      if (static_cast<unsigned>(place) >= static_cast<unsigned>(a.slots)) continue;
+      const float w = a.weights[t * a.top + j];
+      const uint4 v = *reinterpret_cast<const uint4*>(a.y + place * a.y_stride + f);
+      const uint32_t word[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        sum[2 * i] = fmaf(w, bf16_low(word[i]), sum[2 * i]);
+        sum[2 * i + 1] = fmaf(w, bf16_high(word[i]), sum[2 * i + 1]);
+      }
+    }
+    if (a.add != nullptr) {
+      const uint4 v = *reinterpret_cast<const uint4*>(a.add + t * a.add_stride + f);
+      const uint32_t word[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        sum[2 * i] += bf16_low(word[i]);
+        sum[2 * i + 1] += bf16_high(word[i]);
+      }
+    }
+    *reinterpret_cast<uint4*>(a.out + t * a.out_stride + f) =
+        make_uint4(pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]), pack_bf16(sum[4], sum[5]), pack_bf16(sum[6], sum[7]));
+  }
+}
+
+}  // namespace
+
+uint64_t route_workspace_bytes(int, int experts, int) { return sizeof(int32_t) * kRouteGrid * experts; }
+
+cudaError_t launch_route(const es_route_t& r, void* workspace, cudaStream_t stream) {
+  const RouteArgs a{r.scores, r.chosen, r.weights, r.start, r.rows, r.places, r.scores_stride,
+                    r.tokens, r.experts, r.top, r.normalise, 0};
+  int32_t* counts = static_cast<int32_t*>(workspace);
+  const bool b = r.dtype == ES_BF16;
+  const int n = (r.experts + 31) / 32;
+  if (n <= 1) return b ? route<1, true>(a, counts, stream) : route<1, false>(a, counts, stream);
+  if (n <= 2) return b ? route<2, true>(a, counts, stream) : route<2, false>(a, counts, stream);
+  if (n <= 4) return b ? route<4, true>(a, counts, stream) : route<4, false>(a, counts, stream);
+  if (n <= 8) return b ? route<8, true>(a, counts, stream) : route<8, false>(a, counts, stream);
+  return b ? route<32, true>(a, counts, stream) : route<32, false>(a, counts, stream);
+}
+
+cudaError_t launch_combine(const es_combine_t& c, cudaStream_t stream) {
+  const CombineArgs a{static_cast<const uint16_t*>(c.y), c.places, c.weights, static_cast<const uint16_t*>(c.add),
+                      static_cast<uint16_t*>(c.out), c.y_stride, c.add_stride, c.out_stride, c.slots, c.tokens, c.top, c.features};
+  const int64_t blocks = (static_cast<int64_t>(c.tokens) * (c.features / 8) + 255) / 256;
+  return launch_early(combine_kernel, static_cast<int>(blocks < 152 * 64 ? blocks : 152 * 64), 256, 0, stream, a);
+}
+
+}  // namespace esopt
