@@ -46,7 +46,9 @@ extern "C" {
  * of data, o < out_features, i < in_features.
  *   dtype         ES_BF16, or ES_FP8_E4M3 with one scale a matrix: the value is
  *                 scale[g] * code
- *   scale         [groups] fp32 in device memory (4-byte aligned); NULL for ES_BF16
+ *   scale         [groups] fp32 in device memory (4-byte aligned); NULL for ES_BF16.
+ *                 In es_project with adapters a scale whose reciprocal is infinite
+ *                 counts as 0.
  *   groups        1 .. ES_MAX_EXPERTS
  *   out_features  a multiple of 8, 8 .. 2^20
  *   in_features   a multiple of 8 (FP8: 16), up to 2^17
@@ -109,9 +111,10 @@ es_status_t es_adapters_destroy(es_adapters_t adapters);
 
 /*
  * es_project: for each row i of request r, with adapter m = adapter[r],
- *   h = scale[m] * (A_m x_i)   rounded to bf16,
- *   y_i = W x_i + B_m h        (W x_i alone where m is not within 0 .. count - 1),
- * W with its scale. Sums are fp32, and a result is rounded once.
+ *   y_i = W x_i + B_m (scale[m] * (A_m x_i))
+ *         (W x_i alone where m is not within 0 .. count - 1),
+ * W with its scale. Sums are fp32, A x is kept to 2^-16 of itself, and a result is
+ * rounded once. A row depends on its own adapter alone, whatever others hold.
  *   weights   of one matrix
  *   adapters  of the same sizes, or NULL: y = W x
  *   x         [rows] rows of in_features bf16, x_stride elements apart

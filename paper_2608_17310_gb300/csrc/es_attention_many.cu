@@ -38,6 +38,7 @@
 
 #include "es_attention.cuh"
 #include "es_rollout_internal.h"
+#include "es_tensor.cuh"
 
 namespace esopt {
 namespace {
@@ -235,119 +236,8 @@ plan_kernel(const BatchView batch, const AttentionArgs a, int kv_heads, int grid
   }
 }
 
-// --- barriers, copies and products --------------------------------------------------
+// --- tensor memory ------------------------------------------------------------------
 
-// A wait that outlasts this many tries (1.48 us each where nothing comes, 6 s) has met an error of the
-// kernel's own, which ends the launch with its flag set in place of hanging the GPU. Waits are a tile's
-// work mostly, but a warpgroup without rows in a unit waits through all its tiles, and the others wait where
-// rows look through a unit's values for infinities and NaN (0.3 s for 131,072 keys that are all to be looked at).
-constexpr int kMostTries = 1 << 22;
-
-// What a wait looks at besides its barrier.
-struct Watch {
-  volatile int* failed;  // a wait of the block was given up
-  int tries;
-};
-
-__device__ __forceinline__ void barrier_init(uint64_t* b, int count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(shared_address(b)), "r"(count) : "memory");
-}
-__device__ __forceinline__ void barrier_arrive(uint64_t* b) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(shared_address(b)) : "memory");
-}
-__device__ __forceinline__ void barrier_expect(uint64_t* b, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_address(b)), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool barrier_try(uint64_t* b, uint32_t parity) {
-  uint32_t done;
-  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}"
-               : "=r"(done)
-               : "r"(shared_address(b)), "r"(parity)
-               : "memory");
-  return done != 0;
-}
-// false: the wait was given up, here or by another thread of the block
-__device__ __forceinline__ bool barrier_wait(uint64_t* b, uint32_t parity, const Watch& watch) {
-  for (int i = 0; i < watch.tries; ++i) {
-    if (barrier_try(b, parity)) return true;
-    if (*watch.failed) return false;
-  }
-  *watch.failed = 1;
-  return false;
-}
-
-// By all lanes: through one of them and a shuffle measured 25 % slower over a whole prompt.
-__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, const Watch& watch) {
-  return __all_sync(0xFFFFFFFFu, barrier_wait(b, parity, watch));
-}
-// One lane arrives, with what all lanes did before.
-__device__ __forceinline__ void warp_arrive(uint64_t* b, int lane) {
-  __syncwarp();
-  if (lane == 0) barrier_arrive(b);
-}
-
-// The same, whatever has failed before: for what must not outlive the block.
-__device__ __forceinline__ void barrier_settle(uint64_t* b, uint32_t parity) {
-  for (int i = 0; i < kMostTries; ++i)
-    if (barrier_try(b, parity)) return;
-}
-
-__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
-__device__ __forceinline__ void load_box(const CUtensorMap* map, uint32_t to, uint64_t* barrier, int x, int y, int z) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(to),
-               "l"(map), "r"(shared_address(barrier)), "r"(x), "r"(y), "r"(z)
-               : "memory");
-}
-
-// Shared-memory operands in 128-byte rows, swizzled by 128 bytes, 8 rows to 1024 bytes.
-__device__ __forceinline__ uint64_t operand(uint32_t address, uint32_t leading) {
-  return static_cast<uint64_t>((address & 0x3FFFF) >> 4) | static_cast<uint64_t>(leading >> 4) << 16 |
-         static_cast<uint64_t>(1024 >> 4) << 32 | static_cast<uint64_t>(1) << 46 | static_cast<uint64_t>(2) << 61;
-}
-
-// bf16 x bf16 -> fp32, M = 128; `transposed`: the second operand's rows are its K
-__host__ __device__ constexpr uint32_t product_of(int n, bool transposed) {
-  return 1u << 4 | 1u << 7 | 1u << 10 | (transposed ? 1u << 16 : 0u) | static_cast<uint32_t>(n >> 3) << 17 | (128u >> 4) << 24;
-}
-
-__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t kind, bool add) {
-  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-               "l"(a), "l"(b), "r"(kind), "r"(static_cast<uint32_t>(add))
-               : "memory");
-}
-__device__ __forceinline__ void multiply_from_tensor(uint32_t d, uint32_t a, uint64_t b, uint32_t kind, bool add) {
-  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
-               "r"(a), "l"(b), "r"(kind), "r"(static_cast<uint32_t>(add))
-               : "memory");
-}
-// The barrier completes when the products issued before have.
-__device__ __forceinline__ void commit(uint64_t* b) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_address(b)) : "memory");
-}
-
-__device__ __forceinline__ void tensor_load(uint32_t (&r)[32], uint32_t from) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(from));
-}
-// After this the registers of the loads before are valid.
-__device__ __forceinline__ void tensor_loaded(uint32_t (&r)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
-                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
-                 "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
-                 "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
-               :
-               : "memory");
-}
 __device__ __forceinline__ void tensor_store32(uint32_t to, const uint32_t (&r)[32]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
@@ -803,15 +693,6 @@ __device__ void convert_tiles(Shared<D, true>& sh, const Watch& watch, const Cac
     }
     leave(sh, n, lane);
   }
-}
-
-// True in one lane of a converged warp. The products' operands have to be the warp's own
-// (uniform registers): under a test of the lane number the compiler cannot know that one
-// thread alone is left, and makes every product a loop over the lanes.
-__device__ __forceinline__ bool elected() {
-  uint32_t yes;
-  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(yes));
-  return yes != 0;
 }
 
 // The warp that issues the products.

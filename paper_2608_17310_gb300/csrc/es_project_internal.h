@@ -55,10 +55,19 @@ __device__ __forceinline__ void segment_of(const RowView& r, int s, int& begin, 
 }
 #endif
 
-cudaError_t launch_project(const MatrixView& w, bool fp8, const AdapterView* adapters, const int32_t* adapter, const RowView& rows,
-                           void* workspace, cudaStream_t stream);
-cudaError_t launch_experts(const MatrixView& w, bool fp8, bool gated, const RowView& rows, void* workspace, cudaStream_t stream);
+// For TMA: matrices in boxes of 64 rows by 64 elements, bf16 swizzled by 128 bytes.
+es_status_t map_matrices(CUtensorMap* map, const void* data, uint64_t in, uint64_t out, uint64_t groups, uint64_t row_stride,
+                         uint64_t group_stride, bool fp8, const char* call);
+
+// w_map, b_map: of the matrices and of the adapters' B. These record their own errors.
+es_status_t launch_project(const MatrixView& w, const CUtensorMap& w_map, bool fp8, const AdapterView* adapters, const CUtensorMap* b_map,
+                           const int32_t* adapter, const RowView& rows, void* workspace, cudaStream_t stream, const char* call);
+es_status_t launch_experts(const MatrixView& w, const CUtensorMap& w_map, bool fp8, bool gated, const RowView& rows, void* workspace,
+                           cudaStream_t stream, const char* call);
 uint64_t project_workspace_bytes(int rank, int rows);  // rank 0: no adapters
+// For tests: tries after which the products' waits are given up in calls from now on (0: at once;
+// negative: as it was).
+void set_project_wait_tries(int tries);
 
 cudaError_t launch_route(const es_route_t& args, void* workspace, cudaStream_t stream);
 uint64_t route_workspace_bytes(int tokens, int experts, int top);

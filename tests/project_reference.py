@@ -5,7 +5,7 @@ Tolerances, from the roundings that each operator makes:
   products   a sum of n products in fp32, in any order and with terms cut instead of rounded, is off by
              n 2^-23 of the sum of its terms' sizes; bf16 results by 2^-8 of their size, and 2^-134 (half
              the smallest bf16).
-  project    also 2^-8 of each element of h = scale A x, which is rounded to bf16, through |B|.
+  project    also 2^-16 of each element of h = scale A x, which is kept as two bf16 numbers, through |B|.
   gated      silu has slopes within (-0.1, 1.1); exp and the division are off by 2^-20 of silu.
   route      a weight: exp, the sum of `experts` of them and the division, 2^-20 + experts 2^-23 of it.
   combine    as products, `top` + 1 terms."""
@@ -34,7 +34,7 @@ def project(x, w, a=None, b=None, scale=None, member=None):
         s = 1.0 if scale is None else float(scale[m])
         h, h_size = total(a[m], x[i:i + 1])
         h, h_size = s * h[0], abs(s) * h_size[0]
-        h_off = 2.0 ** -8 * h.abs() + 2.0 ** -134 + (x.shape[1] + 8) * 2.0 ** -23 * h_size
+        h_off = 2.0 ** -16 * h.abs() + 2.0 ** -134 + (x.shape[1] + 8) * 2.0 ** -23 * h_size
         bm = b[m].double()
         y[i] += bm @ h
         off[i] += bm.abs() @ h_off + (len(h) + 8) * 2.0 ** -23 * (bm.abs() @ h.abs() + size[i])
