@@ -32,6 +32,7 @@ struct ExpandView {
   const uint16_t* b;
   const int32_t* of_row;    // adapter of each row, or -1
   const int32_t* of_block;  // of each 16 rows
+  const float* extra;       // [rows][out] B h of the rows of mixed blocks, or NULL: where they are written
   uint64_t b_stride;
   int rank, padded;
 };
@@ -157,6 +158,61 @@ shrink_kernel(const ShrinkArgs a) {
   }
 }
 
+// --- B h of rows beside others' -------------------------------------------------------------
+
+constexpr int kExpandWarps = 4;
+constexpr int kExpandRows = 4;  // of a warp
+
+// extra = B h for the rows of mixed blocks: a warp has kExpandRows rows and 128 features, a lane 4 of them,
+// with B's elements kept from row to row where the adapter stays.
+template <int kChunk>  // ranks at a time
+__global__ void __launch_bounds__(kExpandWarps * 32)
+expand_kernel(const ExpandView e, const int32_t* start, float* extra, int requests, int rows, int out) {
+  let_next_start();
+  wait_for_previous();
+  const int end = start != nullptr ? min(max(start[requests], 0), rows) : rows;
+  const int lane = threadIdx.x % 32, f = (blockIdx.x * kExpandWarps + threadIdx.x / 32) * kFeatures + lane * 4;
+  const int row0 = blockIdx.y * kExpandRows;
+  if (row0 >= end || f >= out || e.of_block[row0 / kBlock] != kMixed) return;
+  float y[kExpandRows][4] = {};
+  int m[kExpandRows];
+#pragma unroll
+  for (int i = 0; i < kExpandRows; ++i) m[i] = row0 + i < end ? e.of_row[row0 + i] : kNone;
+  for (int r0 = 0; r0 < e.rank; r0 += kChunk) {
+    uint4 b[4][kChunk / 8];
+#pragma unroll
+    for (int i = 0; i < kExpandRows; ++i) {
+      if (m[i] < 0) continue;
+      if (i == 0 || m[i] != m[i - 1]) {
+        const uint16_t* from = e.b + m[i] * e.b_stride + static_cast<uint64_t>(f) * e.rank + r0;
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int c = 0; c < kChunk / 8; ++c) b[n][c] = *reinterpret_cast<const uint4*>(from + n * e.rank + c * 8);
+      }
+      const uint16_t* h = e.h + static_cast<uint64_t>(row0 + i) * 2 * e.padded + r0;
+#pragma unroll
+      for (int c = 0; c < kChunk / 8; ++c) {
+        const uint4 p = *reinterpret_cast<const uint4*>(h + c * 8), q = *reinterpret_cast<const uint4*>(h + e.padded + c * 8);
+        const uint32_t pw[4] = {p.x, p.y, p.z, p.w}, qw[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const float lo = bf16_value(pw[d]) + bf16_value(qw[d]), hi = bf16_high(pw[d]) + bf16_high(qw[d]);
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            const uint32_t w = d == 0 ? b[n][c].x : d == 1 ? b[n][c].y : d == 2 ? b[n][c].z : b[n][c].w;
+            y[i][n] = fmaf(hi, bf16_high(w), fmaf(lo, bf16_value(w), y[i][n]));
+          }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kExpandRows; ++i)
+    if (m[i] >= 0)
+      *reinterpret_cast<float4*>(extra + static_cast<uint64_t>(row0 + i) * out + f) = make_float4(y[i][0], y[i][1], y[i][2], y[i][3]);
+}
+
 // --- the products -----------------------------------------------------------------------
 
 template <int kRows, bool kFp8>
@@ -182,6 +238,7 @@ struct Shared {
   uint32_t tensor;
   int failed;
   uint32_t order;
+  int4 named[2][kRows / 8];  // rows of the fours of each copying warp
 };
 
 // What all roles need of a call's tiles. A tile is kFeatures features (gated: 64 and the 64 that
@@ -292,7 +349,7 @@ __device__ __forceinline__ Extra extra_of(int padded, int i) {
 
 template <int kRows, bool kFp8, bool kGated>
 __global__ void __launch_bounds__(Shape<kRows, kFp8>::kThreads, 1)
-product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, uint32_t* counters, int* flag, float* parts, int tries,
+product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, uint32_t* counters, int* flag, float* parts, int tries, bool early,
                const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map,
                const __grid_constant__ CUtensorMap h_map, const __grid_constant__ CUtensorMap b_map) {
   using S = Shape<kRows, kFp8>;
@@ -324,7 +381,9 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
   fence_before();
   __syncthreads();
   fence_after();
-  wait_for_previous();
+  // Behind the kernels of the adapters' part, which wait for all that came before them and then let
+  // the next start, only what they make has to be waited for.
+  if (!early) wait_for_previous();
 
   const int outs = kGated ? w.out / 2 : w.out;
   Plan plan;
@@ -375,17 +434,6 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
     while (fine && walk.next(item)) {
       const int padded = (item.rows + 15) & ~15;
       const int boxes = (padded + S::kBox - 1) / S::kBox;
-      int from[2][4];  // rows of the two fours that this lane asks for
-      if (rows.index != nullptr) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int r = (i * 32 + lane) * 4 + q;
-            const int v = r < item.rows ? rows.index[item.row0 + r] : 0;
-            from[i][q] = static_cast<unsigned>(v) < static_cast<unsigned>(rows.x_rows) ? v : 0;
-          }
-      }
       for (int k = item.k0; k < item.k1; ++k, ++done) {
         const uint32_t stage = done % kStages;
         if (!(fine = warp_wait(&sh.empty[stage], (done / kStages & 1) ^ 1, watch))) break;
@@ -400,15 +448,9 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
               load_box(&x_map, x_to + i * (S::kBox * kDepth * 2), &sh.full[stage], k * kDepth, item.row0 + i * S::kBox);
         }
         __syncwarp();
-        if (rows.index != nullptr) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-            if ((i * 32 + lane) * 4 < padded)
-              gather_rows(&x_map, x_to + (i * 32 + lane) * (4 * kDepth * 2), &sh.full[stage], k * kDepth, from[i]);
-        }
-        __syncwarp();
       }
       if (!fine || expand.h == nullptr || item.k1 < plan.depth) continue;
+      if (early) wait_for_previous();
       const Runs runs(expand, item.row0, item.rows, lane);
       for (int i = 0, j, m; fine && runs.next(i, j, m); i = j) {
         const int run_boxes = ((j - i) * kBlock + S::kBox - 1) / S::kBox;
@@ -457,6 +499,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         __syncwarp();
       }
       if (fine && expand.h != nullptr && item.k1 == plan.depth) {
+        if (early) wait_for_previous();
         const Runs runs(expand, item.row0, item.rows, lane);
         for (int i = 0, j, m; fine && runs.next(i, j, m); i = j) {
           const uint32_t run_kind = product_of(0, false) | static_cast<uint32_t>((j - i) * 2) << 17;
@@ -487,7 +530,44 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
     if (elected()) commit(&sh.drained);  // by the lane that issued the products: none outlives the tensor memory
     __syncwarp();
     barrier_settle(&sh.drained, 0);
-  } else if (warp >= 4 && warp < 8) {
+  } else if (warp < 4) {
+    // --- copies of rows that are named one by one, four at a time, half of them by each of two warps
+    if (rows.index != nullptr) {
+      Walk<Shared<kRows, kFp8>> walk(rows, sh, plan, kRows, kGated);
+      Item item;
+      uint32_t done = 0;
+      bool fine = true;
+      int4* named = sh.named[warp - 2];
+      while (fine && walk.next(item)) {
+        const int fours = (item.rows + 15) / 16 * 4;
+        const int begin = warp == 2 ? 0 : fours / 2, end = warp == 2 ? fours / 2 : fours;
+        __syncwarp();
+        if (lane < end - begin) {
+          int v[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int r = (begin + lane) * 4 + q;
+            v[q] = r < item.rows ? rows.index[item.row0 + r] : 0;
+            if (static_cast<unsigned>(v[q]) >= static_cast<unsigned>(rows.x_rows)) v[q] = 0;
+          }
+          named[lane] = make_int4(v[0], v[1], v[2], v[3]);
+        }
+        __syncwarp();
+        for (int k = item.k0; k < item.k1; ++k, ++done) {
+          const uint32_t stage = done % kStages;
+          if (!(fine = warp_wait(&sh.empty[stage], (done / kStages & 1) ^ 1, watch))) break;
+          if (elected()) {
+            const uint32_t x_to = shared_address(sh.x[stage]);
+#pragma unroll 4
+            for (int i = begin; i < end; ++i)
+              gather_rows(&x_map, x_to + i * (4 * kDepth * 2), &sh.full[stage], k * kDepth, named[i - begin]);
+          }
+          __syncwarp();
+        }
+      }
+      for (uint32_t i = done > kStages ? done - kStages : 0; i < done; ++i) barrier_settle(&sh.full[i % kStages], i / kStages & 1);
+    }
+  } else if (warp < 8) {
     // --- results: a thread reads a feature's lane, and writes four features of a row
     Walk<Shared<kRows, kFp8>> walk(rows, sh, plan, kRows, kGated);
     Item item;
@@ -500,6 +580,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       return warp_wait(&sh.group, syncs++ & 1, watch);
     };
     bool fine = true;
+    if (early) wait_for_previous();
     for (; fine && walk.next(item); ++items) {
       const uint32_t half = items & 1;
       if (!(fine = warp_wait(&sh.sum_full[half], items / 2 & 1, watch))) break;
@@ -577,7 +658,13 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
             float y[4] = {z.x, z.y, z.z, z.w};
             if (expand.h != nullptr && expand.of_block[row / kBlock] == kMixed) {
               const int m = expand.of_row[row];
-              if (m >= 0) {
+              if (m >= 0 && expand.extra != nullptr) {
+                const float4 v = *reinterpret_cast<const float4*>(expand.extra + static_cast<uint64_t>(row) * outs + f);
+                y[0] += v.x;
+                y[1] += v.y;
+                y[2] += v.z;
+                y[3] += v.w;
+              } else if (m >= 0) {
                 const uint16_t* h = expand.h + static_cast<uint64_t>(row) * 2 * expand.padded;
                 const uint16_t* b = expand.b + m * expand.b_stride + static_cast<uint64_t>(f) * expand.rank;
                 for (int r = 0; r < expand.rank; r += 8) {
@@ -614,6 +701,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
     while (fine && walk.next(item)) {
       int extra = 0;
       if (expand.h != nullptr && item.k1 == plan.depth) {
+        if (early) wait_for_previous();
         const Runs runs(expand, item.row0, item.rows, lane);
         for (int i = 0, j, m; runs.next(i, j, m); i = j) extra += extras_of(expand.padded);
       }
@@ -710,7 +798,7 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
   const cudaError_t err =
       launch_early(kernel, std::min(sms, kMaxGrid), S::kThreads, kBytes, stream, w, rows, expand,
                    reinterpret_cast<uint32_t*>(workspace), reinterpret_cast<int*>(workspace + ES_PROJECT_GAVE_UP),
-                   reinterpret_cast<float*>(workspace + kHead), tries_of_a_wait.load(std::memory_order_relaxed), w_map, x_map, h_map,
+                   reinterpret_cast<float*>(workspace + kHead), tries_of_a_wait.load(std::memory_order_relaxed), expand.h != nullptr, w_map, x_map, h_map,
                    expand.h != nullptr ? *b_map : x_map);
   return err != cudaSuccess ? cuda_fail(err, call) : ES_OK;
 }
@@ -724,23 +812,24 @@ es_status_t launch_rows(const MatrixView& w, const CUtensorMap& w_map, bool fp8,
 }
 
 constexpr int kFew = 64, kMany = 256;  // rows of a tile
+constexpr int kMostExtra = 1024;       // rows up to which B h has room in the workspace
 
 uint64_t padded_rank(int rank) { return static_cast<uint64_t>(rank + 15) / 16 * 16; }
 uint64_t rounded(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-template <int kSteps>
-cudaError_t launch_shrink(const ShrinkArgs& a, cudaStream_t stream) {
+// A launch of a grid of two axes that may begin early.
+template <class... P, class... A>
+cudaError_t launch_grid(void (*kernel)(P...), dim3 grid, int block, cudaStream_t stream, const A&... args) {
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t config{};
-  const int most = std::min(std::min(a.requests, a.rows), kBlock);  // adapters that 16 rows can have
-  config.gridDim = dim3((a.rows + kBlock - 1) / kBlock, most);
-  config.blockDim = dim3(kShrinkWarps * 32);
+  config.gridDim = grid;
+  config.blockDim = dim3(static_cast<unsigned>(block));
   config.stream = stream;
   config.attrs = &attr;
   config.numAttrs = 1;
-  const cudaError_t err = cudaLaunchKernelEx(&config, shrink_kernel<kSteps>, a);
+  const cudaError_t err = cudaLaunchKernelEx(&config, kernel, P(args)...);
   const cudaError_t last = cudaGetLastError();
   return err != cudaSuccess ? err : last;
 }
@@ -766,11 +855,12 @@ es_status_t map_matrices(CUtensorMap* map, const void* data, uint64_t in, uint64
   return ES_OK;
 }
 
-// Behind the head: parts of tiles that blocks share; h; the adapters of rows and blocks.
-uint64_t project_workspace_bytes(int rank, int rows) {
+// Behind the head: parts of tiles that blocks share; h; the adapters of rows and blocks; B h of up to
+// kMostExtra rows.
+uint64_t project_workspace_bytes(int rank, int rows, int out) {
   const uint64_t n = rows;
   uint64_t bytes = kHead + parts_bytes(rows > kFew ? kMany : kFew);
-  if (rank > 0) bytes += rounded(n * 4 * padded_rank(rank)) + rounded(n * 4) + rounded((n + kBlock - 1) / kBlock * 4);
+  if (rank > 0) bytes += rounded(n * 4 * padded_rank(rank)) + 2 * rounded(n * 4) + rounded(std::min(rows, kMostExtra) * uint64_t{4} * out);
   return bytes;
 }
 
@@ -788,13 +878,20 @@ es_status_t launch_project(const MatrixView& w, const CUtensorMap& w_map, bool f
     const ShrinkArgs a{rows.x, rows.start, adapter, adapters->a, adapters->scale, w.scale, h, of_row, of_block, rows.x_stride,
                        adapters->a_stride, rows.segments, rows.rows, adapters->count, adapters->rank, padded, w.in};
     const int steps = (adapters->rank + 7) / 8;
-    const cudaError_t err = steps <= 1   ? launch_shrink<1>(a, stream)
-                            : steps <= 2 ? launch_shrink<2>(a, stream)
-                            : steps <= 4 ? launch_shrink<4>(a, stream)
-                            : steps <= 8 ? launch_shrink<8>(a, stream)
-                                         : launch_shrink<16>(a, stream);
+    auto shrink = steps <= 1 ? shrink_kernel<1> : steps <= 2 ? shrink_kernel<2> : steps <= 4 ? shrink_kernel<4>
+                : steps <= 8 ? shrink_kernel<8> : shrink_kernel<16>;
+    const int most = std::min(std::min(rows.segments, rows.rows), kBlock);  // adapters that 16 rows can have
+    cudaError_t err = launch_grid(shrink, dim3((rows.rows + kBlock - 1) / kBlock, most), kShrinkWarps * 32, stream, a);
     if (err != cudaSuccess) return cuda_fail(err, call);
-    expand = ExpandView{h, adapters->b, of_row, of_block, adapters->b_stride, adapters->rank, padded};
+    expand = ExpandView{h, adapters->b, of_row, of_block, nullptr, adapters->b_stride, adapters->rank, padded};
+    if (most > 1 && rows.rows <= kMostExtra) {
+      float* extra = reinterpret_cast<float*>(behind + rounded(n * 4 * padded) + 2 * rounded(n * 4));
+      auto kernel = adapters->rank % 16 == 0 ? expand_kernel<16> : expand_kernel<8>;
+      err = launch_grid(kernel, dim3((w.out + kExpandWarps * kFeatures - 1) / (kExpandWarps * kFeatures), (rows.rows + kExpandRows - 1) / kExpandRows),
+                        kExpandWarps * 32, stream, expand, rows.start, extra, rows.segments, rows.rows, w.out);
+      if (err != cudaSuccess) return cuda_fail(err, call);
+      expand.extra = extra;
+    }
   }
   auto f = rows.rows > kFew ? launch_rows<kMany> : launch_rows<kFew>;
   return f(w, w_map, fp8, false, rows, expand, b_map, at, stream, call);

@@ -166,7 +166,7 @@ es_status_t es_adapters_destroy(es_adapters_t adapters) {
 
 uint64_t es_project_workspace(es_weights_t weights, es_adapters_t adapters, int rows) {
   if (weights == nullptr || rows < 0 || rows > ES_MAX_ROWS) return 0;
-  return esopt::project_workspace_bytes(adapters != nullptr ? adapters->view.rank : 0, rows);
+  return esopt::project_workspace_bytes(adapters != nullptr ? adapters->view.rank : 0, rows, weights->view.out);
 }
 
 es_status_t es_project(es_weights_t w, es_adapters_t m, const es_project_t* a, void* workspace, uint64_t workspace_bytes,

@@ -77,10 +77,10 @@ __device__ __forceinline__ void load_box(const CUtensorMap* map, uint32_t to, ui
                : "memory");
 }
 // Four rows of a map whose box is one row high.
-__device__ __forceinline__ void gather_rows(const CUtensorMap* map, uint32_t to, uint64_t* barrier, int x, const int (&row)[4]) {
+__device__ __forceinline__ void gather_rows(const CUtensorMap* map, uint32_t to, uint64_t* barrier, int x, int4 row) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], "
                "[%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(to),
-               "l"(map), "r"(shared_address(barrier)), "r"(x), "r"(row[0]), "r"(row[1]), "r"(row[2]), "r"(row[3])
+               "l"(map), "r"(shared_address(barrier)), "r"(x), "r"(row.x), "r"(row.y), "r"(row.z), "r"(row.w)
                : "memory");
 }
 
