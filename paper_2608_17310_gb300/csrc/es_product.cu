@@ -15,12 +15,10 @@ namespace {
 
 constexpr int kFeatures = 128;  // of a tile: lanes of the tensor memory
 constexpr int kDepth = 64;      // of a stage: 128 bytes of bf16
-constexpr int kMaxGrid = 192;
-constexpr int kCounters = 1024;
 constexpr int kBand = 8;        // column tiles whose feature tiles are neighbours
 constexpr int kBlock = 16;      // rows whose adapters are looked at together
+constexpr int kMostShares = 8;  // blocks of a cluster
 
-static_assert(kCounters * sizeof(uint32_t) == ES_PROJECT_GAVE_UP, "the flag is behind the counters");
 constexpr uint64_t kHead = ES_PROJECT_GAVE_UP + 256;
 
 // What a block of 16 rows has: one adapter for all of them, none, or several.
@@ -56,7 +54,11 @@ struct ShrinkArgs {
   int requests, rows, count, rank, padded, in;
 };
 
-constexpr int kShrinkWarps = 8;
+constexpr int kShrinkRows = 32;
+template <int kSteps>
+constexpr int kShrinkWarps = kSteps <= 2 ? 16 : kSteps <= 8 ? 8 : 4;
+template <int kSteps>
+constexpr int kShrinkBytes = kShrinkWarps<kSteps> * kShrinkRows * (kSteps * 8 + 1) * 4;
 
 // 1 / scale where the matrix's codes are multiplied by their scale in the end and the adapters'
 // part must not be; 1 where that is infinite: then the codes count as zeros.
@@ -65,88 +67,111 @@ __device__ __forceinline__ float undo_of(const float* w_scale) {
   return isinf(u) ? 1.0f : u;
 }
 
-// h of 16 rows with the (blockIdx.y)-th adapter among them, and which adapters rows and blocks
+// The adapter of row row0 + lane for each lane of a warp, kNone for rows from `end` on.
+__device__ __forceinline__ int adapter_of_lane(const ShrinkArgs& a, int row0, int end, int lane) {
+  const int row = row0 + lane;
+  int r = row;
+  if (a.start != nullptr && row0 < end) {
+    // The last request that starts at or before row0, 32 starts at a time.
+    int lo = 0, span = a.requests;  // among [lo, lo + span)
+    while (span > 1) {
+      const int step = (span + 31) / 32;
+      const int at = lo + lane * step;
+      const uint32_t before = __ballot_sync(0xFFFFFFFFu, lane * step < span && a.start[at] <= row0);
+      const int chosen = before != 0 ? 31 - __clz(before) : 0;
+      lo += chosen * step;
+      span = min(step, span - chosen * step);
+    }
+    // From there on: the requests that start within the 32 rows.
+    r = lo;
+    for (int at = lo + 1; at < a.requests; at += 32) {
+      const int begins = at + lane < a.requests ? a.start[at + lane] : INT32_MAX;
+      for (int i = 0; i < 32; ++i) {
+        const int n = __popc(__ballot_sync(0xFFFFFFFFu, begins <= row0 + i));
+        if (lane == i) r += n;
+      }
+      if (__shfl_sync(0xFFFFFFFFu, begins, 31) > row0 + 31) break;
+    }
+  }
+  if (row >= end) return kNone;
+  const int m = a.adapter[r];
+  return static_cast<unsigned>(m) < static_cast<unsigned>(a.count) ? m : kNone;
+}
+
+// h of 32 rows with the (blockIdx.y)-th adapter among them, and which adapters rows and blocks
 // have. The warps share the depth; the two products of a lane's 16 bytes of x and A take its
 // elements in the order in which they lie, the same in both, so each is one load.
 template <int kSteps>  // of 8 ranks
-__global__ void __launch_bounds__(kShrinkWarps * 32)
+__global__ void __launch_bounds__(kShrinkWarps<kSteps> * 32)
 shrink_kernel(const ShrinkArgs a) {
-  __shared__ float parts[kShrinkWarps][16][kSteps * 8 + 1];
+  constexpr int kWarps = kShrinkWarps<kSteps>, kPitch = kSteps * 8 + 1;
+  extern __shared__ float parts[];  // [warp][row][kPitch]
   wait_for_previous();
   let_next_start();
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int row0 = blockIdx.x * kBlock;
+  const int row0 = blockIdx.x * kShrinkRows;
   const int end = a.start != nullptr ? min(max(a.start[a.requests], 0), a.rows) : a.rows;
-  // the adapter of row `lane`
-  const int row = row0 + lane % kBlock;
-  int mine = kNone;
-  if (row < end) {
-    int r = row;
-    if (a.start != nullptr) {
-      int lo = 0, hi = a.requests;  // the last request that starts at or before the row
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (a.start[mid] <= row) lo = mid;
-        else hi = mid;
-      }
-      r = lo;
-    }
-    mine = a.adapter[r];
-    if (static_cast<unsigned>(mine) >= static_cast<unsigned>(a.count)) mine = kNone;
-  }
-  const uint32_t there = __ballot_sync(0xFFFFFFFFu, row < end) & 0xFFFFu;
+  const int mine = adapter_of_lane(a, row0, end, lane);
+  const uint32_t there = __ballot_sync(0xFFFFFFFFu, row0 + lane < end);
   const uint32_t same = __match_any_sync(0xFFFFFFFFu, mine) & there;
   if (blockIdx.y == 0 && warp == 0) {
-    if (lane < kBlock && row < end) a.of_row[row] = mine;
-    if (lane == 0 && there != 0) a.of_block[blockIdx.x] = same == there ? mine : kMixed;
+    if (row0 + lane < end) a.of_row[row0 + lane] = mine;
+    const uint32_t block = 0xFFFFu << (lane & 16);
+    if (lane % kBlock == 0 && (there & block) != 0)
+      a.of_block[(row0 + lane) / kBlock] = (same & block) == (there & block) ? mine : kMixed;
   }
-  const uint32_t firsts = __ballot_sync(0xFFFFFFFFu, lane < kBlock && mine >= 0 && (same & ((1u << lane) - 1)) == 0);
+  const uint32_t firsts = __ballot_sync(0xFFFFFFFFu, mine >= 0 && (same & ((1u << lane) - 1)) == 0);
   if (static_cast<int>(blockIdx.y) >= __popc(firsts)) return;
   uint32_t left = firsts;
   for (int i = blockIdx.y; i > 0; --i) left &= left - 1;
   const int lead = __ffs(left) - 1;
   const int m = __shfl_sync(0xFFFFFFFFu, mine, lead);
   const uint32_t rows = __shfl_sync(0xFFFFFFFFu, same, lead);
+  const float factor = (a.scale != nullptr ? a.scale[m] : 1.0f) * undo_of(a.w_scale);
 
   const int g = lane / 4, t = lane % 4;
-  const bool low = rows >> g & 1, high = rows >> (g + 8) & 1;
   const uint16_t* x0 = a.x + static_cast<uint64_t>(row0 + g) * a.x_stride;
-  const uint16_t* x1 = x0 + 8 * a.x_stride;
   const uint16_t* from = a.a + m * a.a_stride;
-  float sum[kSteps][4] = {};
+  float sum[2][kSteps][4] = {};
   const uint4 zero = make_uint4(0, 0, 0, 0);
-#pragma unroll 4
-  for (int k0 = warp * 32; k0 < a.in; k0 += kShrinkWarps * 32) {
+#pragma unroll(kSteps <= 4 ? 4 : 1)
+  for (int k0 = warp * 32; k0 < a.in; k0 += kWarps * 32) {
     const int k = k0 + t * 8;
     const bool inside = k < a.in;
-    const uint4 p = low && inside ? *reinterpret_cast<const uint4*>(x0 + k) : zero;
-    const uint4 q = high && inside ? *reinterpret_cast<const uint4*>(x1 + k) : zero;
-    uint4 w[kSteps];
+    uint4 w[kSteps], v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      v[i] = inside && (rows >> (g + 8 * i) & 1) ? *reinterpret_cast<const uint4*>(x0 + 8 * i * a.x_stride + k) : zero;
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
       w[s] = inside && s * 8 + g < a.rank ? *reinterpret_cast<const uint4*>(from + static_cast<uint64_t>(s * 8 + g) * a.in + k) : zero;
-    const uint32_t first[4] = {p.x, q.x, p.y, q.y}, second[4] = {p.z, q.z, p.w, q.w};
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      mma_bf16(sum[s], first, w[s].x, w[s].y);
-      mma_bf16(sum[s], second, w[s].z, w[s].w);
+    for (int half = 0; half < 2; ++half) {
+      if (!(rows >> (16 * half) & 0xFFFFu)) continue;
+      const uint4 p = v[2 * half], q = v[2 * half + 1];
+      const uint32_t first[4] = {p.x, q.x, p.y, q.y}, second[4] = {p.z, q.z, p.w, q.w};
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        mma_bf16(sum[half][s], first, w[s].x, w[s].y);
+        mma_bf16(sum[half][s], second, w[s].z, w[s].w);
+      }
     }
   }
 #pragma unroll
-  for (int s = 0; s < kSteps; ++s) {
-    parts[warp][g][s * 8 + 2 * t] = sum[s][0];
-    parts[warp][g][s * 8 + 2 * t + 1] = sum[s][1];
-    parts[warp][g + 8][s * 8 + 2 * t] = sum[s][2];
-    parts[warp][g + 8][s * 8 + 2 * t + 1] = sum[s][3];
-  }
+  for (int half = 0; half < 2; ++half)
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        parts[(warp * kShrinkRows + half * 16 + g + i / 2 * 8) * kPitch + s * 8 + 2 * t + i % 2] = sum[half][s][i];
   __syncthreads();
-  const float factor = (a.scale != nullptr ? a.scale[m] : 1.0f) * undo_of(a.w_scale);
-  for (int i = threadIdx.x; i < 16 * a.padded; i += kShrinkWarps * 32) {
+  for (int i = threadIdx.x; i < kShrinkRows * a.padded; i += kWarps * 32) {
     const int n = i / a.padded, r = i % a.padded;
     if (!(rows >> n & 1)) continue;
     float h = 0.0f;
     if (r < a.rank) {
-      for (int w = 0; w < kShrinkWarps; ++w) h += parts[w][n][r];
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) h += parts[(w * kShrinkRows + n) * kPitch + r];
       h *= factor;
     }
     const uint32_t hi = pack_bf16(h, 0.0f) & 0xFFFFu;
@@ -155,6 +180,26 @@ shrink_kernel(const ShrinkArgs a) {
     // an infinite or NaN h has no second part
     const float rest = h - bf16_value(hi);
     to[a.padded] = static_cast<uint16_t>(pack_bf16(isfinite(rest) ? rest : 0.0f, 0.0f));
+  }
+}
+
+// --- rows that are named one by one ---------------------------------------------------------
+
+// Copies the rows of x that slots name (zeros for those that do not exist) so that they lie in order. A
+// warp has a slot.
+__global__ void __launch_bounds__(256)
+gather_kernel(const RowView rows, uint16_t* to, int in) {
+  wait_for_previous();
+  let_next_start();
+  const int lane = threadIdx.x % 32;
+  const int end = min(max(rows.start[rows.segments], 0), rows.rows);
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 8 + threadIdx.x / 32; i < end; i += static_cast<int64_t>(gridDim.x) * 8) {
+    const int from = rows.index[i];
+    const bool there = static_cast<unsigned>(from) < static_cast<unsigned>(rows.x_rows);
+    const uint4* x = reinterpret_cast<const uint4*>(rows.x + (there ? from : 0) * rows.x_stride);
+    uint4* y = reinterpret_cast<uint4*>(to + i * in);
+#pragma unroll 4
+    for (int k = lane; k < in / 8; k += 32) y[k] = there ? x[k] : make_uint4(0, 0, 0, 0);
   }
 }
 
@@ -223,6 +268,7 @@ struct Shape {
   static constexpr int kThreads = kFp8 ? 512 : 256;
 };
 
+constexpr int kPitch = kFeatures + 4;  // of a column of sums
 constexpr int kStaged = 16;  // columns that pass through shared memory together
 
 template <int kRows, bool kFp8>
@@ -231,30 +277,28 @@ struct Shared {
   uint8_t w[S::kStages][S::kW];
   uint8_t x[S::kStages][S::kX];
   uint8_t raw[kFp8 ? S::kStages : 1][kFp8 ? S::kRaw : 16];
-  float staged[2][kStaged][kFeatures + 4];
+  float staged[2][kStaged][kPitch];
   uint64_t full[S::kStages], ready[S::kStages], empty[S::kStages], sum_full[2], sum_empty[2], group, drained;
+  uint64_t join_full, join_done, turn;
   int before[ES_MAX_EXPERTS + 1];  // column tiles of the segments before each
   int sums[32];
   uint32_t tensor;
   int failed;
-  uint32_t order;
-  int4 named[2][kRows / 8];  // rows of the fours of each copying warp
+  int4 names[2][kRows / 8];  // rows of the fours of each copying warp
 };
 
 // What all roles need of a call's tiles. A tile is kFeatures features (gated: 64 and the 64 that
-// they are multiplied with) and up to kRows rows of a segment; a whole tile's depth is `depth`
-// stages. Tiles go to blocks in turn, or, where that leaves blocks idle, all tiles' stages
-// lie end to end and each block takes `per` of them.
+// they are multiplied with) and up to kRows rows of a segment; its depth is `depth` stages. Tiles go to
+// clusters in turn, and the blocks of a cluster have a share of the depth each.
 struct Plan {
   int columns, features, depth;  // tiles, tiles, stages
   int tiles;
-  int per;  // 0: whole tiles
+  int shares, rank;  // blocks of a cluster, and this one's place
 };
 
 struct Item {
   int row0, rows, group, f0;
   int k0, k1;  // stages
-  int tile, first, last;  // blocks that share the tile
 };
 
 template <class Sh>
@@ -262,36 +306,21 @@ struct Walk {
   const RowView& rows;
   const Sh& sh;
   Plan plan;
-  int at, end;  // tiles or stages
+  int at;
   int kRowsOf;
   bool gated;
 
   __device__ __forceinline__ Walk(const RowView& r, const Sh& s, const Plan& p, int tile_rows, bool g)
-      : rows(r), sh(s), plan(p), kRowsOf(tile_rows), gated(g) {
-    at = p.per > 0 ? static_cast<int>(min(static_cast<int64_t>(blockIdx.x) * p.per, static_cast<int64_t>(p.tiles) * p.depth))
-                   : blockIdx.x;
-    end = p.per > 0 ? static_cast<int>(min(static_cast<int64_t>(blockIdx.x + 1) * p.per, static_cast<int64_t>(p.tiles) * p.depth))
-                    : p.tiles;
-  }
+      : rows(r), sh(s), plan(p), at(blockIdx.x / p.shares), kRowsOf(tile_rows), gated(g) {}
 
   __device__ __forceinline__ bool next(Item& item) {
-    if (at >= end) return false;
-    if (plan.per > 0) {
-      item.tile = at / plan.depth;
-      item.k0 = at - item.tile * plan.depth;
-      item.k1 = min(plan.depth, item.k0 + end - at);
-      at += item.k1 - item.k0;
-      item.first = item.tile * plan.depth / plan.per;
-      item.last = (item.tile * plan.depth + plan.depth - 1) / plan.per;
-    } else {
-      item.tile = at;
-      item.k0 = 0;
-      item.k1 = plan.depth;
-      item.first = item.last = blockIdx.x;
-      at += gridDim.x;
-    }
-    const int band = item.tile / (kBand * plan.features);
-    const int rest = item.tile - band * kBand * plan.features;
+    if (at >= plan.tiles) return false;
+    const int tile = at;
+    at += gridDim.x / plan.shares;
+    item.k0 = plan.depth * plan.rank / plan.shares;
+    item.k1 = plan.depth * (plan.rank + 1) / plan.shares;
+    const int band = tile / (kBand * plan.features);
+    const int rest = tile - band * kBand * plan.features;
     const int wide = min(kBand, plan.columns - band * kBand);
     const int f = rest / wide;
     const int column = band * kBand + rest - f * wide;
@@ -349,7 +378,7 @@ __device__ __forceinline__ Extra extra_of(int padded, int i) {
 
 template <int kRows, bool kFp8, bool kGated>
 __global__ void __launch_bounds__(Shape<kRows, kFp8>::kThreads, 1)
-product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, uint32_t* counters, int* flag, float* parts, int tries, bool early,
+product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, int* flag, int tries, bool early, int shares,
                const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map,
                const __grid_constant__ CUtensorMap h_map, const __grid_constant__ CUtensorMap b_map) {
   using S = Shape<kRows, kFp8>;
@@ -370,6 +399,9 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       barrier_init(&sh.sum_empty[i], 4);
     }
     barrier_init(&sh.group, 4);
+    barrier_init(&sh.join_full, 4 * shares);
+    barrier_init(&sh.join_done, 4 * shares);
+    barrier_init(&sh.turn, 4);
     barrier_init(&sh.drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sh.failed = 0;
@@ -379,7 +411,8 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   fence_before();
-  __syncthreads();
+  if (shares > 1) cluster_sync();  // no block arrives at another's barriers before they are made
+  else __syncthreads();
   fence_after();
   // Behind the kernels of the adapters' part, which wait for all that came before them and then let
   // the next start, only what they make has to be waited for.
@@ -420,18 +453,19 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
     plan.columns = base;
   }
   plan.tiles = plan.columns * plan.features;
-  plan.per = 0;
-  const int grid = gridDim.x, waves = (plan.tiles + grid - 1) / grid;
-  if (plan.tiles <= kCounters && plan.tiles * 10 < waves * grid * 9)
-    plan.per = max(4, static_cast<int>((static_cast<int64_t>(plan.tiles) * plan.depth + grid - 1) / grid));
+  plan.shares = shares;
+  plan.rank = blockIdx.x % shares;
+  const bool named = rows.index != nullptr && !rows.copied;  // rows of x are asked for one by one
 
   if (warp == 0) {
     // --- copies
     Walk<Shared<kRows, kFp8>> walk(rows, sh, plan, kRows, kGated);
     Item item;
-    uint32_t done = 0;
+    uint32_t done = 0, items = 0;
     bool fine = true;
-    while (fine && walk.next(item)) {
+    for (; fine && walk.next(item); ++items) {
+      // the stages hold what the cluster's blocks have of the tile before
+      if (shares > 1 && items > 0 && !(fine = warp_wait(&sh.turn, (items - 1) & 1, watch))) break;
       const int padded = (item.rows + 15) & ~15;
       const int boxes = (padded + S::kBox - 1) / S::kBox;
       for (int k = item.k0; k < item.k1; ++k, ++done) {
@@ -439,11 +473,11 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         if (!(fine = warp_wait(&sh.empty[stage], (done / kStages & 1) ^ 1, watch))) break;
         const uint32_t x_to = shared_address(sh.x[stage]);
         if (elected()) {
-          barrier_expect(&sh.full[stage], (kFp8 ? S::kRaw : S::kW) + (rows.index != nullptr ? padded : boxes * S::kBox) * kDepth * 2);
+          barrier_expect(&sh.full[stage], (kFp8 ? S::kRaw : S::kW) + (named ? padded : boxes * S::kBox) * kDepth * 2);
           const uint32_t w_to = kFp8 ? shared_address(sh.raw[stage]) : shared_address(sh.w[stage]);
           load_box(&w_map, w_to, &sh.full[stage], k * kDepth, item.f0, item.group);
           load_box(&w_map, w_to + (kFp8 ? S::kRaw : S::kW) / 2, &sh.full[stage], k * kDepth, item.f0 + (kGated ? outs : 64), item.group);
-          if (rows.index == nullptr)
+          if (!named)
             for (int i = 0; i < boxes; ++i)
               load_box(&x_map, x_to + i * (S::kBox * kDepth * 2), &sh.full[stage], k * kDepth, item.row0 + i * S::kBox);
         }
@@ -532,13 +566,14 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
     barrier_settle(&sh.drained, 0);
   } else if (warp < 4) {
     // --- copies of rows that are named one by one, four at a time, half of them by each of two warps
-    if (rows.index != nullptr) {
+    if (named) {
       Walk<Shared<kRows, kFp8>> walk(rows, sh, plan, kRows, kGated);
       Item item;
       uint32_t done = 0;
       bool fine = true;
-      int4* named = sh.named[warp - 2];
-      while (fine && walk.next(item)) {
+      int4* names = sh.names[warp - 2];
+      for (uint32_t items = 0; fine && walk.next(item); ++items) {
+        if (shares > 1 && items > 0 && !(fine = warp_wait(&sh.turn, (items - 1) & 1, watch))) break;
         const int fours = (item.rows + 15) / 16 * 4;
         const int begin = warp == 2 ? 0 : fours / 2, end = warp == 2 ? fours / 2 : fours;
         __syncwarp();
@@ -550,7 +585,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
             v[q] = r < item.rows ? rows.index[item.row0 + r] : 0;
             if (static_cast<unsigned>(v[q]) >= static_cast<unsigned>(rows.x_rows)) v[q] = 0;
           }
-          named[lane] = make_int4(v[0], v[1], v[2], v[3]);
+          names[lane] = make_int4(v[0], v[1], v[2], v[3]);
         }
         __syncwarp();
         for (int k = item.k0; k < item.k1; ++k, ++done) {
@@ -560,7 +595,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
             const uint32_t x_to = shared_address(sh.x[stage]);
 #pragma unroll 4
             for (int i = begin; i < end; ++i)
-              gather_rows(&x_map, x_to + i * (4 * kDepth * 2), &sh.full[stage], k * kDepth, named[i - begin]);
+              gather_rows(&x_map, x_to + i * (4 * kDepth * 2), &sh.full[stage], k * kDepth, names[i - begin]);
           }
           __syncwarp();
         }
@@ -586,107 +621,123 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       if (!(fine = warp_wait(&sh.sum_full[half], items / 2 & 1, watch))) break;
       fence_after();
       const uint32_t sum = sh.tensor + half * 256 + (static_cast<uint32_t>(mine) << 21);
-      const bool alone = item.first == item.last;
-      if (!alone) {
-        const int slot = 2 * blockIdx.x + (item.k0 == 0 ? 1 : 0);
-        float* to = parts + static_cast<uint64_t>(slot) * kRows * kFeatures + feature;
+      float scale = kFp8 ? *(w.scale + item.group) : 1.0f;
+      if (kFp8 && expand.h != nullptr && isinf(1.0f / scale)) scale = 1.0f;
+      // Sums of the lane's features of a column to y: gated two features and the two that they are
+      // multiplied with, else four.
+      auto finish = [&](int column, float4 z) {
+        const int row = item.row0 + column;
+        const bool absent = rows.index != nullptr && static_cast<unsigned>(rows.index[row]) >= static_cast<unsigned>(rows.x_rows);
+        if (kGated) {
+          const int f = item.f0 + lane * 2;
+          if (f >= outs) return;
+          const float g0 = z.x * scale, g1 = z.y * scale;
+          const uint32_t y = pack_bf16(g0 / (1.0f + expf(-g0)) * (z.z * scale), g1 / (1.0f + expf(-g1)) * (z.w * scale));
+          *reinterpret_cast<uint32_t*>(rows.y + row * rows.y_stride + f) = absent ? 0 : y;
+          return;
+        }
+        const int f = item.f0 + lane * 4;
+        if (f >= outs) return;
+        float y[4] = {z.x, z.y, z.z, z.w};
+        if (expand.h != nullptr && expand.of_block[row / kBlock] == kMixed) {
+          const int m = expand.of_row[row];
+          if (m >= 0 && expand.extra != nullptr) {
+            const float4 v = *reinterpret_cast<const float4*>(expand.extra + static_cast<uint64_t>(row) * outs + f);
+            y[0] += v.x;
+            y[1] += v.y;
+            y[2] += v.z;
+            y[3] += v.w;
+          } else if (m >= 0) {
+            const uint16_t* h = expand.h + static_cast<uint64_t>(row) * 2 * expand.padded;
+            const uint16_t* b = expand.b + m * expand.b_stride + static_cast<uint64_t>(f) * expand.rank;
+            for (int r = 0; r < expand.rank; r += 8) {
+              const uint4 p = *reinterpret_cast<const uint4*>(h + r), q = *reinterpret_cast<const uint4*>(h + expand.padded + r);
+              const uint32_t pw[4] = {p.x, p.y, p.z, p.w}, qw[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+              for (int n = 0; n < 4; ++n) {
+                const uint4 o = *reinterpret_cast<const uint4*>(b + n * expand.rank + r);
+                const uint32_t ow[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                  y[n] = fmaf(bf16_value(pw[d]) + bf16_value(qw[d]), bf16_value(ow[d]), y[n]);
+                  y[n] = fmaf(bf16_high(pw[d]) + bf16_high(qw[d]), bf16_high(ow[d]), y[n]);
+                }
+              }
+            }
+          }
+        }
+        const uint2 out = make_uint2(pack_bf16(y[0] * scale, y[1] * scale), pack_bf16(y[2] * scale, y[3] * scale));
+        *reinterpret_cast<uint2*>(rows.y + row * rows.y_stride + f) = absent ? make_uint2(0, 0) : out;
+      };
+      if (shares > 1) {
+        // The blocks' sums of their depth meet in shared memory, where the stages were: each adds up a share of
+        // the columns, in the order of the blocks.
+        float* whole = reinterpret_cast<float*>(sh.w);
         for (int c = 0; c < item.rows; c += kStaged) {
           uint32_t r[kStaged];
           tensor_load(r, sum + c);
           tensor_loaded(r);
 #pragma unroll
-          for (int i = 0; i < kStaged; ++i)
-            if (c + i < item.rows) to[(c + i) * kFeatures] = __uint_as_float(r[i]);
+          for (int i = 0; i < kStaged; ++i) whole[(c + i) * kPitch + feature] = __uint_as_float(r[i]);
         }
         fence_before();
-        if (!(fine = group_sync())) break;
-        if (feature == 0) sh.order = count_done(&counters[item.tile]);
-        if (!(fine = group_sync())) break;
-        const bool last = sh.order == static_cast<uint32_t>(item.last - item.first);
+        __syncwarp();
         if (lane == 0) barrier_arrive(&sh.sum_empty[half]);
-        if (!(fine = group_sync())) break;  // before the next item's count
-        if (!last) continue;
-        if (feature == 0) counters[item.tile] = 0;
+        if (lane < shares) barrier_arrive_at(address_in(shared_address(&sh.join_full), lane));
+        if (!(fine = cluster_wait(&sh.join_full, items & 1, watch))) break;
+        const int width = (item.rows + shares - 1) / shares;
+        const int end = min(item.rows, (plan.rank + 1) * width);
+        const uint32_t base = shared_address(whole) + (kGated ? lane * 8 : lane * 16);
+#pragma unroll 2
+        for (int c = plan.rank * width + mine; c < end; c += 4) {
+          float4 v[kMostShares];
+#pragma unroll
+          for (int q = 0; q < kMostShares; ++q)
+            if (q < shares) {
+              const uint32_t from = address_in(base + c * (kPitch * 4), q);
+              v[q] = kGated ? load_pairs(from, from + kFeatures * 2) : load_from(from);
+            }
+          float4 z = v[0];
+#pragma unroll
+          for (int q = 1; q < kMostShares; ++q)
+            if (q < shares) {
+              z.x += v[q].x;
+              z.y += v[q].y;
+              z.z += v[q].z;
+              z.w += v[q].w;
+            }
+          finish(c, z);
+        }
+        __syncwarp();
+        if (lane < shares) barrier_arrive_at(address_in(shared_address(&sh.join_done), lane));
+        if (!(fine = cluster_wait(&sh.join_done, items & 1, watch))) break;
+        fence_async();  // the stages are written by copies next
+        warp_arrive(&sh.turn, lane);
+        continue;
       }
-      float scale = kFp8 ? *(w.scale + item.group) : 1.0f;
-      if (kFp8 && expand.h != nullptr && isinf(1.0f / scale)) scale = 1.0f;
       for (int c = 0; c < item.rows; c += kStaged, ++chunks) {
-        float v[kStaged];
-        if (alone) {
-          uint32_t r[kStaged];
-          tensor_load(r, sum + c);
-          tensor_loaded(r);
-#pragma unroll
-          for (int i = 0; i < kStaged; ++i) v[i] = __uint_as_float(r[i]);
-          if (c + kStaged >= item.rows) {
-            fence_before();
-            __syncwarp();
-            if (lane == 0) barrier_arrive(&sh.sum_empty[half]);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < kStaged; ++i) v[i] = 0.0f;
-          for (int b = item.first; b <= item.last; ++b) {
-            const int slot = 2 * b + (b == item.first ? 1 : 0);
-            const float* part = parts + static_cast<uint64_t>(slot) * kRows * kFeatures + feature;
-#pragma unroll
-            for (int i = 0; i < kStaged; ++i)
-              if (c + i < item.rows) v[i] += __ldcg(part + (c + i) * kFeatures);
-          }
+        uint32_t r[kStaged];
+        tensor_load(r, sum + c);
+        tensor_loaded(r);
+        if (c + kStaged >= item.rows) {
+          fence_before();
+          __syncwarp();
+          if (lane == 0) barrier_arrive(&sh.sum_empty[half]);
         }
         auto& staged = sh.staged[chunks & 1];
 #pragma unroll
-        for (int i = 0; i < kStaged; ++i) staged[i][feature] = v[i];
+        for (int i = 0; i < kStaged; ++i) staged[i][feature] = __uint_as_float(r[i]);
         if (!(fine = group_sync())) break;
 #pragma unroll
         for (int i = 0; i < kStaged / 4; ++i) {
           const int column = mine * (kStaged / 4) + i;
-          const int row = item.row0 + c + column;
           if (c + column >= item.rows) continue;
           if (kGated) {
-            const int f = item.f0 + lane * 2;
             const float2 gate = *reinterpret_cast<const float2*>(&staged[column][lane * 2]);
             const float2 up = *reinterpret_cast<const float2*>(&staged[column][64 + lane * 2]);
-            const float g0 = gate.x * scale, g1 = gate.y * scale;
-            uint32_t y = pack_bf16(g0 / (1.0f + expf(-g0)) * (up.x * scale), g1 / (1.0f + expf(-g1)) * (up.y * scale));
-            if (rows.index != nullptr && static_cast<unsigned>(rows.index[row]) >= static_cast<unsigned>(rows.x_rows)) y = 0;
-            if (f < outs) *reinterpret_cast<uint32_t*>(rows.y + row * rows.y_stride + f) = y;
+            finish(c + column, make_float4(gate.x, gate.y, up.x, up.y));
           } else {
-            const int f = item.f0 + lane * 4;
-            if (f >= outs) continue;
-            const float4 z = *reinterpret_cast<const float4*>(&staged[column][lane * 4]);
-            float y[4] = {z.x, z.y, z.z, z.w};
-            if (expand.h != nullptr && expand.of_block[row / kBlock] == kMixed) {
-              const int m = expand.of_row[row];
-              if (m >= 0 && expand.extra != nullptr) {
-                const float4 v = *reinterpret_cast<const float4*>(expand.extra + static_cast<uint64_t>(row) * outs + f);
-                y[0] += v.x;
-                y[1] += v.y;
-                y[2] += v.z;
-                y[3] += v.w;
-              } else if (m >= 0) {
-                const uint16_t* h = expand.h + static_cast<uint64_t>(row) * 2 * expand.padded;
-                const uint16_t* b = expand.b + m * expand.b_stride + static_cast<uint64_t>(f) * expand.rank;
-                for (int r = 0; r < expand.rank; r += 8) {
-                  const uint4 p = *reinterpret_cast<const uint4*>(h + r), q = *reinterpret_cast<const uint4*>(h + expand.padded + r);
-                  const uint32_t pw[4] = {p.x, p.y, p.z, p.w}, qw[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-                  for (int n = 0; n < 4; ++n) {
-                    const uint4 o = *reinterpret_cast<const uint4*>(b + n * expand.rank + r);
-                    const uint32_t ow[4] = {o.x, o.y, o.z, o.w};
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) {
-                      y[n] = fmaf(bf16_value(pw[d]) + bf16_value(qw[d]), bf16_value(ow[d]), y[n]);
-                      y[n] = fmaf(bf16_high(pw[d]) + bf16_high(qw[d]), bf16_high(ow[d]), y[n]);
-                    }
-                  }
-                }
-              }
-            }
-            uint2 out = make_uint2(pack_bf16(y[0] * scale, y[1] * scale), pack_bf16(y[2] * scale, y[3] * scale));
-            if (rows.index != nullptr && static_cast<unsigned>(rows.index[row]) >= static_cast<unsigned>(rows.x_rows))
-              out = make_uint2(0, 0);
-            *reinterpret_cast<uint2*>(rows.y + row * rows.y_stride + f) = out;
+            finish(c + column, *reinterpret_cast<const float4*>(&staged[column][lane * 4]));
           }
         }
       }
@@ -735,7 +786,8 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
   __syncwarp();
   let_next_start();
   fence_before();
-  __syncthreads();
+  if (shares > 1) cluster_sync();  // no block leaves while others read its sums or arrive at its barriers
+  else __syncthreads();
   fence_after();
   if (threadIdx.x == 0 && sh.failed) *flag = 1;
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tensor) : "memory");
@@ -760,34 +812,70 @@ es_status_t map_rows(CUtensorMap* map, const void* base, uint64_t width, uint64_
   return ES_OK;
 }
 
-uint64_t parts_bytes(int tile_rows) { return uint64_t{2} * kMaxGrid * tile_rows * kFeatures * sizeof(float); }
-
 template <int kRows, bool kFp8, bool kGated>
 es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView& rows, const ExpandView& expand, const CUtensorMap* b_map,
-                   char* workspace, cudaStream_t stream, const char* call) {
+                   int columns, int join, bool early, char* workspace, cudaStream_t stream, const char* call) {
   using S = Shape<kRows, kFp8>;
   auto kernel = product_kernel<kRows, kFp8, kGated>;
   constexpr int kBytes = static_cast<int>(sizeof(Shared<kRows, kFp8>)) + 1024;
   static_assert(kBytes <= 232448, "shared memory of a block");
   int device = 0;
   cudaGetDevice(&device);
-  // SMs of each device whose kernel has been given its shared memory
-  static std::atomic<int> sms_of[64];
-  int sms = device < 64 ? sms_of[device].load(std::memory_order_relaxed) : 0;
-  if (sms == 0) {
+  // Clusters of 1 to kMostShares blocks that each device holds at once, of a kernel that has been given its
+  // shared memory.
+  static std::atomic<int> held[64][kMostShares + 1];
+  int clusters[kMostShares + 1];
+  if (device < 64 && held[device][1].load(std::memory_order_acquire) != 0) {
+    for (int i = 1; i <= kMostShares; ++i) clusters[i] = held[device][i].load(std::memory_order_relaxed);
+  } else {
     cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
-    if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (err == cudaSuccess) err = cudaDeviceGetAttribute(&clusters[1], cudaDevAttrMultiProcessorCount, device);
+    for (int i = 2; i <= kMostShares && err == cudaSuccess; ++i) {
+      cudaLaunchConfig_t config{};
+      cudaLaunchAttribute attr{};
+      attr.id = cudaLaunchAttributeClusterDimension;
+      attr.val.clusterDim.x = static_cast<unsigned>(i);
+      attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+      config.gridDim = dim3(static_cast<unsigned>(i));
+      config.blockDim = dim3(S::kThreads);
+      config.dynamicSmemBytes = kBytes;
+      config.attrs = &attr;
+      config.numAttrs = 1;
+      if (cudaOccupancyMaxActiveClusters(&clusters[i], kernel, &config) != cudaSuccess) {
+        cudaGetLastError();
+        clusters[i] = 0;
+      }
+    }
     if (err != cudaSuccess) {
       cudaGetLastError();
       return cuda_fail(err, call);
     }
-    if (device < 64) sms_of[device].store(sms, std::memory_order_relaxed);
+    if (device < 64) {
+      for (int i = kMostShares; i > 1; --i) held[device][i].store(clusters[i], std::memory_order_relaxed);
+      held[device][1].store(clusters[1], std::memory_order_release);
+    }
   }
+  // The number of blocks that share a tile's depth: the one whose rounds of tiles take the fewest stages. To
+  // join costs as much as some.
+  const int outs = kGated ? w.out / 2 : w.out, wide = kGated ? kFeatures / 2 : kFeatures;
+  const int64_t tiles = static_cast<int64_t>(columns) * ((outs + wide - 1) / wide);
+  const int depth = (w.in + kDepth - 1) / kDepth;
+  int shares = 1;
+  int64_t best = INT64_MAX;
+  for (int i = 1; i <= kMostShares && i <= depth; ++i) {
+    if (clusters[i] < 1) continue;
+    const int64_t cost = (tiles + clusters[i] - 1) / clusters[i] * ((depth + i - 1) / i + (i > 1 ? join : 0));
+    if (cost < best) {
+      best = cost;
+      shares = i;
+    }
+  }
+  const int grid = static_cast<int>(std::min<int64_t>(tiles, clusters[shares])) * shares;
   CUtensorMap x_map, h_map;
   es_status_t st;
   // without rows of x every slot is absent: what is read in their place does not matter
   if (rows.x_rows > 0)
-    st = map_rows(&x_map, rows.x, w.in, rows.x_rows, rows.x_stride, rows.index != nullptr ? 1 : S::kBox, call);
+    st = map_rows(&x_map, rows.x, w.in, rows.copied ? rows.rows : rows.x_rows, rows.x_stride, rows.index != nullptr && !rows.copied ? 1 : S::kBox, call);
   else
     st = map_rows(&x_map, w.data, w.in, 1, w.in, 1, call);
   if (st != ES_OK) return st;
@@ -795,20 +883,33 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
   if (expand.h != nullptr &&
       (st = map_rows(&h_map, expand.h, 2 * expand.padded, rows.rows, 2 * expand.padded, S::kBox, call)) != ES_OK)
     return st;
-  const cudaError_t err =
-      launch_early(kernel, std::min(sms, kMaxGrid), S::kThreads, kBytes, stream, w, rows, expand,
-                   reinterpret_cast<uint32_t*>(workspace), reinterpret_cast<int*>(workspace + ES_PROJECT_GAVE_UP),
-                   reinterpret_cast<float*>(workspace + kHead), tries_of_a_wait.load(std::memory_order_relaxed), expand.h != nullptr, w_map, x_map, h_map,
-                   expand.h != nullptr ? *b_map : x_map);
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(shares);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t config{};
+  config.gridDim = dim3(static_cast<unsigned>(grid));
+  config.blockDim = dim3(S::kThreads);
+  config.dynamicSmemBytes = kBytes;
+  config.stream = stream;
+  config.attrs = attr;
+  config.numAttrs = shares > 1 ? 2 : 1;
+  cudaError_t err = cudaLaunchKernelEx(&config, kernel, w, rows, expand, reinterpret_cast<int*>(workspace + ES_PROJECT_GAVE_UP),
+                                       tries_of_a_wait.load(std::memory_order_relaxed), early, shares, w_map, x_map, h_map,
+                                       expand.h != nullptr ? *b_map : x_map);
+  const cudaError_t last = cudaGetLastError();
+  if (err == cudaSuccess) err = last;
   return err != cudaSuccess ? cuda_fail(err, call) : ES_OK;
 }
 
 template <int kRows>
 es_status_t launch_rows(const MatrixView& w, const CUtensorMap& w_map, bool fp8, bool gated, const RowView& rows, const ExpandView& expand,
-                        const CUtensorMap* b_map, char* workspace, cudaStream_t stream, const char* call) {
+                        const CUtensorMap* b_map, int columns, int join, bool early, char* workspace, cudaStream_t stream, const char* call) {
   auto f = fp8 ? (gated ? launch<kRows, true, true> : launch<kRows, true, false>)
                : (gated ? launch<kRows, false, true> : launch<kRows, false, false>);
-  return f(w, w_map, rows, expand, b_map, workspace, stream, call);
+  return f(w, w_map, rows, expand, b_map, columns, join, early, workspace, stream, call);
 }
 
 constexpr int kFew = 64, kMany = 256;  // rows of a tile
@@ -819,19 +920,34 @@ uint64_t rounded(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // A launch of a grid of two axes that may begin early.
 template <class... P, class... A>
-cudaError_t launch_grid(void (*kernel)(P...), dim3 grid, int block, cudaStream_t stream, const A&... args) {
+cudaError_t launch_grid(void (*kernel)(P...), dim3 grid, int block, size_t shared, cudaStream_t stream, const A&... args) {
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t config{};
   config.gridDim = grid;
   config.blockDim = dim3(static_cast<unsigned>(block));
+  config.dynamicSmemBytes = shared;
   config.stream = stream;
   config.attrs = &attr;
   config.numAttrs = 1;
   const cudaError_t err = cudaLaunchKernelEx(&config, kernel, P(args)...);
   const cudaError_t last = cudaGetLastError();
   return err != cudaSuccess ? err : last;
+}
+
+template <int kSteps>
+cudaError_t launch_shrink(const ShrinkArgs& a, cudaStream_t stream) {
+  constexpr int kBytes = kShrinkBytes<kSteps>;
+  if (kBytes > 48 * 1024) {
+    const cudaError_t err = cudaFuncSetAttribute(shrink_kernel<kSteps>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    if (err != cudaSuccess) {
+      cudaGetLastError();
+      return err;
+    }
+  }
+  const int most = std::min(std::min(a.requests, a.rows), kShrinkRows);  // adapters that the rows of a block can have
+  return launch_grid(shrink_kernel<kSteps>, dim3((a.rows + kShrinkRows - 1) / kShrinkRows, most), kShrinkWarps<kSteps> * 32, kBytes, stream, a);
 }
 
 }  // namespace
@@ -855,14 +971,16 @@ es_status_t map_matrices(CUtensorMap* map, const void* data, uint64_t in, uint64
   return ES_OK;
 }
 
-// Behind the head: parts of tiles that blocks share; h; the adapters of rows and blocks; B h of up to
-// kMostExtra rows.
-uint64_t project_workspace_bytes(int rank, int rows, int out) {
+// Behind the head: with adapters h, the adapters of rows and blocks, and B h of up to kMostExtra rows;
+// without, rows that are copied in order.
+uint64_t project_workspace_bytes(int rank, int rows, int in, int out) {
   const uint64_t n = rows;
-  uint64_t bytes = kHead + parts_bytes(rows > kFew ? kMany : kFew);
-  if (rank > 0) bytes += rounded(n * 4 * padded_rank(rank)) + 2 * rounded(n * 4) + rounded(std::min(rows, kMostExtra) * uint64_t{4} * out);
-  return bytes;
+  if (rank == 0) return kHead + (rows > kFew ? rounded(n * in * 2) : 0);
+  return kHead + rounded(n * 4 * padded_rank(rank)) + 2 * rounded(n * 4) + rounded(std::min(rows, kMostExtra) * uint64_t{4} * out);
 }
+
+// Stages that a join of up to `rows` columns takes the time of.
+int join_of(int rows) { return 4 + rows / 32; }
 
 es_status_t launch_project(const MatrixView& w, const CUtensorMap& w_map, bool fp8, const AdapterView* adapters, const CUtensorMap* b_map,
                            const int32_t* adapter, const RowView& rows, void* workspace, cudaStream_t stream, const char* call) {
@@ -871,36 +989,55 @@ es_status_t launch_project(const MatrixView& w, const CUtensorMap& w_map, bool f
   if (adapters != nullptr) {
     const uint64_t n = rows.rows;
     const int padded = static_cast<int>(padded_rank(adapters->rank));
-    char* behind = at + kHead + parts_bytes(rows.rows > kFew ? kMany : kFew);
+    char* behind = at + kHead;
     uint16_t* h = reinterpret_cast<uint16_t*>(behind);
     int32_t* of_row = reinterpret_cast<int32_t*>(behind + rounded(n * 4 * padded));
     int32_t* of_block = reinterpret_cast<int32_t*>(behind + rounded(n * 4 * padded) + rounded(n * 4));
     const ShrinkArgs a{rows.x, rows.start, adapter, adapters->a, adapters->scale, w.scale, h, of_row, of_block, rows.x_stride,
                        adapters->a_stride, rows.segments, rows.rows, adapters->count, adapters->rank, padded, w.in};
     const int steps = (adapters->rank + 7) / 8;
-    auto shrink = steps <= 1 ? shrink_kernel<1> : steps <= 2 ? shrink_kernel<2> : steps <= 4 ? shrink_kernel<4>
-                : steps <= 8 ? shrink_kernel<8> : shrink_kernel<16>;
-    const int most = std::min(std::min(rows.segments, rows.rows), kBlock);  // adapters that 16 rows can have
-    cudaError_t err = launch_grid(shrink, dim3((rows.rows + kBlock - 1) / kBlock, most), kShrinkWarps * 32, stream, a);
+    cudaError_t err = steps <= 1   ? launch_shrink<1>(a, stream)
+                      : steps <= 2 ? launch_shrink<2>(a, stream)
+                      : steps <= 4 ? launch_shrink<4>(a, stream)
+                      : steps <= 8 ? launch_shrink<8>(a, stream)
+                                   : launch_shrink<16>(a, stream);
     if (err != cudaSuccess) return cuda_fail(err, call);
     expand = ExpandView{h, adapters->b, of_row, of_block, nullptr, adapters->b_stride, adapters->rank, padded};
-    if (most > 1 && rows.rows <= kMostExtra) {
+    if (std::min(rows.segments, rows.rows) > 1 && rows.rows <= kMostExtra) {
       float* extra = reinterpret_cast<float*>(behind + rounded(n * 4 * padded) + 2 * rounded(n * 4));
       auto kernel = adapters->rank % 16 == 0 ? expand_kernel<16> : expand_kernel<8>;
       err = launch_grid(kernel, dim3((w.out + kExpandWarps * kFeatures - 1) / (kExpandWarps * kFeatures), (rows.rows + kExpandRows - 1) / kExpandRows),
-                        kExpandWarps * 32, stream, expand, rows.start, extra, rows.segments, rows.rows, w.out);
+                        kExpandWarps * 32, 0, stream, expand, rows.start, extra, rows.segments, rows.rows, w.out);
       if (err != cudaSuccess) return cuda_fail(err, call);
       expand.extra = extra;
     }
   }
-  auto f = rows.rows > kFew ? launch_rows<kMany> : launch_rows<kFew>;
-  return f(w, w_map, fp8, false, rows, expand, b_map, at, stream, call);
+  const int tile = rows.rows > kFew ? kMany : kFew;
+  auto f = tile == kMany ? launch_rows<kMany> : launch_rows<kFew>;
+  return f(w, w_map, fp8, false, rows, expand, b_map, (rows.rows + tile - 1) / tile, join_of(std::min(rows.rows, tile)), adapters != nullptr,
+           at, stream, call);
 }
 
 es_status_t launch_experts(const MatrixView& w, const CUtensorMap& w_map, bool fp8, bool gated, const RowView& rows, void* workspace,
                            cudaStream_t stream, const char* call) {
-  auto f = rows.rows > kFew && rows.rows / w.groups > 32 ? launch_rows<kMany> : launch_rows<kFew>;
-  return f(w, w_map, fp8, gated, rows, ExpandView{}, nullptr, static_cast<char*>(workspace), stream, call);
+  char* at = static_cast<char*>(workspace);
+  const int tile = rows.rows > kFew && rows.rows / w.groups > 32 ? kMany : kFew;
+  RowView r = rows;
+  bool early = false;
+  if (tile == kMany && rows.index != nullptr && rows.x_rows > 0) {
+    uint16_t* copy = reinterpret_cast<uint16_t*>(at + kHead);
+    const cudaError_t err = launch_early(gather_kernel, std::min((rows.rows + 7) / 8, 152 * 8), 256, 0, stream, rows, copy, w.in);
+    if (err != cudaSuccess) return cuda_fail(err, call);
+    r.x = copy;
+    r.x_stride = w.in;
+    r.copied = true;
+  }
+  // column tiles as they are where rows are spread evenly
+  const int segments = std::min(rows.rows, w.groups);
+  const int each = (rows.rows + segments - 1) / segments;
+  auto f = tile == kMany ? launch_rows<kMany> : launch_rows<kFew>;
+  return f(w, w_map, fp8, gated, r, ExpandView{}, nullptr, segments * ((each + tile - 1) / tile), join_of(std::min(each, tile)), early, at,
+           stream, call);
 }
 
 }  // namespace esopt

@@ -166,7 +166,7 @@ es_status_t es_adapters_destroy(es_adapters_t adapters) {
 
 uint64_t es_project_workspace(es_weights_t weights, es_adapters_t adapters, int rows) {
   if (weights == nullptr || rows < 0 || rows > ES_MAX_ROWS) return 0;
-  return esopt::project_workspace_bytes(adapters != nullptr ? adapters->view.rank : 0, rows, weights->view.out);
+  return esopt::project_workspace_bytes(adapters != nullptr ? adapters->view.rank : 0, rows, weights->view.in, weights->view.out);
 }
 
 es_status_t es_project(es_weights_t w, es_adapters_t m, const es_project_t* a, void* workspace, uint64_t workspace_bytes,
@@ -201,7 +201,7 @@ es_status_t es_project(es_weights_t w, es_adapters_t m, const es_project_t* a, v
   if ((st = check_optional(a->adapter, 4, dev, call, "adapter")) != ES_OK) return st;
   if ((st = check_workspace(workspace, workspace_bytes, es_project_workspace(w, m, a->rows), dev, call)) != ES_OK) return st;
   const esopt::RowView rows{static_cast<const uint16_t*>(a->x), static_cast<uint16_t*>(a->y), a->start, nullptr, nullptr,
-                            a->x_stride, a->y_stride, a->requests, a->rows, a->rows, true};
+                            a->x_stride, a->y_stride, a->requests, a->rows, a->rows, true, false};
   st = esopt::launch_project(v, w->map, w->dtype == ES_FP8_E4M3, m != nullptr ? &m->view : nullptr, m != nullptr ? &m->map : nullptr,
                              a->adapter, rows, workspace, static_cast<cudaStream_t>(stream), call);
   return st == ES_OK ? ok() : st;
@@ -232,7 +232,7 @@ es_status_t es_project_experts(es_weights_t w, const es_project_experts_t* a, vo
   if ((st = check_buffer(a->y, 16, dev, call, "y")) != ES_OK) return st;
   if ((st = check_workspace(workspace, workspace_bytes, es_project_workspace(w, nullptr, a->slots), dev, call)) != ES_OK) return st;
   const esopt::RowView rows{static_cast<const uint16_t*>(a->x), static_cast<uint16_t*>(a->y), a->start, nullptr, a->rows,
-                            a->x_stride, a->y_stride, v.groups, a->slots, a->x_rows, false};
+                            a->x_stride, a->y_stride, v.groups, a->slots, a->x_rows, false, false};
   st = esopt::launch_experts(v, w->map, w->dtype == ES_FP8_E4M3, a->gated != 0, rows, workspace, static_cast<cudaStream_t>(stream), call);
   return st == ES_OK ? ok() : st;
 }

@@ -38,6 +38,7 @@ struct RowView {
   uint64_t x_stride, y_stride;
   int segments, rows, x_rows;
   bool joined;  // all segments are one, through matrix 0
+  bool copied;  // x holds the rows that index names already, in order
 };
 
 #ifdef __CUDACC__
@@ -64,7 +65,7 @@ es_status_t launch_project(const MatrixView& w, const CUtensorMap& w_map, bool f
                            const int32_t* adapter, const RowView& rows, void* workspace, cudaStream_t stream, const char* call);
 es_status_t launch_experts(const MatrixView& w, const CUtensorMap& w_map, bool fp8, bool gated, const RowView& rows, void* workspace,
                            cudaStream_t stream, const char* call);
-uint64_t project_workspace_bytes(int rank, int rows, int out);  // rank 0: no adapters
+uint64_t project_workspace_bytes(int rank, int rows, int in, int out);  // rank 0: no adapters
 // For tests: tries after which the products' waits are given up in calls from now on (0: at once;
 // negative: as it was).
 void set_project_wait_tries(int tries);
