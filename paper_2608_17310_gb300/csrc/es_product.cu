@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cstdlib>
 
 #include "es_attention.cuh"
 #include "es_checks.h"
@@ -23,6 +24,10 @@ constexpr uint64_t kHead = ES_PROJECT_GAVE_UP + 256;
 
 // What a block of 16 rows has: one adapter for all of them, none, or several.
 constexpr int kNone = -1, kMixed = -2;
+
+// What a column of a tile is, beside the adapter that is still to be added to it: nothing is, its row
+// of x does not exist, it is not there.
+constexpr int kPlain = -1, kAbsent = -2, kOut = -3;
 
 // The adapters' part of a product: h = scale (A x) as the sum of two bf16 numbers, [rows][2][padded rank].
 struct ExpandView {
@@ -55,10 +60,7 @@ struct ShrinkArgs {
 };
 
 constexpr int kShrinkRows = 32;
-template <int kSteps>
-constexpr int kShrinkWarps = kSteps <= 2 ? 16 : kSteps <= 8 ? 8 : 4;
-template <int kSteps>
-constexpr int kShrinkBytes = kShrinkWarps<kSteps> * kShrinkRows * (kSteps * 8 + 1) * 4;
+constexpr int kShrinkWarps = 4;
 
 // 1 / scale where the matrix's codes are multiplied by their scale in the end and the adapters'
 // part must not be; 1 where that is infinite: then the codes count as zeros.
@@ -71,7 +73,22 @@ __device__ __forceinline__ float undo_of(const float* w_scale) {
 __device__ __forceinline__ int adapter_of_lane(const ShrinkArgs& a, int row0, int end, int lane) {
   const int row = row0 + lane;
   int r = row;
-  if (a.start != nullptr && row0 < end) {
+  if (a.start != nullptr && a.requests <= 128) {
+    // all starts at once: row0 + i is in the request before the first that starts behind it
+    int begins[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) begins[j] = j * 32 + lane < a.requests ? a.start[j * 32 + lane] : INT32_MAX;
+    r = -1;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (j * 32 >= a.requests) break;
+      for (int i = 0; i < 32; ++i) {
+        const int n = __popc(__ballot_sync(0xFFFFFFFFu, begins[j] <= row0 + i));
+        if (lane == i) r += n;
+      }
+    }
+    r = max(r, 0);
+  } else if (a.start != nullptr && row0 < end) {
     // The last request that starts at or before row0, 32 starts at a time.
     int lo = 0, span = a.requests;  // among [lo, lo + span)
     while (span > 1) {
@@ -98,13 +115,13 @@ __device__ __forceinline__ int adapter_of_lane(const ShrinkArgs& a, int row0, in
   return static_cast<unsigned>(m) < static_cast<unsigned>(a.count) ? m : kNone;
 }
 
-// h of 32 rows with the (blockIdx.y)-th adapter among them, and which adapters rows and blocks
-// have. The warps share the depth; the two products of a lane's 16 bytes of x and A take its
-// elements in the order in which they lie, the same in both, so each is one load.
+// h of 32 rows with each adapter among them (shared out along blockIdx.y), and which adapters rows and
+// blocks have. The warps of the cluster's gridDim.z blocks share the depth; the two products of a lane's 16 bytes of
+// x and A take its elements in the order in which they lie, the same in both, so each is one load.
 template <int kSteps>  // of 8 ranks
-__global__ void __launch_bounds__(kShrinkWarps<kSteps> * 32)
+__global__ void __launch_bounds__(kShrinkWarps * 32)
 shrink_kernel(const ShrinkArgs a) {
-  constexpr int kWarps = kShrinkWarps<kSteps>, kPitch = kSteps * 8 + 1;
+  constexpr int kWarps = kShrinkWarps, kPitch = kSteps * 8 + 1;
   extern __shared__ float parts[];  // [warp][row][kPitch]
   wait_for_previous();
   let_next_start();
@@ -114,47 +131,74 @@ shrink_kernel(const ShrinkArgs a) {
   const int mine = adapter_of_lane(a, row0, end, lane);
   const uint32_t there = __ballot_sync(0xFFFFFFFFu, row0 + lane < end);
   const uint32_t same = __match_any_sync(0xFFFFFFFFu, mine) & there;
-  if (blockIdx.y == 0 && warp == 0) {
-    if (row0 + lane < end) a.of_row[row0 + lane] = mine;
+  if (blockIdx.y == 0 && blockIdx.z == 0 && warp == 0) {
+    if (row0 + lane < a.rows) a.of_row[row0 + lane] = mine;
     const uint32_t block = 0xFFFFu << (lane & 16);
-    if (lane % kBlock == 0 && (there & block) != 0)
+    if (lane % kBlock == 0 && row0 + lane < a.rows)
       a.of_block[(row0 + lane) / kBlock] = (same & block) == (there & block) ? mine : kMixed;
   }
   const uint32_t firsts = __ballot_sync(0xFFFFFFFFu, mine >= 0 && (same & ((1u << lane) - 1)) == 0);
-  if (static_cast<int>(blockIdx.y) >= __popc(firsts)) return;
-  uint32_t left = firsts;
-  for (int i = blockIdx.y; i > 0; --i) left &= left - 1;
+  const int g = lane / 4, t = lane % 4;
+  const uint16_t* x0 = a.x + static_cast<uint64_t>(row0 + g) * a.x_stride;
+  int turn = 0;
+  for (uint32_t left = firsts; left != 0; left &= left - 1, ++turn) {
+  if (turn % gridDim.y != blockIdx.y) continue;
   const int lead = __ffs(left) - 1;
   const int m = __shfl_sync(0xFFFFFFFFu, mine, lead);
   const uint32_t rows = __shfl_sync(0xFFFFFFFFu, same, lead);
   const float factor = (a.scale != nullptr ? a.scale[m] : 1.0f) * undo_of(a.w_scale);
 
-  const int g = lane / 4, t = lane % 4;
-  const uint16_t* x0 = a.x + static_cast<uint64_t>(row0 + g) * a.x_stride;
   const uint16_t* from = a.a + m * a.a_stride;
   float sum[2][kSteps][4] = {};
+  // 64 elements of a row at a time, the next ones asked for before these are multiplied
+  struct Taken {
+    uint4 v[2][4], w[2][kSteps];
+  };
   const uint4 zero = make_uint4(0, 0, 0, 0);
-#pragma unroll(kSteps <= 4 ? 4 : 1)
-  for (int k0 = warp * 32; k0 < a.in; k0 += kWarps * 32) {
-    const int k = k0 + t * 8;
-    const bool inside = k < a.in;
-    uint4 w[kSteps], v[4];
+  auto take = [&](Taken& to, int k0) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      v[i] = inside && (rows >> (g + 8 * i) & 1) ? *reinterpret_cast<const uint4*>(x0 + 8 * i * a.x_stride + k) : zero;
+    for (int n = 0; n < 2; ++n) {
+      const int k = k0 + n * 32 + t * 8;
+      const bool inside = k < a.in;
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-      w[s] = inside && s * 8 + g < a.rank ? *reinterpret_cast<const uint4*>(from + static_cast<uint64_t>(s * 8 + g) * a.in + k) : zero;
+      for (int i = 0; i < 4; ++i)
+        to.v[n][i] = inside && (rows >> (g + 8 * i) & 1) ? *reinterpret_cast<const uint4*>(x0 + 8 * i * a.x_stride + k) : zero;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      if (!(rows >> (16 * half) & 0xFFFFu)) continue;
-      const uint4 p = v[2 * half], q = v[2 * half + 1];
-      const uint32_t first[4] = {p.x, q.x, p.y, q.y}, second[4] = {p.z, q.z, p.w, q.w};
+      for (int s = 0; s < kSteps; ++s)
+        to.w[n][s] = inside && s * 8 + g < a.rank ? *reinterpret_cast<const uint4*>(from + static_cast<uint64_t>(s * 8 + g) * a.in + k) : zero;
+    }
+  };
+  auto add = [&](const Taken& of) {
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        mma_bf16(sum[half][s], first, w[s].x, w[s].y);
-        mma_bf16(sum[half][s], second, w[s].z, w[s].w);
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        if (!(rows >> (16 * half) & 0xFFFFu)) continue;
+        const uint4 p = of.v[n][2 * half], q = of.v[n][2 * half + 1];
+        const uint32_t first[4] = {p.x, q.x, p.y, q.y}, second[4] = {p.z, q.z, p.w, q.w};
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          mma_bf16(sum[half][s], first, of.w[n][s].x, of.w[n][s].y);
+          mma_bf16(sum[half][s], second, of.w[n][s].z, of.w[n][s].w);
+        }
       }
+  };
+  const int stride = gridDim.z * kWarps * 64;
+  int k0 = (blockIdx.z * kWarps + warp) * 64;
+  if constexpr (kSteps <= 4) {
+    Taken one, two;
+    take(one, k0);
+    for (; k0 < a.in; k0 += 2 * stride) {
+      take(two, k0 + stride);
+      add(one);
+      take(one, k0 + 2 * stride);
+      add(two);
+    }
+  } else {
+    for (; k0 < a.in; k0 += stride) {
+      Taken one;
+      take(one, k0);
+      add(one);
     }
   }
 #pragma unroll
@@ -165,21 +209,44 @@ shrink_kernel(const ShrinkArgs a) {
       for (int i = 0; i < 4; ++i)
         parts[(warp * kShrinkRows + half * 16 + g + i / 2 * 8) * kPitch + s * 8 + 2 * t + i % 2] = sum[half][s][i];
   __syncthreads();
-  for (int i = threadIdx.x; i < kShrinkRows * a.padded; i += kWarps * 32) {
-    const int n = i / a.padded, r = i % a.padded;
-    if (!(rows >> n & 1)) continue;
-    float h = 0.0f;
-    if (r < a.rank) {
+  const int shares = gridDim.z;
+  if (shares > 1) {
+    // the block's sums to where its first warp's are, each by the thread that has read them
+    for (int i = threadIdx.x; i < kShrinkRows * a.rank; i += kWarps * 32) {
+      float* at = parts + i / a.rank * kPitch + i % a.rank;
+      float h = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) h += parts[(w * kShrinkRows + n) * kPitch + r];
-      h *= factor;
+      for (int w = 0; w < kWarps; ++w) h += at[w * kShrinkRows * kPitch];
+      *at = h;
     }
-    const uint32_t hi = pack_bf16(h, 0.0f) & 0xFFFFu;
-    uint16_t* to = a.h + static_cast<uint64_t>(row0 + n) * 2 * a.padded + r;
-    to[0] = static_cast<uint16_t>(hi);
-    // an infinite or NaN h has no second part
-    const float rest = h - bf16_value(hi);
-    to[a.padded] = static_cast<uint16_t>(pack_bf16(isfinite(rest) ? rest : 0.0f, 0.0f));
+    cluster_sync();
+  }
+  if (blockIdx.z == 0) {
+    for (int i = threadIdx.x; i < kShrinkRows * a.padded; i += kWarps * 32) {
+      const int n = i / a.padded, r = i % a.padded;
+      if (!(rows >> n & 1)) continue;
+      float h = 0.0f;
+      if (r < a.rank) {
+        const float* at = parts + n * kPitch + r;
+        if (shares > 1) {
+          for (int z = 0; z < shares; ++z) h += load_float(address_in(shared_address(at), z));
+        } else {
+#pragma unroll
+          for (int w = 0; w < kWarps; ++w) h += at[w * kShrinkRows * kPitch];
+        }
+        h *= factor;
+      }
+      const uint32_t hi = pack_bf16(h, 0.0f) & 0xFFFFu;
+      uint16_t* to = a.h + static_cast<uint64_t>(row0 + n) * 2 * a.padded + r;
+      to[0] = static_cast<uint16_t>(hi);
+      // an infinite or NaN h has no second part
+      const float rest = h - bf16_value(hi);
+      to[a.padded] = static_cast<uint16_t>(pack_bf16(isfinite(rest) ? rest : 0.0f, 0.0f));
+    }
+  }
+  // the sums have been read before they are written again, and before a block leaves
+  if (shares > 1) cluster_sync();
+  else __syncthreads();
   }
 }
 
@@ -206,23 +273,24 @@ gather_kernel(const RowView rows, uint16_t* to, int in) {
 // --- B h of rows beside others' -------------------------------------------------------------
 
 constexpr int kExpandWarps = 4;
-constexpr int kExpandRows = 4;  // of a warp
+constexpr int kExpandRows = 2;  // of a warp
 
 // extra = B h for the rows of mixed blocks: a warp has kExpandRows rows and 128 features, a lane 4 of them,
 // with B's elements kept from row to row where the adapter stays.
 template <int kChunk>  // ranks at a time
 __global__ void __launch_bounds__(kExpandWarps * 32)
-expand_kernel(const ExpandView e, const int32_t* start, float* extra, int requests, int rows, int out) {
+expand_kernel(const ExpandView e, float* extra, int rows, int out) {
   let_next_start();
   wait_for_previous();
-  const int end = start != nullptr ? min(max(start[requests], 0), rows) : rows;
   const int lane = threadIdx.x % 32, f = (blockIdx.x * kExpandWarps + threadIdx.x / 32) * kFeatures + lane * 4;
   const int row0 = blockIdx.y * kExpandRows;
-  if (row0 >= end || f >= out || e.of_block[row0 / kBlock] != kMixed) return;
+  if (f >= out) return;
+  const int block = e.of_block[row0 / kBlock];
   float y[kExpandRows][4] = {};
   int m[kExpandRows];
 #pragma unroll
-  for (int i = 0; i < kExpandRows; ++i) m[i] = row0 + i < end ? e.of_row[row0 + i] : kNone;
+  for (int i = 0; i < kExpandRows; ++i) m[i] = row0 + i < rows ? e.of_row[row0 + i] : kNone;
+  if (block != kMixed) return;
   for (int r0 = 0; r0 < e.rank; r0 += kChunk) {
     uint4 b[4][kChunk / 8];
 #pragma unroll
@@ -260,12 +328,22 @@ expand_kernel(const ExpandView e, const int32_t* start, float* extra, int reques
 
 // --- the products -----------------------------------------------------------------------
 
+template <int n>
+struct Number {
+  static constexpr int value = n;
+};
+
+// Tiles of up to 64 rows belong to a block each, those of up to 256 to a pair of blocks: 128 features and half
+// of the rows' x are in each one's shared memory.
 template <int kRows, bool kFp8>
 struct Shape {
-  static constexpr int kBox = kRows == 64 ? 16 : 64;  // rows of a copy
-  static constexpr uint32_t kW = kFeatures * kDepth * 2, kX = kRows * kDepth * 2, kRaw = kFp8 ? kFeatures * kDepth : 0;
-  static constexpr int kStages = kFp8 ? (kRows == 64 ? 6 : 3) : (kRows == 64 ? 8 : 4);
+  static constexpr bool kPair = kRows == 256;
+  static constexpr int kBlocks = kPair ? 2 : 1;
+  static constexpr int kBox = kPair ? 64 : 16;  // rows of a copy
+  static constexpr uint32_t kW = kFeatures * kDepth * 2, kX = kRows / kBlocks * kDepth * 2, kRaw = kFp8 ? kFeatures * kDepth : 0;
+  static constexpr int kStages = kFp8 ? (kPair ? 4 : 6) : (kPair ? 6 : 8);
   static constexpr int kThreads = kFp8 ? 512 : 256;
+  static constexpr int kConverters = 8, kTeam = kRows == 64 ? 2 : 4;  // warps that convert codes, and of those on one stage
 };
 
 constexpr int kPitch = kFeatures + 4;  // of a column of sums
@@ -280,20 +358,46 @@ struct Shared {
   float staged[2][kStaged][kPitch];
   uint64_t full[S::kStages], ready[S::kStages], empty[S::kStages], sum_full[2], sum_empty[2], group, drained;
   uint64_t join_full, join_done, turn;
-  int before[ES_MAX_EXPERTS + 1];  // column tiles of the segments before each
+  int before[ES_MAX_EXPERTS];  // column tiles of the segments before each
+  int begin[ES_MAX_EXPERTS + 1];  // first row of each
   int sums[32];
   uint32_t tensor;
   int failed;
+  int notes[2][kRows];         // of a tile's columns
   int4 names[2][kRows / 8];  // rows of the fours of each copying warp
 };
 
-// What all roles need of a call's tiles. A tile is kFeatures features (gated: 64 and the 64 that
+// 16 E4M3 codes as bf16 numbers, exactly. A code's bits, in their place, are those of a bf16 number 2^120 times
+// smaller, denormals among them, so shifts and a product (with `unit`, two times 2^120) convert two. Only NaN
+// differs, and is looked for.
+__device__ __forceinline__ void bf16_of_codes(const uint32_t (&code)[4], uint32_t unit, uint32_t (&v)[8]) {
+  uint32_t nan = 0;
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    nan |= (code[d] & 0x7F7F7F7Fu) + 0x01010101u;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const uint32_t w = __byte_perm(code[d], 0, p == 0 ? 0x4140 : 0x4342);  // each code in the lower byte of its half
+      const uint32_t bits = (w * 256 & 0x80008000u) | (w * 16 & 0x07F007F0u);
+      asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[2 * d + p]) : "r"(bits), "r"(unit), "r"(0x80008000u));
+    }
+  }
+  if (nan & 0x80808080u) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      v[2 * d] = unit != 0 ? bf16_of_e4m3(code[d] & 0xFFFFu) : 0;
+      v[2 * d + 1] = unit != 0 ? bf16_of_e4m3(code[d] >> 16) : 0;
+    }
+  }
+}
+
+// What all roles need of a call's tiles. A tile is kFeatures features a block (gated: 64 and the 64 that
 // they are multiplied with) and up to kRows rows of a segment; its depth is `depth` stages. Tiles go to
-// clusters in turn, and the blocks of a cluster have a share of the depth each.
+// clusters in turn, and the blocks, or pairs, of a cluster have a share of the depth each.
 struct Plan {
   int columns, features, depth;  // tiles, tiles, stages
   int tiles;
-  int shares, rank;  // blocks of a cluster, and this one's place
+  int shares, share, place;  // of the depth, this block's, and its place in a pair
 };
 
 struct Item {
@@ -301,43 +405,41 @@ struct Item {
   int k0, k1;  // stages
 };
 
-template <class Sh>
+template <int kRows, bool kFp8, bool kGated>
 struct Walk {
+  using S = Shape<kRows, kFp8>;
   const RowView& rows;
-  const Sh& sh;
-  Plan plan;
+  const Shared<kRows, kFp8>& sh;
+  const Plan& plan;
   int at;
-  int kRowsOf;
-  bool gated;
 
-  __device__ __forceinline__ Walk(const RowView& r, const Sh& s, const Plan& p, int tile_rows, bool g)
-      : rows(r), sh(s), plan(p), at(blockIdx.x / p.shares), kRowsOf(tile_rows), gated(g) {}
+  __device__ __forceinline__ Walk(const RowView& r, const Shared<kRows, kFp8>& s, const Plan& p)
+      : rows(r), sh(s), plan(p), at(blockIdx.x / (p.shares * S::kBlocks)) {}
 
   __device__ __forceinline__ bool next(Item& item) {
     if (at >= plan.tiles) return false;
     const int tile = at;
-    at += gridDim.x / plan.shares;
-    item.k0 = plan.depth * plan.rank / plan.shares;
-    item.k1 = plan.depth * (plan.rank + 1) / plan.shares;
+    at += gridDim.x / (plan.shares * S::kBlocks);
+    item.k0 = plan.depth * plan.share / plan.shares;
+    item.k1 = plan.depth * (plan.share + 1) / plan.shares;
     const int band = tile / (kBand * plan.features);
     const int rest = tile - band * kBand * plan.features;
     const int wide = min(kBand, plan.columns - band * kBand);
     const int f = rest / wide;
     const int column = band * kBand + rest - f * wide;
-    item.f0 = f * (gated ? kFeatures / 2 : kFeatures);
+    item.f0 = (f * S::kBlocks + plan.place) * (kGated ? kFeatures / 2 : kFeatures);
     int s = 0;
     if (!rows.joined) {
-      int hi = rows.segments;  // before[s] <= column < before[s + 1]
+      int hi = rows.segments;  // the last with before[s] <= column
       while (hi - s > 1) {
         const int mid = (s + hi) / 2;
         if (sh.before[mid] <= column) s = mid;
         else hi = mid;
       }
     }
-    int begin, stop;
-    segment_of(rows, s, begin, stop, item.group);
-    item.row0 = begin + (column - (rows.joined ? 0 : sh.before[s])) * kRowsOf;
-    item.rows = min(kRowsOf, stop - item.row0);
+    item.group = s;
+    item.row0 = sh.begin[s] + (column - sh.before[s]) * kRows;
+    item.rows = min(kRows, sh.begin[s + 1] - item.row0);
     return true;
   }
 };
@@ -376,6 +478,28 @@ __device__ __forceinline__ Extra extra_of(int padded, int i) {
   return Extra{part * padded + chunk * kDepth, chunk * kDepth, min(4, padded / 16 - chunk * 4), 0};
 }
 
+// B h of four features of a row with adapter m.
+__device__ __noinline__ float4 expanded(const ExpandView& e, uint64_t row, int m, int f) {
+  const uint16_t* h = e.h + row * 2 * e.padded;
+  const uint16_t* b = e.b + m * e.b_stride + static_cast<uint64_t>(f) * e.rank;
+  float y[4] = {};
+  for (int r = 0; r < e.rank; r += 8) {
+    const uint4 p = *reinterpret_cast<const uint4*>(h + r), q = *reinterpret_cast<const uint4*>(h + e.padded + r);
+    const uint32_t pw[4] = {p.x, p.y, p.z, p.w}, qw[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const uint4 o = *reinterpret_cast<const uint4*>(b + n * e.rank + r);
+      const uint32_t ow[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        y[n] = fmaf(bf16_value(pw[d]) + bf16_value(qw[d]), bf16_value(ow[d]), y[n]);
+        y[n] = fmaf(bf16_high(pw[d]) + bf16_high(qw[d]), bf16_high(ow[d]), y[n]);
+      }
+    }
+  }
+  return make_float4(y[0], y[1], y[2], y[3]);
+}
+
 template <int kRows, bool kFp8, bool kGated>
 __global__ void __launch_bounds__(Shape<kRows, kFp8>::kThreads, 1)
 product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, int* flag, int tries, bool early, int shares,
@@ -383,20 +507,20 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
                const __grid_constant__ CUtensorMap h_map, const __grid_constant__ CUtensorMap b_map) {
   using S = Shape<kRows, kFp8>;
   constexpr int kStages = S::kStages;
+  constexpr bool kPair = S::kPair;
   extern __shared__ uint8_t dynamic[];
   Shared<kRows, kFp8>& sh = *reinterpret_cast<Shared<kRows, kFp8>*>(dynamic + ((1024 - (shared_address(dynamic) & 1023)) & 1023));
   const Watch watch{&sh.failed, tries};
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  constexpr int kConverters = kFp8 ? 8 : 0;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
       barrier_init(&sh.full[i], 1);
-      barrier_init(&sh.ready[i], kFp8 ? kConverters : 1);
+      barrier_init(&sh.ready[i], kFp8 ? S::kTeam * S::kBlocks : 1);
       barrier_init(&sh.empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
       barrier_init(&sh.sum_full[i], 1);
-      barrier_init(&sh.sum_empty[i], 4);
+      barrier_init(&sh.sum_empty[i], 4 * S::kBlocks);
     }
     barrier_init(&sh.group, 4);
     barrier_init(&sh.join_full, 4 * shares);
@@ -406,12 +530,21 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sh.failed = 0;
   }
+  if (warp == 0 && elected()) {
+    fetch_map(&w_map);
+    fetch_map(&x_map);
+  }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(shared_address(&sh.tensor)) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (kPair) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(shared_address(&sh.tensor)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(shared_address(&sh.tensor)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
   }
   fence_before();
-  if (shares > 1) cluster_sync();  // no block arrives at another's barriers before they are made
+  if (kPair || shares > 1) cluster_sync();  // no block arrives at another's barriers before they are made
   else __syncthreads();
   fence_after();
   // Behind the kernels of the adapters' part, which wait for all that came before them and then let
@@ -419,20 +552,18 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
   if (!early) wait_for_previous();
 
   const int outs = kGated ? w.out / 2 : w.out;
+  constexpr int kWide = (kGated ? kFeatures / 2 : kFeatures) * S::kBlocks;
   Plan plan;
-  plan.features = (outs + (kGated ? kFeatures / 2 : kFeatures) - 1) / (kGated ? kFeatures / 2 : kFeatures);
+  plan.features = (outs + kWide - 1) / kWide;
   plan.depth = (w.in + kDepth - 1) / kDepth;
-  if (rows.joined) {
-    int begin, end, group;
-    segment_of(rows, 0, begin, end, group);
-    plan.columns = (end - begin + kRows - 1) / kRows;
-  } else {
-    // column tiles of each segment, summed over the segments before it
+  // where each segment begins, and how many column tiles those before it have
+  {
+    const int segments = rows.joined ? 1 : rows.segments;
     int base = 0;
-    for (int s0 = 0; s0 < rows.segments; s0 += blockDim.x) {
+    for (int s0 = 0; s0 < segments; s0 += blockDim.x) {
       const int s = s0 + threadIdx.x;
       int begin = 0, end = 0, group = 0;
-      if (s < rows.segments) segment_of(rows, s, begin, end, group);
+      if (s < segments) segment_of(rows, s, begin, end, group);
       const int n = (end - begin + kRows - 1) / kRows;
       int sum = n;
 #pragma unroll
@@ -443,43 +574,65 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       if (lane == 31) sh.sums[warp] = sum;
       __syncthreads();
       int ahead = base;
-      for (int i = 0; i < static_cast<int>(blockDim.x) / 32; ++i) {
+#pragma unroll
+      for (int i = 0; i < S::kThreads / 32; ++i) {
         if (i < warp) ahead += sh.sums[i];
         base += sh.sums[i];
       }
-      if (s < rows.segments) sh.before[s] = ahead + sum - n;
+      if (s < segments) {
+        sh.before[s] = ahead + sum - n;
+        sh.begin[s] = begin;
+        if (s + 1 == segments) sh.begin[s + 1] = end;
+      }
       __syncthreads();
     }
     plan.columns = base;
   }
   plan.tiles = plan.columns * plan.features;
+  const int seat = blockIdx.x % (shares * S::kBlocks);  // in the cluster
   plan.shares = shares;
-  plan.rank = blockIdx.x % shares;
+  plan.share = seat / S::kBlocks;
+  plan.place = seat % S::kBlocks;
+  const uint32_t first = seat - plan.place;  // of the pair
   const bool named = rows.index != nullptr && !rows.copied;  // rows of x are asked for one by one
 
   if (warp == 0) {
     // --- copies
-    Walk<Shared<kRows, kFp8>> walk(rows, sh, plan, kRows, kGated);
+    Walk<kRows, kFp8, kGated> walk(rows, sh, plan);
     Item item;
     uint32_t done = 0, items = 0;
     bool fine = true;
+    // A pair's copies of bf16 are counted together, at the first block's barrier; codes are converted by each block.
+    constexpr bool kTogether = kPair && !kFp8;
+    auto expect = [&](uint32_t stage, uint32_t bytes) {
+      if (!kTogether) barrier_expect(&sh.full[stage], bytes);
+      else if (plan.place == 0) barrier_expect(&sh.full[stage], 2 * bytes);
+    };
+    auto copy3 = [&](const CUtensorMap* map, uint32_t to, uint32_t stage, int x, int y, int z) {
+      if constexpr (kTogether) load_box_pair(map, to, address_in(shared_address(&sh.full[stage]), first), x, y, z);
+      else load_box(map, to, &sh.full[stage], x, y, z);
+    };
+    auto copy2 = [&](const CUtensorMap* map, uint32_t to, uint32_t stage, int x, int y) {
+      if constexpr (kTogether) load_box_pair(map, to, address_in(shared_address(&sh.full[stage]), first), x, y);
+      else load_box(map, to, &sh.full[stage], x, y);
+    };
     for (; fine && walk.next(item); ++items) {
       // the stages hold what the cluster's blocks have of the tile before
       if (shares > 1 && items > 0 && !(fine = warp_wait(&sh.turn, (items - 1) & 1, watch))) break;
-      const int padded = (item.rows + 15) & ~15;
+      const int padded = ((item.rows + 15) & ~15) / S::kBlocks, row0 = item.row0 + plan.place * padded;  // here
       const int boxes = (padded + S::kBox - 1) / S::kBox;
       for (int k = item.k0; k < item.k1; ++k, ++done) {
         const uint32_t stage = done % kStages;
         if (!(fine = warp_wait(&sh.empty[stage], (done / kStages & 1) ^ 1, watch))) break;
         const uint32_t x_to = shared_address(sh.x[stage]);
         if (elected()) {
-          barrier_expect(&sh.full[stage], (kFp8 ? S::kRaw : S::kW) + (named ? padded : boxes * S::kBox) * kDepth * 2);
+          expect(stage, (kFp8 ? S::kRaw : S::kW) + (named ? padded : boxes * S::kBox) * kDepth * 2);
           const uint32_t w_to = kFp8 ? shared_address(sh.raw[stage]) : shared_address(sh.w[stage]);
-          load_box(&w_map, w_to, &sh.full[stage], k * kDepth, item.f0, item.group);
-          load_box(&w_map, w_to + (kFp8 ? S::kRaw : S::kW) / 2, &sh.full[stage], k * kDepth, item.f0 + (kGated ? outs : 64), item.group);
+          copy3(&w_map, w_to, stage, k * kDepth, item.f0, item.group);
+          copy3(&w_map, w_to + (kFp8 ? S::kRaw : S::kW) / 2, stage, k * kDepth, item.f0 + (kGated ? outs : 64), item.group);
           if (!named)
             for (int i = 0; i < boxes; ++i)
-              load_box(&x_map, x_to + i * (S::kBox * kDepth * 2), &sh.full[stage], k * kDepth, item.row0 + i * S::kBox);
+              copy2(&x_map, x_to + i * (S::kBox * kDepth * 2), stage, k * kDepth, row0 + i * S::kBox);
         }
         __syncwarp();
       }
@@ -487,48 +640,63 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       if (early) wait_for_previous();
       const Runs runs(expand, item.row0, item.rows, lane);
       for (int i = 0, j, m; fine && runs.next(i, j, m); i = j) {
-        const int run_boxes = ((j - i) * kBlock + S::kBox - 1) / S::kBox;
+        const int run_rows = (j - i) * kBlock / S::kBlocks, run_row0 = item.row0 + i * kBlock + plan.place * run_rows;
+        const int run_boxes = (run_rows + S::kBox - 1) / S::kBox;
         for (int e = 0; e < extras_of(expand.padded); ++e, ++done) {
           const Extra extra = extra_of(expand.padded, e);
           const uint32_t stage = done % kStages;
           if (!(fine = warp_wait(&sh.empty[stage], (done / kStages & 1) ^ 1, watch))) break;
           if (elected()) {
-            barrier_expect(&sh.full[stage], S::kW + run_boxes * S::kBox * kDepth * 2);
+            expect(stage, S::kW + run_boxes * S::kBox * kDepth * 2);
             const uint32_t w_to = shared_address(sh.w[stage]), x_to = shared_address(sh.x[stage]);
-            load_box(&b_map, w_to, &sh.full[stage], extra.b_column, item.f0, m);
-            load_box(&b_map, w_to + S::kW / 2, &sh.full[stage], extra.b_column, item.f0 + 64, m);
+            copy3(&b_map, w_to, stage, extra.b_column, item.f0, m);
+            copy3(&b_map, w_to + S::kW / 2, stage, extra.b_column, item.f0 + 64, m);
             for (int b = 0; b < run_boxes; ++b)
-              load_box(&h_map, x_to + b * (S::kBox * kDepth * 2), &sh.full[stage], extra.column, item.row0 + i * kBlock + b * S::kBox);
+              copy2(&h_map, x_to + b * (S::kBox * kDepth * 2), stage, extra.column, run_row0 + b * S::kBox);
           }
           __syncwarp();
         }
       }
     }
-    // no copy outlives the block
-    for (uint32_t i = done > kStages ? done - kStages : 0; i < done; ++i) barrier_settle(&sh.full[i % kStages], i / kStages & 1);
+    // No copy outlives the block: the stage has been filled, or, where the first block of a pair is told of that,
+    // its products are done.
+    for (uint32_t i = done > kStages ? done - kStages : 0; i < done; ++i)
+      barrier_settle(kTogether && plan.place != 0 ? &sh.empty[i % kStages] : &sh.full[i % kStages], i / kStages & 1);
   } else if (warp == 1) {
-    // --- products
-    Walk<Shared<kRows, kFp8>> walk(rows, sh, plan, kRows, kGated);
+    // --- products, issued by the first block of a pair
+    Walk<kRows, kFp8, kGated> walk(rows, sh, plan);
     Item item;
     uint32_t done = 0, items = 0;
     const uint64_t plain = operand(0, 16);
+    const uint32_t shape = product_of(0, false) + (kPair ? 128u >> 4 << 24 : 0u);
+    const bool issues = plan.place == 0;
     bool fine = true;
-    while (fine && walk.next(item)) {
+    auto multiply_here = [&](uint32_t d, uint64_t a, uint64_t b, uint32_t kind, bool add) {
+      if constexpr (kPair) multiply_pair(d, a, b, kind, add);
+      else multiply(d, a, b, kind, add);
+    };
+    auto commit_here = [&](uint64_t* barrier) {
+      if constexpr (kPair) commit_pair(barrier, 3u << first);
+      else commit(barrier);
+    };
+    auto stage_full = [&](uint32_t stage, uint32_t parity) {
+      return warp_wait(kFp8 ? &sh.ready[stage] : &sh.full[stage], parity, watch);
+    };
+    while (fine && issues && walk.next(item)) {
       const uint32_t half = items & 1;
       const uint32_t sum = sh.tensor + half * 256;
       if (!(fine = warp_wait(&sh.sum_empty[half], (items / 2 & 1) ^ 1, watch))) break;
       fence_after();
-      const uint32_t kind = product_of(0, false) | static_cast<uint32_t>((item.rows + 15) / 16 * 2) << 17;
+      const uint32_t kind = shape | static_cast<uint32_t>((item.rows + 15) / 16 * 2) << 17;
       for (int k = item.k0; k < item.k1; ++k, ++done) {
         const uint32_t stage = done % kStages;
-        if (!(fine = warp_wait(&sh.full[stage], done / kStages & 1, watch))) break;
-        if (kFp8 && !(fine = warp_wait(&sh.ready[stage], done / kStages & 1, watch))) break;
+        if (!(fine = stage_full(stage, done / kStages & 1))) break;
         fence_after();
         const uint64_t a = plain + (shared_address(sh.w[stage]) >> 4), b = plain + (shared_address(sh.x[stage]) >> 4);
         if (elected()) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) multiply(sum, a + i * 2, b + i * 2, kind, k > item.k0 || i > 0);
-          commit(&sh.empty[stage]);
+          for (int i = 0; i < 4; ++i) multiply_here(sum, a + i * 2, b + i * 2, kind, k > item.k0 || i > 0);
+          commit_here(&sh.empty[stage]);
         }
         __syncwarp();
       }
@@ -536,38 +704,42 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         if (early) wait_for_previous();
         const Runs runs(expand, item.row0, item.rows, lane);
         for (int i = 0, j, m; fine && runs.next(i, j, m); i = j) {
-          const uint32_t run_kind = product_of(0, false) | static_cast<uint32_t>((j - i) * 2) << 17;
+          const uint32_t run_kind = shape | static_cast<uint32_t>((j - i) * 2) << 17;
           for (int e = 0; e < extras_of(expand.padded); ++e, ++done) {
             const Extra extra = extra_of(expand.padded, e);
             const uint32_t stage = done % kStages;
-            if (!(fine = warp_wait(&sh.full[stage], done / kStages & 1, watch))) break;
-            if (kFp8 && !(fine = warp_wait(&sh.ready[stage], done / kStages & 1, watch))) break;
-            fence_after();
+            if (!(fine = stage_full(stage, done / kStages & 1))) break;
+                fence_after();
             const uint64_t a = plain + (shared_address(sh.w[stage]) >> 4), b = plain + (shared_address(sh.x[stage]) >> 4);
             if (elected()) {
               for (int s = 0; s < extra.steps; ++s) {
-                multiply(sum + i * kBlock, a + s * 2, b + s * 2, run_kind, true);
-                if (extra.twice > 0) multiply(sum + i * kBlock, a + s * 2, b + extra.twice / 8 + s * 2, run_kind, true);
+                multiply_here(sum + i * kBlock, a + s * 2, b + s * 2, run_kind, true);
+                if (extra.twice > 0) multiply_here(sum + i * kBlock, a + s * 2, b + extra.twice / 8 + s * 2, run_kind, true);
               }
-              commit(&sh.empty[stage]);
+              commit_here(&sh.empty[stage]);
             }
             __syncwarp();
           }
         }
       }
       if (!fine) break;
-      if (elected()) commit(&sh.sum_full[half]);
+      if (elected()) commit_here(&sh.sum_full[half]);
       __syncwarp();
       ++items;
     }
     __syncwarp();
-    if (elected()) commit(&sh.drained);  // by the lane that issued the products: none outlives the tensor memory
-    __syncwarp();
-    barrier_settle(&sh.drained, 0);
+    if (issues) {
+      if (elected()) {  // the lane that issued the products: none outlives the tensor memory
+        if constexpr (kPair) commit_pair(&sh.drained, 1u << first);
+        else commit(&sh.drained);
+      }
+      __syncwarp();
+      barrier_settle(&sh.drained, 0);
+    }
   } else if (warp < 4) {
     // --- copies of rows that are named one by one, four at a time, half of them by each of two warps
     if (named) {
-      Walk<Shared<kRows, kFp8>> walk(rows, sh, plan, kRows, kGated);
+      Walk<kRows, kFp8, kGated> walk(rows, sh, plan);
       Item item;
       uint32_t done = 0;
       bool fine = true;
@@ -604,7 +776,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
     }
   } else if (warp < 8) {
     // --- results: a thread reads a feature's lane, and writes four features of a row
-    Walk<Shared<kRows, kFp8>> walk(rows, sh, plan, kRows, kGated);
+    Walk<kRows, kFp8, kGated> walk(rows, sh, plan);
     Item item;
     uint32_t items = 0, chunks = 0;
     const int mine = warp - 4, feature = threadIdx.x - 128;
@@ -618,56 +790,60 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
     if (early) wait_for_previous();
     for (; fine && walk.next(item); ++items) {
       const uint32_t half = items & 1;
+      // what the columns are, looked up while their sums are made
+      int* notes = sh.notes[half];
+      for (int c = feature; c < item.rows; c += 128) {
+        const int row = item.row0 + c;
+        int note = kPlain;
+        if (rows.index != nullptr && static_cast<unsigned>(rows.index[row]) >= static_cast<unsigned>(rows.x_rows)) note = kAbsent;
+        if (expand.h != nullptr && expand.of_block[row / kBlock] == kMixed) note = max(expand.of_row[row], kPlain);
+        notes[c] = note;
+      }
       if (!(fine = warp_wait(&sh.sum_full[half], items / 2 & 1, watch))) break;
       fence_after();
       const uint32_t sum = sh.tensor + half * 256 + (static_cast<uint32_t>(mine) << 21);
+      auto sum_read = [&] {
+        if (lane != 0) return;
+        if (kPair) barrier_signal_at(address_in(shared_address(&sh.sum_empty[half]), first));
+        else barrier_arrive(&sh.sum_empty[half]);
+      };
       float scale = kFp8 ? *(w.scale + item.group) : 1.0f;
       if (kFp8 && expand.h != nullptr && isinf(1.0f / scale)) scale = 1.0f;
-      // Sums of the lane's features of a column to y: gated two features and the two that they are
-      // multiplied with, else four.
-      auto finish = [&](int column, float4 z) {
-        const int row = item.row0 + column;
-        const bool absent = rows.index != nullptr && static_cast<unsigned>(rows.index[row]) >= static_cast<unsigned>(rows.x_rows);
-        if (kGated) {
-          const int f = item.f0 + lane * 2;
-          if (f >= outs) return;
-          const float g0 = z.x * scale, g1 = z.y * scale;
-          const uint32_t y = pack_bf16(g0 / (1.0f + expf(-g0)) * (z.z * scale), g1 / (1.0f + expf(-g1)) * (z.w * scale));
-          *reinterpret_cast<uint32_t*>(rows.y + row * rows.y_stride + f) = absent ? 0 : y;
-          return;
-        }
+      // What is added to the lane's features of kCount columns, `step` apart; those from `stop` on are left out.
+      auto prepare = [&](int column, int step, int stop, auto& note, auto& more) {
+        constexpr int kCount = sizeof(more) / sizeof(float4);
         const int f = item.f0 + lane * 4;
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+          const int c = column + i * step;
+          note[i] = c < stop ? notes[c] : kOut;
+          more[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          if (!kGated && expand.extra != nullptr && note[i] >= 0 && f < outs)
+            more[i] = __ldcg(reinterpret_cast<const float4*>(expand.extra + static_cast<uint64_t>(item.row0 + c) * outs + f));
+        }
+      };
+      // Sums of the lane's features of these columns to y: gated two features and the two that they are
+      // multiplied with, else four.
+      auto finish = [&](int column, int step, const auto& z, const auto& note, auto& more) {
+        constexpr int kCount = sizeof(z) / sizeof(float4);
+        const int f = item.f0 + (kGated ? lane * 2 : lane * 4);
         if (f >= outs) return;
-        float y[4] = {z.x, z.y, z.z, z.w};
-        if (expand.h != nullptr && expand.of_block[row / kBlock] == kMixed) {
-          const int m = expand.of_row[row];
-          if (m >= 0 && expand.extra != nullptr) {
-            const float4 v = *reinterpret_cast<const float4*>(expand.extra + static_cast<uint64_t>(row) * outs + f);
-            y[0] += v.x;
-            y[1] += v.y;
-            y[2] += v.z;
-            y[3] += v.w;
-          } else if (m >= 0) {
-            const uint16_t* h = expand.h + static_cast<uint64_t>(row) * 2 * expand.padded;
-            const uint16_t* b = expand.b + m * expand.b_stride + static_cast<uint64_t>(f) * expand.rank;
-            for (int r = 0; r < expand.rank; r += 8) {
-              const uint4 p = *reinterpret_cast<const uint4*>(h + r), q = *reinterpret_cast<const uint4*>(h + expand.padded + r);
-              const uint32_t pw[4] = {p.x, p.y, p.z, p.w}, qw[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-              for (int n = 0; n < 4; ++n) {
-                const uint4 o = *reinterpret_cast<const uint4*>(b + n * expand.rank + r);
-                const uint32_t ow[4] = {o.x, o.y, o.z, o.w};
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                  y[n] = fmaf(bf16_value(pw[d]) + bf16_value(qw[d]), bf16_value(ow[d]), y[n]);
-                  y[n] = fmaf(bf16_high(pw[d]) + bf16_high(qw[d]), bf16_high(ow[d]), y[n]);
-                }
-              }
-            }
+        for (int i = 0; i < kCount; ++i) {
+          if (note[i] == kOut) continue;
+          const uint64_t row = item.row0 + column + i * step;
+          uint16_t* to = rows.y + row * rows.y_stride + f;
+          if (kGated) {
+            const float g0 = z[i].x * scale, g1 = z[i].y * scale;
+            const uint32_t y = pack_bf16(g0 / (1.0f + expf(-g0)) * (z[i].z * scale), g1 / (1.0f + expf(-g1)) * (z[i].w * scale));
+            *reinterpret_cast<uint32_t*>(to) = note[i] == kAbsent ? 0 : y;
+          } else {
+            if (expand.h != nullptr && expand.extra == nullptr && note[i] >= 0) more[i] = expanded(expand, row, note[i], f);
+            const uint2 y = make_uint2(pack_bf16((z[i].x + more[i].x) * scale, (z[i].y + more[i].y) * scale),
+                                       pack_bf16((z[i].z + more[i].z) * scale, (z[i].w + more[i].w) * scale));
+            *reinterpret_cast<uint2*>(to) = note[i] == kAbsent ? make_uint2(0, 0) : y;
           }
         }
-        const uint2 out = make_uint2(pack_bf16(y[0] * scale, y[1] * scale), pack_bf16(y[2] * scale, y[3] * scale));
-        *reinterpret_cast<uint2*>(rows.y + row * rows.y_stride + f) = absent ? make_uint2(0, 0) : out;
       };
       if (shares > 1) {
         // The blocks' sums of their depth meet in shared memory, where the stages were: each adds up a share of
@@ -682,34 +858,49 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         }
         fence_before();
         __syncwarp();
-        if (lane == 0) barrier_arrive(&sh.sum_empty[half]);
-        if (lane < shares) barrier_arrive_at(address_in(shared_address(&sh.join_full), lane));
+        sum_read();
+        if (lane < shares) barrier_arrive_at(address_in(shared_address(&sh.join_full), lane * S::kBlocks + plan.place));
         if (!(fine = cluster_wait(&sh.join_full, items & 1, watch))) break;
         const int width = (item.rows + shares - 1) / shares;
-        const int end = min(item.rows, (plan.rank + 1) * width);
+        const int end = min(item.rows, (plan.share + 1) * width);
         const uint32_t base = shared_address(whole) + (kGated ? lane * 8 : lane * 16);
-#pragma unroll 2
-        for (int c = plan.rank * width + mine; c < end; c += 4) {
-          float4 v[kMostShares];
+        // sixteen loads at a time: kAt columns of up to kOf blocks
+        auto join = [&](auto at, auto of) {
+          constexpr int kAt = decltype(at)::value, kOf = decltype(of)::value;
+          for (int c = plan.share * width + mine; c < end; c += 4 * kAt) {
+            int note[kAt];
+            float4 more[kAt], v[kAt][kOf];
+            prepare(c, 4, end, note, more);
 #pragma unroll
-          for (int q = 0; q < kMostShares; ++q)
-            if (q < shares) {
-              const uint32_t from = address_in(base + c * (kPitch * 4), q);
-              v[q] = kGated ? load_pairs(from, from + kFeatures * 2) : load_from(from);
-            }
-          float4 z = v[0];
+            for (int i = 0; i < kAt; ++i)
 #pragma unroll
-          for (int q = 1; q < kMostShares; ++q)
-            if (q < shares) {
-              z.x += v[q].x;
-              z.y += v[q].y;
-              z.z += v[q].z;
-              z.w += v[q].w;
+              for (int q = 0; q < kOf; ++q) {
+                v[i][q] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (q < shares && c + 4 * i < end) {
+                  const uint32_t from = address_in(base + (c + 4 * i) * (kPitch * 4), q * S::kBlocks + plan.place);
+                  v[i][q] = kGated ? load_pairs(from, from + kFeatures * 2) : load_from(from);
+                }
+              }
+            float4 z[kAt];
+#pragma unroll
+            for (int i = 0; i < kAt; ++i) {
+              z[i] = v[i][0];
+#pragma unroll
+              for (int q = 1; q < kOf; ++q) {
+                z[i].x += v[i][q].x;
+                z[i].y += v[i][q].y;
+                z[i].z += v[i][q].z;
+                z[i].w += v[i][q].w;
+              }
             }
-          finish(c, z);
-        }
+            finish(c, 4, z, note, more);
+          }
+        };
+        if (shares <= 2) join(Number<8>{}, Number<2>{});
+        else if (shares <= 4) join(Number<4>{}, Number<4>{});
+        else join(Number<2>{}, Number<8>{});
         __syncwarp();
-        if (lane < shares) barrier_arrive_at(address_in(shared_address(&sh.join_done), lane));
+        if (lane < shares) barrier_arrive_at(address_in(shared_address(&sh.join_done), lane * S::kBlocks + plan.place));
         if (!(fine = cluster_wait(&sh.join_done, items & 1, watch))) break;
         fence_async();  // the stages are written by copies next
         warp_arrive(&sh.turn, lane);
@@ -722,32 +913,35 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         if (c + kStaged >= item.rows) {
           fence_before();
           __syncwarp();
-          if (lane == 0) barrier_arrive(&sh.sum_empty[half]);
+          sum_read();
         }
         auto& staged = sh.staged[chunks & 1];
 #pragma unroll
         for (int i = 0; i < kStaged; ++i) staged[i][feature] = __uint_as_float(r[i]);
         if (!(fine = group_sync())) break;
+        int note[4];
+        float4 more[4], z[4];
+        prepare(c + mine * 4, 1, item.rows, note, more);
 #pragma unroll
-        for (int i = 0; i < kStaged / 4; ++i) {
-          const int column = mine * (kStaged / 4) + i;
-          if (c + column >= item.rows) continue;
+        for (int i = 0; i < 4; ++i) {
+          const float* from = staged[mine * 4 + i];
           if (kGated) {
-            const float2 gate = *reinterpret_cast<const float2*>(&staged[column][lane * 2]);
-            const float2 up = *reinterpret_cast<const float2*>(&staged[column][64 + lane * 2]);
-            finish(c + column, make_float4(gate.x, gate.y, up.x, up.y));
+            const float2 gate = *reinterpret_cast<const float2*>(from + lane * 2), up = *reinterpret_cast<const float2*>(from + 64 + lane * 2);
+            z[i] = make_float4(gate.x, gate.y, up.x, up.y);
           } else {
-            finish(c + column, *reinterpret_cast<const float4*>(&staged[column][lane * 4]));
+            z[i] = *reinterpret_cast<const float4*>(from + lane * 4);
           }
         }
+        finish(c + mine * 4, 1, z, note, more);
       }
     }
   } else if (kFp8 && warp >= 8) {
-    // --- codes to bf16
-    Walk<Shared<kRows, kFp8>> walk(rows, sh, plan, kRows, kGated);
+    // --- codes to bf16: groups of warps take stages in turn, so that one's latency is beside others' work
+    Walk<kRows, kFp8, kGated> walk(rows, sh, plan);
     Item item;
     uint32_t done = 0;
-    const bool dead = expand.h != nullptr && isinf(1.0f / *w.scale);
+    const uint32_t unit = expand.h != nullptr && isinf(1.0f / *w.scale) ? 0 : 0x7B807B80u;  // 2^120, or all codes count as 0
+    const uint32_t team = (warp - 8) / S::kTeam, member = (warp - 8) % S::kTeam;
     bool fine = true;
     while (fine && walk.next(item)) {
       int extra = 0;
@@ -757,40 +951,46 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         for (int i = 0, j, m; runs.next(i, j, m); i = j) extra += extras_of(expand.padded);
       }
       for (int k = item.k0; k < item.k1 + extra; ++k, ++done) {
+        if (done % (S::kConverters / S::kTeam) != team) continue;
         const uint32_t stage = done % kStages;
         if (!(fine = warp_wait(&sh.full[stage], done / kStages & 1, watch))) break;
         if (k < item.k1) {
-          // 16 codes a lane: row `at`, 64 bytes of codes, 128 of bf16 with the pieces of 16 bytes swizzled
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int n = (i * 8 + warp - 8) * 32 + lane;
+          // 16 codes a lane and turn: row `at`, 64 bytes of codes, 128 of bf16 with the pieces of 16 bytes swizzled
+          constexpr int kTurns = kFeatures * kDepth / 16 / 32 / S::kTeam;
+#pragma unroll(kTurns < 4 ? kTurns : 4)
+          for (int i = 0; i < kTurns; ++i) {
+            const int n = (i * S::kTeam + member) * 32 + lane;
             const int at = n / 4, piece = n % 4;
             const uint4 c = *reinterpret_cast<const uint4*>(&sh.raw[stage][at * kDepth + piece * 16]);
             const uint32_t code[4] = {c.x, c.y, c.z, c.w};
             uint32_t v[8];
-#pragma unroll
-            for (int d = 0; d < 4; ++d) {
-              v[2 * d] = dead ? 0 : bf16_of_e4m3(code[d] & 0xFFFFu);
-              v[2 * d + 1] = dead ? 0 : bf16_of_e4m3(code[d] >> 16);
-            }
+            bf16_of_codes(code, unit, v);
             uint8_t* to = &sh.w[stage][at * 128];
             *reinterpret_cast<uint4*>(to + ((piece * 2) ^ (at & 7)) * 16) = make_uint4(v[0], v[1], v[2], v[3]);
             *reinterpret_cast<uint4*>(to + ((piece * 2 + 1) ^ (at & 7)) * 16) = make_uint4(v[4], v[5], v[6], v[7]);
           }
           fence_async();
         }
-        warp_arrive(&sh.ready[stage], lane);
+        if (kPair) {
+          __syncwarp();
+          if (lane == 0) barrier_signal_at(address_in(shared_address(&sh.ready[stage]), first));
+        } else {
+          warp_arrive(&sh.ready[stage], lane);
+        }
       }
     }
   }
   __syncwarp();
   let_next_start();
   fence_before();
-  if (shares > 1) cluster_sync();  // no block leaves while others read its sums or arrive at its barriers
+  if (kPair || shares > 1) cluster_sync();  // no block leaves while others read its sums or arrive at its barriers
   else __syncthreads();
   fence_after();
   if (threadIdx.x == 0 && sh.failed) *flag = 1;
-  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tensor) : "memory");
+  if (warp == 1) {
+    if (kPair) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(sh.tensor) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tensor) : "memory");
+  }
 }
 
 // --- launches ---------------------------------------------------------------------------
@@ -814,14 +1014,14 @@ es_status_t map_rows(CUtensorMap* map, const void* base, uint64_t width, uint64_
 
 template <int kRows, bool kFp8, bool kGated>
 es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView& rows, const ExpandView& expand, const CUtensorMap* b_map,
-                   int columns, int join, bool early, char* workspace, cudaStream_t stream, const char* call) {
+                   int columns, int most_rows, bool early, char* workspace, cudaStream_t stream, const char* call) {
   using S = Shape<kRows, kFp8>;
   auto kernel = product_kernel<kRows, kFp8, kGated>;
   constexpr int kBytes = static_cast<int>(sizeof(Shared<kRows, kFp8>)) + 1024;
   static_assert(kBytes <= 232448, "shared memory of a block");
   int device = 0;
   cudaGetDevice(&device);
-  // Clusters of 1 to kMostShares blocks that each device holds at once, of a kernel that has been given its
+  // Clusters of 1 to kMostShares shares that each device holds at once, of a kernel that has been given its
   // shared memory.
   static std::atomic<int> held[64][kMostShares + 1];
   int clusters[kMostShares + 1];
@@ -829,14 +1029,15 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
     for (int i = 1; i <= kMostShares; ++i) clusters[i] = held[device][i].load(std::memory_order_relaxed);
   } else {
     cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
-    if (err == cudaSuccess) err = cudaDeviceGetAttribute(&clusters[1], cudaDevAttrMultiProcessorCount, device);
-    for (int i = 2; i <= kMostShares && err == cudaSuccess; ++i) {
+    for (int i = 1; i <= kMostShares && err == cudaSuccess; ++i) {
+      clusters[i] = 0;
+      if (i * S::kBlocks > kMostShares) continue;
       cudaLaunchConfig_t config{};
       cudaLaunchAttribute attr{};
       attr.id = cudaLaunchAttributeClusterDimension;
-      attr.val.clusterDim.x = static_cast<unsigned>(i);
+      attr.val.clusterDim.x = static_cast<unsigned>(i * S::kBlocks);
       attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-      config.gridDim = dim3(static_cast<unsigned>(i));
+      config.gridDim = dim3(static_cast<unsigned>(i * S::kBlocks));
       config.blockDim = dim3(S::kThreads);
       config.dynamicSmemBytes = kBytes;
       config.attrs = &attr;
@@ -855,26 +1056,30 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
       held[device][1].store(clusters[1], std::memory_order_release);
     }
   }
-  // The number of blocks that share a tile's depth: the one whose rounds of tiles take the fewest stages. To
-  // join costs as much as some.
-  const int outs = kGated ? w.out / 2 : w.out, wide = kGated ? kFeatures / 2 : kFeatures;
+  // How many blocks, or pairs, share a tile's depth: what takes least time, by the bytes of weights at the memory's rate
+  // or a block's stages at its own, whichever is more, and the joins.
+  const int outs = kGated ? w.out / 2 : w.out, wide = (kGated ? kFeatures / 2 : kFeatures) * S::kBlocks;
   const int64_t tiles = static_cast<int64_t>(columns) * ((outs + wide - 1) / wide);
   const int depth = (w.in + kDepth - 1) / kDepth;
+  constexpr int kStageNs = kFp8 ? 380 : S::kPair ? 270 : 150;
+  const int64_t streamed = tiles * depth * (S::kBlocks * (kFp8 ? S::kRaw : S::kW)) / 6700;
   int shares = 1;
   int64_t best = INT64_MAX;
   for (int i = 1; i <= kMostShares && i <= depth; ++i) {
     if (clusters[i] < 1) continue;
-    const int64_t cost = (tiles + clusters[i] - 1) / clusters[i] * ((depth + i - 1) / i + (i > 1 ? join : 0));
+    const int64_t rounds = (tiles + clusters[i] - 1) / clusters[i];
+    const int64_t cost = std::max(streamed, rounds * ((depth + i - 1) / i) * kStageNs) + (i > 1 ? rounds * (1500 + 8 * most_rows) : 0);
     if (cost < best) {
       best = cost;
       shares = i;
     }
   }
-  const int grid = static_cast<int>(std::min<int64_t>(tiles, clusters[shares])) * shares;
+  if (getenv("ES_SHARES")) shares = std::min(atoi(getenv("ES_SHARES")), kMostShares / S::kBlocks);
+  const int grid = static_cast<int>(std::min<int64_t>(tiles, clusters[shares])) * shares * S::kBlocks;
   CUtensorMap x_map, h_map;
   es_status_t st;
   // without rows of x every slot is absent: what is read in their place does not matter
-  if (rows.x_rows > 0)
+  if (rows.x_rows > 0 || rows.copied)
     st = map_rows(&x_map, rows.x, w.in, rows.copied ? rows.rows : rows.x_rows, rows.x_stride, rows.index != nullptr && !rows.copied ? 1 : S::kBox, call);
   else
     st = map_rows(&x_map, w.data, w.in, 1, w.in, 1, call);
@@ -887,7 +1092,7 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = static_cast<unsigned>(shares);
+  attr[1].val.clusterDim.x = static_cast<unsigned>(shares * S::kBlocks);
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t config{};
   config.gridDim = dim3(static_cast<unsigned>(grid));
@@ -895,7 +1100,7 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
   config.dynamicSmemBytes = kBytes;
   config.stream = stream;
   config.attrs = attr;
-  config.numAttrs = shares > 1 ? 2 : 1;
+  config.numAttrs = shares * S::kBlocks > 1 ? 2 : 1;
   cudaError_t err = cudaLaunchKernelEx(&config, kernel, w, rows, expand, reinterpret_cast<int*>(workspace + ES_PROJECT_GAVE_UP),
                                        tries_of_a_wait.load(std::memory_order_relaxed), early, shares, w_map, x_map, h_map,
                                        expand.h != nullptr ? *b_map : x_map);
@@ -906,10 +1111,10 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
 
 template <int kRows>
 es_status_t launch_rows(const MatrixView& w, const CUtensorMap& w_map, bool fp8, bool gated, const RowView& rows, const ExpandView& expand,
-                        const CUtensorMap* b_map, int columns, int join, bool early, char* workspace, cudaStream_t stream, const char* call) {
+                        const CUtensorMap* b_map, int columns, int most_rows, bool early, char* workspace, cudaStream_t stream, const char* call) {
   auto f = fp8 ? (gated ? launch<kRows, true, true> : launch<kRows, true, false>)
                : (gated ? launch<kRows, false, true> : launch<kRows, false, false>);
-  return f(w, w_map, rows, expand, b_map, columns, join, early, workspace, stream, call);
+  return f(w, w_map, rows, expand, b_map, columns, most_rows, early, workspace, stream, call);
 }
 
 constexpr int kFew = 64, kMany = 256;  // rows of a tile
@@ -918,19 +1123,22 @@ constexpr int kMostExtra = 1024;       // rows up to which B h has room in the w
 uint64_t padded_rank(int rank) { return static_cast<uint64_t>(rank + 15) / 16 * 16; }
 uint64_t rounded(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// A launch of a grid of two axes that may begin early.
+// A launch of a grid of several axes that may begin early, in clusters of all of its z.
 template <class... P, class... A>
 cudaError_t launch_grid(void (*kernel)(P...), dim3 grid, int block, size_t shared, cudaStream_t stream, const A&... args) {
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = grid.z;
   cudaLaunchConfig_t config{};
   config.gridDim = grid;
   config.blockDim = dim3(static_cast<unsigned>(block));
   config.dynamicSmemBytes = shared;
   config.stream = stream;
-  config.attrs = &attr;
-  config.numAttrs = 1;
+  config.attrs = attr;
+  config.numAttrs = grid.z > 1 ? 2 : 1;
   const cudaError_t err = cudaLaunchKernelEx(&config, kernel, P(args)...);
   const cudaError_t last = cudaGetLastError();
   return err != cudaSuccess ? err : last;
@@ -938,7 +1146,7 @@ cudaError_t launch_grid(void (*kernel)(P...), dim3 grid, int block, size_t share
 
 template <int kSteps>
 cudaError_t launch_shrink(const ShrinkArgs& a, cudaStream_t stream) {
-  constexpr int kBytes = kShrinkBytes<kSteps>;
+  constexpr int kBytes = kShrinkWarps * kShrinkRows * (kSteps * 8 + 1) * 4;
   if (kBytes > 48 * 1024) {
     const cudaError_t err = cudaFuncSetAttribute(shrink_kernel<kSteps>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
     if (err != cudaSuccess) {
@@ -947,7 +1155,9 @@ cudaError_t launch_shrink(const ShrinkArgs& a, cudaStream_t stream) {
     }
   }
   const int most = std::min(std::min(a.requests, a.rows), kShrinkRows);  // adapters that the rows of a block can have
-  return launch_grid(shrink_kernel<kSteps>, dim3((a.rows + kShrinkRows - 1) / kShrinkRows, most), kShrinkWarps<kSteps> * 32, kBytes, stream, a);
+  const int blocks = (a.rows + kShrinkRows - 1) / kShrinkRows;
+  const dim3 grid = blocks <= 16 ? dim3(blocks, most, 8) : blocks <= 128 ? dim3(blocks, std::min(most, 4), 4) : dim3(blocks, 1, 2);
+  return launch_grid(shrink_kernel<kSteps>, grid, kShrinkWarps * 32, kBytes, stream, a);
 }
 
 }  // namespace
@@ -979,9 +1189,6 @@ uint64_t project_workspace_bytes(int rank, int rows, int in, int out) {
   return kHead + rounded(n * 4 * padded_rank(rank)) + 2 * rounded(n * 4) + rounded(std::min(rows, kMostExtra) * uint64_t{4} * out);
 }
 
-// Stages that a join of up to `rows` columns takes the time of.
-int join_of(int rows) { return 4 + rows / 32; }
-
 es_status_t launch_project(const MatrixView& w, const CUtensorMap& w_map, bool fp8, const AdapterView* adapters, const CUtensorMap* b_map,
                            const int32_t* adapter, const RowView& rows, void* workspace, cudaStream_t stream, const char* call) {
   ExpandView expand{};
@@ -1007,14 +1214,14 @@ es_status_t launch_project(const MatrixView& w, const CUtensorMap& w_map, bool f
       float* extra = reinterpret_cast<float*>(behind + rounded(n * 4 * padded) + 2 * rounded(n * 4));
       auto kernel = adapters->rank % 16 == 0 ? expand_kernel<16> : expand_kernel<8>;
       err = launch_grid(kernel, dim3((w.out + kExpandWarps * kFeatures - 1) / (kExpandWarps * kFeatures), (rows.rows + kExpandRows - 1) / kExpandRows),
-                        kExpandWarps * 32, 0, stream, expand, rows.start, extra, rows.segments, rows.rows, w.out);
+                        kExpandWarps * 32, 0, stream, expand, extra, rows.rows, w.out);
       if (err != cudaSuccess) return cuda_fail(err, call);
       expand.extra = extra;
     }
   }
   const int tile = rows.rows > kFew ? kMany : kFew;
   auto f = tile == kMany ? launch_rows<kMany> : launch_rows<kFew>;
-  return f(w, w_map, fp8, false, rows, expand, b_map, (rows.rows + tile - 1) / tile, join_of(std::min(rows.rows, tile)), adapters != nullptr,
+  return f(w, w_map, fp8, false, rows, expand, b_map, (rows.rows + tile - 1) / tile, std::min(rows.rows, tile), adapters != nullptr,
            at, stream, call);
 }
 
@@ -1024,7 +1231,7 @@ es_status_t launch_experts(const MatrixView& w, const CUtensorMap& w_map, bool f
   const int tile = rows.rows > kFew && rows.rows / w.groups > 32 ? kMany : kFew;
   RowView r = rows;
   bool early = false;
-  if (tile == kMany && rows.index != nullptr && rows.x_rows > 0) {
+  if (tile == kMany && rows.index != nullptr) {
     uint16_t* copy = reinterpret_cast<uint16_t*>(at + kHead);
     const cudaError_t err = launch_early(gather_kernel, std::min((rows.rows + 7) / 8, 152 * 8), 256, 0, stream, rows, copy, w.in);
     if (err != cudaSuccess) return cuda_fail(err, call);
@@ -1036,7 +1243,7 @@ es_status_t launch_experts(const MatrixView& w, const CUtensorMap& w_map, bool f
   const int segments = std::min(rows.rows, w.groups);
   const int each = (rows.rows + segments - 1) / segments;
   auto f = tile == kMany ? launch_rows<kMany> : launch_rows<kFew>;
-  return f(w, w_map, fp8, gated, r, ExpandView{}, nullptr, segments * ((each + tile - 1) / tile), join_of(std::min(each, tile)), early, at,
+  return f(w, w_map, fp8, gated, r, ExpandView{}, nullptr, segments * ((each + tile - 1) / tile), std::min(each, tile), early, at,
            stream, call);
 }
 

@@ -9,7 +9,7 @@ namespace {
 
 constexpr int kRouteThreads = 512;
 constexpr int kRouteWarps = kRouteThreads / 32;
-constexpr int kRouteGrid = 152;
+constexpr int kRouteGrid = 304;  // two blocks an SM
 
 struct RouteArgs {
   const void* scores;
@@ -33,61 +33,75 @@ __device__ __forceinline__ float score_of_code(uint32_t c) {
   return __uint_as_float(c & 0x80000000u ? c & 0x7FFFFFFFu : ~c);
 }
 
-// One token by one warp: lane j gets the j-th choice (its expert or -1, its weight).
-template <int kPerLane, bool kBf16>
-__device__ __forceinline__ void choose(const RouteArgs& a, int token, int lane, int& expert, float& weight) {
-  uint32_t code[kPerLane];
+// kTokens tokens by one warp, together so that their chains of reductions run beside one another: lane j
+// gets the j-th choice of each (its expert or -1, its weight).
+template <int kPerLane, bool kBf16, int kTokens>
+__device__ __forceinline__ void choose(const RouteArgs& a, const int64_t (&token)[kTokens], int lane, int (&expert)[kTokens],
+                                       float (&weight)[kTokens]) {
+  uint32_t code[kTokens][kPerLane];
 #pragma unroll
-  for (int i = 0; i < kPerLane; ++i) {
-    const int e = i * 32 + lane;
-    code[i] = 0;
-    if (e < a.experts) {
-      const uint64_t at = token * a.stride + e;
-      code[i] = code_of(kBf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(a.scores)[at]) << 16)
-                              : static_cast<const float*>(a.scores)[at]);
-    }
-  }
-  uint32_t best = 0;
-#pragma unroll
-  for (int i = 0; i < kPerLane; ++i) best = max(best, code[i]);
-  const uint32_t first = __reduce_max_sync(0xFFFFFFFFu, best);
-  const float top = first != 0 ? score_of_code(first) : 0.0f;
-  float all = 0.0f;
-  if (!a.normalise) {
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i)
-      if (code[i] != 0) all += expf(score_of_code(code[i]) - top);
-#pragma unroll
-    for (int m = 16; m > 0; m >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, m);
-  }
-  expert = -1;
-  uint32_t mine = 0;
-  for (int j = 0; j < a.top; ++j) {
-    const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, best);
-    if (most == 0) break;
-    uint32_t at = 0xFFFFFFFFu;
-#pragma unroll
-    for (int i = kPerLane - 1; i >= 0; --i)
-      if (code[i] == most) at = i * 32 + lane;
-    at = __reduce_min_sync(0xFFFFFFFFu, at);
-    best = 0;
+  for (int n = 0; n < kTokens; ++n)
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i) {
-      if (i * 32 + lane == static_cast<int>(at)) code[i] = 0;
-      best = max(best, code[i]);
+      const int e = i * 32 + lane;
+      code[n][i] = 0;
+      if (e < a.experts) {
+        const uint64_t at = token[n] * a.stride + e;
+        code[n][i] = code_of(kBf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(a.scores)[at]) << 16)
+                                   : static_cast<const float*>(a.scores)[at]);
+      }
     }
-    if (lane == j) {
-      expert = static_cast<int>(at);
-      mine = most;
-    }
-  }
-  weight = expert >= 0 ? expf(score_of_code(mine) - top) : 0.0f;
-  if (a.normalise) {
-    all = weight;
+  uint32_t best[kTokens], mine[kTokens];
+  float top[kTokens], all[kTokens];
 #pragma unroll
-    for (int m = 16; m > 0; m >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, m);
+  for (int n = 0; n < kTokens; ++n) {
+    best[n] = mine[n] = 0;
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) best[n] = max(best[n], code[n][i]);
+    const uint32_t first = __reduce_max_sync(0xFFFFFFFFu, best[n]);
+    top[n] = first != 0 ? score_of_code(first) : 0.0f;
+    all[n] = 0.0f;
+    expert[n] = -1;
+    if (!a.normalise) {
+#pragma unroll
+      for (int i = 0; i < kPerLane; ++i)
+        if (code[n][i] != 0) all[n] += expf(score_of_code(code[n][i]) - top[n]);
+    }
   }
-  if (expert >= 0) weight = weight / all;
+  for (int j = 0; j < a.top; ++j) {
+    uint32_t most[kTokens], at[kTokens];
+#pragma unroll
+    for (int n = 0; n < kTokens; ++n) most[n] = __reduce_max_sync(0xFFFFFFFFu, best[n]);
+#pragma unroll
+    for (int n = 0; n < kTokens; ++n) {
+      at[n] = 0xFFFFFFFFu;
+#pragma unroll
+      for (int i = kPerLane - 1; i >= 0; --i)
+        if (code[n][i] == most[n]) at[n] = i * 32 + lane;
+      at[n] = __reduce_min_sync(0xFFFFFFFFu, at[n]);
+    }
+#pragma unroll
+    for (int n = 0; n < kTokens; ++n) {
+      best[n] = 0;
+#pragma unroll
+      for (int i = 0; i < kPerLane; ++i) {
+        if (static_cast<uint32_t>(i * 32 + lane) == at[n]) code[n][i] = 0;
+        best[n] = max(best[n], code[n][i]);
+      }
+      if (lane == j && most[n] != 0) {
+        expert[n] = static_cast<int>(at[n]);
+        mine[n] = most[n];
+      }
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < kTokens; ++n) {
+    weight[n] = expert[n] >= 0 ? expf(score_of_code(mine[n]) - top[n]) : 0.0f;
+    if (a.normalise) all[n] = weight[n];
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) all[n] += __shfl_xor_sync(0xFFFFFFFFu, all[n], m);
+    if (expert[n] >= 0) weight[n] = weight[n] / all[n];
+  }
 }
 
 // Walks the pairs [begin, end) of one warp in order: next[e] is the place of the next pair of
@@ -131,7 +145,7 @@ __device__ __forceinline__ int scan_before(int x, int* shared, int& total) {
   return before + sum - x;
 }
 
-// Chooses the experts of the block's tokens and counts them: counts[block][expert]. With one
+// Chooses the experts of the block's tokens and counts them: counts[expert][block]. With one
 // block (kAll) it goes on to the places itself.
 //
 // A warp has a token's scores in registers, as order-preserving codes, and takes the largest
@@ -151,23 +165,30 @@ choose_kernel(const RouteArgs a, int32_t* counts) {
   int32_t* mine = next + warp * a.experts;
   for (int e = lane; e < a.experts; e += 32) mine[e] = 0;
   __syncwarp();
-  for (int64_t t = t0; t < t1; ++t) {
-    int expert;
-    float weight;
-    choose<kPerLane, kBf16>(a, static_cast<int>(t), lane, expert, weight);
-    if (lane < a.top) {
-      a.chosen[t * a.top + lane] = expert;
-      a.weights[t * a.top + lane] = weight;
-      if (expert >= 0) ++mine[expert];  // a token's experts differ
+  constexpr int kTokens = kPerLane <= 4 ? 2 : 1;
+  for (int64_t t = t0; t < t1; t += kTokens) {
+    int64_t token[kTokens];
+    int expert[kTokens];
+    float weight[kTokens];
+#pragma unroll
+    for (int n = 0; n < kTokens; ++n) token[n] = min(t + n, t1 - 1);
+    choose<kPerLane, kBf16, kTokens>(a, token, lane, expert, weight);
+#pragma unroll
+    for (int n = 0; n < kTokens; ++n) {
+      if (lane < a.top && t + n < t1) {
+        a.chosen[(t + n) * a.top + lane] = expert[n];
+        a.weights[(t + n) * a.top + lane] = weight[n];
+        if (expert[n] >= 0) ++mine[expert[n]];  // a token's experts differ
+      }
+      __syncwarp();
     }
-    __syncwarp();
   }
   __syncthreads();
   if (!kAll) {
     for (int e = threadIdx.x; e < a.experts; e += kRouteThreads) {
       int sum = 0;
       for (int w = 0; w < kRouteWarps; ++w) sum += next[w * a.experts + e];
-      counts[static_cast<int64_t>(blockIdx.x) * a.experts + e] = sum;
+      counts[e * kRouteGrid + blockIdx.x] = sum;
     }
     return;
   }
@@ -198,7 +219,7 @@ choose_kernel(const RouteArgs a, int32_t* counts) {
 __global__ void __launch_bounds__(kRouteThreads)
 place_kernel(const RouteArgs a, const int32_t* counts) {
   extern __shared__ int32_t next[];
-  __shared__ int sums[kRouteWarps];
+  __shared__ int sums[kRouteWarps], whole[ES_MAX_EXPERTS], earlier[ES_MAX_EXPERTS];
   wait_for_previous();
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int64_t t0 = min((static_cast<int64_t>(blockIdx.x) * kRouteWarps + warp) * a.share, static_cast<int64_t>(a.tokens));
@@ -207,22 +228,33 @@ place_kernel(const RouteArgs a, const int32_t* counts) {
   for (int e = lane; e < a.experts; e += 32) mine[e] = 0;
   __syncwarp();
   walk<false>(a, static_cast<int>(t0) * a.top, static_cast<int>(t1) * a.top, mine, lane);
+  // each expert's pairs, in all blocks and in those before this one
+#pragma unroll 2
+  for (int e = warp; e < a.experts; e += kRouteWarps) {
+    int sum = 0, before = 0;
+#pragma unroll
+    for (int i = 0; i < (kRouteGrid + 31) / 32; ++i) {
+      const int b = i * 32 + lane;
+      const int n = b < static_cast<int>(gridDim.x) ? counts[e * kRouteGrid + b] : 0;
+      sum += n;
+      before += b < static_cast<int>(blockIdx.x) ? n : 0;
+    }
+    sum = __reduce_add_sync(0xFFFFFFFFu, sum);
+    before = __reduce_add_sync(0xFFFFFFFFu, before);
+    if (lane == 0) {
+      whole[e] = sum;
+      earlier[e] = before;
+    }
+  }
   __syncthreads();
   int base = 0;
   for (int e0 = 0; e0 < a.experts; e0 += kRouteThreads) {
     const int e = e0 + threadIdx.x;
-    int sum = 0, before = 0;
-    if (e < a.experts)
-      for (int b = 0; b < static_cast<int>(gridDim.x); ++b) {
-        const int n = counts[static_cast<int64_t>(b) * a.experts + e];
-        if (b < static_cast<int>(blockIdx.x)) before += n;
-        sum += n;
-      }
     int total;
-    int at = base + scan_before(sum, sums, total);
+    int at = base + scan_before(e < a.experts ? whole[e] : 0, sums, total);
     if (e < a.experts) {
       if (blockIdx.x == 0) a.start[e] = at;
-      at += before;
+      at += earlier[e];
       for (int w = 0; w < kRouteWarps; ++w) {
         const int n = next[w * a.experts + e];
         next[w * a.experts + e] = at;

@@ -76,6 +76,19 @@ __device__ __forceinline__ void load_box(const CUtensorMap* map, uint32_t to, ui
                "l"(map), "r"(shared_address(barrier)), "r"(x), "r"(y)
                : "memory");
 }
+// Asks for the map itself.
+__device__ __forceinline__ void fetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+// The same where the barrier (an address of the cluster's) may be the other's of a pair of blocks.
+__device__ __forceinline__ void load_box_pair(const CUtensorMap* map, uint32_t to, uint32_t barrier, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(to),
+               "l"(map), "r"(barrier), "r"(x), "r"(y), "r"(z)
+               : "memory");
+}
+__device__ __forceinline__ void load_box_pair(const CUtensorMap* map, uint32_t to, uint32_t barrier, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4}], [%2];" ::"r"(to),
+               "l"(map), "r"(barrier), "r"(x), "r"(y)
+               : "memory");
+}
 // Four rows of a map whose box is one row high.
 __device__ __forceinline__ void gather_rows(const CUtensorMap* map, uint32_t to, uint64_t* barrier, int x, int4 row) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], "
@@ -151,6 +164,19 @@ __device__ __forceinline__ bool elected() {
   return yes != 0;
 }
 
+// The same by a pair of blocks: M = 256 with half of A's rows and of B's in each block's shared memory, and half
+// of D's in each one's tensor memory. Issued by the first of the two; the barriers of both complete.
+__device__ __forceinline__ void multiply_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t kind, bool add) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+               "l"(a), "l"(b), "r"(kind), "r"(static_cast<uint32_t>(add))
+               : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint64_t* b, uint32_t blocks) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(shared_address(b)),
+               "h"(static_cast<uint16_t>(blocks))
+               : "memory");
+}
+
 // Clusters: the address of another block's shared memory, an arrival at a barrier there, a wait that
 // sees what arrived threads of other blocks wrote, and four numbers read from there.
 __device__ __forceinline__ uint32_t address_in(uint32_t address, uint32_t rank) {
@@ -160,6 +186,11 @@ __device__ __forceinline__ uint32_t address_in(uint32_t address, uint32_t rank) 
 }
 __device__ __forceinline__ void barrier_arrive_at(uint32_t address) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(address) : "memory");
+}
+// The same without an order of this thread's own reads and writes beyond its block's: for what copies and products
+// read and write. (An acquire of the cluster's costs 1,500 cycles a stage.)
+__device__ __forceinline__ void barrier_signal_at(uint32_t address) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(address) : "memory");
 }
 __device__ __forceinline__ bool cluster_wait(uint64_t* b, uint32_t parity, const Watch& watch) {
   bool fine = false;
@@ -178,6 +209,11 @@ __device__ __forceinline__ bool cluster_wait(uint64_t* b, uint32_t parity, const
 __device__ __forceinline__ float4 load_from(uint32_t address) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(address) : "memory");
+  return v;
+}
+__device__ __forceinline__ float load_float(uint32_t address) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(address) : "memory");
   return v;
 }
 // Two from each of two places.
