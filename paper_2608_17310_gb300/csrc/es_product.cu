@@ -333,17 +333,18 @@ struct Number {
   static constexpr int value = n;
 };
 
-// Tiles of up to 64 rows belong to a block each, those of up to 256 to a pair of blocks: 128 features and half
+// Tiles of up to 16 or 64 rows belong to a block each, those of up to 256 to a pair of blocks: 128 features and half
 // of the rows' x are in each one's shared memory.
 template <int kRows, bool kFp8>
 struct Shape {
   static constexpr bool kPair = kRows == 256;
   static constexpr int kBlocks = kPair ? 2 : 1;
   static constexpr int kBox = kPair ? 64 : 16;  // rows of a copy
+  static constexpr int kSlots = 4;              // of converted codes
   static constexpr uint32_t kW = kFeatures * kDepth * 2, kX = kRows / kBlocks * kDepth * 2, kRaw = kFp8 ? kFeatures * kDepth : 0;
-  static constexpr int kStages = kFp8 ? (kPair ? 4 : 6) : (kPair ? 6 : 8);
+  static constexpr int kStages = kFp8 ? (kPair ? 5 : kRows == 64 ? 8 : 12) : (kPair ? 6 : kRows == 64 ? 8 : 10);
   static constexpr int kThreads = kFp8 ? 512 : 256;
-  static constexpr int kConverters = 8, kTeam = kRows == 64 ? 2 : 4;  // warps that convert codes, and of those on one stage
+  static constexpr int kTeam = 2;  // warps that convert a stage's codes, into the team's own slot
 };
 
 constexpr int kPitch = kFeatures + 4;  // of a column of sums
@@ -352,11 +353,11 @@ constexpr int kStaged = 16;  // columns that pass through shared memory together
 template <int kRows, bool kFp8>
 struct Shared {
   using S = Shape<kRows, kFp8>;
-  uint8_t w[S::kStages][S::kW];
+  uint8_t w[kFp8 ? S::kSlots : S::kStages][S::kW];
   uint8_t x[S::kStages][S::kX];
   uint8_t raw[kFp8 ? S::kStages : 1][kFp8 ? S::kRaw : 16];
   float staged[2][kStaged][kPitch];
-  uint64_t full[S::kStages], ready[S::kStages], empty[S::kStages], sum_full[2], sum_empty[2], group, drained;
+  uint64_t full[S::kStages], empty[S::kStages], ready[S::kSlots], free[S::kSlots], sum_full[2], sum_empty[2], group, drained;
   uint64_t join_full, join_done, turn;
   int before[ES_MAX_EXPERTS];  // column tiles of the segments before each
   int begin[ES_MAX_EXPERTS + 1];  // first row of each
@@ -364,7 +365,7 @@ struct Shared {
   uint32_t tensor;
   int failed;
   int notes[2][kRows];         // of a tile's columns
-  int4 names[2][kRows / 8];  // rows of the fours of each copying warp
+  int4 names[2][kRows / 8 > 0 ? kRows / 8 : 1];  // rows of the fours of each copying warp
 };
 
 // 16 E4M3 codes as bf16 numbers, exactly. A code's bits, in their place, are those of a bf16 number 2^120 times
@@ -515,8 +516,11 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
       barrier_init(&sh.full[i], 1);
-      barrier_init(&sh.ready[i], kFp8 ? S::kTeam * S::kBlocks : 1);
       barrier_init(&sh.empty[i], 1);
+    }
+    for (int i = 0; i < S::kSlots; ++i) {
+      barrier_init(&sh.ready[i], S::kTeam * S::kBlocks);
+      barrier_init(&sh.free[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
       barrier_init(&sh.sum_full[i], 1);
@@ -646,9 +650,12 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
           const Extra extra = extra_of(expand.padded, e);
           const uint32_t stage = done % kStages;
           if (!(fine = warp_wait(&sh.empty[stage], (done / kStages & 1) ^ 1, watch))) break;
+          // the slot's products before; by their stage's barrier, since this warp may be several turns of the slots ahead
+          const uint32_t before = done - S::kSlots;
+          if (kFp8 && done >= S::kSlots && !(fine = warp_wait(&sh.empty[before % kStages], before / kStages & 1, watch))) break;
           if (elected()) {
             expect(stage, S::kW + run_boxes * S::kBox * kDepth * 2);
-            const uint32_t w_to = shared_address(sh.w[stage]), x_to = shared_address(sh.x[stage]);
+            const uint32_t w_to = shared_address(sh.w[kFp8 ? done % S::kSlots : stage]), x_to = shared_address(sh.x[stage]);
             copy3(&b_map, w_to, stage, extra.b_column, item.f0, m);
             copy3(&b_map, w_to + S::kW / 2, stage, extra.b_column, item.f0 + 64, m);
             for (int b = 0; b < run_boxes; ++b)
@@ -679,8 +686,13 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       if constexpr (kPair) commit_pair(barrier, 3u << first);
       else commit(barrier);
     };
-    auto stage_full = [&](uint32_t stage, uint32_t parity) {
-      return warp_wait(kFp8 ? &sh.ready[stage] : &sh.full[stage], parity, watch);
+    auto stage_full = [&] {
+      return kFp8 ? warp_wait(&sh.ready[done % S::kSlots], done / S::kSlots & 1, watch)
+                  : warp_wait(&sh.full[done % kStages], done / kStages & 1, watch);
+    };
+    auto stage_done = [&] {
+      commit_here(&sh.empty[done % kStages]);
+      if (kFp8) commit_here(&sh.free[done % S::kSlots]);
     };
     while (fine && issues && walk.next(item)) {
       const uint32_t half = items & 1;
@@ -690,13 +702,13 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       const uint32_t kind = shape | static_cast<uint32_t>((item.rows + 15) / 16 * 2) << 17;
       for (int k = item.k0; k < item.k1; ++k, ++done) {
         const uint32_t stage = done % kStages;
-        if (!(fine = stage_full(stage, done / kStages & 1))) break;
+        if (!(fine = stage_full())) break;
         fence_after();
-        const uint64_t a = plain + (shared_address(sh.w[stage]) >> 4), b = plain + (shared_address(sh.x[stage]) >> 4);
+        const uint64_t a = plain + (shared_address(sh.w[kFp8 ? done % S::kSlots : stage]) >> 4), b = plain + (shared_address(sh.x[stage]) >> 4);
         if (elected()) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) multiply_here(sum, a + i * 2, b + i * 2, kind, k > item.k0 || i > 0);
-          commit_here(&sh.empty[stage]);
+          stage_done();
         }
         __syncwarp();
       }
@@ -708,15 +720,15 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
           for (int e = 0; e < extras_of(expand.padded); ++e, ++done) {
             const Extra extra = extra_of(expand.padded, e);
             const uint32_t stage = done % kStages;
-            if (!(fine = stage_full(stage, done / kStages & 1))) break;
+            if (!(fine = stage_full())) break;
                 fence_after();
-            const uint64_t a = plain + (shared_address(sh.w[stage]) >> 4), b = plain + (shared_address(sh.x[stage]) >> 4);
+            const uint64_t a = plain + (shared_address(sh.w[kFp8 ? done % S::kSlots : stage]) >> 4), b = plain + (shared_address(sh.x[stage]) >> 4);
             if (elected()) {
               for (int s = 0; s < extra.steps; ++s) {
                 multiply_here(sum + i * kBlock, a + s * 2, b + s * 2, run_kind, true);
                 if (extra.twice > 0) multiply_here(sum + i * kBlock, a + s * 2, b + extra.twice / 8 + s * 2, run_kind, true);
               }
-              commit_here(&sh.empty[stage]);
+              stage_done();
             }
             __syncwarp();
           }
@@ -951,9 +963,10 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         for (int i = 0, j, m; runs.next(i, j, m); i = j) extra += extras_of(expand.padded);
       }
       for (int k = item.k0; k < item.k1 + extra; ++k, ++done) {
-        if (done % (S::kConverters / S::kTeam) != team) continue;
+        if (done % S::kSlots != team) continue;
         const uint32_t stage = done % kStages;
         if (!(fine = warp_wait(&sh.full[stage], done / kStages & 1, watch))) break;
+        if (!(fine = warp_wait(&sh.free[team], (done / S::kSlots & 1) ^ 1, watch))) break;
         if (k < item.k1) {
           // 16 codes a lane and turn: row `at`, 64 bytes of codes, 128 of bf16 with the pieces of 16 bytes swizzled
           constexpr int kTurns = kFeatures * kDepth / 16 / 32 / S::kTeam;
@@ -965,7 +978,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
             const uint32_t code[4] = {c.x, c.y, c.z, c.w};
             uint32_t v[8];
             bf16_of_codes(code, unit, v);
-            uint8_t* to = &sh.w[stage][at * 128];
+            uint8_t* to = &sh.w[team][at * 128];
             *reinterpret_cast<uint4*>(to + ((piece * 2) ^ (at & 7)) * 16) = make_uint4(v[0], v[1], v[2], v[3]);
             *reinterpret_cast<uint4*>(to + ((piece * 2 + 1) ^ (at & 7)) * 16) = make_uint4(v[4], v[5], v[6], v[7]);
           }
@@ -973,9 +986,9 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         }
         if (kPair) {
           __syncwarp();
-          if (lane == 0) barrier_signal_at(address_in(shared_address(&sh.ready[stage]), first));
+          if (lane == 0) barrier_signal_at(address_in(shared_address(&sh.ready[team]), first));
         } else {
-          warp_arrive(&sh.ready[stage], lane);
+          warp_arrive(&sh.ready[team], lane);
         }
       }
     }
@@ -1061,7 +1074,7 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
   const int outs = kGated ? w.out / 2 : w.out, wide = (kGated ? kFeatures / 2 : kFeatures) * S::kBlocks;
   const int64_t tiles = static_cast<int64_t>(columns) * ((outs + wide - 1) / wide);
   const int depth = (w.in + kDepth - 1) / kDepth;
-  constexpr int kStageNs = kFp8 ? 380 : S::kPair ? 270 : 150;
+  constexpr int kStageNs = kFp8 ? 200 : S::kPair ? 270 : 200;
   const int64_t streamed = tiles * depth * (S::kBlocks * (kFp8 ? S::kRaw : S::kW)) / 6700;
   int shares = 1;
   int64_t best = INT64_MAX;
@@ -1117,7 +1130,7 @@ es_status_t launch_rows(const MatrixView& w, const CUtensorMap& w_map, bool fp8,
   return f(w, w_map, rows, expand, b_map, columns, most_rows, early, workspace, stream, call);
 }
 
-constexpr int kFew = 64, kMany = 256;  // rows of a tile
+constexpr int kLeast = 16, kFew = 64, kMany = 256;  // rows of a tile
 constexpr int kMostExtra = 1024;       // rows up to which B h has room in the workspace
 
 uint64_t padded_rank(int rank) { return static_cast<uint64_t>(rank + 15) / 16 * 16; }
@@ -1219,8 +1232,8 @@ es_status_t launch_project(const MatrixView& w, const CUtensorMap& w_map, bool f
       expand.extra = extra;
     }
   }
-  const int tile = rows.rows > kFew ? kMany : kFew;
-  auto f = tile == kMany ? launch_rows<kMany> : launch_rows<kFew>;
+  const int tile = rows.rows > kFew ? kMany : rows.rows > kLeast ? kFew : kLeast;
+  auto f = tile == kMany ? launch_rows<kMany> : tile == kFew ? launch_rows<kFew> : launch_rows<kLeast>;
   return f(w, w_map, fp8, false, rows, expand, b_map, (rows.rows + tile - 1) / tile, std::min(rows.rows, tile), adapters != nullptr,
            at, stream, call);
 }
@@ -1228,7 +1241,7 @@ es_status_t launch_project(const MatrixView& w, const CUtensorMap& w_map, bool f
 es_status_t launch_experts(const MatrixView& w, const CUtensorMap& w_map, bool fp8, bool gated, const RowView& rows, void* workspace,
                            cudaStream_t stream, const char* call) {
   char* at = static_cast<char*>(workspace);
-  const int tile = rows.rows > kFew && rows.rows / w.groups > 32 ? kMany : kFew;
+  const int tile = rows.rows > kFew && rows.rows / w.groups > 32 ? kMany : rows.rows > kLeast ? kFew : kLeast;
   RowView r = rows;
   bool early = false;
   if (tile == kMany && rows.index != nullptr) {
@@ -1242,7 +1255,7 @@ es_status_t launch_experts(const MatrixView& w, const CUtensorMap& w_map, bool f
   // column tiles as they are where rows are spread evenly
   const int segments = std::min(rows.rows, w.groups);
   const int each = (rows.rows + segments - 1) / segments;
-  auto f = tile == kMany ? launch_rows<kMany> : launch_rows<kFew>;
+  auto f = tile == kMany ? launch_rows<kMany> : tile == kFew ? launch_rows<kFew> : launch_rows<kLeast>;
   return f(w, w_map, fp8, gated, r, ExpandView{}, nullptr, segments * ((each + tile - 1) / tile), std::min(each, tile), early, at,
            stream, call);
 }
