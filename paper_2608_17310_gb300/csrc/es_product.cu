@@ -339,10 +339,13 @@ template <int kRows, bool kFp8>
 struct Shape {
   static constexpr bool kPair = kRows == 256;
   static constexpr int kBlocks = kPair ? 2 : 1;
-  static constexpr int kBox = kPair ? 64 : 16;  // rows of a copy
+  static constexpr int kBox = kPair ? 64 : 16;  // rows of a copy of h
   static constexpr int kSlots = 4;              // of converted codes
-  static constexpr uint32_t kW = kFeatures * kDepth * 2, kX = kRows / kBlocks * kDepth * 2, kRaw = kFp8 ? kFeatures * kDepth : 0;
-  static constexpr int kStages = kFp8 ? (kPair ? 5 : kRows == 64 ? 8 : 12) : (kPair ? 6 : kRows == 64 ? 8 : 10);
+  // Elements of a row in a stage, and products' depths of 64 of them. What an SM has under way is bound by requests,
+  // so codes come 128 bytes at a time where the stages have room (a step's experts 56 us by 64 bytes).
+  static constexpr int kDeep = kFp8 && !kPair ? 128 : 64, kParts = kDeep / kDepth;
+  static constexpr uint32_t kW = kFeatures * kDepth * 2, kX = kRows / kBlocks * kDepth * 2, kRaw = kFp8 ? kFeatures * kDeep : 0;
+  static constexpr int kStages = kFp8 ? (kPair ? 5 : kRows == 64 ? 4 : 6) : (kPair ? 6 : kRows == 64 ? 8 : 10);
   static constexpr int kThreads = kFp8 ? 512 : 256;
   static constexpr int kTeam = 2;  // warps that convert a stage's codes, into the team's own slot
 };
@@ -354,7 +357,7 @@ template <int kRows, bool kFp8>
 struct Shared {
   using S = Shape<kRows, kFp8>;
   uint8_t w[kFp8 ? S::kSlots : S::kStages][S::kW];
-  uint8_t x[S::kStages][S::kX];
+  uint8_t x[S::kStages][S::kX * S::kParts];
   uint8_t raw[kFp8 ? S::kStages : 1][kFp8 ? S::kRaw : 16];
   float staged[2][kStaged][kPitch];
   uint64_t full[S::kStages], empty[S::kStages], ready[S::kSlots], free[S::kSlots], sum_full[2], sum_empty[2], group, drained;
@@ -503,7 +506,7 @@ __device__ __noinline__ float4 expanded(const ExpandView& e, uint64_t row, int m
 
 template <int kRows, bool kFp8, bool kGated>
 __global__ void __launch_bounds__(Shape<kRows, kFp8>::kThreads, 1)
-product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, int* flag, int tries, bool early, int shares,
+product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, int* flag, int tries, bool early, int shares, int box,
                const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map,
                const __grid_constant__ CUtensorMap h_map, const __grid_constant__ CUtensorMap b_map) {
   using S = Shape<kRows, kFp8>;
@@ -559,7 +562,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
   constexpr int kWide = (kGated ? kFeatures / 2 : kFeatures) * S::kBlocks;
   Plan plan;
   plan.features = (outs + kWide - 1) / kWide;
-  plan.depth = (w.in + kDepth - 1) / kDepth;
+  plan.depth = (w.in + S::kDeep - 1) / S::kDeep;
   // where each segment begins, and how many column tiles those before it have
   {
     const int segments = rows.joined ? 1 : rows.segments;
@@ -624,19 +627,21 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       // the stages hold what the cluster's blocks have of the tile before
       if (shares > 1 && items > 0 && !(fine = warp_wait(&sh.turn, (items - 1) & 1, watch))) break;
       const int padded = ((item.rows + 15) & ~15) / S::kBlocks, row0 = item.row0 + plan.place * padded;  // here
-      const int boxes = (padded + S::kBox - 1) / S::kBox;
+      const int boxes = (padded + box - 1) / box;
       for (int k = item.k0; k < item.k1; ++k, ++done) {
         const uint32_t stage = done % kStages;
         if (!(fine = warp_wait(&sh.empty[stage], (done / kStages & 1) ^ 1, watch))) break;
         const uint32_t x_to = shared_address(sh.x[stage]);
         if (elected()) {
-          expect(stage, (kFp8 ? S::kRaw : S::kW) + (named ? padded : boxes * S::kBox) * kDepth * 2);
+          expect(stage, (kFp8 ? S::kRaw : S::kW) + (named ? padded : boxes * box) * S::kDeep * 2);
           const uint32_t w_to = kFp8 ? shared_address(sh.raw[stage]) : shared_address(sh.w[stage]);
-          copy3(&w_map, w_to, stage, k * kDepth, item.f0, item.group);
-          copy3(&w_map, w_to + (kFp8 ? S::kRaw : S::kW) / 2, stage, k * kDepth, item.f0 + (kGated ? outs : 64), item.group);
+          copy3(&w_map, w_to, stage, k * S::kDeep, item.f0, item.group);
+          if (kGated) copy3(&w_map, w_to + (kFp8 ? S::kRaw : S::kW) / 2, stage, k * S::kDeep, item.f0 + outs, item.group);
           if (!named)
-            for (int i = 0; i < boxes; ++i)
-              copy2(&x_map, x_to + i * (S::kBox * kDepth * 2), stage, k * kDepth, row0 + i * S::kBox);
+#pragma unroll
+            for (int j = 0; j < S::kParts; ++j)
+              for (int i = 0; i < boxes; ++i)
+                copy2(&x_map, x_to + j * S::kX + i * (box * kDepth * 2), stage, k * S::kDeep + j * kDepth, row0 + i * box);
         }
         __syncwarp();
       }
@@ -650,14 +655,15 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
           const Extra extra = extra_of(expand.padded, e);
           const uint32_t stage = done % kStages;
           if (!(fine = warp_wait(&sh.empty[stage], (done / kStages & 1) ^ 1, watch))) break;
-          // the slot's products before; by their stage's barrier, since this warp may be several turns of the slots ahead
-          const uint32_t before = done - S::kSlots;
-          if (kFp8 && done >= S::kSlots && !(fine = warp_wait(&sh.empty[before % kStages], before / kStages & 1, watch))) break;
+          // the products of the slot's part before; by their stage's barrier, since this warp may be several turns of
+          // the slots ahead
+          constexpr uint32_t kTurn = S::kSlots / S::kParts;
+          const uint32_t before = done - kTurn;
+          if (kFp8 && done >= kTurn && !(fine = warp_wait(&sh.empty[before % kStages], before / kStages & 1, watch))) break;
           if (elected()) {
             expect(stage, S::kW + run_boxes * S::kBox * kDepth * 2);
-            const uint32_t w_to = shared_address(sh.w[kFp8 ? done % S::kSlots : stage]), x_to = shared_address(sh.x[stage]);
+            const uint32_t w_to = shared_address(sh.w[kFp8 ? done * S::kParts % S::kSlots : stage]), x_to = shared_address(sh.x[stage]);
             copy3(&b_map, w_to, stage, extra.b_column, item.f0, m);
-            copy3(&b_map, w_to + S::kW / 2, stage, extra.b_column, item.f0 + 64, m);
             for (int b = 0; b < run_boxes; ++b)
               copy2(&h_map, x_to + b * (S::kBox * kDepth * 2), stage, extra.column, run_row0 + b * S::kBox);
           }
@@ -686,31 +692,40 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       if constexpr (kPair) commit_pair(barrier, 3u << first);
       else commit(barrier);
     };
-    auto stage_full = [&] {
-      return kFp8 ? warp_wait(&sh.ready[done % S::kSlots], done / S::kSlots & 1, watch)
+    // Part j of stage `done` is there.
+    auto part_full = [&](int j) {
+      const uint32_t part = done * S::kParts + j;
+      return kFp8 ? warp_wait(&sh.ready[part % S::kSlots], part / S::kSlots & 1, watch)
                   : warp_wait(&sh.full[done % kStages], done / kStages & 1, watch);
     };
-    auto stage_done = [&] {
-      commit_here(&sh.empty[done % kStages]);
-      if (kFp8) commit_here(&sh.free[done % S::kSlots]);
+    auto part_done = [&](int j) {
+      if (kFp8) commit_here(&sh.free[(done * S::kParts + j) % S::kSlots]);
+      if (j == S::kParts - 1) commit_here(&sh.empty[done % kStages]);
     };
+    auto w_of = [&](int j) {
+      return plain + (shared_address(sh.w[kFp8 ? (done * S::kParts + j) % S::kSlots : done % kStages]) >> 4);
+    };
+    auto x_of = [&](int j) { return plain + (shared_address(sh.x[done % kStages] + j * S::kX) >> 4); };
     while (fine && issues && walk.next(item)) {
       const uint32_t half = items & 1;
       const uint32_t sum = sh.tensor + half * 256;
       if (!(fine = warp_wait(&sh.sum_empty[half], (items / 2 & 1) ^ 1, watch))) break;
       fence_after();
       const uint32_t kind = shape | static_cast<uint32_t>((item.rows + 15) / 16 * 2) << 17;
-      for (int k = item.k0; k < item.k1; ++k, ++done) {
-        const uint32_t stage = done % kStages;
-        if (!(fine = stage_full())) break;
-        fence_after();
-        const uint64_t a = plain + (shared_address(sh.w[kFp8 ? done % S::kSlots : stage]) >> 4), b = plain + (shared_address(sh.x[stage]) >> 4);
-        if (elected()) {
+      for (int k = item.k0; fine && k < item.k1; ++k, ++done) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) multiply_here(sum, a + i * 2, b + i * 2, kind, k > item.k0 || i > 0);
-          stage_done();
+        for (int j = 0; j < S::kParts; ++j) {
+          if (!(fine = part_full(j))) break;
+          fence_after();
+          const uint64_t a = w_of(j), b = x_of(j);
+          if (elected()) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) multiply_here(sum, a + i * 2, b + i * 2, kind, k > item.k0 || j > 0 || i > 0);
+            part_done(j);
+          }
+          __syncwarp();
         }
-        __syncwarp();
+        if (!fine) break;
       }
       if (fine && expand.h != nullptr && item.k1 == plan.depth) {
         if (early) wait_for_previous();
@@ -719,18 +734,21 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
           const uint32_t run_kind = shape | static_cast<uint32_t>((j - i) * 2) << 17;
           for (int e = 0; e < extras_of(expand.padded); ++e, ++done) {
             const Extra extra = extra_of(expand.padded, e);
-            const uint32_t stage = done % kStages;
-            if (!(fine = stage_full())) break;
-                fence_after();
-            const uint64_t a = plain + (shared_address(sh.w[kFp8 ? done % S::kSlots : stage]) >> 4), b = plain + (shared_address(sh.x[stage]) >> 4);
-            if (elected()) {
-              for (int s = 0; s < extra.steps; ++s) {
-                multiply_here(sum + i * kBlock, a + s * 2, b + s * 2, run_kind, true);
-                if (extra.twice > 0) multiply_here(sum + i * kBlock, a + s * 2, b + extra.twice / 8 + s * 2, run_kind, true);
+#pragma unroll
+            for (int p = 0; p < S::kParts; ++p) {
+              if (!(fine = part_full(p))) break;
+              fence_after();
+              const uint64_t a = w_of(p), b = x_of(p);
+              if (elected()) {
+                for (int s = 0; p == 0 && s < extra.steps; ++s) {
+                  multiply_here(sum + i * kBlock, a + s * 2, b + s * 2, run_kind, true);
+                  if (extra.twice > 0) multiply_here(sum + i * kBlock, a + s * 2, b + extra.twice / 8 + s * 2, run_kind, true);
+                }
+                part_done(p);
               }
-              stage_done();
+              __syncwarp();
             }
-            __syncwarp();
+            if (!fine) break;
           }
         }
       }
@@ -779,7 +797,9 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
             const uint32_t x_to = shared_address(sh.x[stage]);
 #pragma unroll 4
             for (int i = begin; i < end; ++i)
-              gather_rows(&x_map, x_to + i * (4 * kDepth * 2), &sh.full[stage], k * kDepth, names[i - begin]);
+#pragma unroll
+              for (int j = 0; j < S::kParts; ++j)
+                gather_rows(&x_map, x_to + j * S::kX + i * (4 * kDepth * 2), &sh.full[stage], k * S::kDeep + j * kDepth, names[i - begin]);
           }
           __syncwarp();
         }
@@ -954,6 +974,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
     uint32_t done = 0;
     const uint32_t unit = expand.h != nullptr && isinf(1.0f / *w.scale) ? 0 : 0x7B807B80u;  // 2^120, or all codes count as 0
     const uint32_t team = (warp - 8) / S::kTeam, member = (warp - 8) % S::kTeam;
+    uint32_t part = team;  // the team's next one
     bool fine = true;
     while (fine && walk.next(item)) {
       int extra = 0;
@@ -962,25 +983,28 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         const Runs runs(expand, item.row0, item.rows, lane);
         for (int i = 0, j, m; runs.next(i, j, m); i = j) extra += extras_of(expand.padded);
       }
-      for (int k = item.k0; k < item.k1 + extra; ++k, ++done) {
-        if (done % S::kSlots != team) continue;
-        const uint32_t stage = done % kStages;
-        if (!(fine = warp_wait(&sh.full[stage], done / kStages & 1, watch))) break;
-        if (!(fine = warp_wait(&sh.free[team], (done / S::kSlots & 1) ^ 1, watch))) break;
-        if (k < item.k1) {
-          // 16 codes a lane and turn: row `at`, 64 bytes of codes, 128 of bf16 with the pieces of 16 bytes swizzled
+      const uint32_t end = (done + item.k1 - item.k0 + extra) * S::kParts, codes = (done + item.k1 - item.k0) * S::kParts;
+      done += item.k1 - item.k0 + extra;
+      for (; part < end; part += S::kSlots) {
+        const uint32_t stage = part / S::kParts % kStages;
+        if (!(fine = warp_wait(&sh.full[stage], part / S::kParts / kStages & 1, watch))) break;
+        if (!(fine = warp_wait(&sh.free[team], (part / S::kSlots & 1) ^ 1, watch))) break;
+        if (part < codes) {
+          // 16 codes a lane and turn, of row `at`. Rows of 128 bytes of codes are swizzled, as those of bf16 are; eight
+          // lanes have four pieces of two rows, r and r ^ 5, which neither read nor write a bank twice.
           constexpr int kTurns = kFeatures * kDepth / 16 / 32 / S::kTeam;
+          const int within = lane & 4 ? lane >> 3 ^ 5 : lane >> 3, piece = lane & 3;
+          const int from = S::kParts == 2 ? ((part % 2 * 4 + piece) ^ within) * 16 : piece * 16;
 #pragma unroll(kTurns < 4 ? kTurns : 4)
           for (int i = 0; i < kTurns; ++i) {
-            const int n = (i * S::kTeam + member) * 32 + lane;
-            const int at = n / 4, piece = n % 4;
-            const uint4 c = *reinterpret_cast<const uint4*>(&sh.raw[stage][at * kDepth + piece * 16]);
+            const int at = (i * S::kTeam + member) * 8 + within;
+            const uint4 c = *reinterpret_cast<const uint4*>(&sh.raw[stage][at * S::kDeep + from]);
             const uint32_t code[4] = {c.x, c.y, c.z, c.w};
             uint32_t v[8];
             bf16_of_codes(code, unit, v);
             uint8_t* to = &sh.w[team][at * 128];
-            *reinterpret_cast<uint4*>(to + ((piece * 2) ^ (at & 7)) * 16) = make_uint4(v[0], v[1], v[2], v[3]);
-            *reinterpret_cast<uint4*>(to + ((piece * 2 + 1) ^ (at & 7)) * 16) = make_uint4(v[4], v[5], v[6], v[7]);
+            *reinterpret_cast<uint4*>(to + ((piece * 2) ^ within) * 16) = make_uint4(v[0], v[1], v[2], v[3]);
+            *reinterpret_cast<uint4*>(to + ((piece * 2 + 1) ^ within) * 16) = make_uint4(v[4], v[5], v[6], v[7]);
           }
           fence_async();
         }
@@ -1073,8 +1097,8 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
   // or a block's stages at its own, whichever is more, and the joins.
   const int outs = kGated ? w.out / 2 : w.out, wide = (kGated ? kFeatures / 2 : kFeatures) * S::kBlocks;
   const int64_t tiles = static_cast<int64_t>(columns) * ((outs + wide - 1) / wide);
-  const int depth = (w.in + kDepth - 1) / kDepth;
-  constexpr int kStageNs = kFp8 ? 200 : S::kPair ? 270 : 200;
+  const int depth = (w.in + S::kDeep - 1) / S::kDeep;
+  constexpr int kStageNs = S::kPair ? (kFp8 ? 400 : 270) : kFp8 ? 300 : 220;
   const int64_t streamed = tiles * depth * (S::kBlocks * (kFp8 ? S::kRaw : S::kW)) / 6700;
   int shares = 1;
   int64_t best = INT64_MAX;
@@ -1089,11 +1113,17 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
   }
   if (getenv("ES_SHARES")) shares = std::min(atoi(getenv("ES_SHARES")), kMostShares / S::kBlocks);
   const int grid = static_cast<int>(std::min<int64_t>(tiles, clusters[shares])) * shares * S::kBlocks;
+  // rows of a copy of x: all that a tile has where there is one column of tiles, else as many as most have
+  const int here = (std::min(most_rows, kRows) + 15) / 16 * 16 / S::kBlocks;
+  int box = kRows / S::kBlocks;
+  if (rows.joined && columns == 1) box = here;
+  else
+    while (box >= 32 && box / 2 >= here) box /= 2;
   CUtensorMap x_map, h_map;
   es_status_t st;
   // without rows of x every slot is absent: what is read in their place does not matter
   if (rows.x_rows > 0 || rows.copied)
-    st = map_rows(&x_map, rows.x, w.in, rows.copied ? rows.rows : rows.x_rows, rows.x_stride, rows.index != nullptr && !rows.copied ? 1 : S::kBox, call);
+    st = map_rows(&x_map, rows.x, w.in, rows.copied ? rows.rows : rows.x_rows, rows.x_stride, rows.index != nullptr && !rows.copied ? 1 : box, call);
   else
     st = map_rows(&x_map, w.data, w.in, 1, w.in, 1, call);
   if (st != ES_OK) return st;
@@ -1115,7 +1145,7 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
   config.attrs = attr;
   config.numAttrs = shares * S::kBlocks > 1 ? 2 : 1;
   cudaError_t err = cudaLaunchKernelEx(&config, kernel, w, rows, expand, reinterpret_cast<int*>(workspace + ES_PROJECT_GAVE_UP),
-                                       tries_of_a_wait.load(std::memory_order_relaxed), early, shares, w_map, x_map, h_map,
+                                       tries_of_a_wait.load(std::memory_order_relaxed), early, shares, box, w_map, x_map, h_map,
                                        expand.h != nullptr ? *b_map : x_map);
   const cudaError_t last = cudaGetLastError();
   if (err == cudaSuccess) err = last;
@@ -1178,17 +1208,17 @@ cudaError_t launch_shrink(const ShrinkArgs& a, cudaStream_t stream) {
 void set_project_wait_tries(int tries) { tries_of_a_wait.store(tries < 0 ? kMostTries : tries, std::memory_order_relaxed); }
 
 es_status_t map_matrices(CUtensorMap* map, const void* data, uint64_t in, uint64_t out, uint64_t groups, uint64_t row_stride,
-                         uint64_t group_stride, bool fp8, const char* call) {
+                         uint64_t group_stride, bool fp8, int wide, int rows, const char* call) {
   EncodeTiled encode = nullptr;
   const es_status_t st = encode_tiled(&encode);
   if (st != ES_OK) return st;
   const cuuint64_t size = fp8 ? 1 : 2;
   const cuuint64_t dims[3] = {in, out, groups};
   const cuuint64_t strides[2] = {row_stride * size, group_stride * size};
-  const cuuint32_t box[3] = {kDepth, kFeatures / 2, 1}, steps[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {static_cast<cuuint32_t>(wide), static_cast<cuuint32_t>(rows), 1}, steps[3] = {1, 1, 1};
   const CUresult made = encode(map, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(data),
                                dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                               fp8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                               wide * size == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (made != CUDA_SUCCESS) return fail(ES_ERR_CUDA, "%s: cuTensorMapEncodeTiled returned %d", call, static_cast<int>(made));
   return ES_OK;
@@ -1202,7 +1232,7 @@ uint64_t project_workspace_bytes(int rank, int rows, int in, int out) {
   return kHead + rounded(n * 4 * padded_rank(rank)) + 2 * rounded(n * 4) + rounded(std::min(rows, kMostExtra) * uint64_t{4} * out);
 }
 
-es_status_t launch_project(const MatrixView& w, const CUtensorMap& w_map, bool fp8, const AdapterView* adapters, const CUtensorMap* b_map,
+es_status_t launch_project(const MatrixView& w, const CUtensorMap* w_maps, bool fp8, const AdapterView* adapters, const CUtensorMap* b_map,
                            const int32_t* adapter, const RowView& rows, void* workspace, cudaStream_t stream, const char* call) {
   ExpandView expand{};
   char* at = static_cast<char*>(workspace);
@@ -1234,11 +1264,11 @@ es_status_t launch_project(const MatrixView& w, const CUtensorMap& w_map, bool f
   }
   const int tile = rows.rows > kFew ? kMany : rows.rows > kLeast ? kFew : kLeast;
   auto f = tile == kMany ? launch_rows<kMany> : tile == kFew ? launch_rows<kFew> : launch_rows<kLeast>;
-  return f(w, w_map, fp8, false, rows, expand, b_map, (rows.rows + tile - 1) / tile, std::min(rows.rows, tile), adapters != nullptr,
+  return f(w, w_maps[tile == kMany ? 0 : 2], fp8, false, rows, expand, b_map, (rows.rows + tile - 1) / tile, std::min(rows.rows, tile), adapters != nullptr,
            at, stream, call);
 }
 
-es_status_t launch_experts(const MatrixView& w, const CUtensorMap& w_map, bool fp8, bool gated, const RowView& rows, void* workspace,
+es_status_t launch_experts(const MatrixView& w, const CUtensorMap* w_maps, bool fp8, bool gated, const RowView& rows, void* workspace,
                            cudaStream_t stream, const char* call) {
   char* at = static_cast<char*>(workspace);
   const int tile = rows.rows > kFew && rows.rows / w.groups > 32 ? kMany : rows.rows > kLeast ? kFew : kLeast;
@@ -1256,7 +1286,7 @@ es_status_t launch_experts(const MatrixView& w, const CUtensorMap& w_map, bool f
   const int segments = std::min(rows.rows, w.groups);
   const int each = (rows.rows + segments - 1) / segments;
   auto f = tile == kMany ? launch_rows<kMany> : tile == kFew ? launch_rows<kFew> : launch_rows<kLeast>;
-  return f(w, w_map, fp8, gated, r, ExpandView{}, nullptr, segments * ((each + tile - 1) / tile), std::min(each, tile), early, at,
+  return f(w, w_maps[(tile == kMany ? 0 : 2) + gated], fp8, gated, r, ExpandView{}, nullptr, segments * ((each + tile - 1) / tile), std::min(each, tile), early, at,
            stream, call);
 }
 

@@ -11,7 +11,7 @@ struct es_weights {
   int device;
   es_dtype_t dtype;
   esopt::MatrixView view;
-  CUtensorMap map;
+  CUtensorMap maps[4];  // by 64 elements, in boxes of 128 rows and of 64, and by 128 bytes
 };
 
 struct es_adapters {
@@ -106,11 +106,12 @@ es_status_t es_weights_create(const es_weights_desc_t* d, es_weights_t* out) {
   const uint64_t whole = static_cast<uint64_t>(d->out_features) * d->row_stride;
   w->view = esopt::MatrixView{d->data, d->scale, d->groups > 1 ? d->group_stride : whole, d->row_stride, d->groups,
                               d->out_features, d->in_features};
-  if ((st = esopt::map_matrices(&w->map, d->data, w->view.in, w->view.out, w->view.groups, w->view.row_stride, w->view.group_stride, fp8,
-                                call)) != ES_OK) {
-    delete w;
-    return st;
-  }
+  for (int i = 0; i < 4; ++i)
+    if ((st = esopt::map_matrices(&w->maps[i], d->data, w->view.in, w->view.out, w->view.groups, w->view.row_stride,
+                                  w->view.group_stride, fp8, fp8 && i >= 2 ? 128 : 64, 128 >> i % 2, call)) != ES_OK) {
+      delete w;
+      return st;
+    }
   *out = w;
   return ok();
 }
@@ -151,7 +152,7 @@ es_status_t es_adapters_create(const es_adapters_desc_t* d, es_adapters_t* out) 
   m->in = d->in_features;
   m->view = esopt::AdapterView{static_cast<const uint16_t*>(d->a), static_cast<const uint16_t*>(d->b), d->scale,
                                d->count > 1 ? d->a_stride : a, d->count > 1 ? d->b_stride : b, d->count, d->rank};
-  if ((st = esopt::map_matrices(&m->map, d->b, m->view.rank, m->out, m->view.count, m->view.rank, m->view.b_stride, false, call)) != ES_OK) {
+  if ((st = esopt::map_matrices(&m->map, d->b, m->view.rank, m->out, m->view.count, m->view.rank, m->view.b_stride, false, 64, 128, call)) != ES_OK) {
     delete m;
     return st;
   }
@@ -202,7 +203,7 @@ es_status_t es_project(es_weights_t w, es_adapters_t m, const es_project_t* a, v
   if ((st = check_workspace(workspace, workspace_bytes, es_project_workspace(w, m, a->rows), dev, call)) != ES_OK) return st;
   const esopt::RowView rows{static_cast<const uint16_t*>(a->x), static_cast<uint16_t*>(a->y), a->start, nullptr, nullptr,
                             a->x_stride, a->y_stride, a->requests, a->rows, a->rows, true, false};
-  st = esopt::launch_project(v, w->map, w->dtype == ES_FP8_E4M3, m != nullptr ? &m->view : nullptr, m != nullptr ? &m->map : nullptr,
+  st = esopt::launch_project(v, w->maps, w->dtype == ES_FP8_E4M3, m != nullptr ? &m->view : nullptr, m != nullptr ? &m->map : nullptr,
                              a->adapter, rows, workspace, static_cast<cudaStream_t>(stream), call);
   return st == ES_OK ? ok() : st;
 }
@@ -233,7 +234,7 @@ es_status_t es_project_experts(es_weights_t w, const es_project_experts_t* a, vo
   if ((st = check_workspace(workspace, workspace_bytes, es_project_workspace(w, nullptr, a->slots), dev, call)) != ES_OK) return st;
   const esopt::RowView rows{static_cast<const uint16_t*>(a->x), static_cast<uint16_t*>(a->y), a->start, nullptr, a->rows,
                             a->x_stride, a->y_stride, v.groups, a->slots, a->x_rows, false, false};
-  st = esopt::launch_experts(v, w->map, w->dtype == ES_FP8_E4M3, a->gated != 0, rows, workspace, static_cast<cudaStream_t>(stream), call);
+  st = esopt::launch_experts(v, w->maps, w->dtype == ES_FP8_E4M3, a->gated != 0, rows, workspace, static_cast<cudaStream_t>(stream), call);
   return st == ES_OK ? ok() : st;
 }
 

@@ -56,14 +56,15 @@ __device__ __forceinline__ void segment_of(const RowView& r, int s, int& begin, 
 }
 #endif
 
-// For TMA: matrices in boxes of 64 rows by 64 elements, bf16 swizzled by 128 bytes.
+// For TMA: matrices in boxes of `rows` rows by `wide` elements, swizzled where those are 128 bytes.
 es_status_t map_matrices(CUtensorMap* map, const void* data, uint64_t in, uint64_t out, uint64_t groups, uint64_t row_stride,
-                         uint64_t group_stride, bool fp8, const char* call);
+                         uint64_t group_stride, bool fp8, int wide, int rows, const char* call);
 
-// w_map, b_map: of the matrices and of the adapters' B. These record their own errors.
-es_status_t launch_project(const MatrixView& w, const CUtensorMap& w_map, bool fp8, const AdapterView* adapters, const CUtensorMap* b_map,
+// w_maps, b_map: of the matrices by 64 elements, in boxes of 128 rows and of 64, then the same by 128 bytes; and
+// of the adapters' B by 64 elements in boxes of 128. These record their own errors.
+es_status_t launch_project(const MatrixView& w, const CUtensorMap* w_maps, bool fp8, const AdapterView* adapters, const CUtensorMap* b_map,
                            const int32_t* adapter, const RowView& rows, void* workspace, cudaStream_t stream, const char* call);
-es_status_t launch_experts(const MatrixView& w, const CUtensorMap& w_map, bool fp8, bool gated, const RowView& rows, void* workspace,
+es_status_t launch_experts(const MatrixView& w, const CUtensorMap* w_maps, bool fp8, bool gated, const RowView& rows, void* workspace,
                            cudaStream_t stream, const char* call);
 uint64_t project_workspace_bytes(int rank, int rows, int in, int out);  // rank 0: no adapters
 // For tests: tries after which the products' waits are given up in calls from now on (0: at once;
