@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cstddef>
 #include <cstdlib>
 
 #include "es_attention.cuh"
@@ -18,7 +19,7 @@ constexpr int kFeatures = 128;  // of a tile: lanes of the tensor memory
 constexpr int kDepth = 64;      // of a stage: 128 bytes of bf16
 constexpr int kBand = 8;        // column tiles whose feature tiles are neighbours
 constexpr int kBlock = 16;      // rows whose adapters are looked at together
-constexpr int kMostShares = 8;  // blocks of a cluster
+constexpr int kMostShares = 8;  // of a tile's depth
 
 constexpr uint64_t kHead = ES_PROJECT_GAVE_UP + 256;
 
@@ -328,11 +329,6 @@ expand_kernel(const ExpandView e, float* extra, int rows, int out) {
 
 // --- the products -----------------------------------------------------------------------
 
-template <int n>
-struct Number {
-  static constexpr int value = n;
-};
-
 // Tiles of up to 16 or 64 rows belong to a block each, those of up to 256 to a pair of blocks: 128 features and half
 // of the rows' x are in each one's shared memory.
 template <int kRows, bool kFp8>
@@ -347,6 +343,8 @@ struct Shape {
   static constexpr uint32_t kW = kFeatures * kDepth * 2, kX = kRows / kBlocks * kDepth * 2, kRaw = kFp8 ? kFeatures * kDeep : 0;
   static constexpr int kStages = kFp8 ? (kPair ? 5 : kRows == 64 ? 4 : 6) : (kPair ? 6 : kRows == 64 ? 8 : 10);
   static constexpr int kThreads = kFp8 ? 512 : 256;
+  // blocks or pairs that share a tile: what they send and receive has room in the stages
+  static constexpr int kMostShares = kPair ? 3 : 8;
   static constexpr int kTeam = 2;  // warps that convert a stage's codes, into the team's own slot
 };
 
@@ -361,7 +359,7 @@ struct Shared {
   uint8_t raw[kFp8 ? S::kStages : 1][kFp8 ? S::kRaw : 16];
   float staged[2][kStaged][kPitch];
   uint64_t full[S::kStages], empty[S::kStages], ready[S::kSlots], free[S::kSlots], sum_full[2], sum_empty[2], group, drained;
-  uint64_t join_full, join_done, turn;
+  uint64_t open, joined, taken, turn;  // of blocks that share a tile
   int before[ES_MAX_EXPERTS];  // column tiles of the segments before each
   int begin[ES_MAX_EXPERTS + 1];  // first row of each
   int sums[32];
@@ -530,8 +528,11 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       barrier_init(&sh.sum_empty[i], 4 * S::kBlocks);
     }
     barrier_init(&sh.group, 4);
-    barrier_init(&sh.join_full, 4 * shares);
-    barrier_init(&sh.join_done, 4 * shares);
+    if (shares > 1) {
+      barrier_init(&sh.open, shares - 1);
+      barrier_init(&sh.joined, 1);
+      barrier_init(&sh.taken, shares - 1);
+    }
     barrier_init(&sh.turn, 4);
     barrier_init(&sh.drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -624,8 +625,9 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       else load_box(map, to, &sh.full[stage], x, y);
     };
     for (; fine && walk.next(item); ++items) {
-      // the stages hold what the cluster's blocks have of the tile before
-      if (shares > 1 && items > 0 && !(fine = warp_wait(&sh.turn, (items - 1) & 1, watch))) break;
+      // the stages hold what the cluster's blocks have of the tile before, and what others are still to take
+      if (shares > 1 && items > 0 && !(fine = warp_wait(&sh.turn, (items - 1) & 1, watch) && warp_wait(&sh.taken, (items - 1) & 1, watch)))
+        break;
       const int padded = ((item.rows + 15) & ~15) / S::kBlocks, row0 = item.row0 + plan.place * padded;  // here
       const int boxes = (padded + box - 1) / box;
       for (int k = item.k0; k < item.k1; ++k, ++done) {
@@ -775,7 +777,8 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       bool fine = true;
       int4* names = sh.names[warp - 2];
       for (uint32_t items = 0; fine && walk.next(item); ++items) {
-        if (shares > 1 && items > 0 && !(fine = warp_wait(&sh.turn, (items - 1) & 1, watch))) break;
+        if (shares > 1 && items > 0 && !(fine = warp_wait(&sh.turn, (items - 1) & 1, watch) && warp_wait(&sh.taken, (items - 1) & 1, watch)))
+          break;
         const int fours = (item.rows + 15) / 16 * 4;
         const int begin = warp == 2 ? 0 : fours / 2, end = warp == 2 ? fours / 2 : fours;
         __syncwarp();
@@ -831,6 +834,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         if (expand.h != nullptr && expand.of_block[row / kBlock] == kMixed) note = max(expand.of_row[row], kPlain);
         notes[c] = note;
       }
+      if (!(fine = group_sync())) break;
       if (!(fine = warp_wait(&sh.sum_full[half], items / 2 & 1, watch))) break;
       fence_after();
       const uint32_t sum = sh.tensor + half * 256 + (static_cast<uint32_t>(mine) << 21);
@@ -841,13 +845,12 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       };
       float scale = kFp8 ? *(w.scale + item.group) : 1.0f;
       if (kFp8 && expand.h != nullptr && isinf(1.0f / scale)) scale = 1.0f;
-      // What is added to the lane's features of kCount columns, `step` apart; those from `stop` on are left out.
-      auto prepare = [&](int column, int step, int stop, auto& note, auto& more) {
-        constexpr int kCount = sizeof(more) / sizeof(float4);
+      // What is added to the lane's features of four columns; those from `stop` on are left out.
+      auto prepare = [&](int column, int stop, int (&note)[4], float4 (&more)[4]) {
         const int f = item.f0 + lane * 4;
 #pragma unroll
-        for (int i = 0; i < kCount; ++i) {
-          const int c = column + i * step;
+        for (int i = 0; i < 4; ++i) {
+          const int c = column + i;
           note[i] = c < stop ? notes[c] : kOut;
           more[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
           if (!kGated && expand.extra != nullptr && note[i] >= 0 && f < outs)
@@ -856,14 +859,13 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       };
       // Sums of the lane's features of these columns to y: gated two features and the two that they are
       // multiplied with, else four.
-      auto finish = [&](int column, int step, const auto& z, const auto& note, auto& more) {
-        constexpr int kCount = sizeof(z) / sizeof(float4);
+      auto finish = [&](int column, const float4 (&z)[4], const int (&note)[4], float4 (&more)[4]) {
         const int f = item.f0 + (kGated ? lane * 2 : lane * 4);
         if (f >= outs) return;
 #pragma unroll
-        for (int i = 0; i < kCount; ++i) {
+        for (int i = 0; i < 4; ++i) {
           if (note[i] == kOut) continue;
-          const uint64_t row = item.row0 + column + i * step;
+          const uint64_t row = item.row0 + column + i;
           uint16_t* to = rows.y + row * rows.y_stride + f;
           if (kGated) {
             const float g0 = z[i].x * scale, g1 = z[i].y * scale;
@@ -877,83 +879,78 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
           }
         }
       };
+      // Columns [lo, hi) are this block's to finish. Where others share the tile's depth, each sends it what it has of
+      // these, and is sent what this one has of theirs, through the memory of the stages, which are empty now.
+      int lo = 0, hi = item.rows;
+      float* send = reinterpret_cast<float*>(sh.w);  // of other blocks' columns, in their order
+      const float* received = send;                  // of these, from each other block in turn
       if (shares > 1) {
-        // The blocks' sums of their depth meet in shared memory, where the stages were: each adds up a share of
-        // the columns, in the order of the blocks.
-        float* whole = reinterpret_cast<float*>(sh.w);
+        const int width = ((item.rows + shares - 1) / shares + kStaged - 1) / kStaged * kStaged;
+        auto from_of = [&](int q) { return min(q * width, item.rows); };
+        lo = from_of(plan.share);
+        hi = from_of(plan.share + 1);
+        received = send + (item.rows - (hi - lo)) * kPitch;
+        if (feature == 0) barrier_expect(&sh.joined, (shares - 1) * (hi - lo) * kPitch * 4);
+        if (mine == 0 && lane < shares && lane != plan.share)
+          barrier_signal_at(address_in(shared_address(&sh.open), lane * S::kBlocks + plan.place));
         for (int c = 0; c < item.rows; c += kStaged) {
+          if (c >= lo && c < hi) continue;
           uint32_t r[kStaged];
           tensor_load(r, sum + c);
           tensor_loaded(r);
 #pragma unroll
-          for (int i = 0; i < kStaged; ++i) whole[(c + i) * kPitch + feature] = __uint_as_float(r[i]);
+          for (int i = 0; i < kStaged; ++i)
+            if (c + i < item.rows) send[(c < lo ? c + i : c + i - (hi - lo)) * kPitch + feature] = __uint_as_float(r[i]);
         }
-        fence_before();
-        __syncwarp();
-        sum_read();
-        if (lane < shares) barrier_arrive_at(address_in(shared_address(&sh.join_full), lane * S::kBlocks + plan.place));
-        if (!(fine = cluster_wait(&sh.join_full, items & 1, watch))) break;
-        const int width = (item.rows + shares - 1) / shares;
-        const int end = min(item.rows, (plan.share + 1) * width);
-        const uint32_t base = shared_address(whole) + (kGated ? lane * 8 : lane * 16);
-        // sixteen loads at a time: kAt columns of up to kOf blocks
-        auto join = [&](auto at, auto of) {
-          constexpr int kAt = decltype(at)::value, kOf = decltype(of)::value;
-          for (int c = plan.share * width + mine; c < end; c += 4 * kAt) {
-            int note[kAt];
-            float4 more[kAt], v[kAt][kOf];
-            prepare(c, 4, end, note, more);
-#pragma unroll
-            for (int i = 0; i < kAt; ++i)
-#pragma unroll
-              for (int q = 0; q < kOf; ++q) {
-                v[i][q] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                if (q < shares && c + 4 * i < end) {
-                  const uint32_t from = address_in(base + (c + 4 * i) * (kPitch * 4), q * S::kBlocks + plan.place);
-                  v[i][q] = kGated ? load_pairs(from, from + kFeatures * 2) : load_from(from);
-                }
-              }
-            float4 z[kAt];
-#pragma unroll
-            for (int i = 0; i < kAt; ++i) {
-              z[i] = v[i][0];
-#pragma unroll
-              for (int q = 1; q < kOf; ++q) {
-                z[i].x += v[i][q].x;
-                z[i].y += v[i][q].y;
-                z[i].z += v[i][q].z;
-                z[i].w += v[i][q].w;
-              }
-            }
-            finish(c, 4, z, note, more);
+        if (lo == hi) {
+          fence_before();
+          __syncwarp();
+          sum_read();
+        }
+        fence_async();
+        if (!(fine = group_sync())) break;
+        if (mine == 0) {
+          if (!(fine = warp_wait(&sh.open, items & 1, watch))) break;
+          if (lane < shares && lane != plan.share) {
+            const int q = lane, begin = from_of(q), wide = from_of(q + 1) - begin;
+            const int place = (item.rows - wide) + (plan.share < q ? plan.share : plan.share - 1) * wide;  // there
+            const uint32_t there = q * S::kBlocks + plan.place;
+            if (wide > 0)
+              copy_to_block(address_in(shared_address(send + place * kPitch), there),
+                            shared_address(send + (q < plan.share ? begin : begin - (hi - lo)) * kPitch), wide * kPitch * 4,
+                            address_in(shared_address(&sh.joined), there));
           }
-        };
-        if (shares <= 2) join(Number<8>{}, Number<2>{});
-        else if (shares <= 4) join(Number<4>{}, Number<4>{});
-        else join(Number<2>{}, Number<8>{});
-        __syncwarp();
-        if (lane < shares) barrier_arrive_at(address_in(shared_address(&sh.join_done), lane * S::kBlocks + plan.place));
-        if (!(fine = cluster_wait(&sh.join_done, items & 1, watch))) break;
-        fence_async();  // the stages are written by copies next
-        warp_arrive(&sh.turn, lane);
-        continue;
+          __syncwarp();
+        }
+        if (!(fine = warp_wait(&sh.joined, items & 1, watch))) break;
+        if (mine == 0 && lane < shares && lane != plan.share)
+          barrier_signal_at(address_in(shared_address(&sh.taken), lane * S::kBlocks + plan.place));
       }
-      for (int c = 0; c < item.rows; c += kStaged, ++chunks) {
+      for (int c = lo; c < hi; c += kStaged, ++chunks) {
         uint32_t r[kStaged];
         tensor_load(r, sum + c);
+        int note[4];
+        float4 more[4], z[4];
+        prepare(c + mine * 4, hi, note, more);
         tensor_loaded(r);
-        if (c + kStaged >= item.rows) {
+        if (c + kStaged >= hi) {
           fence_before();
           __syncwarp();
           sum_read();
         }
         auto& staged = sh.staged[chunks & 1];
+        float v[kStaged];
 #pragma unroll
-        for (int i = 0; i < kStaged; ++i) staged[i][feature] = __uint_as_float(r[i]);
+        for (int i = 0; i < kStaged; ++i) v[i] = __uint_as_float(r[i]);
+        for (int q = 0; q < shares - 1; ++q) {
+          const float* from = received + (q * (hi - lo) + c - lo) * kPitch + feature;
+#pragma unroll
+          for (int i = 0; i < kStaged; ++i)
+            if (c + i < hi) v[i] += from[i * kPitch];
+        }
+#pragma unroll
+        for (int i = 0; i < kStaged; ++i) staged[i][feature] = v[i];
         if (!(fine = group_sync())) break;
-        int note[4];
-        float4 more[4], z[4];
-        prepare(c + mine * 4, 1, item.rows, note, more);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float* from = staged[mine * 4 + i];
@@ -964,7 +961,12 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
             z[i] = *reinterpret_cast<const float4*>(from + lane * 4);
           }
         }
-        finish(c + mine * 4, 1, z, note, more);
+        finish(c + mine * 4, z, note, more);
+      }
+      if (!fine) break;
+      if (shares > 1) {
+        fence_async();  // the stages are written by copies next
+        warp_arrive(&sh.turn, lane);
       }
     }
   } else if (kFp8 && warp >= 8) {
@@ -977,15 +979,23 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
     uint32_t part = team;  // the team's next one
     bool fine = true;
     while (fine && walk.next(item)) {
-      int extra = 0;
-      if (expand.h != nullptr && item.k1 == plan.depth) {
-        if (early) wait_for_previous();
-        const Runs runs(expand, item.row0, item.rows, lane);
-        for (int i = 0, j, m; runs.next(i, j, m); i = j) extra += extras_of(expand.padded);
-      }
-      const uint32_t end = (done + item.k1 - item.k0 + extra) * S::kParts, codes = (done + item.k1 - item.k0) * S::kParts;
-      done += item.k1 - item.k0 + extra;
-      for (; part < end; part += S::kSlots) {
+      const uint32_t codes = (done + item.k1 - item.k0) * S::kParts;
+      uint32_t end = codes;
+      bool more = expand.h != nullptr && item.k1 == plan.depth;
+      done += item.k1 - item.k0;
+      for (;;) {
+        if (part >= end) {
+          if (!more) break;
+          // the adapters' stages, which are bf16 already, once it is known how many there are
+          more = false;
+          if (early) wait_for_previous();
+          const Runs runs(expand, item.row0, item.rows, lane);
+          int extra = 0;
+          for (int i = 0, j, m; runs.next(i, j, m); i = j) extra += extras_of(expand.padded);
+          done += extra;
+          end += extra * S::kParts;
+          continue;
+        }
         const uint32_t stage = part / S::kParts % kStages;
         if (!(fine = warp_wait(&sh.full[stage], part / S::kParts / kStages & 1, watch))) break;
         if (!(fine = warp_wait(&sh.free[team], (part / S::kSlots & 1) ^ 1, watch))) break;
@@ -1014,6 +1024,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         } else {
           warp_arrive(&sh.ready[team], lane);
         }
+        part += S::kSlots;
       }
     }
   }
@@ -1054,8 +1065,12 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
                    int columns, int most_rows, bool early, char* workspace, cudaStream_t stream, const char* call) {
   using S = Shape<kRows, kFp8>;
   auto kernel = product_kernel<kRows, kFp8, kGated>;
-  constexpr int kBytes = static_cast<int>(sizeof(Shared<kRows, kFp8>)) + 1024;
+  using Sh = Shared<kRows, kFp8>;
+  constexpr int kBytes = static_cast<int>(sizeof(Sh)) + 1024;
   static_assert(kBytes <= 232448, "shared memory of a block");
+  constexpr int kWidth = ((kRows + S::kMostShares - 1) / S::kMostShares + kStaged - 1) / kStaged * kStaged;
+  static_assert((kRows + (S::kMostShares - 2) * kWidth) * kPitch * 4 <= offsetof(Sh, staged),
+                "the stages hold what blocks that share a tile exchange");
   int device = 0;
   cudaGetDevice(&device);
   // Clusters of 1 to kMostShares shares that each device holds at once, of a kernel that has been given its
@@ -1068,7 +1083,7 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
     cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
     for (int i = 1; i <= kMostShares && err == cudaSuccess; ++i) {
       clusters[i] = 0;
-      if (i * S::kBlocks > kMostShares) continue;
+      if (i > S::kMostShares) continue;
       cudaLaunchConfig_t config{};
       cudaLaunchAttribute attr{};
       attr.id = cudaLaunchAttributeClusterDimension;
@@ -1102,7 +1117,7 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
   const int64_t streamed = tiles * depth * (S::kBlocks * (kFp8 ? S::kRaw : S::kW)) / 6700;
   int shares = 1;
   int64_t best = INT64_MAX;
-  for (int i = 1; i <= kMostShares && i <= depth; ++i) {
+  for (int i = 1; i <= S::kMostShares && i <= depth; ++i) {
     if (clusters[i] < 1) continue;
     const int64_t rounds = (tiles + clusters[i] - 1) / clusters[i];
     const int64_t cost = std::max(streamed, rounds * ((depth + i - 1) / i) * kStageNs) + (i > 1 ? rounds * (1500 + 8 * most_rows) : 0);
@@ -1111,7 +1126,7 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
       shares = i;
     }
   }
-  if (getenv("ES_SHARES")) shares = std::min(atoi(getenv("ES_SHARES")), kMostShares / S::kBlocks);
+  if (getenv("ES_SHARES")) shares = std::min(atoi(getenv("ES_SHARES")), S::kMostShares);
   const int grid = static_cast<int>(std::min<int64_t>(tiles, clusters[shares])) * shares * S::kBlocks;
   // rows of a copy of x: all that a tile has where there is one column of tiles, else as many as most have
   const int here = (std::min(most_rows, kRows) + 15) / 16 * 16 / S::kBlocks;

@@ -177,50 +177,25 @@ __device__ __forceinline__ void commit_pair(uint64_t* b, uint32_t blocks) {
                : "memory");
 }
 
-// Clusters: the address of another block's shared memory, an arrival at a barrier there, a wait that
-// sees what arrived threads of other blocks wrote, and four numbers read from there.
+// Clusters: the address of another block's shared memory, an arrival at a barrier there (for what copies and
+// products read and write: it orders none of this thread's own reads and writes beyond its block's), a copy of
+// whole 16 bytes to there that a barrier there counts, and a number read from there.
 __device__ __forceinline__ uint32_t address_in(uint32_t address, uint32_t rank) {
   uint32_t a;
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(address), "r"(rank));
   return a;
 }
-__device__ __forceinline__ void barrier_arrive_at(uint32_t address) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(address) : "memory");
-}
-// The same without an order of this thread's own reads and writes beyond its block's: for what copies and products
-// read and write. (An acquire of the cluster's costs 1,500 cycles a stage.)
 __device__ __forceinline__ void barrier_signal_at(uint32_t address) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(address) : "memory");
 }
-__device__ __forceinline__ bool cluster_wait(uint64_t* b, uint32_t parity, const Watch& watch) {
-  bool fine = false;
-  for (int i = 0; i < watch.tries && !fine; ++i) {
-    uint32_t done;
-    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}"
-                 : "=r"(done)
-                 : "r"(shared_address(b)), "r"(parity)
-                 : "memory");
-    fine = done != 0;
-    if (!fine && *watch.failed) break;
-  }
-  if (!fine) *watch.failed = 1;
-  return __all_sync(0xFFFFFFFFu, fine);
-}
-__device__ __forceinline__ float4 load_from(uint32_t address) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(address) : "memory");
-  return v;
+__device__ __forceinline__ void copy_to_block(uint32_t to, uint32_t from, uint32_t bytes, uint32_t barrier) {
+  asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "r"(from), "r"(bytes),
+               "r"(barrier)
+               : "memory");
 }
 __device__ __forceinline__ float load_float(uint32_t address) {
   float v;
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(address) : "memory");
-  return v;
-}
-// Two from each of two places.
-__device__ __forceinline__ float4 load_pairs(uint32_t first, uint32_t second) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(first) : "memory");
-  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.z), "=f"(v.w) : "r"(second) : "memory");
   return v;
 }
 // All threads of all blocks of the cluster.
