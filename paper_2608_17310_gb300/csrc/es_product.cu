@@ -56,8 +56,10 @@ struct ShrinkArgs {
   uint16_t* h;
   int32_t* of_row;
   int32_t* of_block;
-  uint64_t x_stride, a_stride;
-  int requests, rows, count, rank, padded, in;
+  const uint16_t* b;
+  float* extra;  // [rows][out] B h of the rows of mixed blocks, or NULL
+  uint64_t x_stride, a_stride, b_stride;
+  int requests, rows, count, rank, padded, in, out;
 };
 
 constexpr int kShrinkRows = 32;
@@ -116,6 +118,26 @@ __device__ __forceinline__ int adapter_of_lane(const ShrinkArgs& a, int row0, in
   return static_cast<unsigned>(m) < static_cast<unsigned>(a.count) ? m : kNone;
 }
 
+// Eight ranks of B for four features, and their part of B h.
+struct Factors {
+  uint4 b[4];
+  __device__ __forceinline__ void take(const uint16_t* from, int rank) {
+#pragma unroll
+    for (int n = 0; n < 4; ++n) b[n] = *reinterpret_cast<const uint4*>(from + n * rank);
+  }
+  __device__ __forceinline__ void add(float (&y)[4], const float* h) const {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const float low = h[d * 2], high = h[d * 2 + 1];
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const uint32_t w = d == 0 ? b[n].x : d == 1 ? b[n].y : d == 2 ? b[n].z : b[n].w;
+        y[n] = fmaf(high, bf16_high(w), fmaf(low, bf16_value(w), y[n]));
+      }
+    }
+  }
+};
+
 // h of 32 rows with each adapter among them (shared out along blockIdx.y), and which adapters rows and
 // blocks have. The warps of the cluster's gridDim.z blocks share the depth; the two products of a lane's 16 bytes of
 // x and A take its elements in the order in which they lie, the same in both, so each is one load.
@@ -138,6 +160,12 @@ shrink_kernel(const ShrinkArgs a) {
     if (lane % kBlock == 0 && row0 + lane < a.rows)
       a.of_block[(row0 + lane) / kBlock] = (same & block) == (there & block) ? mine : kMixed;
   }
+  // rows of blocks of 16 that have one adapter alone get B h by products
+  const uint32_t low = 0xFFFFu, high = 0xFFFF0000u;
+  const uint32_t alone_low = __match_any_sync(0xFFFFFFFFu, mine) & there & low, alone_high = __match_any_sync(0xFFFFFFFFu, mine) & there & high;
+  const bool mixed_low = __shfl_sync(0xFFFFFFFFu, alone_low, 0) != (there & low);
+  const bool mixed_high = __shfl_sync(0xFFFFFFFFu, alone_high, 16) != (there & high);
+  const uint32_t mixed = (mixed_low ? low : 0u) | (mixed_high ? high : 0u);
   const uint32_t firsts = __ballot_sync(0xFFFFFFFFu, mine >= 0 && (same & ((1u << lane) - 1)) == 0);
   const int g = lane / 4, t = lane % 4;
   const uint16_t* x0 = a.x + static_cast<uint64_t>(row0 + g) * a.x_stride;
@@ -150,6 +178,11 @@ shrink_kernel(const ShrinkArgs a) {
   const float factor = (a.scale != nullptr ? a.scale[m] : 1.0f) * undo_of(a.w_scale);
 
   const uint16_t* from = a.a + m * a.a_stride;
+  const uint32_t expanded = a.extra != nullptr ? rows & mixed : 0;
+  if (expanded != 0)  // B to L2 meanwhile
+    for (int f = ((blockIdx.z * kWarps + warp) * 32 + lane) * 4; f < a.out; f += gridDim.z * kWarps * kFeatures)
+      for (int i = 0; i < a.rank * 8; i += 128)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(a.b + m * a.b_stride + static_cast<uint64_t>(f) * a.rank) + i));
   float sum[2][kSteps][4] = {};
   // 64 elements of a row at a time, the next ones asked for before these are multiplied
   struct Taken {
@@ -222,7 +255,8 @@ shrink_kernel(const ShrinkArgs a) {
     }
     cluster_sync();
   }
-  if (blockIdx.z == 0) {
+  float* whole = parts + kWarps * kShrinkRows * kPitch;  // [row][padded]
+  if (blockIdx.z == 0 || expanded != 0) {
     for (int i = threadIdx.x; i < kShrinkRows * a.padded; i += kWarps * 32) {
       const int n = i / a.padded, r = i % a.padded;
       if (!(rows >> n & 1)) continue;
@@ -230,6 +264,7 @@ shrink_kernel(const ShrinkArgs a) {
       if (r < a.rank) {
         const float* at = parts + n * kPitch + r;
         if (shares > 1) {
+#pragma unroll 8
           for (int z = 0; z < shares; ++z) h += load_float(address_in(shared_address(at), z));
         } else {
 #pragma unroll
@@ -237,12 +272,56 @@ shrink_kernel(const ShrinkArgs a) {
         }
         h *= factor;
       }
+      whole[i] = h;
+      if (blockIdx.z != 0) continue;
       const uint32_t hi = pack_bf16(h, 0.0f) & 0xFFFFu;
       uint16_t* to = a.h + static_cast<uint64_t>(row0 + n) * 2 * a.padded + r;
       to[0] = static_cast<uint16_t>(hi);
       // an infinite or NaN h has no second part
       const float rest = h - bf16_value(hi);
       to[a.padded] = static_cast<uint16_t>(pack_bf16(isfinite(rest) ? rest : 0.0f, 0.0f));
+    }
+  }
+  if (expanded != 0) {
+    __syncthreads();
+    // the cluster's warps share the features
+    for (int f = ((blockIdx.z * kWarps + warp) * 32 + lane) * 4; f < a.out; f += shares * kWarps * kFeatures) {
+      const uint16_t* factors = a.b + m * a.b_stride + static_cast<uint64_t>(f) * a.rank;
+      if constexpr (kSteps <= 2) {
+        Factors b[kSteps];
+#pragma unroll
+        for (int r = 0; r < kSteps; ++r) b[r].take(factors + r * 8, a.rank);
+        for (uint32_t left = expanded; left != 0; left &= left - 1) {
+          const int row = __ffs(left) - 1;
+          float y[4] = {};
+#pragma unroll
+          for (int r = 0; r < kSteps; ++r) b[r].add(y, whole + row * a.padded + r * 8);
+          *reinterpret_cast<float4*>(a.extra + static_cast<uint64_t>(row0 + row) * a.out + f) = make_float4(y[0], y[1], y[2], y[3]);
+        }
+        continue;
+      }
+      for (uint32_t left = expanded; left != 0;) {
+        int row[4];
+        float y[4][4] = {};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          row[i] = left != 0 ? __ffs(left) - 1 : -1;
+          left &= left - 1;
+        }
+#pragma unroll 2
+        for (int r = 0; r < a.rank; r += 8) {
+          Factors b;
+          b.take(factors + r, a.rank);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (row[i] >= 0) b.add(y[i], whole + row[i] * a.padded + r);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (row[i] >= 0)
+            *reinterpret_cast<float4*>(a.extra + static_cast<uint64_t>(row0 + row[i]) * a.out + f) =
+                make_float4(y[i][0], y[i][1], y[i][2], y[i][3]);
+      }
     }
   }
   // the sums have been read before they are written again, and before a block leaves
@@ -271,62 +350,6 @@ gather_kernel(const RowView rows, uint16_t* to, int in) {
   }
 }
 
-// --- B h of rows beside others' -------------------------------------------------------------
-
-constexpr int kExpandWarps = 4;
-constexpr int kExpandRows = 2;  // of a warp
-
-// extra = B h for the rows of mixed blocks: a warp has kExpandRows rows and 128 features, a lane 4 of them,
-// with B's elements kept from row to row where the adapter stays.
-template <int kChunk>  // ranks at a time
-__global__ void __launch_bounds__(kExpandWarps * 32)
-expand_kernel(const ExpandView e, float* extra, int rows, int out) {
-  let_next_start();
-  wait_for_previous();
-  const int lane = threadIdx.x % 32, f = (blockIdx.x * kExpandWarps + threadIdx.x / 32) * kFeatures + lane * 4;
-  const int row0 = blockIdx.y * kExpandRows;
-  if (f >= out) return;
-  const int block = e.of_block[row0 / kBlock];
-  float y[kExpandRows][4] = {};
-  int m[kExpandRows];
-#pragma unroll
-  for (int i = 0; i < kExpandRows; ++i) m[i] = row0 + i < rows ? e.of_row[row0 + i] : kNone;
-  if (block != kMixed) return;
-  for (int r0 = 0; r0 < e.rank; r0 += kChunk) {
-    uint4 b[4][kChunk / 8];
-#pragma unroll
-    for (int i = 0; i < kExpandRows; ++i) {
-      if (m[i] < 0) continue;
-      if (i == 0 || m[i] != m[i - 1]) {
-        const uint16_t* from = e.b + m[i] * e.b_stride + static_cast<uint64_t>(f) * e.rank + r0;
-#pragma unroll
-        for (int n = 0; n < 4; ++n)
-#pragma unroll
-          for (int c = 0; c < kChunk / 8; ++c) b[n][c] = *reinterpret_cast<const uint4*>(from + n * e.rank + c * 8);
-      }
-      const uint16_t* h = e.h + static_cast<uint64_t>(row0 + i) * 2 * e.padded + r0;
-#pragma unroll
-      for (int c = 0; c < kChunk / 8; ++c) {
-        const uint4 p = *reinterpret_cast<const uint4*>(h + c * 8), q = *reinterpret_cast<const uint4*>(h + e.padded + c * 8);
-        const uint32_t pw[4] = {p.x, p.y, p.z, p.w}, qw[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          const float lo = bf16_value(pw[d]) + bf16_value(qw[d]), hi = bf16_high(pw[d]) + bf16_high(qw[d]);
-#pragma unroll
-          for (int n = 0; n < 4; ++n) {
-            const uint32_t w = d == 0 ? b[n][c].x : d == 1 ? b[n][c].y : d == 2 ? b[n][c].z : b[n][c].w;
-            y[i][n] = fmaf(hi, bf16_high(w), fmaf(lo, bf16_value(w), y[i][n]));
-          }
-        }
-      }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < kExpandRows; ++i)
-    if (m[i] >= 0)
-      *reinterpret_cast<float4*>(extra + static_cast<uint64_t>(row0 + i) * out + f) = make_float4(y[i][0], y[i][1], y[i][2], y[i][3]);
-}
-
 // --- the products -----------------------------------------------------------------------
 
 // Tiles of up to 16 or 64 rows belong to a block each, those of up to 256 to a pair of blocks: 128 features and half
@@ -343,6 +366,7 @@ struct Shape {
   static constexpr uint32_t kW = kFeatures * kDepth * 2, kX = kRows / kBlocks * kDepth * 2, kRaw = kFp8 ? kFeatures * kDeep : 0;
   static constexpr int kStages = kFp8 ? (kPair ? 5 : kRows == 64 ? 4 : 6) : (kPair ? 6 : kRows == 64 ? 8 : 10);
   static constexpr int kThreads = kFp8 ? 512 : 256;
+  static constexpr int kBound = kFp8 ? 640 : 256;  // so that registers are left for the adapters' kernel beside it
   // blocks or pairs that share a tile: what they send and receive has room in the stages
   static constexpr int kMostShares = kPair ? 3 : 8;
   static constexpr int kTeam = 2;  // warps that convert a stage's codes, into the team's own slot
@@ -358,16 +382,17 @@ struct Shared {
   uint8_t x[S::kStages][S::kX * S::kParts];
   uint8_t raw[kFp8 ? S::kStages : 1][kFp8 ? S::kRaw : 16];
   float staged[2][kStaged][kPitch];
-  uint64_t full[S::kStages], empty[S::kStages], ready[S::kSlots], free[S::kSlots], sum_full[2], sum_empty[2], group, drained;
+  uint64_t full[S::kStages], empty[S::kStages], ready[S::kSlots], free[S::kSlots], sum_full[2], sum_empty[2], drained;
   uint64_t open, joined, taken, turn;  // of blocks that share a tile
-  int before[ES_MAX_EXPERTS];  // column tiles of the segments before each
-  int begin[ES_MAX_EXPERTS + 1];  // first row of each
   int sums[32];
   uint32_t tensor;
   int failed;
   int notes[2][kRows];         // of a tile's columns
-  int4 names[2][kRows / 8 > 0 ? kRows / 8 : 1];  // rows of the fours of each copying warp
+  int4 names[2][S::kPair ? 1 : kRows / 8];  // rows of the fours of each copying warp
+  // Behind it: for each segment, the column tiles of those before it; then the first row of each, and the last one's end.
+  __device__ __forceinline__ int* before() { return reinterpret_cast<int*>(this + 1); }
 };
+constexpr int segment_bytes(int segments) { return (2 * segments + 1) * 4; }
 
 // 16 E4M3 codes as bf16 numbers, exactly. A code's bits, in their place, are those of a bf16 number 2^120 times
 // smaller, denormals among them, so shifts and a product (with `unit`, two times 2^120) convert two. Only NaN
@@ -411,12 +436,13 @@ template <int kRows, bool kFp8, bool kGated>
 struct Walk {
   using S = Shape<kRows, kFp8>;
   const RowView& rows;
-  const Shared<kRows, kFp8>& sh;
+  const int* before;
+  const int* begin;
   const Plan& plan;
   int at;
 
-  __device__ __forceinline__ Walk(const RowView& r, const Shared<kRows, kFp8>& s, const Plan& p)
-      : rows(r), sh(s), plan(p), at(blockIdx.x / (p.shares * S::kBlocks)) {}
+  __device__ __forceinline__ Walk(const RowView& r, Shared<kRows, kFp8>& s, const Plan& p)
+      : rows(r), before(s.before()), begin(before + (r.joined ? 1 : r.segments)), plan(p), at(blockIdx.x / (p.shares * S::kBlocks)) {}
 
   __device__ __forceinline__ bool next(Item& item) {
     if (at >= plan.tiles) return false;
@@ -435,13 +461,13 @@ struct Walk {
       int hi = rows.segments;  // the last with before[s] <= column
       while (hi - s > 1) {
         const int mid = (s + hi) / 2;
-        if (sh.before[mid] <= column) s = mid;
+        if (before[mid] <= column) s = mid;
         else hi = mid;
       }
     }
     item.group = s;
-    item.row0 = sh.begin[s] + (column - sh.before[s]) * kRows;
-    item.rows = min(kRows, sh.begin[s + 1] - item.row0);
+    item.row0 = begin[s] + (column - before[s]) * kRows;
+    item.rows = min(kRows, begin[s + 1] - item.row0);
     return true;
   }
 };
@@ -503,7 +529,7 @@ __device__ __noinline__ float4 expanded(const ExpandView& e, uint64_t row, int m
 }
 
 template <int kRows, bool kFp8, bool kGated>
-__global__ void __launch_bounds__(Shape<kRows, kFp8>::kThreads, 1)
+__global__ void __launch_bounds__(Shape<kRows, kFp8>::kBound, 1)
 product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, int* flag, int tries, bool early, int shares, int box,
                const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map,
                const __grid_constant__ CUtensorMap h_map, const __grid_constant__ CUtensorMap b_map) {
@@ -527,7 +553,6 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       barrier_init(&sh.sum_full[i], 1);
       barrier_init(&sh.sum_empty[i], 4 * S::kBlocks);
     }
-    barrier_init(&sh.group, 4);
     if (shares > 1) {
       barrier_init(&sh.open, shares - 1);
       barrier_init(&sh.joined, 1);
@@ -555,8 +580,8 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
   if (kPair || shares > 1) cluster_sync();  // no block arrives at another's barriers before they are made
   else __syncthreads();
   fence_after();
-  // Behind the kernels of the adapters' part, which wait for all that came before them and then let
-  // the next start, only what they make has to be waited for.
+  // Behind the kernel of the adapters' part, which waits for all that came before it and then lets
+  // the next start, only what it makes has to be waited for.
   if (!early) wait_for_previous();
 
   const int outs = kGated ? w.out / 2 : w.out;
@@ -588,9 +613,9 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         base += sh.sums[i];
       }
       if (s < segments) {
-        sh.before[s] = ahead + sum - n;
-        sh.begin[s] = begin;
-        if (s + 1 == segments) sh.begin[s + 1] = end;
+        sh.before()[s] = ahead + sum - n;
+        sh.before()[segments + s] = begin;
+        if (s + 1 == segments) sh.before()[segments + s + 1] = end;
       }
       __syncthreads();
     }
@@ -815,11 +840,16 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
     Item item;
     uint32_t items = 0, chunks = 0;
     const int mine = warp - 4, feature = threadIdx.x - 128;
-    uint32_t syncs = 0;
-    // the four warps; false as barrier_wait
-    auto group_sync = [&] {
-      warp_arrive(&sh.group, lane);
-      return warp_wait(&sh.group, syncs++ & 1, watch);
+    // The four warps meet, as often in each whatever a wait has come to (through a barrier in shared memory a tile of
+    // 256 rows took 27,000 cycles to write); and agree whether all of their waits were fine.
+    auto meet = [] { asm volatile("bar.sync 1, 128;" ::: "memory"); };
+    auto agree = [](bool fine) {
+      uint32_t all;
+      asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 q, %1, 0;\n bar.red.and.pred p, 1, 128, q;\n selp.b32 %0, 1, 0, p;\n}"
+                   : "=r"(all)
+                   : "r"(static_cast<uint32_t>(fine))
+                   : "memory");
+      return all != 0;
     };
     bool fine = true;
     if (early) wait_for_previous();
@@ -834,8 +864,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         if (expand.h != nullptr && expand.of_block[row / kBlock] == kMixed) note = max(expand.of_row[row], kPlain);
         notes[c] = note;
       }
-      if (!(fine = group_sync())) break;
-      if (!(fine = warp_wait(&sh.sum_full[half], items / 2 & 1, watch))) break;
+      if (!(fine = agree(warp_wait(&sh.sum_full[half], items / 2 & 1, watch)))) break;
       fence_after();
       const uint32_t sum = sh.tensor + half * 256 + (static_cast<uint32_t>(mine) << 21);
       auto sum_read = [&] {
@@ -884,12 +913,16 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       int lo = 0, hi = item.rows;
       float* send = reinterpret_cast<float*>(sh.w);  // of other blocks' columns, in their order
       const float* received = send;                  // of these, from each other block in turn
+      int next_note[4];
+      float4 next_more[4];
+      if (shares == 1) prepare(mine * 4, hi, next_note, next_more);
       if (shares > 1) {
         const int width = ((item.rows + shares - 1) / shares + kStaged - 1) / kStaged * kStaged;
         auto from_of = [&](int q) { return min(q * width, item.rows); };
         lo = from_of(plan.share);
         hi = from_of(plan.share + 1);
         received = send + (item.rows - (hi - lo)) * kPitch;
+        prepare(lo + mine * 4, hi, next_note, next_more);
         if (feature == 0) barrier_expect(&sh.joined, (shares - 1) * (hi - lo) * kPitch * 4);
         if (mine == 0 && lane < shares && lane != plan.share)
           barrier_signal_at(address_in(shared_address(&sh.open), lane * S::kBlocks + plan.place));
@@ -908,10 +941,10 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
           sum_read();
         }
         fence_async();
-        if (!(fine = group_sync())) break;
+        meet();
         if (mine == 0) {
-          if (!(fine = warp_wait(&sh.open, items & 1, watch))) break;
-          if (lane < shares && lane != plan.share) {
+          fine = warp_wait(&sh.open, items & 1, watch);
+          if (fine && lane < shares && lane != plan.share) {
             const int q = lane, begin = from_of(q), wide = from_of(q + 1) - begin;
             const int place = (item.rows - wide) + (plan.share < q ? plan.share : plan.share - 1) * wide;  // there
             const uint32_t there = q * S::kBlocks + plan.place;
@@ -922,16 +955,13 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
           }
           __syncwarp();
         }
-        if (!(fine = warp_wait(&sh.joined, items & 1, watch))) break;
+        if (!(fine = agree(fine && warp_wait(&sh.joined, items & 1, watch)))) break;
         if (mine == 0 && lane < shares && lane != plan.share)
           barrier_signal_at(address_in(shared_address(&sh.taken), lane * S::kBlocks + plan.place));
       }
       for (int c = lo; c < hi; c += kStaged, ++chunks) {
         uint32_t r[kStaged];
         tensor_load(r, sum + c);
-        int note[4];
-        float4 more[4], z[4];
-        prepare(c + mine * 4, hi, note, more);
         tensor_loaded(r);
         if (c + kStaged >= hi) {
           fence_before();
@@ -950,7 +980,15 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         }
 #pragma unroll
         for (int i = 0; i < kStaged; ++i) staged[i][feature] = v[i];
-        if (!(fine = group_sync())) break;
+        meet();
+        int note[4];
+        float4 more[4], z[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          note[i] = next_note[i];
+          more[i] = next_more[i];
+        }
+        prepare(c + kStaged + mine * 4, hi, next_note, next_more);  // under way during this chunk
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float* from = staged[mine * 4 + i];
@@ -963,7 +1001,6 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         }
         finish(c + mine * 4, z, note, more);
       }
-      if (!fine) break;
       if (shares > 1) {
         fence_async();  // the stages are written by copies next
         warp_arrive(&sh.turn, lane);
@@ -1066,7 +1103,7 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
   using S = Shape<kRows, kFp8>;
   auto kernel = product_kernel<kRows, kFp8, kGated>;
   using Sh = Shared<kRows, kFp8>;
-  constexpr int kBytes = static_cast<int>(sizeof(Sh)) + 1024;
+  constexpr int kLeastBytes = static_cast<int>(sizeof(Sh)) + 1024, kBytes = kLeastBytes + segment_bytes(ES_MAX_EXPERTS);
   static_assert(kBytes <= 232448, "shared memory of a block");
   constexpr int kWidth = ((kRows + S::kMostShares - 1) / S::kMostShares + kStaged - 1) / kStaged * kStaged;
   static_assert((kRows + (S::kMostShares - 2) * kWidth) * kPitch * 4 <= offsetof(Sh, staged),
@@ -1155,7 +1192,7 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
   cudaLaunchConfig_t config{};
   config.gridDim = dim3(static_cast<unsigned>(grid));
   config.blockDim = dim3(S::kThreads);
-  config.dynamicSmemBytes = kBytes;
+  config.dynamicSmemBytes = kLeastBytes + segment_bytes(rows.joined ? 1 : rows.segments);
   config.stream = stream;
   config.attrs = attr;
   config.numAttrs = shares * S::kBlocks > 1 ? 2 : 1;
@@ -1204,7 +1241,7 @@ cudaError_t launch_grid(void (*kernel)(P...), dim3 grid, int block, size_t share
 
 template <int kSteps>
 cudaError_t launch_shrink(const ShrinkArgs& a, cudaStream_t stream) {
-  constexpr int kBytes = kShrinkWarps * kShrinkRows * (kSteps * 8 + 1) * 4;
+  constexpr int kBytes = (kShrinkWarps * (kSteps * 8 + 1) + (kSteps * 8 + 15) / 16 * 16) * kShrinkRows * 4;
   if (kBytes > 48 * 1024) {
     const cudaError_t err = cudaFuncSetAttribute(shrink_kernel<kSteps>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
     if (err != cudaSuccess) {
@@ -1258,24 +1295,19 @@ es_status_t launch_project(const MatrixView& w, const CUtensorMap* w_maps, bool 
     uint16_t* h = reinterpret_cast<uint16_t*>(behind);
     int32_t* of_row = reinterpret_cast<int32_t*>(behind + rounded(n * 4 * padded));
     int32_t* of_block = reinterpret_cast<int32_t*>(behind + rounded(n * 4 * padded) + rounded(n * 4));
-    const ShrinkArgs a{rows.x, rows.start, adapter, adapters->a, adapters->scale, w.scale, h, of_row, of_block, rows.x_stride,
-                       adapters->a_stride, rows.segments, rows.rows, adapters->count, adapters->rank, padded, w.in};
+    float* extra = std::min(rows.segments, rows.rows) > 1 && rows.rows <= kMostExtra
+                       ? reinterpret_cast<float*>(behind + rounded(n * 4 * padded) + 2 * rounded(n * 4)) : nullptr;
+    const ShrinkArgs a{rows.x, rows.start, adapter, adapters->a, adapters->scale, w.scale, h, of_row, of_block, adapters->b, extra,
+                       rows.x_stride, adapters->a_stride, adapters->b_stride, rows.segments, rows.rows, adapters->count, adapters->rank,
+                       padded, w.in, w.out};
     const int steps = (adapters->rank + 7) / 8;
-    cudaError_t err = steps <= 1   ? launch_shrink<1>(a, stream)
-                      : steps <= 2 ? launch_shrink<2>(a, stream)
-                      : steps <= 4 ? launch_shrink<4>(a, stream)
-                      : steps <= 8 ? launch_shrink<8>(a, stream)
-                                   : launch_shrink<16>(a, stream);
+    const cudaError_t err = steps <= 1   ? launch_shrink<1>(a, stream)
+                            : steps <= 2 ? launch_shrink<2>(a, stream)
+                            : steps <= 4 ? launch_shrink<4>(a, stream)
+                            : steps <= 8 ? launch_shrink<8>(a, stream)
+                                         : launch_shrink<16>(a, stream);
     if (err != cudaSuccess) return cuda_fail(err, call);
-    expand = ExpandView{h, adapters->b, of_row, of_block, nullptr, adapters->b_stride, adapters->rank, padded};
-    if (std::min(rows.segments, rows.rows) > 1 && rows.rows <= kMostExtra) {
-      float* extra = reinterpret_cast<float*>(behind + rounded(n * 4 * padded) + 2 * rounded(n * 4));
-      auto kernel = adapters->rank % 16 == 0 ? expand_kernel<16> : expand_kernel<8>;
-      err = launch_grid(kernel, dim3((w.out + kExpandWarps * kFeatures - 1) / (kExpandWarps * kFeatures), (rows.rows + kExpandRows - 1) / kExpandRows),
-                        kExpandWarps * 32, 0, stream, expand, extra, rows.rows, w.out);
-      if (err != cudaSuccess) return cuda_fail(err, call);
-      expand.extra = extra;
-    }
+    expand = ExpandView{h, adapters->b, of_row, of_block, extra, adapters->b_stride, adapters->rank, padded};
   }
   const int tile = rows.rows > kFew ? kMany : rows.rows > kLeast ? kFew : kLeast;
   auto f = tile == kMany ? launch_rows<kMany> : tile == kFew ? launch_rows<kFew> : launch_rows<kLeast>;
