@@ -913,16 +913,21 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       int lo = 0, hi = item.rows;
       float* send = reinterpret_cast<float*>(sh.w);  // of other blocks' columns, in their order
       const float* received = send;                  // of these, from each other block in turn
-      int next_note[4];
-      float4 next_more[4];
-      if (shares == 1) prepare(mine * 4, hi, next_note, next_more);
+      // of two chunks of columns, each asked for two chunks ahead
+      int note_a[4], note_b[4];
+      float4 more_a[4], more_b[4];
+      auto prepare_both = [&] {
+        prepare(lo + mine * 4, hi, note_a, more_a);
+        prepare(lo + kStaged + mine * 4, hi, note_b, more_b);
+      };
+      if (shares == 1) prepare_both();
       if (shares > 1) {
         const int width = ((item.rows + shares - 1) / shares + kStaged - 1) / kStaged * kStaged;
         auto from_of = [&](int q) { return min(q * width, item.rows); };
         lo = from_of(plan.share);
         hi = from_of(plan.share + 1);
         received = send + (item.rows - (hi - lo)) * kPitch;
-        prepare(lo + mine * 4, hi, next_note, next_more);
+        prepare_both();
         if (feature == 0) barrier_expect(&sh.joined, (shares - 1) * (hi - lo) * kPitch * 4);
         if (mine == 0 && lane < shares && lane != plan.share)
           barrier_signal_at(address_in(shared_address(&sh.open), lane * S::kBlocks + plan.place));
@@ -959,7 +964,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         if (mine == 0 && lane < shares && lane != plan.share)
           barrier_signal_at(address_in(shared_address(&sh.taken), lane * S::kBlocks + plan.place));
       }
-      for (int c = lo; c < hi; c += kStaged, ++chunks) {
+      auto write_chunk = [&](int c, int (&note)[4], float4 (&more)[4]) {
         uint32_t r[kStaged];
         tensor_load(r, sum + c);
         tensor_loaded(r);
@@ -981,14 +986,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
 #pragma unroll
         for (int i = 0; i < kStaged; ++i) staged[i][feature] = v[i];
         meet();
-        int note[4];
-        float4 more[4], z[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          note[i] = next_note[i];
-          more[i] = next_more[i];
-        }
-        prepare(c + kStaged + mine * 4, hi, next_note, next_more);  // under way during this chunk
+        float4 z[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float* from = staged[mine * 4 + i];
@@ -1000,6 +998,12 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
           }
         }
         finish(c + mine * 4, z, note, more);
+        prepare(c + 2 * kStaged + mine * 4, hi, note, more);
+        ++chunks;
+      };
+      for (int c = lo; c < hi; c += 2 * kStaged) {
+        write_chunk(c, note_a, more_a);
+        if (c + kStaged < hi) write_chunk(c + kStaged, note_b, more_b);
       }
       if (shares > 1) {
         fence_async();  // the stages are written by copies next
@@ -1251,7 +1255,7 @@ cudaError_t launch_shrink(const ShrinkArgs& a, cudaStream_t stream) {
   }
   const int most = std::min(std::min(a.requests, a.rows), kShrinkRows);  // adapters that the rows of a block can have
   const int blocks = (a.rows + kShrinkRows - 1) / kShrinkRows;
-  const dim3 grid = blocks <= 16 ? dim3(blocks, most, 8) : blocks <= 128 ? dim3(blocks, std::min(most, 4), 4) : dim3(blocks, 1, 2);
+  const dim3 grid = blocks <= 16 ? dim3(blocks, std::min(most, std::max(8, 48 / blocks)), 8) : blocks <= 128 ? dim3(blocks, std::min(most, 4), 4) : dim3(blocks, 1, 2);
   return launch_grid(shrink_kernel<kSteps>, grid, kShrinkWarps * 32, kBytes, stream, a);
 }
 
