@@ -396,27 +396,27 @@ constexpr int segment_bytes(int segments) { return (2 * segments + 1) * 4; }
 
 // 16 E4M3 codes as bf16 numbers, exactly. A code's bits, in their place, are those of a bf16 number 2^120 times
 // smaller, denormals among them, so shifts and a product (with `unit`, two times 2^120) convert two. Only NaN
-// differs, and is looked for.
-__device__ __forceinline__ void bf16_of_codes(const uint32_t (&code)[4], uint32_t unit, uint32_t (&v)[8]) {
-  uint32_t nan = 0;
+// differs: bits of `nan` 0x80808080 say that there is one.
+__device__ __forceinline__ void bf16_of_codes(uint4 code, uint32_t unit, uint4 (&v)[2], uint32_t& nan) {
+  const uint32_t in[4] = {code.x, code.y, code.z, code.w};
+  uint32_t out[8];
 #pragma unroll
   for (int d = 0; d < 4; ++d) {
-    nan |= (code[d] & 0x7F7F7F7Fu) + 0x01010101u;
+    nan |= (in[d] & 0x7F7F7F7Fu) + 0x01010101u;
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-      const uint32_t w = __byte_perm(code[d], 0, p == 0 ? 0x4140 : 0x4342);  // each code in the lower byte of its half
+      const uint32_t w = __byte_perm(in[d], 0, p == 0 ? 0x4140 : 0x4342);  // each code in the lower byte of its half
       const uint32_t bits = (w * 256 & 0x80008000u) | (w * 16 & 0x07F007F0u);
-      asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[2 * d + p]) : "r"(bits), "r"(unit), "r"(0x80008000u));
+      asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(out[2 * d + p]) : "r"(bits), "r"(unit), "r"(0x80008000u));
     }
   }
-  if (nan & 0x80808080u) {
-#pragma unroll
-    for (int d = 0; d < 4; ++d) {
-      v[2 * d] = unit != 0 ? bf16_of_e4m3(code[d] & 0xFFFFu) : 0;
-      v[2 * d + 1] = unit != 0 ? bf16_of_e4m3(code[d] >> 16) : 0;
-    }
-  }
+  v[0] = make_uint4(out[0], out[1], out[2], out[3]);
+  v[1] = make_uint4(out[4], out[5], out[6], out[7]);
 }
+
+// x / (1 + exp(-x)) by the fast exponential and division, each off by some 2^-21 of it at the sizes where it is not
+// far below what bf16 keeps beside it.
+__device__ __forceinline__ float silu(float x) { return __fdividef(x, 1.0f + exp2_approx(x * -kLog2e)); }
 
 // What all roles need of a call's tiles. A tile is kFeatures features a block (gated: 64 and the 64 that
 // they are multiplied with) and up to kRows rows of a segment; its depth is `depth` stages. Tiles go to
@@ -649,7 +649,10 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       if constexpr (kTogether) load_box_pair(map, to, address_in(shared_address(&sh.full[stage]), first), x, y);
       else load_box(map, to, &sh.full[stage], x, y);
     };
-    for (; fine && walk.next(item); ++items) {
+    Item upcoming;
+    bool more = walk.next(upcoming);
+    for (; fine && more; ++items) {
+      item = upcoming;
       // the stages hold what the cluster's blocks have of the tile before, and what others are still to take
       if (shares > 1 && items > 0 && !(fine = warp_wait(&sh.turn, (items - 1) & 1, watch) && warp_wait(&sh.taken, (items - 1) & 1, watch)))
         break;
@@ -671,6 +674,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
                 copy2(&x_map, x_to + j * S::kX + i * (box * kDepth * 2), stage, k * S::kDeep + j * kDepth, row0 + i * box);
         }
         __syncwarp();
+        if (k == item.k0) more = walk.next(upcoming);
       }
       if (!fine || expand.h == nullptr || item.k1 < plan.depth) continue;
       if (early) wait_for_previous();
@@ -897,8 +901,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
           const uint64_t row = item.row0 + column + i;
           uint16_t* to = rows.y + row * rows.y_stride + f;
           if (kGated) {
-            const float g0 = z[i].x * scale, g1 = z[i].y * scale;
-            const uint32_t y = pack_bf16(g0 / (1.0f + expf(-g0)) * (z[i].z * scale), g1 / (1.0f + expf(-g1)) * (z[i].w * scale));
+            const uint32_t y = pack_bf16(silu(z[i].x * scale) * (z[i].z * scale), silu(z[i].y * scale) * (z[i].w * scale));
             *reinterpret_cast<uint32_t*>(to) = note[i] == kAbsent ? 0 : y;
           } else {
             if (expand.h != nullptr && expand.extra == nullptr && note[i] >= 0) more[i] = expanded(expand, row, note[i], f);
@@ -1046,16 +1049,32 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
           constexpr int kTurns = kFeatures * kDepth / 16 / 32 / S::kTeam;
           const int within = lane & 4 ? lane >> 3 ^ 5 : lane >> 3, piece = lane & 3;
           const int from = S::kParts == 2 ? ((part % 2 * 4 + piece) ^ within) * 16 : piece * 16;
-#pragma unroll(kTurns < 4 ? kTurns : 4)
-          for (int i = 0; i < kTurns; ++i) {
-            const int at = (i * S::kTeam + member) * 8 + within;
-            const uint4 c = *reinterpret_cast<const uint4*>(&sh.raw[stage][at * S::kDeep + from]);
-            const uint32_t code[4] = {c.x, c.y, c.z, c.w};
-            uint32_t v[8];
-            bf16_of_codes(code, unit, v);
-            uint8_t* to = &sh.w[team][at * 128];
-            *reinterpret_cast<uint4*>(to + ((piece * 2) ^ within) * 16) = make_uint4(v[0], v[1], v[2], v[3]);
-            *reinterpret_cast<uint4*>(to + ((piece * 2 + 1) ^ within) * 16) = make_uint4(v[4], v[5], v[6], v[7]);
+          const uint8_t* codes_at = &sh.raw[stage][(member * 8 + within) * S::kDeep + from];
+          uint8_t* to = &sh.w[team][(member * 8 + within) * 128];
+          const int place[2] = {((piece * 2) ^ within) * 16, ((piece * 2 + 1) ^ within) * 16};
+          uint32_t nan = 0;
+          constexpr int kAtOnce = 4;
+#pragma unroll 1
+          for (int i0 = 0; i0 < kTurns; i0 += kAtOnce) {
+            uint4 c[kAtOnce];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+              c[i] = *reinterpret_cast<const uint4*>(codes_at + (i0 + i) * (S::kTeam * 8 * S::kDeep));
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+              uint4 v[2];
+              bf16_of_codes(c[i], unit, v, nan);
+#pragma unroll
+              for (int h = 0; h < 2; ++h) *reinterpret_cast<uint4*>(to + (i0 + i) * (S::kTeam * 8 * 128) + place[h]) = v[h];
+            }
+          }
+          if (nan & 0x80808080u && unit != 0) {
+            for (int i = 0; i < kTurns; ++i) {
+              const uint4 c = *reinterpret_cast<const uint4*>(codes_at + i * (S::kTeam * 8 * S::kDeep));
+              const uint4 v[2] = {make_uint4(bf16_of_e4m3(c.x & 0xFFFFu), bf16_of_e4m3(c.x >> 16), bf16_of_e4m3(c.y & 0xFFFFu), bf16_of_e4m3(c.y >> 16)),
+                                  make_uint4(bf16_of_e4m3(c.z & 0xFFFFu), bf16_of_e4m3(c.z >> 16), bf16_of_e4m3(c.w & 0xFFFFu), bf16_of_e4m3(c.w >> 16))};
+              for (int h = 0; h < 2; ++h) *reinterpret_cast<uint4*>(to + i * (S::kTeam * 8 * 128) + place[h]) = v[h];
+            }
           }
           fence_async();
         }
