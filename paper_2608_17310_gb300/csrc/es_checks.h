@@ -4,6 +4,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
@@ -56,14 +57,18 @@ using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, 
                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// The driver's cuTensorMapEncodeTiled, which the library is not linked against.
+// The driver's cuTensorMapEncodeTiled, which the library is not linked against; looked up once.
 inline es_status_t encode_tiled(EncodeTiled* out) {
+  static std::atomic<EncodeTiled> kept{nullptr};
+  *out = kept.load(std::memory_order_acquire);
+  if (*out != nullptr) return ES_OK;
   void* found = nullptr;
   cudaDriverEntryPointQueryResult result;
   const cudaError_t err = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &found, 12000, cudaEnableDefault, &result);
   if (err != cudaSuccess || found == nullptr)
     return cuda_fail(err != cudaSuccess ? err : cudaErrorNotSupported, "cuTensorMapEncodeTiled");
   *out = reinterpret_cast<EncodeTiled>(found);
+  kept.store(*out, std::memory_order_release);
   return ES_OK;
 }
 

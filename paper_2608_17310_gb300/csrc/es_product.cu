@@ -5,7 +5,6 @@
 #include <algorithm>
 #include <atomic>
 #include <cstddef>
-#include <cstdlib>
 
 #include "es_attention.cuh"
 #include "es_checks.h"
@@ -703,9 +702,10 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       }
     }
     // No copy outlives the block: the stage has been filled, or, where the first block of a pair is told of that,
-    // its products are done.
-    for (uint32_t i = done > kStages ? done - kStages : 0; i < done; ++i)
-      barrier_settle(kTogether && plan.place != 0 ? &sh.empty[i % kStages] : &sh.full[i % kStages], i / kStages & 1);
+    // its products are done. After a wait that was given up a pair's copies may be counted nowhere (see the end).
+    if (fine || !kTogether)
+      for (uint32_t i = done > kStages ? done - kStages : 0; i < done; ++i)
+        barrier_settle(kTogether && plan.place != 0 ? &sh.empty[i % kStages] : &sh.full[i % kStages], i / kStages & 1);
   } else if (warp == 1) {
     // --- products, issued by the first block of a pair
     Walk<kRows, kFp8, kGated> walk(rows, sh, plan);
@@ -1089,6 +1089,9 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
     }
   }
   __syncwarp();
+  // Copies between blocks that nobody waits for any more end within microseconds.
+  if ((kPair || shares > 1) && sh.failed)
+    for (int i = 0; i < 1000; ++i) __nanosleep(1000);
   let_next_start();
   fence_before();
   if (kPair || shares > 1) cluster_sync();  // no block leaves while others read its sums or arrive at its barriers
@@ -1186,7 +1189,6 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
       shares = i;
     }
   }
-  if (getenv("ES_SHARES")) shares = std::min(atoi(getenv("ES_SHARES")), S::kMostShares);
   const int grid = static_cast<int>(std::min<int64_t>(tiles, clusters[shares])) * shares * S::kBlocks;
   // rows of a copy of x: all that a tile has where there is one column of tiles, else as many as most have
   const int here = (std::min(most_rows, kRows) + 15) / 16 * 16 / S::kBlocks;
@@ -1341,7 +1343,7 @@ es_status_t launch_project(const MatrixView& w, const CUtensorMap* w_maps, bool 
 es_status_t launch_experts(const MatrixView& w, const CUtensorMap* w_maps, bool fp8, bool gated, const RowView& rows, void* workspace,
                            cudaStream_t stream, const char* call) {
   char* at = static_cast<char*>(workspace);
-  const int tile = rows.rows > kFew && rows.rows / w.groups > 32 ? kMany : rows.rows > kLeast ? kFew : kLeast;
+  const int tile = rows.rows > kFew && rows.rows / w.groups > 48 ? kMany : rows.rows > kLeast ? kFew : kLeast;
   RowView r = rows;
   bool early = false;
   if (tile == kMany && rows.index != nullptr) {

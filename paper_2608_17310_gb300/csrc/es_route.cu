@@ -7,8 +7,7 @@
 namespace esopt {
 namespace {
 
-constexpr int kRouteThreads = 512;
-constexpr int kRouteWarps = kRouteThreads / 32;
+constexpr int kRouteWarps = 16, kAloneWarps = 32;  // of a block among others, and of one alone
 constexpr int kRouteGrid = 304;  // two blocks an SM
 
 struct RouteArgs {
@@ -68,29 +67,74 @@ __device__ __forceinline__ void choose(const RouteArgs& a, const int64_t (&token
         if (code[n][i] != 0) all[n] += expf(score_of_code(code[n][i]) - top[n]);
     }
   }
-  for (int j = 0; j < a.top; ++j) {
-    uint32_t most[kTokens], at[kTokens];
-#pragma unroll
-    for (int n = 0; n < kTokens; ++n) most[n] = __reduce_max_sync(0xFFFFFFFFu, best[n]);
+  if constexpr (kPerLane <= 4) {
+    // A lane keeps its scores in order (equal ones by the lower expert), so only their first takes part, and the
+    // reduction for the lowest expert is left for scores that several lanes have.
+    int of[kTokens][kPerLane];
 #pragma unroll
     for (int n = 0; n < kTokens; ++n) {
-      at[n] = 0xFFFFFFFFu;
 #pragma unroll
-      for (int i = kPerLane - 1; i >= 0; --i)
-        if (code[n][i] == most[n]) at[n] = i * 32 + lane;
-      at[n] = __reduce_min_sync(0xFFFFFFFFu, at[n]);
+      for (int i = 0; i < kPerLane; ++i) of[n][i] = i * 32 + lane;
+#pragma unroll
+      for (int end = kPerLane - 1; end > 0; --end)
+#pragma unroll
+        for (int i = 0; i < end; ++i)
+          if (code[n][i + 1] > code[n][i]) {
+            const uint32_t c = code[n][i];
+            code[n][i] = code[n][i + 1];
+            code[n][i + 1] = c;
+            const int o = of[n][i];
+            of[n][i] = of[n][i + 1];
+            of[n][i + 1] = o;
+          }
     }
+    for (int j = 0; j < a.top; ++j) {
 #pragma unroll
-    for (int n = 0; n < kTokens; ++n) {
-      best[n] = 0;
+      for (int n = 0; n < kTokens; ++n) {
+        const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, code[n][0]);
+        const bool has = code[n][0] == most;
+        const uint32_t those = __ballot_sync(0xFFFFFFFFu, has);
+        int at = __shfl_sync(0xFFFFFFFFu, of[n][0], __ffs(those) - 1);
+        if (those & (those - 1)) at = static_cast<int>(__reduce_min_sync(0xFFFFFFFFu, has ? static_cast<uint32_t>(of[n][0]) : 0xFFFFFFFFu));
+        if (lane == j && most != 0) {
+          expert[n] = at;
+          mine[n] = most;
+        }
+        if (has && of[n][0] == at) {
 #pragma unroll
-      for (int i = 0; i < kPerLane; ++i) {
-        if (static_cast<uint32_t>(i * 32 + lane) == at[n]) code[n][i] = 0;
-        best[n] = max(best[n], code[n][i]);
+          for (int i = 0; i + 1 < kPerLane; ++i) {
+            code[n][i] = code[n][i + 1];
+            of[n][i] = of[n][i + 1];
+          }
+          code[n][kPerLane - 1] = 0;
+        }
       }
-      if (lane == j && most[n] != 0) {
-        expert[n] = static_cast<int>(at[n]);
-        mine[n] = most[n];
+    }
+  } else {
+    for (int j = 0; j < a.top; ++j) {
+      uint32_t most[kTokens], at[kTokens];
+#pragma unroll
+      for (int n = 0; n < kTokens; ++n) most[n] = __reduce_max_sync(0xFFFFFFFFu, best[n]);
+#pragma unroll
+      for (int n = 0; n < kTokens; ++n) {
+        at[n] = 0xFFFFFFFFu;
+#pragma unroll
+        for (int i = kPerLane - 1; i >= 0; --i)
+          if (code[n][i] == most[n]) at[n] = i * 32 + lane;
+        at[n] = __reduce_min_sync(0xFFFFFFFFu, at[n]);
+      }
+#pragma unroll
+      for (int n = 0; n < kTokens; ++n) {
+        best[n] = 0;
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i) {
+          if (static_cast<uint32_t>(i * 32 + lane) == at[n]) code[n][i] = 0;
+          best[n] = max(best[n], code[n][i]);
+        }
+        if (lane == j && most[n] != 0) {
+          expert[n] = static_cast<int>(at[n]);
+          mine[n] = most[n];
+        }
       }
     }
   }
@@ -125,6 +169,7 @@ __device__ __forceinline__ void walk(const RouteArgs& a, int begin, int end, int
 }
 
 // Sum over the block's threads before this one; total: over all.
+template <int kWarps>
 __device__ __forceinline__ int scan_before(int x, int* shared, int& total) {
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   int sum = x;
@@ -137,7 +182,8 @@ __device__ __forceinline__ int scan_before(int x, int* shared, int& total) {
   __syncthreads();
   int before = 0;
   total = 0;
-  for (int w = 0; w < kRouteWarps; ++w) {
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
     if (w < warp) before += shared[w];
     total += shared[w];
   }
@@ -154,13 +200,14 @@ __device__ __forceinline__ int scan_before(int x, int* shared, int& total) {
 // expert's start, the pairs of earlier blocks and warps, and those before it in the warp
 // (__match_any_sync), whatever the timing.
 template <int kPerLane, bool kBf16, bool kAll>
-__global__ void __launch_bounds__(kRouteThreads)
+__global__ void __launch_bounds__((kAll ? kAloneWarps : kRouteWarps) * 32)
 choose_kernel(const RouteArgs a, int32_t* counts) {
+  constexpr int kWarps = kAll ? kAloneWarps : kRouteWarps;
   extern __shared__ int32_t next[];  // [warp][expert]
-  __shared__ int sums[kRouteWarps];
+  __shared__ int sums[kWarps];
   wait_for_previous();
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  const int64_t t0 = min((static_cast<int64_t>(blockIdx.x) * kRouteWarps + warp) * a.share, static_cast<int64_t>(a.tokens));
+  const int64_t t0 = min((static_cast<int64_t>(blockIdx.x) * kWarps + warp) * a.share, static_cast<int64_t>(a.tokens));
   const int64_t t1 = min(t0 + a.share, static_cast<int64_t>(a.tokens));
   int32_t* mine = next + warp * a.experts;
   for (int e = lane; e < a.experts; e += 32) mine[e] = 0;
@@ -185,24 +232,24 @@ choose_kernel(const RouteArgs a, int32_t* counts) {
   }
   __syncthreads();
   if (!kAll) {
-    for (int e = threadIdx.x; e < a.experts; e += kRouteThreads) {
+    for (int e = threadIdx.x; e < a.experts; e += kWarps * 32) {
       int sum = 0;
-      for (int w = 0; w < kRouteWarps; ++w) sum += next[w * a.experts + e];
+      for (int w = 0; w < kWarps; ++w) sum += next[w * a.experts + e];
       counts[e * kRouteGrid + blockIdx.x] = sum;
     }
     return;
   }
   int base = 0;
-  for (int e0 = 0; e0 < a.experts; e0 += kRouteThreads) {
+  for (int e0 = 0; e0 < a.experts; e0 += kWarps * 32) {
     const int e = e0 + threadIdx.x;
     int sum = 0;
     if (e < a.experts)
-      for (int w = 0; w < kRouteWarps; ++w) sum += next[w * a.experts + e];
+      for (int w = 0; w < kWarps; ++w) sum += next[w * a.experts + e];
     int total;
-    int at = base + scan_before(sum, sums, total);
+    int at = base + scan_before<kWarps>(sum, sums, total);
     if (e < a.experts) {
       a.start[e] = at;
-      for (int w = 0; w < kRouteWarps; ++w) {
+      for (int w = 0; w < kWarps; ++w) {
         const int n = next[w * a.experts + e];
         next[w * a.experts + e] = at;
         at += n;
@@ -216,7 +263,7 @@ choose_kernel(const RouteArgs a, int32_t* counts) {
 }
 
 // Places the pairs of the block's tokens, with the counts of all blocks.
-__global__ void __launch_bounds__(kRouteThreads)
+__global__ void __launch_bounds__(kRouteWarps * 32)
 place_kernel(const RouteArgs a, const int32_t* counts) {
   extern __shared__ int32_t next[];
   __shared__ int sums[kRouteWarps], whole[ES_MAX_EXPERTS], earlier[ES_MAX_EXPERTS];
@@ -229,7 +276,7 @@ place_kernel(const RouteArgs a, const int32_t* counts) {
   __syncwarp();
   walk<false>(a, static_cast<int>(t0) * a.top, static_cast<int>(t1) * a.top, mine, lane);
   // each expert's pairs, in all blocks and in those before this one
-#pragma unroll 2
+#pragma unroll 4
   for (int e = warp; e < a.experts; e += kRouteWarps) {
     int sum = 0, before = 0;
 #pragma unroll
@@ -248,10 +295,10 @@ place_kernel(const RouteArgs a, const int32_t* counts) {
   }
   __syncthreads();
   int base = 0;
-  for (int e0 = 0; e0 < a.experts; e0 += kRouteThreads) {
+  for (int e0 = 0; e0 < a.experts; e0 += kRouteWarps * 32) {
     const int e = e0 + threadIdx.x;
     int total;
-    int at = base + scan_before(e < a.experts ? whole[e] : 0, sums, total);
+    int at = base + scan_before<kRouteWarps>(e < a.experts ? whole[e] : 0, sums, total);
     if (e < a.experts) {
       if (blockIdx.x == 0) a.start[e] = at;
       at += earlier[e];
@@ -270,11 +317,11 @@ place_kernel(const RouteArgs a, const int32_t* counts) {
 
 template <int kPerLane, bool kBf16>
 cudaError_t route(RouteArgs a, int32_t* counts, cudaStream_t stream) {
-  const size_t shared = sizeof(int32_t) * kRouteWarps * a.experts;
+  const size_t alone = sizeof(int32_t) * kAloneWarps * a.experts, shared = sizeof(int32_t) * kRouteWarps * a.experts;
   auto one = choose_kernel<kPerLane, kBf16, true>;
   auto many = choose_kernel<kPerLane, kBf16, false>;
-  if (shared > 48 * 1024) {
-    cudaError_t err = cudaFuncSetAttribute(one, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
+  if (alone > 48 * 1024) {
+    cudaError_t err = cudaFuncSetAttribute(one, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(alone));
     if (err == cudaSuccess) err = cudaFuncSetAttribute(many, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
     if (err == cudaSuccess) err = cudaFuncSetAttribute(place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
     if (err != cudaSuccess) {
@@ -282,15 +329,15 @@ cudaError_t route(RouteArgs a, int32_t* counts, cudaStream_t stream) {
       return err;
     }
   }
-  if (a.tokens <= 16 * kRouteWarps) {
-    a.share = (a.tokens + kRouteWarps - 1) / kRouteWarps;
-    return launch_early(one, 1, kRouteThreads, shared, stream, a, counts);
+  if (a.tokens <= 8 * kAloneWarps) {
+    a.share = (a.tokens + kAloneWarps - 1) / kAloneWarps;
+    return launch_early(one, 1, kAloneWarps * 32, alone, stream, a, counts);
   }
   a.share = (a.tokens + kRouteWarps * kRouteGrid - 1) / (kRouteWarps * kRouteGrid);
   const int grid = (a.tokens + kRouteWarps * a.share - 1) / (kRouteWarps * a.share);
-  const cudaError_t err = launch_early(many, grid, kRouteThreads, shared, stream, a, counts);
+  const cudaError_t err = launch_early(many, grid, kRouteWarps * 32, shared, stream, a, counts);
   if (err != cudaSuccess) return err;
-  return launch_early(place_kernel, grid, kRouteThreads, shared, stream, a, static_cast<const int32_t*>(counts));
+  return launch_early(place_kernel, grid, kRouteWarps * 32, shared, stream, a, static_cast<const int32_t*>(counts));
 }
 
 struct CombineArgs {
