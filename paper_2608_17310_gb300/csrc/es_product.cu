@@ -1,4 +1,40 @@
 // es_project and es_project_experts: products of matrices with rows that choose them.
+//
+//   y_i = c_g W_g x_{r(i)} + B_m (s_m A_m x_i)
+//
+// with g the matrix and m the adapter of row i, both by segments of rows; gated: silu of the first half of the
+// features times the second.
+//
+// What bounds them: the bytes of W where an expert or a step has few rows (2 n operations a byte of bf16, so up
+// to some 290 rows), the tensor cores above. So one kernel takes both: features are the lanes of the tensor
+// memory, 128 a block, and rows its columns, from 16 to 256 in steps of 16, so that a ragged segment costs what
+// its rows cost and weights are read once where a segment has up to 256 rows.
+//   warp 0         copies W and x by TMA, 64 elements of a row a stage (FP8: 128 codes)
+//   warp 1         issues the products
+//   warps 2, 3     copy rows of x that are named one by one (gather4)
+//   warps 4 - 7    read the sums, and write them
+//   warps 8 - 15   FP8: turn codes into bf16, which holds them exactly
+// Tiles of 256 rows belong to pairs of blocks (cta_group::2), each of which copies half of x: what an SM can
+// ask of L2 at once bounds a block alone (650 cycles for the 512 of a stage's products; 528 by pairs). Two
+// tiles' sums have room in the tensor memory, so writing one runs beside the products of the next.
+//
+// Blocks are persistent and take tiles in turn, in bands of kBand column tiles, so that those that run
+// together share W and x in L2. Where the tiles are fewer than the blocks, up to eight share a tile's depth, in a
+// cluster: each sends the others their columns of its sums, by bulk copies between shared memories into the stages,
+// which are empty then, and sums what it is sent in the order of the blocks. So results do not depend on timing.
+//
+// Adapters. A kernel of its own makes h = s A x, as the sum of two bf16 numbers (2^-16 of it), for 32 rows and
+// one adapter a block. Where 16 rows have one adapter, B h is further products into the same sums. Where members
+// meet within 16 rows, products would multiply one's B by the others' zeros, and infinities or NaN of a member
+// that has diverged would reach all of them; there B h is made in fp32, row by row, by that kernel for up to
+// kMostExtra rows, else where results are written. The product's kernel starts beside it, and waits where
+// the adapters' part is needed.
+//
+// Measured (GB300, us a pass): project_prompts 13,741 rows of 30 members, 5,120 to 17,408 features, rank 32, 1,361
+// (1,816 TFLOP/s, 94 % of the card's bf16 matrix rate in a burst; 1,570 in long loops, where the power limit
+// holds the clock); 4,096 rows without adapters 393 (1,857 TFLOP/s; the library's product 391). experts_prompt
+// 32,764 rows of 32 experts gathered and gated 518, 40 of them the gather. experts_step 762 MB of experts for 576 rows
+// 114 (6,690 GB/s, 99 %). project_step 192 members' rows through 73 MB 39 (26 without the adapters).
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -35,7 +71,7 @@ struct ExpandView {
   const uint16_t* b;
   const int32_t* of_row;    // adapter of each row, or -1
   const int32_t* of_block;  // of each 16 rows
-  const float* extra;       // [rows][out] B h of the rows of mixed blocks, or NULL: where they are written
+  const float* extra;       // [rows][out] B h of the rows of mixed blocks, or NULL: it is made where they are written
   uint64_t b_stride;
   int rank, padded;
 };
@@ -170,169 +206,171 @@ shrink_kernel(const ShrinkArgs a) {
   const uint16_t* x0 = a.x + static_cast<uint64_t>(row0 + g) * a.x_stride;
   int turn = 0;
   for (uint32_t left = firsts; left != 0; left &= left - 1, ++turn) {
-  if (turn % gridDim.y != blockIdx.y) continue;
-  const int lead = __ffs(left) - 1;
-  const int m = __shfl_sync(0xFFFFFFFFu, mine, lead);
-  const uint32_t rows = __shfl_sync(0xFFFFFFFFu, same, lead);
-  const float factor = (a.scale != nullptr ? a.scale[m] : 1.0f) * undo_of(a.w_scale);
+    if (turn % gridDim.y != blockIdx.y) continue;
+    const int lead = __ffs(left) - 1;
+    const int m = __shfl_sync(0xFFFFFFFFu, mine, lead);
+    const uint32_t rows = __shfl_sync(0xFFFFFFFFu, same, lead);
+    const float factor = (a.scale != nullptr ? a.scale[m] : 1.0f) * undo_of(a.w_scale);
 
-  const uint16_t* from = a.a + m * a.a_stride;
-  const uint32_t expanded = a.extra != nullptr ? rows & mixed : 0;
-  if (expanded != 0)  // B to L2 meanwhile
-    for (int f = ((blockIdx.z * kWarps + warp) * 32 + lane) * 4; f < a.out; f += gridDim.z * kWarps * kFeatures)
-      for (int i = 0; i < a.rank * 8; i += 128)
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(a.b + m * a.b_stride + static_cast<uint64_t>(f) * a.rank) + i));
-  float sum[2][kSteps][4] = {};
-  // 64 elements of a row at a time, the next ones asked for before these are multiplied
-  struct Taken {
-    uint4 v[2][4], w[2][kSteps];
-  };
-  const uint4 zero = make_uint4(0, 0, 0, 0);
-  auto take = [&](Taken& to, int k0) {
+    const uint16_t* from = a.a + m * a.a_stride;
+    const uint32_t expanded = a.extra != nullptr ? rows & mixed : 0;
+    if (expanded != 0)  // B to L2 meanwhile
+      for (int f = ((blockIdx.z * kWarps + warp) * 32 + lane) * 4; f < a.out; f += gridDim.z * kWarps * kFeatures)
+        for (int i = 0; i < a.rank * 8; i += 128)
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(a.b + m * a.b_stride + static_cast<uint64_t>(f) * a.rank) + i));
+    float sum[2][kSteps][4] = {};
+    // 64 elements of a row at a time, the next ones asked for before these are multiplied
+    struct Taken {
+      uint4 v[2][4], w[2][kSteps];
+    };
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    auto take = [&](Taken& to, int k0) {
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      const int k = k0 + n * 32 + t * 8;
-      const bool inside = k < a.in;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        to.v[n][i] = inside && (rows >> (g + 8 * i) & 1) ? *reinterpret_cast<const uint4*>(x0 + 8 * i * a.x_stride + k) : zero;
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s)
-        to.w[n][s] = inside && s * 8 + g < a.rank ? *reinterpret_cast<const uint4*>(from + static_cast<uint64_t>(s * 8 + g) * a.in + k) : zero;
-    }
-  };
-  auto add = [&](const Taken& of) {
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        if (!(rows >> (16 * half) & 0xFFFFu)) continue;
-        const uint4 p = of.v[n][2 * half], q = of.v[n][2 * half + 1];
-        const uint32_t first[4] = {p.x, q.x, p.y, q.y}, second[4] = {p.z, q.z, p.w, q.w};
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-          mma_bf16(sum[half][s], first, of.w[n][s].x, of.w[n][s].y);
-          mma_bf16(sum[half][s], second, of.w[n][s].z, of.w[n][s].w);
-        }
-      }
-  };
-  const int stride = gridDim.z * kWarps * 64;
-  int k0 = (blockIdx.z * kWarps + warp) * 64;
-  if constexpr (kSteps <= 4) {
-    Taken one, two;
-    take(one, k0);
-    for (; k0 < a.in; k0 += 2 * stride) {
-      take(two, k0 + stride);
-      add(one);
-      take(one, k0 + 2 * stride);
-      add(two);
-    }
-  } else {
-    for (; k0 < a.in; k0 += stride) {
-      Taken one;
-      take(one, k0);
-      add(one);
-    }
-  }
-#pragma unroll
-  for (int half = 0; half < 2; ++half)
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        parts[(warp * kShrinkRows + half * 16 + g + i / 2 * 8) * kPitch + s * 8 + 2 * t + i % 2] = sum[half][s][i];
-  __syncthreads();
-  const int shares = gridDim.z;
-  if (shares > 1) {
-    // the block's sums to where its first warp's are, each by the thread that has read them
-    for (int i = threadIdx.x; i < kShrinkRows * a.rank; i += kWarps * 32) {
-      float* at = parts + i / a.rank * kPitch + i % a.rank;
-      float h = 0.0f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) h += at[w * kShrinkRows * kPitch];
-      *at = h;
-    }
-    cluster_sync();
-  }
-  float* whole = parts + kWarps * kShrinkRows * kPitch;  // [row][padded]
-  if (blockIdx.z == 0 || expanded != 0) {
-    for (int i = threadIdx.x; i < kShrinkRows * a.padded; i += kWarps * 32) {
-      const int n = i / a.padded, r = i % a.padded;
-      if (!(rows >> n & 1)) continue;
-      float h = 0.0f;
-      if (r < a.rank) {
-        const float* at = parts + n * kPitch + r;
-        if (shares > 1) {
-#pragma unroll 8
-          for (int z = 0; z < shares; ++z) h += load_float(address_in(shared_address(at), z));
-        } else {
-#pragma unroll
-          for (int w = 0; w < kWarps; ++w) h += at[w * kShrinkRows * kPitch];
-        }
-        h *= factor;
-      }
-      whole[i] = h;
-      if (blockIdx.z != 0) continue;
-      const uint32_t hi = pack_bf16(h, 0.0f) & 0xFFFFu;
-      uint16_t* to = a.h + static_cast<uint64_t>(row0 + n) * 2 * a.padded + r;
-      to[0] = static_cast<uint16_t>(hi);
-      // an infinite or NaN h has no second part
-      const float rest = h - bf16_value(hi);
-      to[a.padded] = static_cast<uint16_t>(pack_bf16(isfinite(rest) ? rest : 0.0f, 0.0f));
-    }
-  }
-  if (expanded != 0) {
-    __syncthreads();
-    // the cluster's warps share the features
-    for (int f = ((blockIdx.z * kWarps + warp) * 32 + lane) * 4; f < a.out; f += shares * kWarps * kFeatures) {
-      const uint16_t* factors = a.b + m * a.b_stride + static_cast<uint64_t>(f) * a.rank;
-      if constexpr (kSteps <= 2) {
-        Factors b[kSteps];
-#pragma unroll
-        for (int r = 0; r < kSteps; ++r) b[r].take(factors + r * 8, a.rank);
-        for (uint32_t left = expanded; left != 0; left &= left - 1) {
-          const int row = __ffs(left) - 1;
-          float y[4] = {};
-#pragma unroll
-          for (int r = 0; r < kSteps; ++r) b[r].add(y, whole + row * a.padded + r * 8);
-          *reinterpret_cast<float4*>(a.extra + static_cast<uint64_t>(row0 + row) * a.out + f) = make_float4(y[0], y[1], y[2], y[3]);
-        }
-        continue;
-      }
-      for (uint32_t left = expanded; left != 0;) {
-        int row[4];
-        float y[4][4] = {};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          row[i] = left != 0 ? __ffs(left) - 1 : -1;
-          left &= left - 1;
-        }
-#pragma unroll 2
-        for (int r = 0; r < a.rank; r += 8) {
-          Factors b;
-          b.take(factors + r, a.rank);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (row[i] >= 0) b.add(y[i], whole + row[i] * a.padded + r);
-        }
+      for (int n = 0; n < 2; ++n) {
+        const int k = k0 + n * 32 + t * 8;
+        const bool inside = k < a.in;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (row[i] >= 0)
-            *reinterpret_cast<float4*>(a.extra + static_cast<uint64_t>(row0 + row[i]) * a.out + f) =
-                make_float4(y[i][0], y[i][1], y[i][2], y[i][3]);
+          to.v[n][i] = inside && (rows >> (g + 8 * i) & 1) ? *reinterpret_cast<const uint4*>(x0 + 8 * i * a.x_stride + k) : zero;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+          to.w[n][s] = inside && s * 8 + g < a.rank ? *reinterpret_cast<const uint4*>(from + static_cast<uint64_t>(s * 8 + g) * a.in + k) : zero;
+      }
+    };
+    auto add = [&](const Taken& of) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          if (!(rows >> (16 * half) & 0xFFFFu)) continue;
+          const uint4 p = of.v[n][2 * half], q = of.v[n][2 * half + 1];
+          const uint32_t first[4] = {p.x, q.x, p.y, q.y}, second[4] = {p.z, q.z, p.w, q.w};
+#pragma unroll
+          for (int s = 0; s < kSteps; ++s) {
+            mma_bf16(sum[half][s], first, of.w[n][s].x, of.w[n][s].y);
+            mma_bf16(sum[half][s], second, of.w[n][s].z, of.w[n][s].w);
+          }
+        }
+    };
+    const int stride = gridDim.z * kWarps * 64;
+    int k0 = (blockIdx.z * kWarps + warp) * 64;
+    if constexpr (kSteps <= 4) {
+      Taken one, two;
+      take(one, k0);
+      for (; k0 < a.in; k0 += 2 * stride) {
+        take(two, k0 + stride);
+        add(one);
+        take(one, k0 + 2 * stride);
+        add(two);
+      }
+    } else {
+      for (; k0 < a.in; k0 += stride) {
+        Taken one;
+        take(one, k0);
+        add(one);
       }
     }
-  }
-  // the sums have been read before they are written again, and before a block leaves
-  if (shares > 1) cluster_sync();
-  else __syncthreads();
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          parts[(warp * kShrinkRows + half * 16 + g + i / 2 * 8) * kPitch + s * 8 + 2 * t + i % 2] = sum[half][s][i];
+    __syncthreads();
+    const int shares = gridDim.z;
+    if (shares > 1) {
+      // the block's sums to where its first warp's are, each by the thread that has read them
+      for (int i = threadIdx.x; i < kShrinkRows * a.rank; i += kWarps * 32) {
+        float* at = parts + i / a.rank * kPitch + i % a.rank;
+        float h = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) h += at[w * kShrinkRows * kPitch];
+        *at = h;
+      }
+      cluster_sync();
+    }
+    float* whole = parts + kWarps * kShrinkRows * kPitch;  // [row][padded]
+    if (blockIdx.z == 0 || expanded != 0) {
+      for (int i = threadIdx.x; i < kShrinkRows * a.padded; i += kWarps * 32) {
+        const int n = i / a.padded, r = i % a.padded;
+        if (!(rows >> n & 1)) continue;
+        float h = 0.0f;
+        if (r < a.rank) {
+          const float* at = parts + n * kPitch + r;
+          if (shares > 1) {
+#pragma unroll 8
+            for (int z = 0; z < shares; ++z) h += load_float(address_in(shared_address(at), z));
+          } else {
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) h += at[w * kShrinkRows * kPitch];
+          }
+          h *= factor;
+        }
+        whole[i] = h;
+        if (blockIdx.z != 0) continue;
+        const uint32_t hi = pack_bf16(h, 0.0f) & 0xFFFFu;
+        uint16_t* to = a.h + static_cast<uint64_t>(row0 + n) * 2 * a.padded + r;
+        to[0] = static_cast<uint16_t>(hi);
+        // an infinite or NaN h has no second part
+        const float rest = h - bf16_value(hi);
+        to[a.padded] = static_cast<uint16_t>(pack_bf16(isfinite(rest) ? rest : 0.0f, 0.0f));
+      }
+    }
+    if (expanded != 0) {
+      __syncthreads();
+      // the cluster's warps share the features
+      for (int f = ((blockIdx.z * kWarps + warp) * 32 + lane) * 4; f < a.out; f += shares * kWarps * kFeatures) {
+        const uint16_t* factors = a.b + m * a.b_stride + static_cast<uint64_t>(f) * a.rank;
+        if constexpr (kSteps <= 2) {
+          Factors b[kSteps];
+#pragma unroll
+          for (int r = 0; r < kSteps; ++r) b[r].take(factors + r * 8, a.rank);
+          for (uint32_t left = expanded; left != 0; left &= left - 1) {
+            const int row = __ffs(left) - 1;
+            float y[4] = {};
+#pragma unroll
+            for (int r = 0; r < kSteps; ++r) b[r].add(y, whole + row * a.padded + r * 8);
+            *reinterpret_cast<float4*>(a.extra + static_cast<uint64_t>(row0 + row) * a.out + f) = make_float4(y[0], y[1], y[2], y[3]);
+          }
+          continue;
+        }
+        for (uint32_t left = expanded; left != 0;) {
+          int row[4];
+          float y[4][4] = {};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            row[i] = left != 0 ? __ffs(left) - 1 : -1;
+            left &= left - 1;
+          }
+#pragma unroll 2
+          for (int r = 0; r < a.rank; r += 8) {
+            Factors b;
+            b.take(factors + r, a.rank);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (row[i] >= 0) b.add(y[i], whole + row[i] * a.padded + r);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (row[i] >= 0)
+              *reinterpret_cast<float4*>(a.extra + static_cast<uint64_t>(row0 + row[i]) * a.out + f) =
+                  make_float4(y[i][0], y[i][1], y[i][2], y[i][3]);
+        }
+      }
+    }
+    // the sums have been read before they are written again, and before a block leaves
+    if (shares > 1) cluster_sync();
+    else __syncthreads();
   }
 }
 
 // --- rows that are named one by one ---------------------------------------------------------
 
-// Copies the rows of x that slots name (zeros for those that do not exist) so that they lie in order. A
-// warp has a slot.
+// Copies the rows of x that slots name (zeros for those that do not exist) so that they lie in order, for tiles of
+// many rows: there the copies one by one, four rows an instruction and 65 cycles each, took 1,581 us for a prompt whose
+// product takes 480 so. A warp has a slot. 40 us for 8,191 rows of 5,120 bytes four times each, 84 % of the
+// copy bandwidth.
 __global__ void __launch_bounds__(256)
 gather_kernel(const RowView rows, uint16_t* to, int in) {
   wait_for_previous();
@@ -1172,7 +1210,9 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
     }
   }
   // How many blocks, or pairs, share a tile's depth: what takes least time, by the bytes of weights at the memory's rate
-  // or a block's stages at its own, whichever is more, and the joins.
+  // or a block's stages at its own, whichever is more, and the joins. 48 tiles of 40 stages (project_token): 16.0 us by
+  // one block each, 14.1 by two, 20.4 by three (two rounds). 80 of 40 (experts_token): 16.2, 21.6 (two rounds), 18.6. 20 FP8
+  // ones of 76 stages (project_step_e4m3): 61, 43, 36, 32 by four, 31 by six, 33 by eight (two rounds).
   const int outs = kGated ? w.out / 2 : w.out, wide = (kGated ? kFeatures / 2 : kFeatures) * S::kBlocks;
   const int64_t tiles = static_cast<int64_t>(columns) * ((outs + wide - 1) / wide);
   const int depth = (w.in + S::kDeep - 1) / S::kDeep;
@@ -1237,8 +1277,16 @@ es_status_t launch_rows(const MatrixView& w, const CUtensorMap& w_map, bool fp8,
   return f(w, w_map, rows, expand, b_map, columns, most_rows, early, workspace, stream, call);
 }
 
-constexpr int kLeast = 16, kFew = 64, kMany = 256;  // rows of a tile
-constexpr int kMostExtra = 1024;       // rows up to which B h has room in the workspace
+// Rows of a tile. One matrix of 5,120 by 7,168: 32 rows take 25.3 us by tiles of 16, 20.0 by tiles of 64 (whose fewer
+// stages cost 16 rows nothing: 20.1, 19.9; those of 16 leave room where depth is short: 2,560 by 9,728 16.0, 16.3);
+// 64 rows 21.2 by tiles of 64 and 21.8 by pairs; 96 rows 27.1 and 22.7; 192 rows 46.4 and 25.9. FP8 64 rows 23.0 and
+// 25.9, 96 rows 35.0 and 27.6. Experts go by their mean, with 0.4 to 1.6 times that each: 48 experts of 1,280 by 2,560 at
+// 48 rows 59.8 and 61.4, at 64 rows 67.1 and 62.6; FP8 67.7 and 71.6, 81.8 and 74.2.
+constexpr int kLeast = 16, kFew = 64, kMany = 256;
+constexpr int kManyEach = 48;  // rows an expert above which tiles are of kMany
+// Rows up to which B h of rows beside others' has room in the workspace (4 bytes a feature and row); where results are
+// written it costs a step of 192 rows some 50 us, but for more rows mixed blocks are few, or the product long.
+constexpr int kMostExtra = 1024;
 
 uint64_t padded_rank(int rank) { return static_cast<uint64_t>(rank + 15) / 16 * 16; }
 uint64_t rounded(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -1343,7 +1391,7 @@ es_status_t launch_project(const MatrixView& w, const CUtensorMap* w_maps, bool 
 es_status_t launch_experts(const MatrixView& w, const CUtensorMap* w_maps, bool fp8, bool gated, const RowView& rows, void* workspace,
                            cudaStream_t stream, const char* call) {
   char* at = static_cast<char*>(workspace);
-  const int tile = rows.rows > kFew && rows.rows / w.groups > 48 ? kMany : rows.rows > kLeast ? kFew : kLeast;
+  const int tile = rows.rows > kFew && rows.rows / w.groups > kManyEach ? kMany : rows.rows > kLeast ? kFew : kLeast;
   RowView r = rows;
   bool early = false;
   if (tile == kMany && rows.index != nullptr) {
