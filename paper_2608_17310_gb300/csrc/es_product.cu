@@ -396,17 +396,20 @@ struct Shape {
   static constexpr bool kPair = kRows == 256;
   static constexpr int kBlocks = kPair ? 2 : 1;
   static constexpr int kBox = kPair ? 64 : 16;  // rows of a copy of h
-  static constexpr int kSlots = 4;              // of converted codes
-  // Elements of a row in a stage, and products' depths of 64 of them. What an SM has under way is bound by requests,
+  // Converted codes of four stages, in the tensor memory behind two tiles' sums, or for pairs in shared memory.
+  static constexpr int kSlots = 4;
+  static constexpr bool kInTensor = kFp8 && !kPair;
+  static constexpr int kSums = kInTensor ? 64 : 256;  // columns from one tile's sums to the next one's
+  // Elements of a row in a stage, and how many times 64 of them. What an SM has under way is bound by requests,
   // so codes come 128 bytes at a time where the stages have room (a step's experts 56 us by 64 bytes).
-  static constexpr int kDeep = kFp8 && !kPair ? 128 : 64, kParts = kDeep / kDepth;
+  static constexpr int kDeep = kFp8 && !kPair ? 128 : 64, kHalves = kDeep / kDepth;
   static constexpr uint32_t kW = kFeatures * kDepth * 2, kX = kRows / kBlocks * kDepth * 2, kRaw = kFp8 ? kFeatures * kDeep : 0;
-  static constexpr int kStages = kFp8 ? (kPair ? 5 : kRows == 64 ? 4 : 6) : (kPair ? 6 : kRows == 64 ? 8 : 10);
+  static constexpr int kStages = kFp8 ? (kPair ? 5 : kRows == 64 ? 6 : 9) : (kPair ? 6 : kRows == 64 ? 8 : 10);
   static constexpr int kThreads = kFp8 ? 512 : 256;
   static constexpr int kBound = kFp8 ? 640 : 256;  // so that registers are left for the adapters' kernel beside it
   // blocks or pairs that share a tile: what they send and receive has room in the stages
   static constexpr int kMostShares = kPair ? 3 : 8;
-  static constexpr int kTeam = 2;  // warps that convert a stage's codes, into the team's own slot
+  static constexpr int kTeam = kInTensor ? 4 : 2;  // of the eight warps that convert codes, those on one part of a stage
 };
 
 constexpr int kPitch = kFeatures + 4;  // of a column of sums
@@ -415,8 +418,8 @@ constexpr int kStaged = 16;  // columns that pass through shared memory together
 template <int kRows, bool kFp8>
 struct Shared {
   using S = Shape<kRows, kFp8>;
-  uint8_t w[kFp8 ? S::kSlots : S::kStages][S::kW];
-  uint8_t x[S::kStages][S::kX * S::kParts];
+  uint8_t w[S::kInTensor ? 1 : kFp8 ? S::kSlots : S::kStages][S::kInTensor ? 1024 : S::kW];
+  uint8_t x[S::kStages][S::kX * S::kHalves];
   uint8_t raw[kFp8 ? S::kStages : 1][kFp8 ? S::kRaw : 16];
   float staged[2][kStaged][kPitch];
   uint64_t full[S::kStages], empty[S::kStages], ready[S::kSlots], free[S::kSlots], sum_full[2], sum_empty[2], drained;
@@ -706,7 +709,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
           if (kGated) copy3(&w_map, w_to + (kFp8 ? S::kRaw : S::kW) / 2, stage, k * S::kDeep, item.f0 + outs, item.group);
           if (!named)
 #pragma unroll
-            for (int j = 0; j < S::kParts; ++j)
+            for (int j = 0; j < S::kHalves; ++j)
               for (int i = 0; i < boxes; ++i)
                 copy2(&x_map, x_to + j * S::kX + i * (box * kDepth * 2), stage, k * S::kDeep + j * kDepth, row0 + i * box);
         }
@@ -723,14 +726,13 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
           const Extra extra = extra_of(expand.padded, e);
           const uint32_t stage = done % kStages;
           if (!(fine = warp_wait(&sh.empty[stage], (done / kStages & 1) ^ 1, watch))) break;
-          // the products of the slot's part before; by their stage's barrier, since this warp may be several turns of
-          // the slots ahead
-          constexpr uint32_t kTurn = S::kSlots / S::kParts;
-          const uint32_t before = done - kTurn;
-          if (kFp8 && done >= kTurn && !(fine = warp_wait(&sh.empty[before % kStages], before / kStages & 1, watch))) break;
+          // in shared memory, the products of the slot's stage before; by that stage's barrier, since this warp may be several
+          // turns of the slots ahead
+          const uint32_t before = done - S::kSlots;
+          if (kFp8 && kPair && done >= S::kSlots && !(fine = warp_wait(&sh.empty[before % kStages], before / kStages & 1, watch))) break;
           if (elected()) {
             expect(stage, S::kW + run_boxes * S::kBox * kDepth * 2);
-            const uint32_t w_to = shared_address(sh.w[kFp8 ? done * S::kParts % S::kSlots : stage]), x_to = shared_address(sh.x[stage]);
+            const uint32_t w_to = shared_address(S::kInTensor ? sh.raw[stage] : sh.w[kFp8 ? done % S::kSlots : stage]), x_to = shared_address(sh.x[stage]);
             copy3(&b_map, w_to, stage, extra.b_column, item.f0, m);
             for (int b = 0; b < run_boxes; ++b)
               copy2(&h_map, x_to + b * (S::kBox * kDepth * 2), stage, extra.column, run_row0 + b * S::kBox);
@@ -761,40 +763,42 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       if constexpr (kPair) commit_pair(barrier, 3u << first);
       else commit(barrier);
     };
-    // Part j of stage `done` is there.
-    auto part_full = [&](int j) {
-      const uint32_t part = done * S::kParts + j;
-      return kFp8 ? warp_wait(&sh.ready[part % S::kSlots], part / S::kSlots & 1, watch)
+    auto stage_full = [&] {
+      return kFp8 ? warp_wait(&sh.ready[done % S::kSlots], done / S::kSlots & 1, watch)
                   : warp_wait(&sh.full[done % kStages], done / kStages & 1, watch);
     };
-    auto part_done = [&](int j) {
-      if (kFp8) commit_here(&sh.free[(done * S::kParts + j) % S::kSlots]);
-      if (j == S::kParts - 1) commit_here(&sh.empty[done % kStages]);
+    auto stage_done = [&] {
+      if (kFp8) commit_here(&sh.free[done % S::kSlots]);
+      commit_here(&sh.empty[done % kStages]);
     };
-    auto w_of = [&](int j) {
-      return plain + (shared_address(sh.w[kFp8 ? (done * S::kParts + j) % S::kSlots : done % kStages]) >> 4);
+    // of shared memory; adapters' B is where a stage's codes were
+    auto w_of = [&] {
+      return plain + (shared_address(S::kInTensor ? sh.raw[done % kStages] : sh.w[kFp8 ? done % S::kSlots : done % kStages]) >> 4);
     };
-    auto x_of = [&](int j) { return plain + (shared_address(sh.x[done % kStages] + j * S::kX) >> 4); };
+    auto x_of = [&] { return plain + (shared_address(sh.x[done % kStages]) >> 4); };
     while (fine && issues && walk.next(item)) {
       const uint32_t half = items & 1;
-      const uint32_t sum = sh.tensor + half * 256;
+      const uint32_t sum = sh.tensor + half * S::kSums;
       if (!(fine = warp_wait(&sh.sum_empty[half], (items / 2 & 1) ^ 1, watch))) break;
       fence_after();
       const uint32_t kind = shape | static_cast<uint32_t>((item.rows + 15) / 16 * 2) << 17;
-      for (int k = item.k0; fine && k < item.k1; ++k, ++done) {
+      for (int k = item.k0; k < item.k1; ++k, ++done) {
+        if (!(fine = stage_full())) break;
+        fence_after();
+        const uint64_t a = w_of(), b = x_of();
+        const uint32_t slot = sh.tensor + 128 + done % S::kSlots * 64;
+        if (elected()) {
 #pragma unroll
-        for (int j = 0; j < S::kParts; ++j) {
-          if (!(fine = part_full(j))) break;
-          fence_after();
-          const uint64_t a = w_of(j), b = x_of(j);
-          if (elected()) {
+          for (int j = 0; j < S::kHalves; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) multiply_here(sum, a + i * 2, b + i * 2, kind, k > item.k0 || j > 0 || i > 0);
-            part_done(j);
-          }
-          __syncwarp();
+            for (int i = 0; i < 4; ++i) {
+              const bool add = k > item.k0 || j > 0 || i > 0;
+              if constexpr (S::kInTensor) multiply_from_tensor(sum, slot + j * 32 + i * 8, b + j * (S::kX >> 4) + i * 2, kind, add);
+              else multiply_here(sum, a + i * 2, b + i * 2, kind, add);
+            }
+          stage_done();
         }
-        if (!fine) break;
+        __syncwarp();
       }
       if (fine && expand.h != nullptr && item.k1 == plan.depth) {
         if (early) wait_for_previous();
@@ -803,21 +807,17 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
           const uint32_t run_kind = shape | static_cast<uint32_t>((j - i) * 2) << 17;
           for (int e = 0; e < extras_of(expand.padded); ++e, ++done) {
             const Extra extra = extra_of(expand.padded, e);
-#pragma unroll
-            for (int p = 0; p < S::kParts; ++p) {
-              if (!(fine = part_full(p))) break;
-              fence_after();
-              const uint64_t a = w_of(p), b = x_of(p);
-              if (elected()) {
-                for (int s = 0; p == 0 && s < extra.steps; ++s) {
-                  multiply_here(sum + i * kBlock, a + s * 2, b + s * 2, run_kind, true);
-                  if (extra.twice > 0) multiply_here(sum + i * kBlock, a + s * 2, b + extra.twice / 8 + s * 2, run_kind, true);
-                }
-                part_done(p);
+            if (!(fine = stage_full())) break;
+            fence_after();
+            const uint64_t a = w_of(), b = x_of();
+            if (elected()) {
+              for (int s = 0; s < extra.steps; ++s) {
+                multiply_here(sum + i * kBlock, a + s * 2, b + s * 2, run_kind, true);
+                if (extra.twice > 0) multiply_here(sum + i * kBlock, a + s * 2, b + extra.twice / 8 + s * 2, run_kind, true);
               }
-              __syncwarp();
+              stage_done();
             }
-            if (!fine) break;
+            __syncwarp();
           }
         }
       }
@@ -868,7 +868,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
 #pragma unroll 4
             for (int i = begin; i < end; ++i)
 #pragma unroll
-              for (int j = 0; j < S::kParts; ++j)
+              for (int j = 0; j < S::kHalves; ++j)
                 gather_rows(&x_map, x_to + j * S::kX + i * (4 * kDepth * 2), &sh.full[stage], k * S::kDeep + j * kDepth, names[i - begin]);
           }
           __syncwarp();
@@ -908,7 +908,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       }
       if (!(fine = agree(warp_wait(&sh.sum_full[half], items / 2 & 1, watch)))) break;
       fence_after();
-      const uint32_t sum = sh.tensor + half * 256 + (static_cast<uint32_t>(mine) << 21);
+      const uint32_t sum = sh.tensor + half * S::kSums + (static_cast<uint32_t>(mine) << 21);
       auto sum_read = [&] {
         if (lane != 0) return;
         if (kPair) barrier_signal_at(address_in(shared_address(&sh.sum_empty[half]), first));
@@ -952,7 +952,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       // Columns [lo, hi) are this block's to finish. Where others share the tile's depth, each sends it what it has of
       // these, and is sent what this one has of theirs, through the memory of the stages, which are empty now.
       int lo = 0, hi = item.rows;
-      float* send = reinterpret_cast<float*>(sh.w);  // of other blocks' columns, in their order
+      float* send = reinterpret_cast<float*>(&sh);  // of other blocks' columns, in their order
       const float* received = send;                  // of these, from each other block in turn
       // of two chunks of columns, each asked for two chunks ahead
       int note_a[4], note_b[4];
@@ -1061,7 +1061,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
     uint32_t part = team;  // the team's next one
     bool fine = true;
     while (fine && walk.next(item)) {
-      const uint32_t codes = (done + item.k1 - item.k0) * S::kParts;
+      const uint32_t codes = (done + item.k1 - item.k0);
       uint32_t end = codes;
       bool more = expand.h != nullptr && item.k1 == plan.depth;
       done += item.k1 - item.k0;
@@ -1075,54 +1075,94 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
           int extra = 0;
           for (int i = 0, j, m; runs.next(i, j, m); i = j) extra += extras_of(expand.padded);
           done += extra;
-          end += extra * S::kParts;
+          end += extra;
           continue;
         }
-        const uint32_t stage = part / S::kParts % kStages;
-        if (!(fine = warp_wait(&sh.full[stage], part / S::kParts / kStages & 1, watch))) break;
-        if (!(fine = warp_wait(&sh.free[team], (part / S::kSlots & 1) ^ 1, watch))) break;
+        const uint32_t stage = part % kStages;
+        if (!(fine = warp_wait(&sh.full[stage], part / kStages & 1, watch))) break;
+        auto slot_free = [&] { return warp_wait(&sh.free[part % S::kSlots], (part / S::kSlots & 1) ^ 1, watch); };
+        if (!S::kInTensor || part >= codes)
+          if (!(fine = slot_free())) break;
         if (part < codes) {
-          // 16 codes a lane and turn, of row `at`. Rows of 128 bytes of codes are swizzled, as those of bf16 are; eight
-          // lanes have four pieces of two rows, r and r ^ 5, which neither read nor write a bank twice.
-          constexpr int kTurns = kFeatures * kDepth / 16 / 32 / S::kTeam;
-          const int within = lane & 4 ? lane >> 3 ^ 5 : lane >> 3, piece = lane & 3;
-          const int from = S::kParts == 2 ? ((part % 2 * 4 + piece) ^ within) * 16 : piece * 16;
-          const uint8_t* codes_at = &sh.raw[stage][(member * 8 + within) * S::kDeep + from];
-          uint8_t* to = &sh.w[team][(member * 8 + within) * 128];
-          const int place[2] = {((piece * 2) ^ within) * 16, ((piece * 2 + 1) ^ within) * 16};
-          uint32_t nan = 0;
-          constexpr int kAtOnce = 4;
+          if constexpr (S::kInTensor) {
+            // a thread has a row, which is a lane of the tensor memory; rows of 128 bytes of codes are swizzled
+            const int at = (warp % 4) * 32 + lane;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              uint4 c[4], v[4][2];
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                c[i] = *reinterpret_cast<const uint4*>(&sh.raw[stage][at * S::kDeep + (((half * 4 + i) ^ (at & 7)) * 16)]);
+              uint32_t nan = 0;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) bf16_of_codes(c[i], unit, v[i], nan);
+              if (nan & 0x80808080u && unit != 0)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  v[i][0] = make_uint4(bf16_of_e4m3(c[i].x & 0xFFFFu), bf16_of_e4m3(c[i].x >> 16), bf16_of_e4m3(c[i].y & 0xFFFFu), bf16_of_e4m3(c[i].y >> 16));
+                  v[i][1] = make_uint4(bf16_of_e4m3(c[i].z & 0xFFFFu), bf16_of_e4m3(c[i].z >> 16), bf16_of_e4m3(c[i].w & 0xFFFFu), bf16_of_e4m3(c[i].w >> 16));
+                }
+              uint32_t words[32];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const uint4 q = v[i / 2][i % 2];
+                words[4 * i] = q.x;
+                words[4 * i + 1] = q.y;
+                words[4 * i + 2] = q.z;
+                words[4 * i + 3] = q.w;
+              }
+              __syncwarp();
+              if (half == 0) {
+                if (!(fine = slot_free())) break;
+                fence_after();
+              }
+              tensor_store32(sh.tensor + 128 + part % S::kSlots * 64 + half * 32 + (static_cast<uint32_t>(warp % 4) << 21), words);
+            }
+            if (!fine) break;
+            tensor_stored();
+            fence_before();
+          } else {
+            // 16 codes a lane and turn; eight lanes have four pieces of two rows, r and r ^ 5, which write no bank twice
+            constexpr int kTurns = kFeatures * kDepth / 16 / 32 / S::kTeam;
+            const int within = lane & 4 ? lane >> 3 ^ 5 : lane >> 3, piece = lane & 3;
+            const int from = piece * 16;
+            const uint8_t* codes_at = &sh.raw[stage][(member * 8 + within) * S::kDeep + from];
+            uint8_t* to = &sh.w[part % S::kSlots][(member * 8 + within) * 128];
+            const int place[2] = {((piece * 2) ^ within) * 16, ((piece * 2 + 1) ^ within) * 16};
+            uint32_t nan = 0;
+            constexpr int kAtOnce = 4;
 #pragma unroll 1
-          for (int i0 = 0; i0 < kTurns; i0 += kAtOnce) {
-            uint4 c[kAtOnce];
+            for (int i0 = 0; i0 < kTurns; i0 += kAtOnce) {
+              uint4 c[kAtOnce];
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i)
-              c[i] = *reinterpret_cast<const uint4*>(codes_at + (i0 + i) * (S::kTeam * 8 * S::kDeep));
+              for (int i = 0; i < kAtOnce; ++i)
+                c[i] = *reinterpret_cast<const uint4*>(codes_at + (i0 + i) * (S::kTeam * 8 * S::kDeep));
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) {
-              uint4 v[2];
-              bf16_of_codes(c[i], unit, v, nan);
+              for (int i = 0; i < kAtOnce; ++i) {
+                uint4 v[2];
+                bf16_of_codes(c[i], unit, v, nan);
 #pragma unroll
-              for (int h = 0; h < 2; ++h) *reinterpret_cast<uint4*>(to + (i0 + i) * (S::kTeam * 8 * 128) + place[h]) = v[h];
+                for (int h = 0; h < 2; ++h) *reinterpret_cast<uint4*>(to + (i0 + i) * (S::kTeam * 8 * 128) + place[h]) = v[h];
+              }
             }
-          }
-          if (nan & 0x80808080u && unit != 0) {
-            for (int i = 0; i < kTurns; ++i) {
-              const uint4 c = *reinterpret_cast<const uint4*>(codes_at + i * (S::kTeam * 8 * S::kDeep));
-              const uint4 v[2] = {make_uint4(bf16_of_e4m3(c.x & 0xFFFFu), bf16_of_e4m3(c.x >> 16), bf16_of_e4m3(c.y & 0xFFFFu), bf16_of_e4m3(c.y >> 16)),
-                                  make_uint4(bf16_of_e4m3(c.z & 0xFFFFu), bf16_of_e4m3(c.z >> 16), bf16_of_e4m3(c.w & 0xFFFFu), bf16_of_e4m3(c.w >> 16))};
-              for (int h = 0; h < 2; ++h) *reinterpret_cast<uint4*>(to + i * (S::kTeam * 8 * 128) + place[h]) = v[h];
+            if (nan & 0x80808080u && unit != 0) {
+              for (int i = 0; i < kTurns; ++i) {
+                const uint4 c = *reinterpret_cast<const uint4*>(codes_at + i * (S::kTeam * 8 * S::kDeep));
+                const uint4 v[2] = {make_uint4(bf16_of_e4m3(c.x & 0xFFFFu), bf16_of_e4m3(c.x >> 16), bf16_of_e4m3(c.y & 0xFFFFu), bf16_of_e4m3(c.y >> 16)),
+                                    make_uint4(bf16_of_e4m3(c.z & 0xFFFFu), bf16_of_e4m3(c.z >> 16), bf16_of_e4m3(c.w & 0xFFFFu), bf16_of_e4m3(c.w >> 16))};
+                for (int h = 0; h < 2; ++h) *reinterpret_cast<uint4*>(to + i * (S::kTeam * 8 * 128) + place[h]) = v[h];
+              }
             }
+            fence_async();
           }
-          fence_async();
         }
         if (kPair) {
           __syncwarp();
-          if (lane == 0) barrier_signal_at(address_in(shared_address(&sh.ready[team]), first));
+          if (lane == 0) barrier_signal_at(address_in(shared_address(&sh.ready[part % S::kSlots]), first));
         } else {
-          warp_arrive(&sh.ready[team], lane);
+          warp_arrive(&sh.ready[part % S::kSlots], lane);
         }
-        part += S::kSlots;
+        part += 8 / S::kTeam;
       }
     }
   }
