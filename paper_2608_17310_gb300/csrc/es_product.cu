@@ -26,8 +26,8 @@
 // Adapters. A kernel of its own makes h = s A x, as the sum of two bf16 numbers (2^-16 of it), for 32 rows and
 // one adapter a block. Where 16 rows have one adapter, B h is further products into the same sums. Where members
 // meet within 16 rows, products would multiply one's B by the others' zeros, and infinities or NaN of a member
-// that has diverged would reach all of them; there B h is made in fp32, row by row, by that kernel for up to
-// kMostExtra rows, else where results are written. The product's kernel starts beside it, and waits where
+// that has diverged would reach all of them; there B h is made in fp32, row by row, by that kernel where it
+// has room in the workspace (kMostExtra), else where results are written. The product's kernel starts beside it, and waits where
 // the adapters' part is needed.
 //
 // Measured (GB300, us a pass): project_prompts 13,741 rows of 30 members, 5,120 to 17,408 features, rank 32, 1,361
@@ -319,10 +319,10 @@ shrink_kernel(const ShrinkArgs a) {
     }
     if (expanded != 0) {
       __syncthreads();
-      // the cluster's warps share the features
-      for (int f = ((blockIdx.z * kWarps + warp) * 32 + lane) * 4; f < a.out; f += shares * kWarps * kFeatures) {
-        const uint16_t* factors = a.b + m * a.b_stride + static_cast<uint64_t>(f) * a.rank;
-        if constexpr (kSteps <= 2) {
+      // The cluster's warps share the features, 128 at a time, a lane 4 of them; for ranks above 16 also the rows, by eights.
+      if constexpr (kSteps <= 2) {
+        for (int f = ((blockIdx.z * kWarps + warp) * 32 + lane) * 4; f < a.out; f += shares * kWarps * kFeatures) {
+          const uint16_t* factors = a.b + m * a.b_stride + static_cast<uint64_t>(f) * a.rank;
           Factors b[kSteps];
 #pragma unroll
           for (int r = 0; r < kSteps; ++r) b[r].take(factors + r * 8, a.rank);
@@ -333,26 +333,37 @@ shrink_kernel(const ShrinkArgs a) {
             for (int r = 0; r < kSteps; ++r) b[r].add(y, whole + row * a.padded + r * 8);
             *reinterpret_cast<float4*>(a.extra + static_cast<uint64_t>(row0 + row) * a.out + f) = make_float4(y[0], y[1], y[2], y[3]);
           }
-          continue;
         }
-        for (uint32_t left = expanded; left != 0;) {
-          int row[4];
-          float y[4][4] = {};
+      } else {
+        constexpr int kRows = 8, kAtOnce = 4;  // kAtOnce: eights of ranks whose B is under way together
+        const int groups = (__popc(expanded) + kRows - 1) / kRows, tiles = (a.out + kFeatures - 1) / kFeatures;
+        for (int u = blockIdx.z * kWarps + warp; u < tiles * groups; u += shares * kWarps) {
+          const int f = u / groups * kFeatures + lane * 4;
+          if (f >= a.out) continue;
+          uint32_t left = expanded;
+          for (int i = u % groups * kRows; i > 0; --i) left &= left - 1;
+          int row[kRows];
+          float y[kRows][4] = {};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < kRows; ++i) {
             row[i] = left != 0 ? __ffs(left) - 1 : -1;
             left &= left - 1;
           }
-#pragma unroll 2
-          for (int r = 0; r < a.rank; r += 8) {
-            Factors b;
-            b.take(factors + r, a.rank);
+          const uint16_t* factors = a.b + m * a.b_stride + static_cast<uint64_t>(f) * a.rank;
+          for (int r0 = 0; r0 < a.rank; r0 += 8 * kAtOnce) {
+            Factors b[kAtOnce];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (row[i] >= 0) b.add(y[i], whole + row[i] * a.padded + r);
+            for (int r = 0; r < kAtOnce; ++r)
+              if (r0 + r * 8 < a.rank) b[r].take(factors + r0 + r * 8, a.rank);
+#pragma unroll
+            for (int r = 0; r < kAtOnce; ++r)
+              if (r0 + r * 8 < a.rank)
+#pragma unroll
+                for (int i = 0; i < kRows; ++i)
+                  if (row[i] >= 0) b[r].add(y[i], whole + row[i] * a.padded + r0 + r * 8);
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < kRows; ++i)
             if (row[i] >= 0)
               *reinterpret_cast<float4*>(a.extra + static_cast<uint64_t>(row0 + row[i]) * a.out + f) =
                   make_float4(y[i][0], y[i][1], y[i][2], y[i][3]);
@@ -1324,9 +1335,11 @@ es_status_t launch_rows(const MatrixView& w, const CUtensorMap& w_map, bool fp8,
 // 48 rows 59.8 and 61.4, at 64 rows 67.1 and 62.6; FP8 67.7 and 71.6, 81.8 and 74.2.
 constexpr int kLeast = 16, kFew = 64, kMany = 256;
 constexpr int kManyEach = 48;  // rows an expert above which tiles are of kMany
-// Rows up to which B h of rows beside others' has room in the workspace (4 bytes a feature and row); where results are
-// written it costs a step of 192 rows some 50 us, but for more rows mixed blocks are few, or the product long.
-constexpr int kMostExtra = 1024;
+// B h of rows beside others' has room in the workspace (4 bytes a feature and row) up to here. Beyond, where it is made
+// where results are written, mixed blocks are few or the product long. (8,500 rows of 69 members, 1,264 to 1,000 features,
+// FP8: 87 us so.)
+constexpr uint64_t kMostExtra = uint64_t{128} << 20;
+uint64_t extra_bytes(uint64_t rows, uint64_t out) { return rows * out * 4; }
 
 uint64_t padded_rank(int rank) { return static_cast<uint64_t>(rank + 15) / 16 * 16; }
 uint64_t rounded(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -1389,12 +1402,12 @@ es_status_t map_matrices(CUtensorMap* map, const void* data, uint64_t in, uint64
   return ES_OK;
 }
 
-// Behind the head: with adapters h, the adapters of rows and blocks, and B h of up to kMostExtra rows;
+// Behind the head: with adapters h, the adapters of rows and blocks, and B h of up to kMostExtra bytes;
 // without, rows that are copied in order.
 uint64_t project_workspace_bytes(int rank, int rows, int in, int out) {
   const uint64_t n = rows;
   if (rank == 0) return kHead + (rows > kFew ? rounded(n * in * 2) : 0);
-  return kHead + rounded(n * 4 * padded_rank(rank)) + 2 * rounded(n * 4) + rounded(std::min(rows, kMostExtra) * uint64_t{4} * out);
+  return kHead + rounded(n * 4 * padded_rank(rank)) + 2 * rounded(n * 4) + rounded(std::min(extra_bytes(n, out), kMostExtra));
 }
 
 es_status_t launch_project(const MatrixView& w, const CUtensorMap* w_maps, bool fp8, const AdapterView* adapters, const CUtensorMap* b_map,
@@ -1408,7 +1421,7 @@ es_status_t launch_project(const MatrixView& w, const CUtensorMap* w_maps, bool 
     uint16_t* h = reinterpret_cast<uint16_t*>(behind);
     int32_t* of_row = reinterpret_cast<int32_t*>(behind + rounded(n * 4 * padded));
     int32_t* of_block = reinterpret_cast<int32_t*>(behind + rounded(n * 4 * padded) + rounded(n * 4));
-    float* extra = std::min(rows.segments, rows.rows) > 1 && rows.rows <= kMostExtra
+    float* extra = std::min(rows.segments, rows.rows) > 1 && extra_bytes(n, w.out) <= kMostExtra
                        ? reinterpret_cast<float*>(behind + rounded(n * 4 * padded) + 2 * rounded(n * 4)) : nullptr;
     const ShrinkArgs a{rows.x, rows.start, adapter, adapters->a, adapters->scale, w.scale, h, of_row, of_block, adapters->b, extra,
                        rows.x_stride, adapters->a_stride, adapters->b_stride, rows.segments, rows.rows, adapters->count, adapters->rank,

@@ -12,9 +12,17 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
 @pytest.mark.parametrize("rank", [8, 24, 64])
 def test_many_rows_of_members_beside_one_another(pj, dtype, rank):  # noqa: F811
-    """Above 1,024 rows B h of mixed blocks is added where results are written."""
+    """B h of mixed blocks of many rows."""
     counts = [1, 7, 40, 3, 0, 16, 90, 2] * 8 + [33]
     Case(pj, counts, [i % 6 - 1 for i in range(len(counts))], 320, 392, count=5, rank=rank, dtype=dtype, spare=7).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("rank", [8, 40])
+def test_members_beside_one_another_through_many_features(pj, dtype, rank):  # noqa: F811
+    """With more than 2^25 results B h of mixed blocks has no room and is made where they are written."""
+    counts = [1, 7, 40, 3, 0, 16, 90, 2, 1] * 7
+    Case(pj, counts, [i % 6 - 1 for i in range(len(counts))], 64, 30008, count=5, rank=rank, dtype=dtype, spare=3).check()
 
 
 @pytest.mark.parametrize("requests", [127, 128, 129, 1000, 4096])
