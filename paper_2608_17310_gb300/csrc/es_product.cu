@@ -1377,7 +1377,14 @@ cudaError_t launch_shrink(const ShrinkArgs& a, cudaStream_t stream) {
   }
   const int most = std::min(std::min(a.requests, a.rows), kShrinkRows);  // adapters that the rows of a block can have
   const int blocks = (a.rows + kShrinkRows - 1) / kShrinkRows;
-  const dim3 grid = blocks <= 16 ? dim3(blocks, std::min(most, std::max(8, 48 / blocks)), 8) : blocks <= 128 ? dim3(blocks, std::min(most, 4), 4) : dim3(blocks, 1, 2);
+  // Few blocks share their depth, so that its loads are all under way, and B's features (1,000 rows, 9,728 features, rank
+  // 40: 80 us by four, 71 by eight); adapters of a block go to blocks of their own as far as there are likely so many, since
+  // one without any costs a look at the requests.
+  const int likely = std::min(std::min(most, 4), a.requests / blocks + 2);
+  const dim3 grid = blocks <= 16   ? dim3(blocks, std::min(most, std::max(8, 48 / blocks)), 8)
+                    : blocks <= 64 ? dim3(blocks, likely, 8)
+                    : blocks <= 128 ? dim3(blocks, likely, 4)
+                                    : dim3(blocks, 1, 2);
   return launch_grid(shrink_kernel<kSteps>, grid, kShrinkWarps * 32, kBytes, stream, a);
 }
 
