@@ -1090,10 +1090,13 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
           continue;
         }
         const uint32_t stage = part % kStages;
-        if (!(fine = warp_wait(&sh.full[stage], part / kStages & 1, watch))) break;
         auto slot_free = [&] { return warp_wait(&sh.free[part % S::kSlots], (part / S::kSlots & 1) ^ 1, watch); };
+        // The stage's barrier cannot be a phase behind the one that is waited for: the products of kSlots stages before are
+        // done, or, where the slot is waited for later, those of the slots and of the teams' turn before.
+        static_assert(!kFp8 || S::kStages >= (S::kInTensor ? S::kSlots + 8 / S::kTeam : S::kSlots), "stages that a team may be ahead");
         if (!S::kInTensor || part >= codes)
           if (!(fine = slot_free())) break;
+        if (!(fine = warp_wait(&sh.full[stage], part / kStages & 1, watch))) break;
         if (part < codes) {
           if constexpr (S::kInTensor) {
             // a thread has a row, which is a lane of the tensor memory; rows of 128 bytes of codes are swizzled

@@ -104,3 +104,31 @@ def test_experts_of_many_and_few_rows_at_once(pj, dtype):  # noqa: F811
 def test_rows_around_the_tiles(pj, rows, width, out):  # noqa: F811
     """Both sides of where tiles of other sizes begin, with a depth that blocks share and with many features."""
     Case(pj, [rows - 5, 5], [0, 1], width, out, seed=rows).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("each,width,out", [(169, 2560, 1280), (78, 2432, 640), (20, 1280, 1280)])
+def test_calls_over_cold_weights_agree(pj, dtype, each, width, out):  # noqa: F811
+    """Many calls whose copies come in in any order: bit-identical. (A team of warps once took a stage's barrier
+    for the one of five stages later, where a copy came in after the one behind it: one call of some thousand.)"""
+    groups = 16
+    w = [torch.randn(groups, out, width, device="cuda", dtype=torch.bfloat16).mul_(0.02) for _ in range(3)]
+    if dtype == "e4m3":
+        scale = torch.full((groups,), 2.0 ** -11, device="cuda")
+        handles = [pj.es_weights_create((v * 2 ** 11).to(torch.float8_e4m3fn), scale) for v in w]
+    else:
+        handles = [pj.es_weights_create(v) for v in w]
+    start = i32(bounds([each + (7 * i) % 13 - 6 for i in range(groups)]))
+    slots = int(start[-1])
+    x = torch.randn(slots, width, device="cuda").bfloat16()
+    space = room(pj, handles[0], slots)
+    first, flush = [], torch.empty(192 << 20, dtype=torch.uint8, device="cuda")
+    for i in range(450):
+        y = torch.empty(slots, out, dtype=torch.bfloat16, device="cuda")
+        pj.es_project_experts(handles[i % 3], x, y, start, space)
+        if i % 5 == 0:
+            flush.zero_()
+        if i < 3:
+            first.append(y)
+        elif not torch.equal(y.view(torch.int16), first[i % 3].view(torch.int16)):
+            raise AssertionError(f"call {i} differs")
