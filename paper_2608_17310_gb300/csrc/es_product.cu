@@ -1172,7 +1172,7 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
         }
         if (kPair) {
           __syncwarp();
-          if (lane == 0) barrier_signal_at(address_in(shared_address(&sh.ready[part % S::kSlots]), first));
+          if (lane == 0) barrier_release_at(address_in(shared_address(&sh.ready[part % S::kSlots]), first));
         } else {
           warp_arrive(&sh.ready[part % S::kSlots], lane);
         }

@@ -200,6 +200,10 @@ __device__ __forceinline__ uint32_t address_in(uint32_t address, uint32_t rank) 
 __device__ __forceinline__ void barrier_signal_at(uint32_t address) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(address) : "memory");
 }
+// The same behind what this thread's warp has written to its own block's shared memory.
+__device__ __forceinline__ void barrier_release_at(uint32_t address) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(address) : "memory");
+}
 __device__ __forceinline__ void copy_to_block(uint32_t to, uint32_t from, uint32_t bytes, uint32_t barrier) {
   asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "r"(from), "r"(bytes),
                "r"(barrier)
