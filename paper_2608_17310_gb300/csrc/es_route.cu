@@ -320,7 +320,7 @@ cudaError_t route(RouteArgs a, int32_t* counts, cudaStream_t stream) {
   const size_t alone = sizeof(int32_t) * kAloneWarps * a.experts, shared = sizeof(int32_t) * kRouteWarps * a.experts;
   auto one = choose_kernel<kPerLane, kBf16, true>;
   auto many = choose_kernel<kPerLane, kBf16, false>;
-  if (alone > 48 * 1024) {
+  if (alone + sizeof(int) * kAloneWarps > 48 * 1024) {  // with what the kernel declares itself
     cudaError_t err = cudaFuncSetAttribute(one, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(alone));
     if (err == cudaSuccess) err = cudaFuncSetAttribute(many, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
     if (err == cudaSuccess) err = cudaFuncSetAttribute(place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
