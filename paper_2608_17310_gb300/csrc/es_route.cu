@@ -321,9 +321,11 @@ cudaError_t route(RouteArgs a, int32_t* counts, cudaStream_t stream) {
   auto one = choose_kernel<kPerLane, kBf16, true>;
   auto many = choose_kernel<kPerLane, kBf16, false>;
   if (alone + sizeof(int) * kAloneWarps > 48 * 1024) {  // with what the kernel declares itself
-    cudaError_t err = cudaFuncSetAttribute(one, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(alone));
-    if (err == cudaSuccess) err = cudaFuncSetAttribute(many, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
-    if (err == cudaSuccess) err = cudaFuncSetAttribute(place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
+    // The limit is the kernel's, in all threads: each call sets the same one, that of the most experts.
+    constexpr int kMostAlone = sizeof(int32_t) * kAloneWarps * ES_MAX_EXPERTS, kMost = sizeof(int32_t) * kRouteWarps * ES_MAX_EXPERTS;
+    cudaError_t err = cudaFuncSetAttribute(one, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostAlone);
+    if (err == cudaSuccess) err = cudaFuncSetAttribute(many, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+    if (err == cudaSuccess) err = cudaFuncSetAttribute(place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
     if (err != cudaSuccess) {
       cudaGetLastError();
       return err;

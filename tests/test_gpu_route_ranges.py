@@ -4,6 +4,7 @@ import os
 import subprocess
 import sys
 import textwrap
+import threading
 
 import pytest
 import torch
@@ -64,3 +65,30 @@ def alone(text, **kw):
 def test_counts_around_the_default_shared_memory(pj, tokens, counts):  # noqa: F811
     """384 experts' counters by 32 warps are just the 48 KB that a block has without asking for more, and the block has others."""
     alone(ALONE, counts=counts, tokens=tokens)
+
+
+def test_calls_of_different_sizes_from_two_threads(pj):  # noqa: F811
+    """What a launch may use of shared memory is a property of the kernel in the whole process: no call takes it
+    from another."""
+    calls = [Routed(pj, torch.randn(tokens, count, generator=torch.Generator().manual_seed(count)), 3)
+             for count, tokens in ((1024, 200), (400, 200), (1024, 400), (400, 400))]
+    torch.cuda.synchronize()
+    failed = []
+
+    def loop(mine):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(2000):
+                    mine.run()
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:
+            failed.append(e)
+
+    threads = [threading.Thread(target=loop, args=(c,)) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
+    for c in calls:
+        c.check()
