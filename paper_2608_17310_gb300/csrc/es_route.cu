@@ -22,10 +22,11 @@ struct RouteArgs {
   int share;  // tokens of a warp
 };
 
-// Order-preserving code of a score; 0 for one that is never chosen.
+// Order-preserving code of a score; 0 for one that is never chosen. Zeros of both signs are equal scores: 0 added to
+// the negative one makes it the other.
 __device__ __forceinline__ uint32_t code_of(float x) {
   if (!(x > -INFINITY)) return 0;
-  const uint32_t w = __float_as_uint(fminf(x, FLT_MAX));
+  const uint32_t w = __float_as_uint(fminf(x, FLT_MAX) + 0.0f);
   return w & 0x80000000u ? ~w : w | 0x80000000u;
 }
 __device__ __forceinline__ float score_of_code(uint32_t c) {

@@ -92,3 +92,20 @@ def test_calls_of_different_sizes_from_two_threads(pj):  # noqa: F811
     assert not failed, failed
     for c in calls:
         c.check()
+
+
+@pytest.mark.parametrize("count", [2, 31, 64, 100, 200, 700])
+@pytest.mark.parametrize("tokens", [5, 400])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_zeros_of_both_signs_are_equal_scores(pj, count, tokens, dtype):  # noqa: F811
+    """In one lane's scores and across lanes, as the largest scores and among others."""
+    g = torch.Generator().manual_seed(count + tokens)
+    scores = torch.randn(tokens, count, generator=g)
+    zero = torch.rand(tokens, count, generator=g) < 0.6
+    scores = torch.where(zero, torch.where(torch.rand(tokens, count, generator=g) < 0.5, 0.0, -0.0), scores)
+    scores[::2] = torch.where(zero[::2], scores[::2], -scores[::2].abs())  # zeros are the largest
+    scores[0] = -0.0
+    scores[0, count - 1] = 0.0
+    r = Routed(pj, scores.to(dtype), min(4, count))
+    r.run()
+    r.check()
