@@ -48,7 +48,9 @@ extern "C" {
  *                 scale[g] * code
  *   scale         [groups] fp32 in device memory (4-byte aligned); NULL for ES_BF16.
  *                 In es_project with adapters a scale whose reciprocal is infinite
- *                 counts as 0.
+ *                 (below 2.94e-39) counts as 0. Sums are of codes and scaled in the
+ *                 end, so one beyond 2^127 scale is infinite; so is an adapter's part
+ *                 beyond that, but for scales outside 2^-32 .. 2^32.
  *   groups        1 .. ES_MAX_EXPERTS
  *   out_features  a multiple of 8, 8 .. 2^20
  *   in_features   a multiple of 8 (FP8: 16), up to 2^17

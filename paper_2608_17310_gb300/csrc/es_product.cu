@@ -101,10 +101,19 @@ constexpr int kShrinkRows = 32;
 constexpr int kShrinkWarps = 4;
 
 // 1 / scale where the matrix's codes are multiplied by their scale in the end and the adapters'
-// part must not be; 1 where that is infinite: then the codes count as zeros.
+// part, made by products into the same sums, must not be; 1 where that is infinite: then the codes count as zeros.
 __device__ __forceinline__ float undo_of(const float* w_scale) {
   const float u = w_scale != nullptr ? 1.0f / *w_scale : 1.0f;
   return isinf(u) ? 1.0f : u;
+}
+
+// Whether the scale is so far from 1 that the adapters' part in its units could be infinite, or lose its second
+// part, where it is an ordinary number itself (1 / 1.2e-38 times an h of 5 is infinite): then every block with adapters counts as
+// mixed, and B h is added behind the scale. Real scales, max|w| / 448, are near 2^-12.
+__device__ __forceinline__ bool apart_of(const float* w_scale) {
+  if (w_scale == nullptr || isinf(1.0f / *w_scale)) return false;
+  const float size = fabsf(*w_scale);
+  return !(size >= 0x1p-32f && size <= 0x1p32f);
 }
 
 // The adapter of row row0 + lane for each lane of a warp, kNone for rows from `end` on.
@@ -189,18 +198,19 @@ shrink_kernel(const ShrinkArgs a) {
   const int mine = adapter_of_lane(a, row0, end, lane);
   const uint32_t there = __ballot_sync(0xFFFFFFFFu, row0 + lane < end);
   const uint32_t same = __match_any_sync(0xFFFFFFFFu, mine) & there;
+  const bool apart = apart_of(a.w_scale);
   if (blockIdx.y == 0 && blockIdx.z == 0 && warp == 0) {
     if (row0 + lane < a.rows) a.of_row[row0 + lane] = mine;
     const uint32_t block = 0xFFFFu << (lane & 16);
     if (lane % kBlock == 0 && row0 + lane < a.rows)
-      a.of_block[(row0 + lane) / kBlock] = (same & block) == (there & block) ? mine : kMixed;
+      a.of_block[(row0 + lane) / kBlock] = (same & block) == (there & block) && !(apart && mine >= 0) ? mine : kMixed;
   }
   // rows of blocks of 16 that have one adapter alone get B h by products
   const uint32_t low = 0xFFFFu, high = 0xFFFF0000u;
   const uint32_t alone_low = __match_any_sync(0xFFFFFFFFu, mine) & there & low, alone_high = __match_any_sync(0xFFFFFFFFu, mine) & there & high;
   const bool mixed_low = __shfl_sync(0xFFFFFFFFu, alone_low, 0) != (there & low);
   const bool mixed_high = __shfl_sync(0xFFFFFFFFu, alone_high, 16) != (there & high);
-  const uint32_t mixed = (mixed_low ? low : 0u) | (mixed_high ? high : 0u);
+  const uint32_t mixed = (mixed_low || apart ? low : 0u) | (mixed_high || apart ? high : 0u);
   const uint32_t firsts = __ballot_sync(0xFFFFFFFFu, mine >= 0 && (same & ((1u << lane) - 1)) == 0);
   const int g = lane / 4, t = lane % 4;
   const uint16_t* x0 = a.x + static_cast<uint64_t>(row0 + g) * a.x_stride;
@@ -210,8 +220,7 @@ shrink_kernel(const ShrinkArgs a) {
     const int lead = __ffs(left) - 1;
     const int m = __shfl_sync(0xFFFFFFFFu, mine, lead);
     const uint32_t rows = __shfl_sync(0xFFFFFFFFu, same, lead);
-    const float factor = (a.scale != nullptr ? a.scale[m] : 1.0f) * undo_of(a.w_scale);
-
+    const float factor = a.scale != nullptr ? a.scale[m] : 1.0f, undo = undo_of(a.w_scale);
     const uint16_t* from = a.a + m * a.a_stride;
     const uint32_t expanded = a.extra != nullptr ? rows & mixed : 0;
     if (expanded != 0)  // B to L2 meanwhile
@@ -305,7 +314,7 @@ shrink_kernel(const ShrinkArgs a) {
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) h += at[w * kShrinkRows * kPitch];
           }
-          h *= factor;
+          h *= mixed >> n & 1 ? factor : factor * undo;
         }
         whole[i] = h;
         if (blockIdx.z != 0) continue;
@@ -954,8 +963,8 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
             *reinterpret_cast<uint32_t*>(to) = note[i] == kAbsent ? 0 : y;
           } else {
             if (expand.h != nullptr && expand.extra == nullptr && note[i] >= 0) more[i] = expanded(expand, row, note[i], f);
-            const uint2 y = make_uint2(pack_bf16((z[i].x + more[i].x) * scale, (z[i].y + more[i].y) * scale),
-                                       pack_bf16((z[i].z + more[i].z) * scale, (z[i].w + more[i].w) * scale));
+            const uint2 y = make_uint2(pack_bf16(fmaf(z[i].x, scale, more[i].x), fmaf(z[i].y, scale, more[i].y)),
+                                       pack_bf16(fmaf(z[i].z, scale, more[i].z), fmaf(z[i].w, scale, more[i].w)));
             *reinterpret_cast<uint2*>(to) = note[i] == kAbsent ? make_uint2(0, 0) : y;
           }
         }
