@@ -788,8 +788,11 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       if constexpr (kPair) commit_pair(barrier, 3u << first);
       else commit(barrier);
     };
+    // Both blocks of a pair write converted codes, so there arrivals release and this wait acquires at the cluster's scope
+    // (4,096 rows of 5,120 to 17,408 features 687 us either way, by 30 members 861 and 841; by one lane's wait 931, by a fence of the lane
+    // that issues the products 1,118).
     auto stage_full = [&] {
-      return kFp8 ? warp_wait(&sh.ready[done % S::kSlots], done / S::kSlots & 1, watch)
+      return kFp8 ? warp_wait<kPair>(&sh.ready[done % S::kSlots], done / S::kSlots & 1, watch)
                   : warp_wait(&sh.full[done % kStages], done / kStages & 1, watch);
     };
     auto stage_done = [&] {

@@ -35,10 +35,20 @@ __device__ __forceinline__ bool barrier_try(uint64_t* b, uint32_t parity) {
                : "memory");
   return done != 0;
 }
+// The same where threads of another block of the cluster arrive behind what they have written (barrier_release_at).
+__device__ __forceinline__ bool barrier_try_cluster(uint64_t* b, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}"
+               : "=r"(done)
+               : "r"(shared_address(b)), "r"(parity)
+               : "memory");
+  return done != 0;
+}
 // false: the wait was given up, here or by another thread of the block
+template <bool kCluster = false>
 __device__ __forceinline__ bool barrier_wait(uint64_t* b, uint32_t parity, const Watch& watch) {
   for (int i = 0; i < watch.tries; ++i) {
-    if (barrier_try(b, parity)) return true;
+    if (kCluster ? barrier_try_cluster(b, parity) : barrier_try(b, parity)) return true;
     if (*watch.failed) return false;
   }
   *watch.failed = 1;
@@ -46,8 +56,9 @@ __device__ __forceinline__ bool barrier_wait(uint64_t* b, uint32_t parity, const
 }
 
 // By all lanes: through one of them and a shuffle measured 25 % slower over a whole prompt.
+template <bool kCluster = false>
 __device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, const Watch& watch) {
-  return __all_sync(0xFFFFFFFFu, barrier_wait(b, parity, watch));
+  return __all_sync(0xFFFFFFFFu, barrier_wait<kCluster>(b, parity, watch));
 }
 // One lane arrives, with what all lanes did before.
 __device__ __forceinline__ void warp_arrive(uint64_t* b, int lane) {
