@@ -158,7 +158,9 @@ es_status_t es_project(es_weights_t weights, es_adapters_t adapters, const es_pr
 
 /* Bytes of workspace that es_project (with these adapters or NULL) and
    es_project_experts need for up to `rows` rows or slots (0 for a NULL handle or rows
-   outside 0 .. ES_MAX_ROWS). Grows with rows. */
+   outside 0 .. ES_MAX_ROWS). Grows with rows. Without adapters es_project, and without rows
+   es_project_experts, use only its first ES_PROJECT_GAVE_UP + 256 bytes and take a workspace
+   of that size. */
 uint64_t es_project_workspace(es_weights_t weights, es_adapters_t adapters, int rows);
 
 /*

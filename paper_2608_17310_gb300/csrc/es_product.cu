@@ -1437,6 +1437,8 @@ uint64_t project_workspace_bytes(int rank, int rows, int in, int out) {
   return kHead + rounded(n * 4 * padded_rank(rank)) + 2 * rounded(n * 4) + rounded(std::min(extra_bytes(n, out), kMostExtra));
 }
 
+uint64_t project_workspace_head() { return kHead; }
+
 es_status_t launch_project(const MatrixView& w, const CUtensorMap* w_maps, bool fp8, const AdapterView* adapters, const CUtensorMap* b_map,
                            const int32_t* adapter, const RowView& rows, void* workspace, cudaStream_t stream, const char* call) {
   ExpandView expand{};

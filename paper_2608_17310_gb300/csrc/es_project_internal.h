@@ -67,6 +67,7 @@ es_status_t launch_project(const MatrixView& w, const CUtensorMap* w_maps, bool 
 es_status_t launch_experts(const MatrixView& w, const CUtensorMap* w_maps, bool fp8, bool gated, const RowView& rows, void* workspace,
                            cudaStream_t stream, const char* call);
 uint64_t project_workspace_bytes(int rank, int rows, int in, int out);  // rank 0: no adapters
+uint64_t project_workspace_head();  // what calls without adapters and without named rows use of it
 // For tests: tries after which the products' waits are given up in calls from now on (0: at once;
 // negative: as it was).
 void set_project_wait_tries(int tries);

@@ -114,3 +114,21 @@ CAPTURED = """
 @pytest.mark.parametrize("kind,size", [("layer", 5), ("layer", 700), ("bf16", 300), ("e4m3", 3)])
 def test_a_programs_first_calls_can_be_captured(pj, kind, size):  # noqa: F811
     alone(CAPTURED, kind=kind, size=size)
+
+
+def test_calls_without_adapters_and_named_rows_take_a_small_workspace(pj, es):  # noqa: F811
+    """One that was made for adapters serves them too, and so does its head alone; nothing smaller does."""
+    c = Case(pj, [90, 10], [0, 1], 512, 136, rank=8)
+    y = torch.empty(c.n, c.out, dtype=torch.bfloat16, device="cuda")
+    head = torch.zeros(pj.ES_PROJECT_GAVE_UP + 256, dtype=torch.uint8, device="cuda")
+    for space in (c.workspace, head):
+        pj.es_project(c.weights, c.xc, y, space)
+        close(y, *R.project(c.x, c.values[0]))
+        pj.es_project_experts(c.weights, c.xc, y, i32([0, c.n]), space)
+        close(y, *R.experts(c.x, c.values, [0, c.n]))
+    for call in (lambda: pj.es_project(c.weights, c.xc, y, head[:-1]),
+                 lambda: pj.es_project_experts(c.weights, c.xc, y, i32([0, c.n]), head[:-1]),
+                 lambda: pj.es_project_experts(c.weights, c.xc, y, i32([0, c.n]), head, rows=i32(list(range(c.n))))):
+        with pytest.raises(es.EsError) as e:
+            call()
+        assert e.value.status == es.ES_ERR_INVALID_ARG
