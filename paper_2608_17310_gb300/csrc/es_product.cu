@@ -660,8 +660,8 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
     int base = 0;
     for (int s0 = 0; s0 < segments; s0 += blockDim.x) {
       const int s = s0 + threadIdx.x;
-      int begin = 0, end = 0, group = 0;
-      if (s < segments) segment_of(rows, s, begin, end, group);
+      int begin = 0, end = 0;
+      if (s < segments) segment_of(rows, s, begin, end);
       const int n = (end - begin + kRows - 1) / kRows;
       int sum = n;
 #pragma unroll

@@ -202,7 +202,7 @@ es_status_t es_project(es_weights_t w, es_adapters_t m, const es_project_t* a, v
   if ((st = check_optional(a->adapter, 4, dev, call, "adapter")) != ES_OK) return st;
   const uint64_t need = m != nullptr ? es_project_workspace(w, m, a->rows) : esopt::project_workspace_head();
   if ((st = check_workspace(workspace, workspace_bytes, need, dev, call)) != ES_OK) return st;
-  const esopt::RowView rows{static_cast<const uint16_t*>(a->x), static_cast<uint16_t*>(a->y), a->start, nullptr, nullptr,
+  const esopt::RowView rows{static_cast<const uint16_t*>(a->x), static_cast<uint16_t*>(a->y), a->start, nullptr,
                             a->x_stride, a->y_stride, a->requests, a->rows, a->rows, true, false};
   st = esopt::launch_project(v, w->maps, w->dtype == ES_FP8_E4M3, m != nullptr ? &m->view : nullptr, m != nullptr ? &m->map : nullptr,
                              a->adapter, rows, workspace, static_cast<cudaStream_t>(stream), call);
@@ -234,7 +234,7 @@ es_status_t es_project_experts(es_weights_t w, const es_project_experts_t* a, vo
   if ((st = check_buffer(a->y, 16, dev, call, "y")) != ES_OK) return st;
   const uint64_t need = a->rows != nullptr ? es_project_workspace(w, nullptr, a->slots) : esopt::project_workspace_head();
   if ((st = check_workspace(workspace, workspace_bytes, need, dev, call)) != ES_OK) return st;
-  const esopt::RowView rows{static_cast<const uint16_t*>(a->x), static_cast<uint16_t*>(a->y), a->start, nullptr, a->rows,
+  const esopt::RowView rows{static_cast<const uint16_t*>(a->x), static_cast<uint16_t*>(a->y), a->start, a->rows,
                             a->x_stride, a->y_stride, v.groups, a->slots, a->x_rows, false, false};
   st = esopt::launch_experts(v, w->maps, w->dtype == ES_FP8_E4M3, a->gated != 0, rows, workspace, static_cast<cudaStream_t>(stream), call);
   return st == ES_OK ? ok() : st;

@@ -27,13 +27,12 @@ struct AdapterView {
   int count, rank;
 };
 
-// The rows of a product, in segments that go through one matrix each. start comes from device
+// The rows of a product, in segments that go through one matrix each, the matrix of the segment's number. start comes from device
 // memory and is taken through segment_of, which bounds it.
 struct RowView {
   const uint16_t* x;
   uint16_t* y;
   const int32_t* start;  // NULL: one row a segment
-  const int32_t* group;  // matrix of each segment; NULL: its number
   const int32_t* index;  // row of x of each row; NULL: its number
   uint64_t x_stride, y_stride;
   int segments, rows, x_rows;
@@ -42,17 +41,16 @@ struct RowView {
 };
 
 #ifdef __CUDACC__
-// Rows [begin, end) of segment s and its matrix (outside [0, groups): none).
-__device__ __forceinline__ void segment_of(const RowView& r, int s, int& begin, int& end, int& group) {
+// Rows [begin, end) of segment s.
+__device__ __forceinline__ void segment_of(const RowView& r, int s, int& begin, int& end) {
   if (r.joined) {
-    begin = group = 0;
+    begin = 0;
     end = r.start != nullptr ? min(max(r.start[r.segments], 0), r.rows) : r.rows;
     return;
   }
   begin = r.start != nullptr ? min(max(r.start[s], 0), r.rows) : min(s, r.rows);
   end = r.start != nullptr ? min(max(r.start[s + 1], 0), r.rows) : min(s + 1, r.rows);
   end = max(begin, end);
-  group = r.group != nullptr ? r.group[s] : s;
 }
 #endif
 
