@@ -684,7 +684,8 @@ product_kernel(const MatrixView w, const RowView rows, const ExpandView expand, 
       }
       __syncthreads();
     }
-    plan.columns = base;
+    // Starts that decrease could name rows many times over: no more column tiles than starts in order have.
+    plan.columns = min(base, rows.rows / kRows + segments);
   }
   plan.tiles = plan.columns * plan.features;
   const int seat = blockIdx.x % (shares * S::kBlocks);  // in the cluster

@@ -84,6 +84,31 @@ def test_single_rows_of_members_beyond_the_workspaces_room(pj, dtype, rank):  # 
     Case(pj, counts, [i % 7 - 1 for i in range(len(counts))], 64, 28008, count=6, rank=rank, dtype=dtype).check()
 
 
+@pytest.mark.parametrize("loads", [[65] * 40, [257] * 9 + [1], [1] * 80, [64, 1, 129] * 20, [256, 513, 1, 1, 257]])
+def test_most_tiles_that_rows_have(pj, loads):  # noqa: F811
+    """Each matrix has a tile of a single row at most behind its full ones."""
+    check_experts(pj, loads, 64, 136, "bf16")
+
+
+@pytest.mark.parametrize("groups,slots", [(1024, 900), (1024, 60000), (33, 16), (5, 4000)])
+def test_starts_that_decrease(pj, groups, slots):  # noqa: F811
+    """What is written then is not said, but it ends, and nothing is written around y."""
+    w = torch.ones(groups, 16, 16, dtype=torch.bfloat16, device="cuda")
+    weights = pj.es_weights_create(w)
+    x = torch.ones(slots, 16, dtype=torch.bfloat16, device="cuda")
+    around = torch.full((slots + 20, 16), 3.0, dtype=torch.bfloat16, device="cuda")
+    space = room(pj, weights, slots)
+    for start in ([slots * (g % 2) for g in range(groups + 1)], [slots - g * slots // groups for g in range(groups + 1)],
+                  [(g * 7919) % (2 * slots) - slots // 2 for g in range(groups + 1)]):
+        for rows in (None, i32(list(range(slots)))):
+            around.fill_(3.0)
+            pj.es_project_experts(weights, x, around[10:-10], i32(start), space, rows=rows)
+            assert not pj.es_project_gave_up(space)
+            assert (around[:10] == 3).all() and (around[-10:] == 3).all()
+            if rows is None:
+                assert ((around == 3) | (around == 16)).all()
+
+
 CAPTURED = """
     import sys
     sys.path[:0] = [{root!r}, {tests!r}]
