@@ -116,7 +116,9 @@ es_status_t es_adapters_destroy(es_adapters_t adapters);
  *   y_i = W x_i + B_m (scale[m] * (A_m x_i))
  *         (W x_i alone where m is not within 0 .. count - 1),
  * W with its scale. Sums are fp32, A x is kept to 2^-16 of itself, and a result is
- * rounded once. A row depends on its own adapter alone, whatever others hold.
+ * rounded once. A row depends on its own adapter alone, whatever others hold; in which
+ * order B h is summed, and so a result's last bit, also goes by whether the 16 rows
+ * around it have one adapter, and by the number of rows.
  *   weights   of one matrix
  *   adapters  of the same sizes, or NULL: y = W x
  *   x         [rows] rows of in_features bf16, x_stride elements apart

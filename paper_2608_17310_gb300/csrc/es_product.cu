@@ -23,18 +23,19 @@
 // cluster: each sends the others their columns of its sums, by bulk copies between shared memories into the stages,
 // which are empty then, and sums what it is sent in the order of the blocks. So results do not depend on timing.
 //
-// Adapters. A kernel of its own makes h = s A x, as the sum of two bf16 numbers (2^-16 of it), for 32 rows and
-// one adapter a block. Where 16 rows have one adapter, B h is further products into the same sums. Where members
-// meet within 16 rows, products would multiply one's B by the others' zeros, and infinities or NaN of a member
-// that has diverged would reach all of them; there B h is made in fp32, row by row, by that kernel where it
-// has room in the workspace (kMostExtra), else where results are written. The product's kernel starts beside it, and waits where
-// the adapters' part is needed.
+// Adapters. A kernel of its own makes h = s A x, for 32 rows and one adapter a block, and keeps it as the sum of two bf16
+// numbers (2^-16 of it, where a result's rounding is 2^-9; and as it is, in fp32, where that kernel makes B h too). Where 16
+// rows have one adapter, B h is further products into the same sums. Where members meet within 16 rows, products would
+// multiply one's B by the others' zeros, and infinities or NaN of a member that has diverged would reach all of them; there
+// B h is made in fp32, row by row, by that kernel where it has room in the workspace (kMostExtra), else where results are
+// written. The product's kernel starts beside it, and waits where the adapters' part is needed.
 //
-// Measured (GB300, us a pass): project_prompts 13,741 rows of 30 members, 5,120 to 17,408 features, rank 32, 1,361
-// (1,816 TFLOP/s, 94 % of the card's bf16 matrix rate in a burst; 1,570 in long loops, where the power limit
-// holds the clock); 4,096 rows without adapters 393 (1,857 TFLOP/s; the library's product 391). experts_prompt
-// 32,764 rows of 32 experts gathered and gated 518, 40 of them the gather. experts_step 762 MB of experts for 576 rows
-// 114 (6,690 GB/s, 99 %). project_step 192 members' rows through 73 MB 39 (26 without the adapters).
+// Measured (GB300, us a pass): project_prompts 13,741 rows of 30 members, 5,120 to 17,408 features, rank 32, 1,395 in ten
+// passes (1,772 TFLOP/s, 91 % of the card's bf16 matrix rate in a burst), 1,544 to 1,590 in long loops (1,440 MHz at 1,373 W, the power
+// limit); FP8 2,316. 4,096 rows without adapters 368 to 393 (FP8 687; the library's bf16 product 391). experts_prompt
+// 32,764 rows of 29 experts gathered and gated 550 in ten passes, 43 of them the gather, 597 to 605 in long loops (1,530 MHz at
+// 1,372 W); FP8 874. experts_step 762 MB of experts for 576 rows 114 to 116 (6,680 to 6,550 GB/s, 98 to 97 %). project_step 192 members' rows
+// through 73 MB 36 (22 without the adapters).
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -389,7 +390,7 @@ shrink_kernel(const ShrinkArgs a) {
 
 // Copies the rows of x that slots name (zeros for those that do not exist) so that they lie in order, for tiles of
 // many rows: there the copies one by one, four rows an instruction and 65 cycles each, took 1,581 us for a prompt whose
-// product takes 480 so. A warp has a slot. 40 us for 8,191 rows of 5,120 bytes four times each, 84 % of the
+// product takes 480 so. A warp has a slot. 40 us for 8,191 rows of 5,120 bytes, read once and written four times (210 MB), 77 % of the
 // copy bandwidth.
 __global__ void __launch_bounds__(256)
 gather_kernel(const RowView rows, uint16_t* to, int in) {
@@ -426,7 +427,9 @@ struct Shape {
   static constexpr uint32_t kW = kFeatures * kDepth * 2, kX = kRows / kBlocks * kDepth * 2, kRaw = kFp8 ? kFeatures * kDeep : 0;
   static constexpr int kStages = kFp8 ? (kPair ? 5 : kRows == 64 ? 6 : 9) : (kPair ? 6 : kRows == 64 ? 8 : 10);
   static constexpr int kThreads = kFp8 ? 512 : 256;
-  static constexpr int kBound = kFp8 ? 640 : 256;  // so that registers are left for the adapters' kernel beside it
+  // FP8: 96 registers, so that some are left for the adapters' kernel beside it. (The kernels that are not gated spill 208 to
+  // 220 bytes for it, around `expanded`.)
+  static constexpr int kBound = kFp8 ? 640 : 256;
   // blocks or pairs that share a tile: what they send and receive has room in the stages
   static constexpr int kMostShares = kPair ? 3 : 8;
   static constexpr int kTeam = kInTensor ? 4 : 2;  // of the eight warps that convert codes, those on one part of a stage
@@ -1288,7 +1291,7 @@ es_status_t launch(const MatrixView& w, const CUtensorMap& w_map, const RowView&
   const int outs = kGated ? w.out / 2 : w.out, wide = (kGated ? kFeatures / 2 : kFeatures) * S::kBlocks;
   const int64_t tiles = static_cast<int64_t>(columns) * ((outs + wide - 1) / wide);
   const int depth = (w.in + S::kDeep - 1) / S::kDeep;
-  constexpr int kStageNs = S::kPair ? (kFp8 ? 400 : 270) : kFp8 ? 300 : 220;
+  constexpr int kStageNs = S::kPair ? (kFp8 ? 400 : 270) : kFp8 ? 300 : 220;  // a pair's FP8 stages are the converters'
   const int64_t streamed = tiles * depth * (S::kBlocks * (kFp8 ? S::kRaw : S::kW)) / 6700;
   int shares = 1;
   int64_t best = INT64_MAX;
@@ -1352,13 +1355,16 @@ es_status_t launch_rows(const MatrixView& w, const CUtensorMap& w_map, bool fp8,
 // Rows of a tile. One matrix of 5,120 by 7,168: 32 rows take 25.3 us by tiles of 16, 20.0 by tiles of 64 (whose fewer
 // stages cost 16 rows nothing: 20.1, 19.9; those of 16 leave room where depth is short: 2,560 by 9,728 16.0, 16.3);
 // 64 rows 21.2 by tiles of 64 and 21.8 by pairs; 96 rows 27.1 and 22.7; 192 rows 46.4 and 25.9. FP8 64 rows 23.0 and
-// 25.9, 96 rows 35.0 and 27.6. Experts go by their mean, with 0.4 to 1.6 times that each: 48 experts of 1,280 by 2,560 at
-// 48 rows 59.8 and 61.4, at 64 rows 67.1 and 62.6; FP8 67.7 and 71.6, 81.8 and 74.2.
+// 25.9, 96 rows 35.0 and 27.6. Experts go by their mean, since their loads are not known here. With 0.4 to 1.6 times that each: 48 experts of
+// 1,280 by 2,560 at 48 rows 59.8 and 61.4, at 64 rows 67.1 and 62.6; FP8 67.7 and 71.6, 81.8 and 74.2. Where one of 64 experts (2,560 by
+// 2,560, gated) has three quarters of all rows, the rule's tiles of 64 are slower than pairs' would be: 178 and 157 at a mean of 40
+// rows, 155 and 145 at 20; with a quarter 147 and 147, 135 and 145; even ones 137 and 141 at 40.
 constexpr int kLeast = 16, kFew = 64, kMany = 256;
 constexpr int kManyEach = 48;  // rows an expert above which tiles are of kMany
-// B h of rows beside others' has room in the workspace (4 bytes a feature and row) up to here. Beyond, where it is made
-// where results are written, mixed blocks are few or the product long. (8,500 rows of 69 members, 1,264 to 1,000 features,
-// FP8: 87 us so.)
+// B h of rows beside others' has room in the workspace (4 bytes a feature and row) up to here, which bounds what a workspace
+// takes. Beyond it is made where results are written: nothing where prompts leave few mixed blocks (project_prompts), but slow for
+// single rows: 5,120 to 17,408 features, rank 16, eight rows a member, 1,900 rows 303 us and 1,960 rows 641 (one a member 944); rank 64 708 and
+// 2,169; 2,560 to 9,728, rank 40, 3,400 rows 449 and 3,460 rows 1,037.
 constexpr uint64_t kMostExtra = uint64_t{128} << 20;
 uint64_t extra_bytes(uint64_t rows, uint64_t out) { return rows * out * 4; }
 

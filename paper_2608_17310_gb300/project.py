@@ -220,7 +220,8 @@ def _int(n, what: str) -> int:
 
 
 def es_project_workspace(weights: Weights, rows: int, adapters: Adapters = None) -> int:
-    """Bytes of (zeroed) workspace for es_project, or es_project_experts, of up to ``rows`` rows."""
+    """Bytes of (zeroed) workspace for es_project, or es_project_experts, of up to ``rows`` rows.
+    Without adapters and named rows ES_PROJECT_GAVE_UP + 256 bytes do."""
     return int(_lib().es_project_workspace(weights.handle, adapters.handle if adapters is not None else None, _int(rows, "rows")))
 
 
